@@ -444,6 +444,141 @@ lipcache_status lipcache_lookup_filter_dump(const lipcache_cache* c, const float
                                             void* ws, size_t ws_bytes,
                                             lipcache_stream_t stream);
 
+/* ------------------------------------------------- adapting a shared head
+ *
+ * The two operators below personalise and train a projection that many
+ * sites share.  Their matrices take float32, bfloat16 or float16 (`dtype`),
+ * any sizes >= 1, and rows at a stride where an `ld*` argument is given (in
+ * elements, at least the row's width).  Widths reach 2^20, rows 2^31 - 1,
+ * pairs and stacks 65,535 (beyond: EUNSUPPORTED).  16-bit rows that start on 16-byte
+ * boundaries are read in place; others are first copied into the workspace.
+ * A workspace may be reused by the next call on the same stream.
+ */
+
+/*
+ * The low-rank pairs of S sites and the requests of one batch.  Request i
+ * owns the rows offsets[i] .. offsets[i+1) and names the pair adapter[i];
+ * an index outside [0, S), -1 by custom, means none.  Rows that no request
+ * owns have none either.  The offsets lie on the device and are not checked:
+ * they must not decrease (values outside [0, T] are clamped, so no access
+ * leaves the arrays whatever they hold).
+ */
+typedef struct lipcache_adapters {
+  const void*    A;        /* [S][r][K], dtype                                */
+  const void*    B;        /* [S][N][r], dtype                                */
+  const float*   scale;    /* [S]                                             */
+  const int32_t* offsets;  /* [R+1]                                           */
+  const int32_t* adapter;  /* [R]                                             */
+  int32_t        S;        /* pairs; 0 = none (A, B, scale may be NULL)       */
+  int32_t        r;        /* rank, 1 <= r <= 128 (zero rows of A and zero
+                              columns of B pad a smaller one)                 */
+  int32_t        R;        /* requests; 0 = none                              */
+} lipcache_adapters;
+
+/*
+ * The shared projection with the adapters of many requests at once.  For
+ * every row t of a request with pair a
+ *   v_t = A_a x_t,    y_t = W x_t + bias + scale_a B_a v_t,
+ * and y_t = W x_t + bias, v_t = 0 for rows without one.  Sums are held in
+ * float32; v is never rounded to 16 bits in one piece (the product B_a v_t
+ * takes it as a sum of two such numbers), y is rounded once.  A value that is
+ * not finite stays in its own request's rows (in W or bias: in its outputs).
+ *
+ *  x [T][K] (ldx), W [N][K] (ldw), bias [N] float or NULL
+ *  y [T][N] (ldy) out;  v [T][r] float out, or NULL (the backward pass takes it)
+ *  ws lipcache_adapter_forward_workspace_bytes(T, K, N, r, S, dtype) bytes
+ * T = 0 is valid and does nothing. (async)
+ */
+lipcache_status lipcache_adapter_forward(const void* x, int64_t ldx, int64_t T,
+                                         const void* W, int64_t ldw, const float* bias,
+                                         int32_t K, int32_t N, const lipcache_adapters* ad,
+                                         int32_t dtype, void* y, int64_t ldy, float* v,
+                                         void* ws, size_t ws_bytes, lipcache_stream_t stream);
+size_t lipcache_adapter_forward_workspace_bytes(int64_t T, int32_t K, int32_t N, int32_t r,
+                                                int32_t S, int32_t dtype);
+
+/*
+ * Gradients of the same with W and bias frozen.  With u_t = B_a^T dy_t:
+ *   dx_t = W^T dy_t + scale_a A_a^T u_t,
+ *   dA_a = scale_a sum_t u_t x_t^T,   dB_a = scale_a sum_t dy_t v_t^T
+ * over all rows of all requests that name the pair a (zero for a pair that
+ * none names).  The sums run in a fixed order, so equal inputs give equal
+ * bits.
+ *
+ *  dy [T][N] (lddy), x [T][K] (ldx), W [N][K] (ldw)
+ *  v  [T][r] float of the forward pass, or NULL (computed again)
+ *  dx [T][K] (lddx) out, or NULL;  dA [S][r][K], dB [S][N][r] out, both or
+ *  neither NULL
+ *  ws lipcache_adapter_backward_workspace_bytes(T, K, N, r, S, dtype) bytes
+ * T = 0 writes zeros to dA and dB. (async)
+ */
+lipcache_status lipcache_adapter_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                                          int64_t T, const void* W, int64_t ldw,
+                                          int32_t K, int32_t N, const lipcache_adapters* ad,
+                                          int32_t dtype, const float* v, void* dx, int64_t lddx,
+                                          void* dA, void* dB,
+                                          void* ws, size_t ws_bytes, lipcache_stream_t stream);
+size_t lipcache_adapter_backward_workspace_bytes(int64_t T, int32_t K, int32_t N, int32_t r,
+                                                 int32_t S, int32_t dtype);
+
+/*
+ * Orthogonalisation of `batch` matrices by Newton-Schulz products.  With
+ * X_0 = G / (||G||_F + eps) (transposed when m > n), `steps` times
+ *   X <- a X + (b P + c P^2) X,   P = X X^T,
+ * with (a, b, c) = coef[3 k .. 3 k + 3) in step k: every singular value s of
+ * X becomes s (a + b s^2 + c s^4).  (3.4445, -4.775, 2.0315) brings them to
+ * about [0.7, 1.2] in five steps; (15/8, -10/8, 3/8) converges to 1.
+ *
+ * The products run on the matrix cores with float16 operands; float32 and
+ * float16 results take each operand as a sum of two float16 numbers (22
+ * bits).  Operands are scaled by powers of two that no value can overflow:
+ * the bound of the singular values, worked out from the coefficients on the
+ * host, must stay below 16 (else EUNSUPPORTED).
+ *
+ *  G, out [batch][m][n] contiguous, batch >= 0, 1 <= m, n, min(m, n) <= 16384,
+ *         m n <= 2^30; out may be G
+ *  steps  0 <= steps <= 32;  coef (host) [steps][3];  eps (host) >= 0
+ *  ws     lipcache_orthogonalise_workspace_bytes(batch, m, n, dtype) bytes
+ * A zero matrix gives zeros (with eps > 0); one that holds a NaN or an
+ * infinity gives NaN throughout, and leaves the others of the batch alone. (async)
+ */
+lipcache_status lipcache_orthogonalise(const void* G, int64_t batch, int32_t m, int32_t n,
+                                       int32_t dtype, int32_t steps, const float* coef, float eps,
+                                       void* out, void* ws, size_t ws_bytes,
+                                       lipcache_stream_t stream);
+size_t lipcache_orthogonalise_workspace_bytes(int64_t batch, int32_t m, int32_t n, int32_t dtype);
+
+/* What a step along an orthogonalised momentum takes beside its matrices. */
+typedef struct lipcache_muon {
+  float   lr;            /* finite                                                       */
+  float   momentum;      /* mu, finite                                                   */
+  float   weight_decay;  /* finite                                                       */
+  float   scale;         /* factor of the update, finite; sqrt(max(1, m/n)) keeps the
+                            step's operator norm at lr in mean-square terms              */
+  float   eps;           /* as in lipcache_orthogonalise                                 */
+  int32_t nesterov;      /* 1: U = mu M + G; 0: U = M                                    */
+  int32_t steps;
+  const float* coef;     /* (host) [steps][3]                                            */
+} lipcache_muon;
+
+/*
+ * One optimiser step of `batch` matrices, in place:
+ *   M <- mu M + G,   U = mu M + G (nesterov) or M,   O = orthogonalise(U),
+ *   W <- (1 - lr weight_decay) W - lr scale O.
+ * Every singular value of O is at most the last step's bound (1.21 for the
+ * coefficients above), so sigma_max(W) moves by at most 1.21 lr scale and
+ * the decay: what the certified radii are divided by stays known.
+ *
+ *  W, G [batch][m][n] contiguous, dtype;  M [batch][m][n] float
+ *  opt  (host);  sizes as in lipcache_orthogonalise
+ *  ws   lipcache_muon_step_workspace_bytes(batch, m, n, dtype) bytes
+ * (async)
+ */
+lipcache_status lipcache_muon_step(void* W, const void* G, float* M, int64_t batch,
+                                   int32_t m, int32_t n, int32_t dtype, const lipcache_muon* opt,
+                                   void* ws, size_t ws_bytes, lipcache_stream_t stream);
+size_t lipcache_muon_step_workspace_bytes(int64_t batch, int32_t m, int32_t n, int32_t dtype);
+
 /* Static description of a status code. */
 const char* lipcache_status_string(lipcache_status status);
 

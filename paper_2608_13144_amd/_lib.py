@@ -59,6 +59,41 @@ class LipcacheIndex(ctypes.Structure):
 
 _PINDEX = ctypes.POINTER(LipcacheIndex)
 
+
+class LipcacheAdapters(ctypes.Structure):
+    """Mirror of ``lipcache_adapters``."""
+
+    _fields_ = [
+        ("A", ctypes.c_void_p),
+        ("B", ctypes.c_void_p),
+        ("scale", ctypes.c_void_p),
+        ("offsets", ctypes.c_void_p),
+        ("adapter", ctypes.c_void_p),
+        ("S", ctypes.c_int32),
+        ("r", ctypes.c_int32),
+        ("R", ctypes.c_int32),
+    ]
+
+
+class LipcacheMuon(ctypes.Structure):
+    """Mirror of ``lipcache_muon``."""
+
+    _fields_ = [
+        ("lr", ctypes.c_float),
+        ("momentum", ctypes.c_float),
+        ("weight_decay", ctypes.c_float),
+        ("scale", ctypes.c_float),
+        ("eps", ctypes.c_float),
+        ("nesterov", ctypes.c_int32),
+        ("steps", ctypes.c_int32),
+        ("coef", ctypes.POINTER(ctypes.c_float)),
+    ]
+
+
+_PADAPTERS = ctypes.POINTER(LipcacheAdapters)
+_PMUON = ctypes.POINTER(LipcacheMuon)
+_f32, _pf32 = ctypes.c_float, ctypes.POINTER(ctypes.c_float)
+
 SIGNATURES = {
     "lipcache_spectral_norm": (_i32, [_vp, _i32, _i32, _i32, _f64, ctypes.POINTER(_f64), ctypes.POINTER(_i32),
                                       _vp, _sz, _vp]),
@@ -84,6 +119,16 @@ SIGNATURES = {
     "lipcache_lookup_indexed": (_i32, [_PCACHE, _PINDEX, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _vp,
                                        ctypes.POINTER(_i64), _vp, _sz, _vp]),
     "lipcache_lookup_indexed_workspace_bytes": (_sz, [_i64, _i64, _i32, _i32, _i64]),
+    "lipcache_adapter_forward": (_i32, [_vp, _i64, _i64, _vp, _i64, _vp, _i32, _i32, _PADAPTERS, _i32, _vp, _i64,
+                                        _vp, _vp, _sz, _vp]),
+    "lipcache_adapter_forward_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32, _i32, _i32]),
+    "lipcache_adapter_backward": (_i32, [_vp, _i64, _vp, _i64, _i64, _vp, _i64, _i32, _i32, _PADAPTERS, _i32, _vp,
+                                         _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
+    "lipcache_adapter_backward_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32, _i32, _i32]),
+    "lipcache_orthogonalise": (_i32, [_vp, _i64, _i32, _i32, _i32, _i32, _pf32, _f32, _vp, _vp, _sz, _vp]),
+    "lipcache_orthogonalise_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
+    "lipcache_muon_step": (_i32, [_vp, _vp, _vp, _i64, _i32, _i32, _i32, _PMUON, _vp, _sz, _vp]),
+    "lipcache_muon_step_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
     "lipcache_status_string": (ctypes.c_char_p, [_i32]),
     "lipcache_abi_version": (_i32, []),
 }

@@ -381,3 +381,203 @@ def consistency(lookup_label: torch.Tensor, head_label: torch.Tensor) -> tuple[i
     L.check("lipcache_consistency", st)
     h, c = counts.cpu().tolist()
     return int(h), int(c)
+
+
+# ------------------------------------------------------- adapting a shared head
+_DTYPE = {torch.float32: L.F32, torch.bfloat16: L.BF16, torch.float16: L.F16}
+
+
+def _dtype(t: torch.Tensor, name: str) -> int:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    code = _DTYPE.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return code
+
+
+def _need_rows(t: torch.Tensor, name: str, dtype: torch.dtype, device: torch.device, rows: int, width: int) -> int:
+    """Checks a [rows, width] matrix whose rows may lie apart; returns their distance in elements."""
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width:
+        raise ValueError(f"{name} must be [{rows}, {width}], got {list(t.shape)}")
+    if (width > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < width):
+        raise ValueError(f"{name} must have contiguous, non-overlapping rows")
+    return t.stride(0) if rows > 1 else width
+
+
+def _need_shape(t: torch.Tensor, name: str, dtype: torch.dtype, device: torch.device, shape: tuple) -> None:
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _adapters(A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor, offsets: torch.Tensor, adapter: torch.Tensor,
+              dtype: torch.dtype, device: torch.device, K: int, N: int) -> L.LipcacheAdapters:
+    if not isinstance(A, torch.Tensor) or A.dim() != 3:
+        raise ValueError("A must be [S, r, K]")
+    S, r = A.shape[0], A.shape[1]
+    _need_shape(A, "A", dtype, device, (S, r, K))
+    _need_shape(B, "B", dtype, device, (S, N, r))
+    _need_shape(scale, "scale", torch.float32, device, (S,))
+    if not isinstance(adapter, torch.Tensor) or adapter.dim() != 1:
+        raise ValueError("adapter must be [R]")
+    R = adapter.shape[0]
+    _need_shape(adapter, "adapter", torch.int32, device, (R,))
+    _need_shape(offsets, "offsets", torch.int32, device, (R + 1,))
+    return L.LipcacheAdapters(A.data_ptr(), B.data_ptr(), scale.data_ptr(), offsets.data_ptr(), adapter.data_ptr(),
+                              S, r, R)
+
+
+@dataclass
+class AdapterOutput:
+    y: torch.Tensor           # [T, N], x's type
+    v: torch.Tensor | None    # float32 [T, r]: A_a x of every row (zero without a pair)
+
+
+def adapter_forward(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None, A: torch.Tensor, B: torch.Tensor,
+                    scale: torch.Tensor, offsets: torch.Tensor, adapter: torch.Tensor, keep: bool = False,
+                    out: AdapterOutput | None = None) -> AdapterOutput:
+    """lipcache_adapter_forward: W x + bias + scale_a B_a (A_a x) for every row of a batch of requests (async).
+
+    x [T, K] and W [N, K] of one type (float32, bfloat16 or float16; rows may
+    lie apart), bias float32 [N] or None, A [S, r, K], B [S, N, r], scale
+    float32 [S]; request i owns the rows offsets[i]:offsets[i + 1] (int32,
+    R + 1 of them) and names the pair adapter[i] (int32, -1: none).  ``keep``
+    also returns v, which the backward pass takes."""
+    code = _dtype(x, "x")
+    dev, dt = x.device, x.dtype
+    if x.dim() != 2 or not isinstance(W, torch.Tensor) or W.dim() != 2:
+        raise ValueError("x must be [T, K] and W [N, K]")
+    T, K = x.shape
+    N = W.shape[0]
+    ldx = _need_rows(x, "x", dt, dev, T, K)
+    ldw = _need_rows(W, "W", dt, dev, N, K)
+    if bias is not None:
+        _need_shape(bias, "bias", torch.float32, dev, (N,))
+    ad = _adapters(A, B, scale, offsets, adapter, dt, dev, K, N)
+    if out is None:
+        out = AdapterOutput(torch.empty((T, N), dtype=dt, device=dev),
+                            torch.empty((T, ad.r), dtype=torch.float32, device=dev) if keep else None)
+    ldy = _need_rows(out.y, "out.y", dt, dev, T, N)
+    if out.v is not None:
+        _need_shape(out.v, "out.v", torch.float32, dev, (T, ad.r))
+    lib = L.load()
+    ws = workspace(lib.lipcache_adapter_forward_workspace_bytes(T, K, N, ad.r, ad.S, code), dev)
+    st = lib.lipcache_adapter_forward(x.data_ptr(), ldx, T, W.data_ptr(), ldw, None if bias is None else bias.data_ptr(),
+                                      K, N, ctypes.byref(ad), code, out.y.data_ptr(), ldy,
+                                      None if out.v is None else out.v.data_ptr(), ws.data_ptr(), ws.numel(),
+                                      torch.cuda.current_stream(dev).cuda_stream)
+    L.check("lipcache_adapter_forward", st)
+    return out
+
+
+@dataclass
+class AdapterGradients:
+    dx: torch.Tensor | None   # [T, K]
+    dA: torch.Tensor | None   # [S, r, K]
+    dB: torch.Tensor | None   # [S, N, r]
+
+
+def adapter_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
+                     scale: torch.Tensor, offsets: torch.Tensor, adapter: torch.Tensor, v: torch.Tensor | None = None,
+                     want_dx: bool = True, want_pairs: bool = True) -> AdapterGradients:
+    """lipcache_adapter_backward: gradients of the rows and of every pair, W and bias frozen (async).
+
+    dy [T, N] is the gradient of y; ``v`` is the forward pass's (computed
+    again when None); the others are the forward pass's arguments."""
+    code = _dtype(x, "x")
+    dev, dt = x.device, x.dtype
+    if x.dim() != 2 or not isinstance(W, torch.Tensor) or W.dim() != 2:
+        raise ValueError("x must be [T, K] and W [N, K]")
+    T, K = x.shape
+    N = W.shape[0]
+    ldx = _need_rows(x, "x", dt, dev, T, K)
+    lddy = _need_rows(dy, "dy", dt, dev, T, N)
+    ldw = _need_rows(W, "W", dt, dev, N, K)
+    ad = _adapters(A, B, scale, offsets, adapter, dt, dev, K, N)
+    if v is not None:
+        _need_shape(v, "v", torch.float32, dev, (T, ad.r))
+    g = AdapterGradients(torch.empty((T, K), dtype=dt, device=dev) if want_dx else None,
+                         torch.empty_like(A) if want_pairs else None, torch.empty_like(B) if want_pairs else None)
+    lib = L.load()
+    ws = workspace(lib.lipcache_adapter_backward_workspace_bytes(T, K, N, ad.r, ad.S, code), dev)
+    st = lib.lipcache_adapter_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, T, W.data_ptr(), ldw, K, N,
+                                       ctypes.byref(ad), code, None if v is None else v.data_ptr(),
+                                       g.dx.data_ptr() if want_dx else None, K, g.dA.data_ptr() if want_pairs else None,
+                                       g.dB.data_ptr() if want_pairs else None, ws.data_ptr(), ws.numel(),
+                                       torch.cuda.current_stream(dev).cuda_stream)
+    L.check("lipcache_adapter_backward", st)
+    return g
+
+
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)  # brings singular values to about [0.7, 1.2] in five steps
+
+
+def _coefficients(steps: int, coefficients):
+    """float[steps][3] from one (a, b, c) for all steps or one for each."""
+    rows = list(coefficients)
+    if rows and not hasattr(rows[0], "__len__"):
+        rows = [rows] * int(steps)
+    if len(rows) != int(steps) or any(len(row) != 3 for row in rows):
+        raise ValueError("coefficients must be one (a, b, c), or one for each step")
+    return (ctypes.c_float * max(1, 3 * int(steps)))(*[float(c) for row in rows for c in row])
+
+
+def _stack(t: torch.Tensor, name: str) -> tuple[int, int, int]:
+    if t.dim() not in (2, 3):
+        raise ValueError(f"{name} must be a matrix or a stack of them")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return (1, *t.shape) if t.dim() == 2 else tuple(t.shape)
+
+
+def orthogonalise(G: torch.Tensor, steps: int = 5, coefficients=NEWTON_SCHULZ, eps: float = 1e-7,
+                  out: torch.Tensor | None = None) -> torch.Tensor:
+    """lipcache_orthogonalise: Newton-Schulz products of a matrix [m, n] or a stack [b, m, n] (async).
+
+    ``coefficients``: one (a, b, c) for all steps or one for each; ``out`` may be G."""
+    code = _dtype(G, "G")
+    b, m, n = _stack(G, "G")
+    if out is None:
+        out = torch.empty_like(G)
+    else:
+        _need_shape(out, "out", G.dtype, G.device, tuple(G.shape))
+    coef = _coefficients(steps, coefficients)
+    lib = L.load()
+    ws = workspace(lib.lipcache_orthogonalise_workspace_bytes(b, m, n, code), G.device)
+    st = lib.lipcache_orthogonalise(G.data_ptr(), b, m, n, code, int(steps), coef, float(eps), out.data_ptr(),
+                                    ws.data_ptr(), ws.numel(), torch.cuda.current_stream(G.device).cuda_stream)
+    L.check("lipcache_orthogonalise", st)
+    return out
+
+
+def muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, lr: float, momentum: float = 0.95,
+              weight_decay: float = 0.0, nesterov: bool = True, scale: float | None = None, steps: int = 5,
+              coefficients=NEWTON_SCHULZ, eps: float = 1e-7) -> None:
+    """lipcache_muon_step: one step along the orthogonalised momentum, W and M in place (async).
+
+    W and G [m, n] or [b, m, n] of one type, M float32 of the same shape.
+    ``scale``: the update's factor, sqrt(max(1, m / n)) when None."""
+    code = _dtype(W, "W")
+    b, m, n = _stack(W, "W")
+    _need_shape(G, "G", W.dtype, W.device, tuple(W.shape))
+    _need_shape(M, "M", torch.float32, W.device, tuple(W.shape))
+    if scale is None:
+        scale = max(1.0, m / max(n, 1)) ** 0.5
+    coef = _coefficients(steps, coefficients)
+    opt = L.LipcacheMuon(float(lr), float(momentum), float(weight_decay), float(scale), float(eps), int(bool(nesterov)),
+                         int(steps), ctypes.cast(coef, ctypes.POINTER(ctypes.c_float)))
+    lib = L.load()
+    ws = workspace(lib.lipcache_muon_step_workspace_bytes(b, m, n, code), W.device)
+    st = lib.lipcache_muon_step(W.data_ptr(), G.data_ptr(), M.data_ptr(), b, m, n, code, ctypes.byref(opt),
+                                ws.data_ptr(), ws.numel(), torch.cuda.current_stream(W.device).cuda_stream)
+    L.check("lipcache_muon_step", st)

@@ -1,0 +1,293 @@
+"""Low-rank adapters of many requests beside a shared projection, against float64 on the CPU.
+
+Every entry is held to an error bound worked out from the sums of absolute
+values behind it (adapt_ref.bound); a value that is not finite has to stay in
+its own request.
+"""
+import numpy as np
+import pytest
+import torch
+
+import adapt_ref as R
+from gpu_helpers import say
+from paper_2608_13144_amd import api
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def make(seed, T, K, N, S, r, R_, dtype, lengths="ragged", none=0.2, bias=True, pad=0, shift=0):
+    """Device tensors of one batch.  ``pad``: extra columns between rows; ``shift``: elements before the first row."""
+    g = torch.Generator().manual_seed(seed)
+
+    def rows(n, w, f=1.0):
+        flat = torch.empty(shift + n * (w + pad), dtype=DT[dtype], device=DEV)
+        t = flat[shift:].view(n, w + pad)[:, :w]
+        t.copy_((f * torch.randn(n, w, generator=g)).to(DT[dtype]))
+        return t
+    if lengths == "one":
+        offsets = torch.arange(T + 1)
+        R_ = T
+    else:
+        offsets = torch.cat([torch.zeros(1, dtype=torch.int64),
+                             torch.randint(0, T + 1, (max(R_ - 1, 0),), generator=g).sort().values,
+                             torch.full((1,), T)])[:R_ + 1] if R_ else torch.zeros(1, dtype=torch.int64)
+    adapter = torch.randint(0, max(S, 1), (R_,), generator=g)
+    adapter[torch.rand(R_, generator=g) < none] = -1
+    return dict(
+        x=rows(T, K), W=rows(N, K, K ** -0.5), dy=rows(T, N),
+        bias=(torch.randn(N, generator=g).to(DEV) if bias else None),
+        A=(torch.randn(S, r, K, generator=g) * K ** -0.5).to(DT[dtype]).to(DEV),
+        B=torch.randn(S, N, r, generator=g).to(DT[dtype]).to(DEV),
+        scale=(torch.rand(S, generator=g) + 0.5).to(DEV),
+        offsets=offsets.int().to(DEV), adapter=adapter.int().to(DEV))
+
+
+def n64(t):
+    return None if t is None else t.detach().cpu().double().numpy()
+
+
+def pair_of(b):
+    return R.pairs_of_rows(b["x"].shape[0], n64(b["offsets"]), n64(b["adapter"]).astype(int), b["A"].shape[0])
+
+
+def close(got, ref, lim, what):
+    err = np.abs(n64(got) - ref)
+    bad = ~(err <= lim)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.size} past the bound, worst {np.nanmax(err / lim):.3g} of it"
+
+
+def check_forward(b, dtype, what):
+    say("adapter forward", what)
+    out = api.adapter_forward(b["x"], b["W"], b["bias"], b["A"], b["B"], b["scale"], b["offsets"], b["adapter"], keep=True)
+    pair = pair_of(b)
+    y, v, ay, av = R.forward(n64(b["x"]), n64(b["W"]), n64(b["bias"]), n64(b["A"]), n64(b["B"]), n64(b["scale"]), pair)
+    K, r = b["x"].shape[1], b["A"].shape[1]
+    close(out.v, v, R.bound(v, av, K, dtype if dtype == "f32" else "f16", "f32"), what + " v")
+    close(out.y, y, R.bound(y, ay, K + r, dtype), what + " y")
+    assert np.all(n64(out.v)[pair < 0] == 0)
+    again = api.adapter_forward(b["x"], b["W"], b["bias"], b["A"], b["B"], b["scale"], b["offsets"], b["adapter"])
+    assert again.v is None and torch.equal(again.y, out.y), what + ": two calls differ"
+    return out
+
+
+def check_backward(b, dtype, what, v=None):
+    say("adapter backward", what)
+    args = [b[k] for k in ("dy", "x", "W", "A", "B", "scale", "offsets", "adapter")]
+    g = api.adapter_backward(*args, v=v)
+    pair = pair_of(b)
+    x64, A64 = n64(b["x"]), n64(b["A"])
+    v64 = n64(v) if v is not None else R.forward(x64, n64(b["W"]), None, A64, n64(b["B"]), n64(b["scale"]), pair)[1]
+    dx, dA, dB, adx, aA, aB = R.backward(n64(b["dy"]), x64, n64(b["W"]), A64, n64(b["B"]), n64(b["scale"]), pair, v64)
+    T, K = x64.shape
+    N, r = b["W"].shape[0], A64.shape[1]
+    if v is None:  # the sums behind a v that is computed again are part of dB's
+        for a in range(A64.shape[0]):
+            t = np.flatnonzero(pair == a)
+            if t.size:
+                aB[a] = abs(n64(b["scale"])[a]) * (np.abs(n64(b["dy"])[t]).T @ (np.abs(x64[t]) @ np.abs(A64[a]).T))
+    close(g.dx, dx, R.bound(dx, adx, N + r, dtype), what + " dx")
+    close(g.dA, dA, R.bound(dA, aA, N + T, dtype), what + " dA")
+    close(g.dB, dB, R.bound(dB, aB, K + T, dtype), what + " dB")
+    again = api.adapter_backward(*args, v=v)
+    for f in ("dx", "dA", "dB"):
+        assert torch.equal(getattr(g, f), getattr(again, f)), f"{what}: two calls differ in {f}"
+    return g
+
+
+SIZES = [
+    # T, K, N, S, r, R, lengths
+    (1, 64, 10, 1, 1, 1, "one"),
+    (1, 256, 200, 3, 8, 1, "one"),
+    (3, 1, 1, 2, 1, 2, "ragged"),
+    (16, 512, 384, 5, 16, 16, "one"),
+    (17, 96, 33, 5, 3, 4, "ragged"),
+    (64, 320, 200, 64, 16, 64, "one"),
+    (65, 257, 129, 4, 64, 9, "ragged"),
+    (130, 72, 1000, 2, 24, 60, "ragged"),
+    (257, 1024, 136, 3, 32, 7, "ragged"),
+    (300, 200, 256, 7, 128, 5, "ragged"),
+    (513, 128, 264, 1, 8, 1, "ragged"),
+    (700, 40, 640, 6, 5, 300, "ragged"),
+    (1100, 384, 520, 4, 16, 11, "ragged"),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+def test_forward_and_backward(size, dtype):
+    T, K, N, S, r, R_, lengths = size
+    b = make(T + K + N, T, K, N, S, r, R_, dtype, lengths)
+    out = check_forward(b, dtype, f"{size} {dtype}")
+    check_backward(b, dtype, f"{size} {dtype} kept v", out.v)
+    check_backward(b, dtype, f"{size} {dtype} v again")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("pad,shift", [(8, 0), (5, 0), (8, 3), (1, 8)])
+def test_rows_apart_and_unaligned(dtype, pad, shift):
+    b = make(5, 77, 136, 72, 4, 12, 6, dtype, pad=pad, shift=shift)
+    check_forward(b, dtype, f"pad {pad} shift {shift} {dtype}")
+    check_backward(b, dtype, f"pad {pad} shift {shift} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_output_rows_apart(dtype):
+    b = make(6, 70, 128, 200, 3, 8, 5, dtype)
+    ref = api.adapter_forward(b["x"], b["W"], b["bias"], b["A"], b["B"], b["scale"], b["offsets"], b["adapter"])
+    wide = torch.full((70, 211), 7.0, dtype=DT[dtype], device=DEV)
+    out = api.AdapterOutput(wide[:, 5:205], None)
+    api.adapter_forward(b["x"], b["W"], b["bias"], b["A"], b["B"], b["scale"], b["offsets"], b["adapter"], out=out)
+    assert torch.equal(out.y, ref.y)
+    assert bool((wide[:, :5] == 7).all()) and bool((wide[:, 205:] == 7).all())
+
+
+@pytest.mark.parametrize("T", [3, 200])
+def test_no_pairs_no_requests_no_bias(T):
+    for S, R_, none in ((2, 3, 1.0), (2, 0, 0.0), (0, 3, 0.0)):
+        b = make(7, T, 96, 40, S, 4, R_, "bf16", none=none, bias=False)
+        if S == 0:
+            b["adapter"].zero_()  # names a pair that is not there
+        out = check_forward(b, "bf16", f"T {T} S {S} R {R_} none {none}")
+        assert bool((out.v == 0).all())
+        g = check_backward(b, "bf16", f"T {T} S {S} R {R_} none {none}", out.v)
+        assert bool((g.dA == 0).all()) and bool((g.dB == 0).all())
+
+
+def test_no_rows():
+    b = make(8, 0, 96, 40, 2, 4, 3, "f16")
+    out = api.adapter_forward(b["x"], b["W"], b["bias"], b["A"], b["B"], b["scale"], b["offsets"], b["adapter"], keep=True)
+    assert out.y.shape == (0, 40) and out.v.shape == (0, 4)
+    g = api.adapter_backward(b["dy"], b["x"], b["W"], b["A"], b["B"], b["scale"], b["offsets"], b["adapter"], v=out.v)
+    assert g.dx.shape == (0, 96) and bool((g.dA == 0).all()) and bool((g.dB == 0).all())
+
+
+@pytest.mark.parametrize("T", [40, 300])
+def test_offsets_that_reach_past_the_rows(T):
+    """Offsets below 0 and past T are clamped; rows outside every request have no pair; strange indices mean none."""
+    b = make(9, T, 64, 48, 3, 4, 4, "f16")
+    b["offsets"] = torch.tensor([-5, 7, 20, 20, T + 1000], dtype=torch.int32, device=DEV)
+    b["adapter"] = torch.tensor([1, -7, 2, 99], dtype=torch.int32, device=DEV)
+    check_forward(b, "f16", "offsets past the rows")
+    check_backward(b, "f16", "offsets past the rows")
+    b["offsets"] = torch.tensor([5, 7, 20, 20, 30], dtype=torch.int32, device=DEV)
+    b["adapter"] = torch.tensor([1, 0, 2, 2], dtype=torch.int32, device=DEV)
+    check_forward(b, "f16", "rows that no request owns")
+    check_backward(b, "f16", "rows that no request owns")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,lengths", [(24, "one"), (150, "ragged")])
+def test_values_that_are_not_finite_stay_in_their_request(dtype, T, lengths):
+    b = make(10, T, 128, 96, 4, 8, 9, dtype, lengths, none=0.0)
+    if lengths == "ragged":
+        b["offsets"] = torch.tensor([0, 1, 20, 33, 33, 64, 65, 100, 140, T], dtype=torch.int32, device=DEV)
+        b["adapter"] = torch.tensor([0, 1, 2, 1, 3, 2, -1, 0, 1], dtype=torch.int32, device=DEV)
+    args = [b[k] for k in ("dy", "x", "W", "A", "B", "scale", "offsets", "adapter")]
+    fwd = lambda: api.adapter_forward(*[b[k] for k in ("x", "W", "bias", "A", "B", "scale", "offsets", "adapter")], keep=True)  # noqa: E731
+    clean, gclean = fwd(), api.adapter_backward(*args)
+    pair = pair_of(b)
+    # pair 2 holds values that are not finite: only rows of pair 2 may show it
+    b["A"][2, 1, 5], b["B"][2, 3, 0], b["scale"][2] = float("nan"), float("inf"), float("nan")
+    out, g = fwd(), api.adapter_backward(*args)
+    other = torch.from_numpy(pair != 2).to(DEV)
+    assert torch.equal(out.y[other], clean.y[other]) and torch.equal(out.v[other], clean.v[other])
+    assert torch.equal(g.dx[other], gclean.dx[other])
+    for a in (0, 1, 3):
+        assert torch.equal(g.dA[a], gclean.dA[a]) and torch.equal(g.dB[a], gclean.dB[a]), a
+    assert bool(out.y[~other].isnan().any())
+    # a row of pair 2 that is not finite: other rows, and gradients of other pairs, stay
+    row = int(np.flatnonzero(pair == 2)[0])
+    b["x"][row, 3], b["dy"][row, 7] = float("inf"), float("nan")
+    out, g = fwd(), api.adapter_backward(*args)
+    assert torch.equal(out.y[other], clean.y[other])
+    assert torch.equal(g.dx[other], gclean.dx[other])
+    for a in (0, 1, 3):
+        assert torch.equal(g.dA[a], gclean.dA[a]) and torch.equal(g.dB[a], gclean.dB[a]), a
+
+
+@pytest.mark.parametrize("T", [12, 190])
+def test_gradients_against_differences(T):
+    """L = sum(dy * y) is linear in x, in A and in B apart, so a wide difference quotient is exact but for rounding."""
+    b = make(11, T, 96, 72, 3, 6, 5, "f32", none=0.1)
+    g = api.adapter_backward(*[b[k] for k in ("dy", "x", "W", "A", "B", "scale", "offsets", "adapter")])
+
+    def loss(**over):
+        d = dict(b, **over)
+        y = api.adapter_forward(*[d[k] for k in ("x", "W", "bias", "A", "B", "scale", "offsets", "adapter")]).y
+        return float((y.double() * b["dy"].double()).sum())
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    for name, grad in (("x", g.dx), ("A", g.dA), ("B", g.dB)):
+        for _ in range(3):
+            step = torch.randn(b[name].shape, generator=gen, device=DEV)
+            quotient = (loss(**{name: b[name] + step}) - loss(**{name: b[name] - step})) / 2
+            inner = float((grad.double() * step.double()).sum())
+            # rounding of two losses of T N float32 terms (2^-24 each, added with random signs) and of x +- step
+            size = float((b["dy"].double().norm() * T ** 0.5 * 72 ** 0.5) * 8)
+            assert abs(quotient - inner) <= 2.0 ** -20 * size, (name, quotient, inner, size)
+
+
+def test_optional_outputs():
+    b = make(12, 90, 64, 56, 3, 8, 4, "bf16")
+    args = [b[k] for k in ("dy", "x", "W", "A", "B", "scale", "offsets", "adapter")]
+    full = api.adapter_backward(*args)
+    only_dx = api.adapter_backward(*args, want_pairs=False)
+    only_pairs = api.adapter_backward(*args, want_dx=False)
+    assert only_dx.dA is None and only_dx.dB is None and torch.equal(only_dx.dx, full.dx)
+    assert only_pairs.dx is None and torch.equal(only_pairs.dA, full.dA) and torch.equal(only_pairs.dB, full.dB)
+
+
+@pytest.mark.parametrize("T,dtype", [(1, "bf16"), (33, "f32"), (300, "f16")])
+def test_graph_replays_and_side_stream(T, dtype):
+    """Captured once and replayed on new rows, with eager calls between; and on a stream of its own."""
+    b = make(13, T, 128, 104, 4, 8, min(T, 5), dtype)
+    names = ("x", "W", "bias", "A", "B", "scale", "offsets", "adapter")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+
+    def both():
+        out = api.adapter_forward(*[b[k] for k in names], keep=True)
+        return out, api.adapter_backward(*[b[k] for k in ("dy",) + tuple(n for n in names if n != "bias")], v=out.v)
+    with torch.cuda.stream(side):
+        out_side, g_side = both()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    eager, g_eager = both()
+    assert torch.equal(out_side.y, eager.y) and torch.equal(g_side.dA, g_eager.dA)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, g = both()
+    for k in range(3):
+        b["x"].copy_(torch.randn(T, 128, generator=torch.Generator().manual_seed(k)).to(DT[dtype]))
+        b["dy"].copy_(torch.randn(T, 104, generator=torch.Generator().manual_seed(90 + k)).to(DT[dtype]))
+        ref, gref = both()
+        torch.cuda.synchronize()
+        for t in (out.y, out.v, g.dx, g.dA, g.dB):
+            t.fill_(3)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, c in ((out.y, ref.y), (out.v, ref.v), (g.dx, gref.dx), (g.dA, gref.dA), (g.dB, gref.dB)):
+            assert torch.equal(a, c), (T, dtype, k)
+    del graph
+
+
+def test_binding_refuses():
+    b = make(14, 20, 64, 48, 3, 4, 4, "bf16")
+    names = ("x", "W", "bias", "A", "B", "scale", "offsets", "adapter")
+
+    def call(**over):
+        d = dict(b, **over)
+        return api.adapter_forward(*[d[k] for k in names])
+    call()
+    for over in (dict(x=b["x"].cpu()), dict(x=b["x"].double()), dict(W=b["W"].float()), dict(W=b["W"][:, :-1]),
+                 dict(x=b["x"].t()), dict(bias=b["bias"].double()), dict(bias=b["bias"][:-1]), dict(A=b["A"][0]),
+                 dict(B=b["B"][:, :, :-1]), dict(scale=b["scale"][:-1]), dict(offsets=b["offsets"].long()),
+                 dict(offsets=b["offsets"][:-1]), dict(adapter=b["adapter"][:, None])):
+        with pytest.raises(ValueError):
+            call(**over)
+    with pytest.raises(ValueError):
+        api.adapter_backward(b["dy"][:, :-1], *[b[k] for k in ("x", "W", "A", "B", "scale", "offsets", "adapter")])
+    with pytest.raises(ValueError):
+        api.adapter_backward(b["dy"], *[b[k] for k in ("x", "W", "A", "B", "scale", "offsets", "adapter")],
+                             v=torch.zeros(20, 4, dtype=torch.bfloat16, device=DEV))
