@@ -529,18 +529,17 @@ size_t lipcache_adapter_backward_workspace_bytes(int64_t T, int32_t K, int32_t N
  * X becomes s (a + b s^2 + c s^4).  (3.4445, -4.775, 2.0315) brings them to
  * about [0.7, 1.2] in five steps; (15/8, -10/8, 3/8) converges to 1.
  *
- * The products run on the matrix cores with float16 operands; float32 and
- * float16 results take each operand as a sum of two float16 numbers (22
- * bits).  Operands are scaled by powers of two that no value can overflow:
- * the bound of the singular values, worked out from the coefficients on the
- * host, must stay below 16 (else EUNSUPPORTED).
+ * The products run on the matrix cores with float32 sums; each operand is a
+ * sum of two float16 numbers (22 bits).  Operands are scaled by powers of two
+ * that no value can overflow: the bound of the singular values, worked out
+ * from the coefficients on the host, must stay below 16 (else EUNSUPPORTED).
  *
  *  G, out [batch][m][n] contiguous, batch >= 0, 1 <= m, n, min(m, n) <= 16384,
  *         m n <= 2^30; out may be G
  *  steps  0 <= steps <= 32;  coef (host) [steps][3];  eps (host) >= 0
  *  ws     lipcache_orthogonalise_workspace_bytes(batch, m, n, dtype) bytes
- * A zero matrix gives zeros (with eps > 0); one that holds a NaN or an
- * infinity gives NaN throughout, and leaves the others of the batch alone. (async)
+ * A zero matrix gives zeros; one that holds a NaN or an infinity gives NaN
+ * throughout (with steps > 0), and leaves the others of the batch alone. (async)
  */
 lipcache_status lipcache_orthogonalise(const void* G, int64_t batch, int32_t m, int32_t n,
                                        int32_t dtype, int32_t steps, const float* coef, float eps,
@@ -565,6 +564,9 @@ typedef struct lipcache_muon {
  * One optimiser step of `batch` matrices, in place:
  *   M <- mu M + G,   U = mu M + G (nesterov) or M,   O = orthogonalise(U),
  *   W <- (1 - lr weight_decay) W - lr scale O.
+ * For 16-bit W the products behind O take one float16 number an operand: O is
+ * then within 2e-3 to 4e-3 of its norm, and what that moves W by lies below
+ * W's own rounding unless the step is as large as W.
  * Every singular value of O is at most the last step's bound (1.21 for the
  * coefficients above), so sigma_max(W) moves by at most 1.21 lr scale and
  * the decay: what the certified radii are divided by stays known.

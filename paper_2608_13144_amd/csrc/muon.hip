@@ -3,58 +3,328 @@
 #include <math.h>
 
 #include "lc_common.hpp"
-#include "lc_tile.hpp"
+#include "lc_mfma.hpp"
 
 namespace lc {
 
-// ||U||_F of matrix z: float64 sums in a fixed order, one workgroup a matrix.
-// With a momentum (kStep) U is formed first: M <- mu M + G, U = mu M + G or M.
+// X, P = X X^T (or X^T X) and B = b P + c P^2 go to the matrix cores as float16
+// numbers, or as sums of two (22 bits), each times a power of two that keeps
+// the largest possible entry below 2^15; the sums of the products are float32.
+//
+// Where they are single float16 numbers, X's rounding is kept in a second array
+// and comes in with the term a X.  Small singular values grow by a = 3.4 a step
+// through that term alone, and what is lost of X there is lost of them: 2e-2
+// of the result for a matrix of a few strong directions over noise, 5e-4 with
+// the second array.
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+
+template <typename T>
+__device__ __forceinline__ float ns_load(const T* p) { return static_cast<float>(*p); }
+template <typename T>
+__device__ __forceinline__ T ns_round(float v) { return static_cast<T>(v); }  // to nearest even
+
+// U of element i: G itself, or the momentum's direction (M already updated
+// when kUpdate is false).
+template <typename T, bool kStep, bool kUpdate>
+__device__ __forceinline__ float ns_direction(const T* __restrict__ G, float* __restrict__ M, int64_t i, float mu,
+                                              int nesterov) {
+  float u = ns_load(G + i);
+  if constexpr (kStep) {
+    float m = M[i];
+    if constexpr (kUpdate) {
+      m = fmaf(mu, m, u);
+      M[i] = m;
+    }
+    u = nesterov ? fmaf(mu, m, u) : m;
+  }
+  return u;
+}
+
+// Eight directions from element i on; whole vectors where `wide` (i and the arrays are aligned for them), else up to
+// `count` of them one by one (the rest 0).
+template <typename T, bool kStep, bool kUpdate>
+__device__ __forceinline__ void ns_direction8(const T* __restrict__ G, float* __restrict__ M, int64_t i, int count,
+                                              bool wide, float mu, int nesterov, float (&u)[8]) {
+  if (wide) {
+    typedef T vec __attribute__((ext_vector_type(8)));
+    const vec g = *reinterpret_cast<const vec*>(G + i);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = static_cast<float>(g[e]);
+    if constexpr (kStep) {
+      f32x4 m[2] = {reinterpret_cast<const f32x4*>(M + i)[0], reinterpret_cast<const f32x4*>(M + i)[1]};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float v = m[e / 4][e % 4];
+        if constexpr (kUpdate) v = fmaf(mu, v, u[e]);
+        m[e / 4][e % 4] = v;
+        u[e] = nesterov ? fmaf(mu, v, u[e]) : v;
+      }
+      if constexpr (kUpdate) {
+        reinterpret_cast<f32x4*>(M + i)[0] = m[0];
+        reinterpret_cast<f32x4*>(M + i)[1] = m[1];
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = e < count ? ns_direction<T, kStep, kUpdate>(G, M, i + e, mu, nesterov) : 0.0f;
+  }
+}
+
+// Workgroups that sum one matrix's norm: 4096 elements each (two vectors a thread) up to 1024 of them.
+__host__ __device__ inline int ns_chunks(int64_t size) {
+  const int64_t c = (size + 4095) / 4096;
+  return c < 1024 ? static_cast<int>(c) : 1024;
+}
+
+// Partial sums of U^2 in float64, in a fixed order; updates the momentum.
 template <typename T, bool kStep>
 __global__ __launch_bounds__(256) void ns_norm_kernel(const T* __restrict__ G, float* __restrict__ M, int64_t size,
-                                                      float mu, int nesterov, float* __restrict__ X,
-                                                      double* __restrict__ norm2) {
-  __shared__ double part[256 / kWave];
-  const int64_t z = blockIdx.x;
+                                                      float mu, int nesterov, int wide, double* __restrict__ part) {
+  __shared__ double wave_part[256 / kWave];
+  const int64_t z = blockIdx.y;
   double sum = 0.0;
-  for (int64_t i = threadIdx.x; i < size; i += 256) {
-    float u = load_f32(G + z * size + i);
-    if constexpr (kStep) {
-      const float m = fmaf(mu, M[z * size + i], u);
-      M[z * size + i] = m;
-      u = nesterov ? fmaf(mu, m, u) : m;
-    }
-    X[z * size + i] = u;
-    sum += static_cast<double>(u) * static_cast<double>(u);
+#pragma unroll 2
+  for (int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8; i < size;
+       i += 2048 * static_cast<int64_t>(gridDim.x)) {
+    float u[8];
+    ns_direction8<T, kStep, true>(G, M, z * size + i, size - i < 8 ? static_cast<int>(size - i) : 8, wide != 0, mu, nesterov, u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += static_cast<double>(u[e]) * static_cast<double>(u[e]);
   }
   sum = wave_sum(sum);
-  if (lane_id() == 0) part[threadIdx.x / kWave] = sum;
+  if (lane_id() == 0) wave_part[threadIdx.x / kWave] = sum;
   __syncthreads();
-  if (threadIdx.x == 0) norm2[z] = ((part[0] + part[1]) + part[2]) + part[3];
+  if (threadIdx.x == 0)
+    part[z * gridDim.x + blockIdx.x] = ((wave_part[0] + wave_part[1]) + wave_part[2]) + wave_part[3];
 }
 
-// X_0 = U / (||U||_F + eps), transposed to p x q with p <= q.
-__global__ __launch_bounds__(256) void ns_scale_kernel(const float* __restrict__ U, int m, int n,
-                                                       const double* __restrict__ norm2, float eps,
-                                                       float* __restrict__ X) {
-  const int64_t size = static_cast<int64_t>(m) * n, z = blockIdx.y;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= size) return;
-  const double f = sqrt(norm2[z]) + static_cast<double>(eps);
-  const int64_t row = i / n, col = i % n;
-  X[z * size + (m > n ? col * m + row : i)] = static_cast<float>(static_cast<double>(U[z * size + i]) / f);
+// 1 / (||U||_F + eps) from the partial sums; every thread of the workgroup gets it.
+__device__ __forceinline__ double ns_inverse(const double* __restrict__ part, int chunks, float eps, double* lds) {
+  if (threadIdx.x < kWave) {
+    double sum = 0.0;
+    for (int c = threadIdx.x; c < chunks; c += kWave) sum += part[c];
+    sum = wave_sum(sum);
+    if (threadIdx.x == 0) *lds = sum;
+  }
+  __syncthreads();
+  const double f = sqrt(*lds) + static_cast<double>(eps);
+  return f > 0.0 || f != f ? 1.0 / f : 0.0;
 }
 
-// The result (transposed back), rounded; or the update of W.
+// Element (i, j) of a matrix of _Float16 or Split numbers with `width` columns.
+template <class E>
+struct NsAt;
+template <>
+struct NsAt<_Float16> {
+  static constexpr int kPad = 8;  // widths and heights are multiples of this
+  static constexpr bool kLow = true;  // X's rounding is kept apart, for the term a X
+  static __device__ __forceinline__ int64_t at(int64_t i, int j, int width) { return i * width + j; }
+  static __device__ __forceinline__ float get(const _Float16* p) { return static_cast<float>(*p); }
+  static __device__ __forceinline__ void put(_Float16* p, float v) { *p = static_cast<_Float16>(v); }
+  static __device__ __forceinline__ void put4(_Float16* p, f32x4 v) {
+    f16x4 h;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = static_cast<_Float16>(v[e]);
+    *reinterpret_cast<f16x4*>(p) = h;
+  }
+};
+template <>
+struct NsAt<Split> {
+  static constexpr int kPad = 32;
+  static constexpr bool kLow = false;
+  static __device__ __forceinline__ int64_t at(int64_t i, int j, int width) {
+    return i * (2 * width) + (j & ~31) * 2 + (j & 31);
+  }
+  static __device__ __forceinline__ float get(const _Float16* p) {
+    return static_cast<float>(p[0]) + static_cast<float>(p[32]);
+  }
+  static __device__ __forceinline__ void put(_Float16* p, float v) {
+    split_f16(v, p[0], p[32]);
+  }
+  static __device__ __forceinline__ void put4(_Float16* p, f32x4 v) {
+    f16x4 h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      _Float16 first, second;
+      split_f16(v[e], first, second);
+      h[e] = first;
+      l[e] = second;
+    }
+    *reinterpret_cast<f16x4*>(p) = h;
+    *reinterpret_cast<f16x4*>(p + 32) = l;
+  }
+};
+
+// X_0 = U / (||U||_F + eps) on m8 x n8 (zero past m x n), scaled; eight columns a thread.
+template <class E, typename T, bool kStep>
+__global__ __launch_bounds__(256) void ns_start_kernel(const T* __restrict__ G, float* __restrict__ M, int m, int n,
+                                                       int m8, int n8, float mu, int nesterov, int wide,
+                                                       const double* __restrict__ part, int chunks, float eps,
+                                                       float scale, _Float16* __restrict__ X,
+                                                       _Float16* __restrict__ Xlow) {
+  __shared__ double lds;
+  const int64_t z = blockIdx.y, size = static_cast<int64_t>(m) * n, groups = static_cast<int64_t>(m8) * n8 / 8;
+  const float f = static_cast<float>(ns_inverse(part + z * chunks, chunks, eps, &lds) * scale);
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < groups; i += 256 * static_cast<int64_t>(gridDim.x)) {
+    const int row = static_cast<int>(i / (n8 / 8)), col = static_cast<int>(i % (n8 / 8)) * 8;
+    float u[8] = {};
+    if (row < m && col < n)
+      ns_direction8<T, kStep, false>(G, M, z * size + static_cast<int64_t>(row) * n + col, n - col, wide != 0, mu, nesterov, u);
+    f32x4 lo, hi;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      lo[e] = f * u[e];
+      hi[e] = f * u[e + 4];
+    }
+    const int64_t at = NsAt<E>::at(z * m8 + row, col, n8);
+    if constexpr (NsAt<E>::kLow) {
+      f16x8 first, second;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        _Float16 p, r;
+        split_f16(f * u[e], p, r);
+        first[e] = p;
+        second[e] = r;
+      }
+      *reinterpret_cast<f16x8*>(X + at) = first;
+      *reinterpret_cast<f16x8*>(Xlow + at) = second;
+    } else {
+      NsAt<E>::put4(X + at, lo);
+      NsAt<E>::put4(X + at + 4, hi);
+    }
+  }
+}
+
+// No steps at all: the normalised matrix itself.
 template <typename T, bool kStep>
-__global__ __launch_bounds__(256) void ns_out_kernel(const float* __restrict__ X, int m, int n, float keep, float gain,
-                                                     T* __restrict__ out) {
-  const int64_t size = static_cast<int64_t>(m) * n, z = blockIdx.y;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= size) return;
-  const int64_t row = i / n, col = i % n;
-  const float o = X[z * size + (m > n ? col * m + row : i)];
-  T* p = out + z * size + i;
-  *p = round_to<T>(kStep ? fmaf(keep, load_f32(p), -gain * o) : o);
+__global__ __launch_bounds__(256) void ns_plain_kernel(const T* G, float* __restrict__ M, int64_t size, float mu,
+                                                       int nesterov, const double* __restrict__ part, int chunks,
+                                                       float eps, float keep, float gain, T* out) {
+  __shared__ double lds;
+  const int64_t z = blockIdx.y;
+  const double f = ns_inverse(part + z * chunks, chunks, eps, &lds);
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < size; i += 256 * static_cast<int64_t>(gridDim.x)) {
+    const float o = static_cast<float>(f * ns_direction<T, kStep, false>(G, M, z * size + i, mu, nesterov));
+    T* p = out + z * size + i;
+    *p = ns_round<T>(kStep ? fmaf(keep, ns_load(p), -gain * o) : o);
+  }
+}
+
+// A symmetric product: out = f_sum F F^T + f_in in  (F p8 x k8 "row", or k8 x p8 "col" with rows of `width`), the
+// lower tiles computed and mirrored.
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void ns_square_kernel(const _Float16* __restrict__ F, int p8, int k8,
+                                                                int width, const _Float16* __restrict__ in,
+                                                                float f_sum, float f_in, _Float16* __restrict__ out) {
+  typedef NsAt<typename S::E> At;
+  __shared__ __align__(16) char lds[S::kLds];
+  const int rows = (p8 + S::BM - 1) / S::BM, tiles = rows * (rows + 1) / 2;
+  const int all = xcd_order(static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x));
+  const int64_t z = all / tiles;
+  const int t = all % tiles;
+  int bi = static_cast<int>((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+  while ((bi + 1) * (bi + 2) / 2 <= t) ++bi;
+  while (bi * (bi + 1) / 2 > t) --bi;
+  const int bj = t - bi * (bi + 1) / 2;
+  const int i0 = bi * S::BM, j0 = bj * S::BN;
+  Side P{}, Q{};
+  P.p = F + (S::PCOL ? At::at(z * k8, i0, width) : At::at(z * p8 + i0, 0, width));
+  Q.p = F + (S::QCOL ? At::at(z * k8, j0, width) : At::at(z * p8 + j0, 0, width));
+  P.ld = Q.ld = static_cast<int64_t>(width) * sizeof(typename S::E);
+  P.rows = p8 - i0 < S::BM ? p8 - i0 : S::BM;
+  Q.rows = p8 - j0 < S::BN ? p8 - j0 : S::BN;
+  f32x16 acc[S::TM][S::TN] = {};
+  tile_products<S>(P, Q, k8, lds, acc);
+  tile_store<S>(acc, [&](int i, int j, const f32x16& v) {
+    i += i0;
+    j += j0;
+    if (j >= p8) return;
+    float add[16];
+    if (in) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int row = i + acc_row(e) < p8 ? i + acc_row(e) : p8 - 1;
+        add[e] = At::get(in + At::at(z * p8 + row, j, p8));
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (i + 8 * q >= p8) break;  // p8 is a multiple of 8, so four rows stand or fall together
+      f32x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        o[e] = f_sum * v[4 * q + e];
+        if (in) o[e] = fmaf(f_in, add[4 * q + e], o[e]);
+        At::put(out + At::at(z * p8 + i + 8 * q + e, j, p8), o[e]);
+      }
+      if (bi != bj) At::put4(out + At::at(z * p8 + j, i + 8 * q, p8), o);
+    }
+  });
+}
+
+// Where the result of the last step goes: [m][n], rounded, or subtracted from W.
+template <typename T>
+struct NsOut {
+  T* out;
+  int m, n;
+  float keep, gain;
+};
+
+// X' = a X + B X (wide: P = B, Q = X "col") or a X + X B (tall: P = X, Q = B).
+template <class S, bool kWide, bool kLast, typename T, bool kStep>
+__global__ __launch_bounds__(S::kThreads) void ns_apply_kernel(const _Float16* __restrict__ X,
+                                                               const _Float16* __restrict__ B, int m8, int n8,
+                                                               float f_sum, float f_x,
+                                                               const _Float16* __restrict__ Xlow,
+                                                               _Float16* __restrict__ Y, _Float16* __restrict__ Ylow,
+                                                               NsOut<T> o) {
+  typedef NsAt<typename S::E> At;
+  __shared__ __align__(16) char lds[S::kLds];
+  const int p8 = kWide ? m8 : n8;
+  int bi, bj;
+  const int64_t z = tile_of((m8 + S::BM - 1) / S::BM, (n8 + S::BN - 1) / S::BN, bi, bj);
+  const int i0 = bi * S::BM, j0 = bj * S::BN;
+  Side P{}, Q{};
+  if constexpr (kWide) {
+    P.p = B + At::at(z * p8 + i0, 0, p8);
+    Q.p = X + At::at(z * m8, j0, n8);
+  } else {
+    P.p = X + At::at(z * m8 + i0, 0, n8);
+    Q.p = B + At::at(z * p8 + j0, 0, p8);
+  }
+  P.ld = static_cast<int64_t>(kWide ? p8 : n8) * sizeof(typename S::E);
+  Q.ld = static_cast<int64_t>(kWide ? n8 : p8) * sizeof(typename S::E);
+  P.rows = m8 - i0 < S::BM ? m8 - i0 : S::BM;
+  Q.rows = n8 - j0 < S::BN ? n8 - j0 : S::BN;
+  f32x16 acc[S::TM][S::TN] = {};
+  tile_products<S>(P, Q, p8, lds, acc);
+  tile_store<S>(acc, [&](int i, int j, const f32x16& v) {
+    i += i0;
+    j += j0;
+    if (j >= n8) return;
+    float x[16], w[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int row = i + acc_row(e) < m8 ? i + acc_row(e) : m8 - 1;
+      x[e] = At::get(X + At::at(z * m8 + row, j, n8));
+      if constexpr (At::kLow) x[e] += static_cast<float>(Xlow[At::at(z * m8 + row, j, n8)]);
+      if constexpr (kLast && kStep)
+        w[e] = ns_load(o.out + (z * o.m + (row < o.m ? row : o.m - 1)) * o.n + (j < o.n ? j : o.n - 1));
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int row = i + acc_row(e);
+      const float y = fmaf(f_x, x[e], f_sum * v[e]);
+      if constexpr (kLast) {
+        if (row < o.m && j < o.n)
+          o.out[(z * o.m + row) * o.n + j] = ns_round<T>(kStep ? fmaf(o.keep, w[e], -o.gain * y) : y);
+      } else if (row < m8) {
+        const int64_t at = At::at(z * m8 + row, j, n8);
+        if constexpr (At::kLow) split_f16(y, Y[at], Ylow[at]);
+        else At::put(Y + at, y);
+      }
+    }
+  });
 }
 
 struct NsArgs {
@@ -64,59 +334,176 @@ struct NsArgs {
   float eps;
 };
 
-size_t ns_workspace(int64_t batch, int32_t m, int32_t n) {
-  const size_t p = m < n ? m : n, b = static_cast<size_t>(batch);
-  return align_up(b * 8, 256) + 2 * align_up(b * m * n * 4, 256) + 2 * align_up(b * p * p * 4, 256);
+double ns_bound(double a, double b, double c, double h);
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline int round_up(int v, int to) { return (v + to - 1) / to * to; }
+
+// A step takes its orthogonalised direction with 11-bit operands where W has 16 bits: the direction's relative
+// error, 2e-3 (measured against float64), is below W's own rounding unless the step is as large as W.  Results that
+// are the direction itself, and float32 parameters, take 22-bit operands.
+inline bool ns_split(int32_t dtype, bool step) { return !step || dtype == LIPCACHE_F32; }
+
+size_t ns_workspace(int64_t batch, int32_t m, int32_t n, bool split) {
+  const int pad = split ? 32 : 8;
+  const size_t b = static_cast<size_t>(batch), mp = round_up(m, pad), np = round_up(n, pad), p = mp < np ? mp : np,
+               e = split ? 4 : 2;
+  return align_up(b * ns_chunks(static_cast<int64_t>(m) * n) * 8, 256) + 2 * align_up(b * mp * np * e, 256) + (split ? 0 : 2 * align_up(b * mp * np * 2, 256)) +
+         2 * align_up(b * p * p * e, 256);
 }
 
-template <typename T, bool kStep>
-lipcache_status ns_run(const NsArgs& g, const void* G, float* M, float mu, int nesterov, float keep, float gain,
-                       void* out, void* ws, hipStream_t s) {
-  const int64_t p = g.m < g.n ? g.m : g.n, q = g.m < g.n ? g.n : g.m, size = p * q;
-  const size_t b = static_cast<size_t>(g.batch);
-  char* w = static_cast<char*>(ws);
-  double* norm2 = reinterpret_cast<double*>(w);
-  w += align_up(b * 8, 256);
-  float* X = reinterpret_cast<float*>(w);
-  w += align_up(b * size * 4, 256);
-  float* Y = reinterpret_cast<float*>(w);
-  w += align_up(b * size * 4, 256);
-  float* P = reinterpret_cast<float*>(w);
-  w += align_up(b * p * p * 4, 256);
-  float* Q = reinterpret_cast<float*>(w);
-  const unsigned nb = static_cast<unsigned>(g.batch);
-  ns_norm_kernel<T, kStep><<<nb, 256, 0, s>>>(static_cast<const T*>(G), M, size, mu, nesterov, Y, norm2);
-  LC_LAUNCHED();
-  const dim3 grid(static_cast<unsigned>((size + 255) / 256), nb);
-  ns_scale_kernel<<<grid, 256, 0, s>>>(Y, g.m, g.n, norm2, g.eps, X);
-  LC_LAUNCHED();
+inline int64_t tiles_of(int rows, int side) { return (rows + side - 1) / side; }
+
+// Tile sizes.  Small products want many small tiles, large ones the arithmetic intensity of large tiles:
+//   64    64 x 64, three workgroups a CU                       below 128 tiles of 128 x 128
+//   128d  128 x 128, one workgroup of 8 waves, 4 steps ahead   128 to 319 such tiles (about one a CU)
+//   128   128 x 128, two workgroups of 4 waves a CU            from there
+//   192, 256  one workgroup a CU, where their tiles fill at least 4/5 of the rounds of 256 CUs
+// One step of a square matrix in us (P, P^2, X'; 22-bit operands): 1536 wide 26 + 27 + 39 with 64, 32 + 35 + 35
+// with 128d, 40 + 43 + 43 with 128; 2048 wide 48 + 49 + 67, 46 + 47 + 53, 51 + 54 + 61; four of 2048: 140 + 141 + 243,
+// 135 + 139 + 200, 131 + 135 + 189.  4096 wide (11 bits): P 81 with 192, X' 133 with 256, against 100 and 150 with 128.
+enum NsTile { kNs64, kNs128Deep, kNs128, kNs192, kNs256 };
+
+inline bool fills_chip(int64_t tiles) { return 5 * tiles >= 4 * 256 * ((tiles + 255) / 256); }
+
+inline NsTile ns_tile(int64_t tiles128, int64_t large, NsTile large_tile) {
+  if (tiles128 < 128) return kNs64;
+  if (large > 0 && fills_chip(large)) return large_tile;
+  return tiles128 < 320 ? kNs128Deep : kNs128;
+}
+
+struct NsPlan {
+  int m8, n8;
+  unsigned nb;
+  hipStream_t s;
+
+  template <class S>
+  void square_with(const _Float16* F, int k8, int width, const _Float16* in, double f_sum, double f_in, _Float16* out) const {
+    const int p8 = m8 < n8 ? m8 : n8;
+    const unsigned t = static_cast<unsigned>(tiles_of(p8, S::BM));
+    ns_square_kernel<S><<<t * (t + 1) / 2 * nb, S::kThreads, 0, s>>>(F, p8, k8, width, in, static_cast<float>(f_sum),
+                                                                    static_cast<float>(f_in), out);
+  }
+  // out = f_sum F F^T + f_in in
+  template <class E, bool kCol>
+  void square(const _Float16* F, int k8, int width, const _Float16* in, double f_sum, double f_in, _Float16* out) const {
+    const int p8 = m8 < n8 ? m8 : n8;
+    const int64_t t128 = tiles_of(p8, 128), t192 = tiles_of(p8, 192);
+    switch (ns_tile(t128 * (t128 + 1) / 2 * nb, kCol ? 0 : t192 * (t192 + 1) / 2 * nb, kNs192)) {
+      case kNs64: return square_with<TileShape<E, 64, 64, 2, 2, 1, 3, 1, kCol, kCol>>(F, k8, width, in, f_sum, f_in, out);
+      case kNs128Deep: return square_with<TileShape<E, 128, 128, 2, 4, 1, 4, 1, kCol, kCol>>(F, k8, width, in, f_sum, f_in, out);
+      case kNs192:
+        if constexpr (!kCol) return square_with<TileShape<E, 192, 192, 2, 2, 1, 2, 1, false, false>>(F, k8, width, in, f_sum, f_in, out);
+        [[fallthrough]];
+      default: return square_with<TileShape<E, 128, 128, 2, 2, 1, 2, 1, kCol, kCol>>(F, k8, width, in, f_sum, f_in, out);
+    }
+  }
+
+  template <class S, bool kWide, bool kLast, typename T, bool kStep>
+  void apply_with(const _Float16* X, const _Float16* B, double f_sum, double f_x, const _Float16* Xl, _Float16* Y,
+             _Float16* Yl, const NsOut<T>& o) const {
+    const unsigned tiles = static_cast<unsigned>(tiles_of(m8, S::BM) * tiles_of(n8, S::BN));
+    ns_apply_kernel<S, kWide, kLast, T, kStep><<<tiles * nb, S::kThreads, 0, s>>>(
+        X, B, m8, n8, static_cast<float>(f_sum), static_cast<float>(f_x), Xl, Y, Yl, o);
+  }
+  // Y (or the result) = f_sum B X + f_x X, or f_sum X B + f_x X
+  template <class E, bool kWide, bool kLast, typename T, bool kStep>
+  void apply(const _Float16* X, const _Float16* B, double f_sum, double f_x, const _Float16* Xl, _Float16* Y,
+             _Float16* Yl, const NsOut<T>& o) const {
+    constexpr bool kLarge = __is_same(E, _Float16);  // the fragments of 22-bit operands do not fit beside 256 x 256 sums
+    switch (ns_tile(tiles_of(m8, 128) * tiles_of(n8, 128) * nb,
+                    kLarge ? tiles_of(m8, 256) * tiles_of(n8, 256) * nb : 0, kNs256)) {
+      case kNs64: return apply_with<TileShape<E, 64, 64, 2, 2, 1, 3, 1, false, kWide>, kWide, kLast, T, kStep>(X, B, f_sum, f_x, Xl, Y, Yl, o);
+      case kNs128Deep: return apply_with<TileShape<E, 128, 128, 2, 4, 1, 4, 1, false, kWide>, kWide, kLast, T, kStep>(X, B, f_sum, f_x, Xl, Y, Yl, o);
+      case kNs256:
+        if constexpr (kLarge) return apply_with<TileShape<E, 256, 256, 2, 4, 1, 2, 1, false, kWide>, kWide, kLast, T, kStep>(X, B, f_sum, f_x, Xl, Y, Yl, o);
+        [[fallthrough]];
+      default: return apply_with<TileShape<E, 128, 128, 2, 2, 1, 2, 1, false, kWide>, kWide, kLast, T, kStep>(X, B, f_sum, f_x, Xl, Y, Yl, o);
+    }
+  }
+};
+
+template <class E, bool kWide, typename T, bool kStep>
+lipcache_status ns_products(const NsArgs& g, double sx, _Float16* X, _Float16* Xl, _Float16* Y, _Float16* Yl, _Float16* A, _Float16* B, float keep,
+                            float gain, T* out, hipStream_t s) {
+  constexpr int kPad = NsAt<E>::kPad;
+  const int m8 = round_up(g.m, kPad), n8 = round_up(g.n, kPad), p8 = kWide ? m8 : n8, q8 = kWide ? n8 : m8;
+  // powers of two: the largest entry of X is at most the bound h of its singular values, of P h^2, of B |b| h^2 + |c| h^4
+  double h = 1.0, top_x = 1.0, top_b = 1e-30;
   for (int k = 0; k < g.steps; ++k) {
-    const float ca = g.coef[3 * k], cb = g.coef[3 * k + 1], cc = g.coef[3 * k + 2];
-    LC_HIP(tile_product(
-        p, p, q, static_cast<int>(nb), [=] __device__(int z, int64_t i, int64_t k_) { return X[z * size + i * q + k_]; },
-        [=] __device__(int z, int64_t j, int64_t k_) { return X[z * size + j * q + k_]; },
-        [=] __device__(int z, int64_t i, int64_t j, float sum) { P[(z * p + i) * p + j] = sum; }, s));
-    LC_HIP(tile_product(
-        p, p, p, static_cast<int>(nb), [=] __device__(int z, int64_t i, int64_t k_) { return P[(z * p + i) * p + k_]; },
-        [=] __device__(int z, int64_t j, int64_t k_) { return P[(z * p + j) * p + k_]; },
-        [=] __device__(int z, int64_t i, int64_t j, float sum) {
-          Q[(z * p + i) * p + j] = fmaf(cc, sum, cb * P[(z * p + i) * p + j]);
-        },
-        s));
-    LC_HIP(tile_product(
-        p, q, p, static_cast<int>(nb), [=] __device__(int z, int64_t i, int64_t k_) { return Q[(z * p + i) * p + k_]; },
-        [=] __device__(int z, int64_t j, int64_t k_) { return X[z * size + k_ * q + j]; },
-        [=] __device__(int z, int64_t i, int64_t j, float sum) {
-          Y[z * size + i * q + j] = fmaf(ca, X[z * size + i * q + j], sum);
-        },
-        s));
-    float* t = X;
+    const double b = fabs(g.coef[3 * k + 1]), c = fabs(g.coef[3 * k + 2]);
+    top_b = fmax(top_b, b * h * h + c * h * h * h * h);
+    if (k + 1 < g.steps) h = ns_bound(g.coef[3 * k], g.coef[3 * k + 1], g.coef[3 * k + 2], h);
+    top_x = fmax(top_x, h);
+  }
+  const double sp = exp2(floor(log2(32768.0 / (top_x * top_x)))), sb = exp2(fmin(20.0, floor(log2(32768.0 / top_b))));
+  const NsPlan plan{m8, n8, static_cast<unsigned>(g.batch), s};
+  for (int k = 0; k < g.steps; ++k) {
+    const double a = g.coef[3 * k], b = g.coef[3 * k + 1], c = g.coef[3 * k + 2];
+    plan.square<E, !kWide>(X, q8, n8, nullptr, sp / (sx * sx), 0.0, A);
+    LC_LAUNCHED();
+    plan.square<E, false>(A, p8, p8, A, c * sb / (sp * sp), b * sb / sp, B);
+    LC_LAUNCHED();
+    if (k + 1 < g.steps)
+      plan.apply<E, kWide, false, float, false>(X, B, 1.0 / sb, a, Xl, Y, Yl, NsOut<float>{});
+    else
+      plan.apply<E, kWide, true, T, kStep>(X, B, 1.0 / (sb * sx), a / sx, Xl, nullptr, nullptr, NsOut<T>{out, g.m, g.n, keep, gain});
+    LC_LAUNCHED();
+    _Float16* t = X;
     X = Y;
     Y = t;
+    t = Xl;
+    Xl = Yl;
+    Yl = t;
   }
-  ns_out_kernel<T, kStep><<<grid, 256, 0, s>>>(X, g.m, g.n, keep, gain, static_cast<T*>(out));
-  LC_LAUNCHED();
   return LIPCACHE_OK;
+}
+
+template <class E, typename T, bool kStep>
+lipcache_status ns_run(const NsArgs& g, const void* G_, float* M, float mu, int nesterov, float keep, float gain,
+                       void* out_, void* ws, hipStream_t s) {
+  const T* G = static_cast<const T*>(G_);
+  T* out = static_cast<T*>(out_);
+  const int m8 = round_up(g.m, NsAt<E>::kPad), n8 = round_up(g.n, NsAt<E>::kPad);
+  const size_t b = static_cast<size_t>(g.batch), p8 = m8 < n8 ? m8 : n8;
+  const int64_t size = static_cast<int64_t>(g.m) * g.n, room = static_cast<int64_t>(m8) * n8;
+  const int chunks = ns_chunks(size);
+  char* w = static_cast<char*>(ws);
+  auto take = [&](size_t bytes) {
+    char* at = w;
+    w += align_up(bytes, 256);
+    return at;
+  };
+  double* part = reinterpret_cast<double*>(take(b * chunks * 8));
+  _Float16* X = reinterpret_cast<_Float16*>(take(b * room * sizeof(E)));
+  _Float16* Y = reinterpret_cast<_Float16*>(take(b * room * sizeof(E)));
+  const size_t low = NsAt<E>::kLow ? b * room * 2 : 0;
+  _Float16* Xl = reinterpret_cast<_Float16*>(take(low));
+  _Float16* Yl = reinterpret_cast<_Float16*>(take(low));
+  _Float16* A = reinterpret_cast<_Float16*>(take(b * p8 * p8 * sizeof(E)));
+  _Float16* B = reinterpret_cast<_Float16*>(take(b * p8 * p8 * sizeof(E)));
+  const unsigned nb = static_cast<unsigned>(g.batch);
+  const dim3 grid(chunks, nb);
+  const int wide = g.n % 8 == 0 && aligned16(G) && (!kStep || aligned16(M));
+  ns_norm_kernel<T, kStep><<<grid, 256, 0, s>>>(G, M, size, mu, nesterov, wide, part);
+  LC_LAUNCHED();
+  if (g.steps == 0) {
+    ns_plain_kernel<T, kStep><<<grid, 256, 0, s>>>(G, M, size, mu, nesterov, part, chunks, g.eps, keep, gain, out);
+    LC_LAUNCHED();
+    return LIPCACHE_OK;
+  }
+  double top_x = 1.0, h = 1.0;
+  for (int k = 0; k + 1 < g.steps; ++k) {
+    h = ns_bound(g.coef[3 * k], g.coef[3 * k + 1], g.coef[3 * k + 2], h);
+    top_x = fmax(top_x, h);
+  }
+  const double sx = exp2(floor(log2(32768.0 / top_x)));
+  const unsigned blocks = static_cast<unsigned>((room + 2047) / 2048 < 4096 ? (room + 2047) / 2048 : 4096);
+  ns_start_kernel<E, T, kStep><<<dim3(blocks, nb), 256, 0, s>>>(G, M, g.m, g.n, m8, n8, mu, nesterov, wide, part, chunks,
+                                                               g.eps, static_cast<float>(sx), X, Xl);
+  LC_LAUNCHED();
+  if (g.m <= g.n) return ns_products<E, true, T, kStep>(g, sx, X, Xl, Y, Yl, A, B, keep, gain, out, s);
+  return ns_products<E, false, T, kStep>(g, sx, X, Xl, Y, Yl, A, B, keep, gain, out, s);
 }
 
 // The largest |s (a + b s^2 + c s^4)| over 0 <= s <= h, in float64: at h or
@@ -163,12 +550,22 @@ bool ns_unaligned(const void* p, int32_t dtype) {
 }
 
 template <bool kStep>
+struct NsOperand {
+  typedef Split E;
+};
+template <>
+struct NsOperand<true> {
+  typedef _Float16 E;
+};
+
+template <bool kStep>
 lipcache_status ns_dispatch(const NsArgs& g, int32_t dtype, const void* G, float* M, float mu, int nesterov, float keep,
                             float gain, void* out, void* ws, hipStream_t s) {
+  typedef typename NsOperand<kStep>::E E16;  // as ns_split() says
   switch (dtype) {
-    case LIPCACHE_F32: return ns_run<float, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
-    case LIPCACHE_BF16: return ns_run<__bf16, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
-    default: return ns_run<_Float16, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
+    case LIPCACHE_F32: return ns_run<Split, float, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
+    case LIPCACHE_BF16: return ns_run<E16, __bf16, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
+    default: return ns_run<E16, _Float16, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
   }
 }
 
@@ -178,7 +575,7 @@ using namespace lc;
 
 extern "C" size_t lipcache_orthogonalise_workspace_bytes(int64_t batch, int32_t m, int32_t n, int32_t dtype) {
   if (batch < 0 || m < 1 || n < 1 || dtype < LIPCACHE_F32 || dtype > LIPCACHE_F16) return 0;
-  return ns_workspace(batch, m, n);
+  return ns_workspace(batch, m, n, ns_split(dtype, false));
 }
 
 extern "C" lipcache_status lipcache_orthogonalise(const void* G, int64_t batch, int32_t m, int32_t n, int32_t dtype,
@@ -186,14 +583,16 @@ extern "C" lipcache_status lipcache_orthogonalise(const void* G, int64_t batch, 
                                                   size_t ws_bytes, lipcache_stream_t stream) {
   if (lipcache_status st = ns_check(batch, m, n, dtype, steps, coef, eps); st != LIPCACHE_OK) return st;
   if (batch > 0 && (ns_unaligned(G, dtype) || ns_unaligned(out, dtype))) return LIPCACHE_EINVAL;
-  if (!ws || !aligned256(ws) || ws_bytes < ns_workspace(batch, m, n)) return LIPCACHE_EWORKSPACE;
+  if (!ws || !aligned256(ws) || ws_bytes < ns_workspace(batch, m, n, ns_split(dtype, false)))
+    return LIPCACHE_EWORKSPACE;
   if (batch == 0) return LIPCACHE_OK;
   const NsArgs g{batch, m, n, steps, coef, eps};
   return ns_dispatch<false>(g, dtype, G, nullptr, 0.0f, 0, 0.0f, 0.0f, out, ws, stream);
 }
 
 extern "C" size_t lipcache_muon_step_workspace_bytes(int64_t batch, int32_t m, int32_t n, int32_t dtype) {
-  return lipcache_orthogonalise_workspace_bytes(batch, m, n, dtype);
+  if (batch < 0 || m < 1 || n < 1 || dtype < LIPCACHE_F32 || dtype > LIPCACHE_F16) return 0;
+  return ns_workspace(batch, m, n, ns_split(dtype, true));
 }
 
 extern "C" lipcache_status lipcache_muon_step(void* W, const void* G, float* M, int64_t batch, int32_t m, int32_t n,
@@ -205,7 +604,7 @@ extern "C" lipcache_status lipcache_muon_step(void* W, const void* G, float* M, 
     return LIPCACHE_EINVAL;
   if (batch > 0 && (ns_unaligned(W, dtype) || ns_unaligned(G, dtype) || ns_unaligned(M, LIPCACHE_F32)))
     return LIPCACHE_EINVAL;
-  if (!ws || !aligned256(ws) || ws_bytes < ns_workspace(batch, m, n)) return LIPCACHE_EWORKSPACE;
+  if (!ws || !aligned256(ws) || ws_bytes < ns_workspace(batch, m, n, ns_split(dtype, true))) return LIPCACHE_EWORKSPACE;
   if (batch == 0) return LIPCACHE_OK;
   const NsArgs g{batch, m, n, opt->steps, opt->coef, opt->eps};
   const float keep = static_cast<float>(1.0 - static_cast<double>(opt->lr) * opt->weight_decay);

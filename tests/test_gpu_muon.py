@@ -132,6 +132,35 @@ def test_muon_step(shape, dtype, nesterov):
     assert np.linalg.norm(n64(W) - ref) <= lim, (shape, dtype)
 
 
+# Large and many matrices: every tile size of the products, wide and tall.
+LARGE = [("ortho", (1, 2080, 2050), "f32"), ("ortho", (1, 2050, 2080), "f16"), ("ortho", (5, 1100, 1030), "f32"),
+         ("ortho", (5, 1030, 1100), "bf16"), ("ortho", (40, 500, 520), "f32"), ("ortho", (40, 520, 500), "f16"),
+         ("step", (40, 500, 520), "bf16"), ("step", (40, 520, 500), "f16"), ("step", (60, 500, 470), "bf16"),
+         ("step", (60, 470, 500), "f16"), ("step", (5, 1100, 1030), "bf16"), ("step", (1, 2050, 2080), "bf16"),
+         ("step", (8, 1030, 1100), "bf16"), ("step", (5, 1030, 1100), "f32")]
+
+
+@pytest.mark.parametrize("what,shape,dtype", LARGE, ids=lambda v: "x".join(map(str, v)) if isinstance(v, tuple) else v)
+def test_large_and_many(what, shape, dtype):
+    say("large", what, shape, dtype)
+    b, m, n = shape
+    G = matrices(30, *shape, dtype, "strong")
+    if what == "ortho":
+        ref = R.newton_schulz(n64(G), 5, NS5, 1e-7)
+        O = api.orthogonalise(G)
+        assert far(O, ref) <= R.NS_TOL[dtype], far(O, ref)
+        assert float(np.max(np.abs(n64(O) - ref)) / np.sqrt(np.mean(ref * ref))) <= 40 * R.NS_TOL[dtype]
+        return
+    W = torch.zeros_like(G)  # so that W's rounding hides nothing of the step's
+    M = torch.zeros(shape, device=DEV)
+    api.muon_step(W, G, M, lr=1.0, momentum=0.5, scale=1.0)
+    ref = -R.newton_schulz(1.5 * n64(G), 5, NS5, 1e-7)
+    tol = R.NS_TOL["f32" if dtype == "f32" else "bf16"]  # 16-bit steps take 11-bit operands
+    assert far(W, ref) <= tol, far(W, ref)
+    assert float(np.max(np.abs(n64(W) - ref)) / np.sqrt(np.mean(ref * ref))) <= 40 * tol
+    assert np.array_equal(n64(M), n64(G))
+
+
 def test_a_step_bounds_the_spectral_norm():
     """sigma_max moves by at most 1.21 lr scale: what certified radii are divided by stays known."""
     W = matrices(11, 1, 200, 256, "f32", size=256 ** -0.5)[0].contiguous()
