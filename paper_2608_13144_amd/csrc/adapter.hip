@@ -1,55 +1,659 @@
 // Low-rank adapters of many requests beside a shared projection, forward and
 // backward (see lipcache.h for the formulas).
+//
+// Rows of one pair go together: a first kernel sorts the rows by their pair
+// (stable, so every sum has one order), and everything after it works on
+// sorted rows, gathered as they are read.  The low-rank part of the result
+// joins the projection's sums in registers before they are stored, so y (dx)
+// is written once.
+//
+// Rows of one output tile may belong to several pairs.  Each pair multiplies
+// only its own rows and adds only to them by selection, never by a product
+// with zero: what one request's pair or rows hold that is not finite stays
+// with it.
+#include <type_traits>
+
 #include "lc_common.hpp"
-#include "lc_tile.hpp"
+#include "lc_mfma.hpp"
 
 namespace lc {
 
 constexpr int kAdMaxRank = 128;
+constexpr int kAdMaxPairs = 8192;
 constexpr int64_t kAdMaxWidth = 1 << 20;
+constexpr int kThinRows = 32;  // sorted rows of one pair that a workgroup of the thin products takes
 
-// The pair of row t (-1: none): the last request whose first row is at or
-// before t, if t is one of its rows.  Any offsets end the search in range.
-__device__ __forceinline__ int pair_of_row(int64_t t, const int32_t* __restrict__ offsets,
-                                           const int32_t* __restrict__ adapter, int R, int S) {
-  int lo = 0, hi = R + 1;  // first index whose offset is past t
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (offsets[mid] <= t) lo = mid + 1; else hi = mid;
+__host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// ---------------------------------------------------------------- grouping
+// Rows sorted by pair (rows without one last), and the table of the thin
+// products' tiles: up to kThinRows sorted rows of one pair each.
+struct AdGroups {
+  int32_t* order;      // [T] sorted place -> row
+  int32_t* pair;       // [T] sorted place -> pair, S where none
+  int32_t* start;      // [S + 2] first place of each pair, of none, and T
+  int32_t* tile_pair;  // [tiles]
+  int32_t* tile_row;   // [tiles] first sorted place
+  int32_t* tiles;      // number of tiles
+  uint32_t* zeros;     // 16 bytes of zero
+};
+
+__host__ __device__ inline int64_t ad_tiles(int64_t T, int S) { return T / kThinRows + (S < T ? S : T); }
+
+// Workgroup s places the rows of pair s.  Every workgroup counts all pairs'
+// rows (integer sums in LDS: any order gives the same), then walks the
+// requests in order, 256 at a time.  Request -1 is the rows before the first
+// offset, request R those after the last.  Offsets that decrease place rows
+// wrongly or not at all; every index is checked, and places left over hold row
+// 0 without a pair, so whatever they are no access leaves the arrays.
+__global__ __launch_bounds__(256) void ad_group_kernel(int64_t t0, int T, const int32_t* __restrict__ offsets,
+                                                       const int32_t* __restrict__ adapter, int R, int S, AdGroups g) {
+  extern __shared__ int32_t count[];  // [S + 1] rows of each pair, then scratch
+  int32_t* sum = count + S + 1;       // [256]
+  int32_t* first = sum + 256;         // [256]
+  __shared__ uint32_t base_rows, base_tiles;
+  const int tid = static_cast<int>(threadIdx.x), s = static_cast<int>(blockIdx.x);
+  for (int i = tid; i <= S; i += 256) count[i] = 0;
+  if (tid == 0) base_rows = base_tiles = 0;
+  __syncthreads();
+  auto request = [&](int i, int& lo, int& key) {  // i in [-1, R]; returns its rows
+    const int64_t a = i < 0 ? t0 : R > 0 ? offsets[i] : t0, b = i < 0 ? (R > 0 ? offsets[0] : t0) : i < R ? offsets[i + 1] : t0 + T;
+    const int64_t l = a < t0 ? t0 : a, h = b > t0 + T ? t0 + T : b;
+    lo = static_cast<int>(l - t0);
+    key = S;
+    if (i >= 0 && i < R) {
+      const int p = adapter[i];
+      if (p >= 0 && p < S) key = p;
+    }
+    return h > l ? static_cast<int>(h - l) : 0;
+  };
+  for (int i = tid - 1; i <= R; i += 256) {
+    int lo, key;
+    const int n = request(i, lo, key);
+    if (n > 0) atomicAdd(&count[key], n);
   }
-  if (lo < 1 || lo > R) return -1;
-  const int a = adapter[lo - 1];
-  return a >= 0 && a < S ? a : -1;
+  __syncthreads();
+  uint32_t rows = 0, tiles = 0;
+  const uint32_t all = static_cast<uint32_t>(T);
+  for (int i = tid; i < s; i += 256) {
+    const uint32_t n = static_cast<uint32_t>(count[i]);
+    rows += n;
+    tiles += ((n < all ? n : all) + kThinRows - 1) / kThinRows;  // as many as the pair writes below
+  }
+  if (rows > 0) {
+    atomicAdd(&base_rows, rows);
+    atomicAdd(&base_tiles, tiles);
+  }
+  __syncthreads();
+  const uint32_t place0 = base_rows, mine = static_cast<uint32_t>(count[s]);
+  if (tid == 0) {
+    g.start[s] = static_cast<int32_t>(place0 < all ? place0 : all);
+    if (s == S) {
+      g.start[S + 1] = T;
+      *g.tiles = static_cast<int32_t>(base_tiles);
+    }
+  }
+  if (s == S && tid < 4) g.zeros[tid] = 0;
+  if (s < S) {
+    const uint32_t last = static_cast<uint32_t>(ad_tiles(T, S));
+    for (uint32_t i = tid; i * kThinRows < (mine < all ? mine : all); i += 256) {
+      const uint32_t at = base_tiles + i;
+      if (at < last) {
+        g.tile_pair[at] = s;
+        g.tile_row[at] = static_cast<int32_t>(place0 + i * kThinRows);
+      }
+    }
+  }
+  uint32_t place = place0;
+  for (int i0 = -1; i0 <= R && mine > 0 && place < all; i0 += 256) {
+    int lo = 0, key = S, n = 0;
+    if (i0 + tid <= R) {
+      n = request(i0 + tid, lo, key);
+      if (key != s) n = 0;
+    }
+    // exclusive sums of n over the 256 requests
+    __syncthreads();
+    sum[tid] = n;
+    first[tid] = lo;
+    __syncthreads();
+    for (int o = 1; o < 256; o <<= 1) {
+      const int v = tid >= o ? sum[tid - o] : 0;
+      __syncthreads();
+      sum[tid] += v;
+      __syncthreads();
+    }
+    const int total = sum[255];
+    for (int p = tid; p < total && place + p < all; p += 256) {
+      int a = 0, b = 255;  // the request that holds the p-th row: the first whose sum passes p
+      while (a < b) {
+        const int mid = (a + b) >> 1;
+        if (sum[mid] > p) b = mid; else a = mid + 1;
+      }
+      const int before = a > 0 ? sum[a - 1] : 0;
+      const uint32_t row = static_cast<uint32_t>(first[a] + p - before);
+      g.order[place + p] = row < all ? static_cast<int32_t>(row) : 0;
+      g.pair[place + p] = s;
+    }
+    place += static_cast<uint32_t>(total);
+  }
+  if (s == S)
+    for (uint64_t p = static_cast<uint64_t>(place) + tid; p < all; p += 256) {
+      g.order[p] = 0;
+      g.pair[p] = S;
+    }
 }
 
-__global__ __launch_bounds__(256) void ad_pairs_kernel(int64_t T, const int32_t* __restrict__ offsets,
-                                                       const int32_t* __restrict__ adapter, int R, int S,
-                                                       int32_t* __restrict__ pair) {
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (t < T) pair[t] = R > 0 ? pair_of_row(t, offsets, adapter, R, S) : -1;
+// ------------------------------------------------------------ element types
+template <class E>
+struct Vec16;  // 16 bytes of elements
+template <>
+struct Vec16<float> {
+  static constexpr int kCount = 4;
+  typedef f32x4 type;
+};
+template <>
+struct Vec16<__bf16> {
+  static constexpr int kCount = 8;
+  typedef bf16x8 type;
+};
+template <>
+struct Vec16<_Float16> {
+  static constexpr int kCount = 8;
+  typedef f16x8 type;
+};
+
+// A float32 factor as what the matrix cores take: itself, or the sum of two
+// 16-bit numbers (each product then takes two instructions; 16 or 22 bits).
+template <class E>
+__device__ __forceinline__ void two_parts(float v, E& first, E& second) {
+  asm("" : "+v"(v));
+  first = static_cast<E>(v);
+  second = static_cast<E>(v - static_cast<float>(first));
 }
 
-// v_t = A_a x_t (or u_t = B_a^T dy_t): one wave a row and rank.
-template <typename T, bool kTransposed>
-__global__ __launch_bounds__(256) void ad_shrink_kernel(int64_t rows, const T* __restrict__ x, int64_t ldx, int width,
-                                                        const T* __restrict__ F, int r,
-                                                        const int32_t* __restrict__ pair, float* __restrict__ out) {
-  const int64_t w = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave;
-  if (w >= rows * r) return;
-  const int64_t t = w / r;
-  const int rho = static_cast<int>(w % r);
-  const int a = pair[t];
-  float sum = 0.0f;
-  if (a >= 0) {
-    const T* f = F + static_cast<int64_t>(a) * r * width;
-    for (int k = lane_id(); k < width; k += kWave)
-      sum = fmaf(load_f32(x + t * ldx + k),
-                 load_f32(f + (kTransposed ? static_cast<int64_t>(k) * r + rho : static_cast<int64_t>(rho) * width + k)),
-                 sum);
+// ------------------------------------------------------- copies and transposes
+// Rows moved into the workspace: padded with zeros to a width of whole 16-byte
+// vectors, as they are or transposed.
+struct AdCopy {
+  const void* from;
+  void* to;
+  int64_t ld_from, ld_to;     // elements
+  int64_t from_next, to_next; // elements between matrices of a stack
+  int rows, width;            // of the source
+  int to_rows, to_width;      // written, zeros outside the source
+  int stack;
+};
+
+template <typename T, bool kTranspose>
+__global__ __launch_bounds__(256) void ad_copy_kernel(AdCopy c) {
+  __shared__ T tile[32][33];
+  const int x = static_cast<int>(threadIdx.x) & 31, y = static_cast<int>(threadIdx.x) >> 5;
+  // tiles of the result
+  const int64_t tiles_w = ceil_div(c.to_width, 32), tiles = tiles_w * ceil_div(c.to_rows, 32);
+  const int64_t z = blockIdx.x / tiles, t = blockIdx.x % tiles;
+  const int i0 = static_cast<int>(t / tiles_w) * 32, j0 = static_cast<int>(t % tiles_w) * 32;
+  const T* from = static_cast<const T*>(c.from) + z * c.from_next;
+  T* to = static_cast<T*>(c.to) + z * c.to_next;
+  if constexpr (kTranspose) {
+#pragma unroll
+    for (int k = y; k < 32; k += 8) {
+      const int row = j0 + k, col = i0 + x;  // of the source
+      tile[k][x] = row < c.rows && col < c.width ? from[row * c.ld_from + col] : static_cast<T>(0.0f);
+    }
+    __syncthreads();
   }
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, kWave);
-  if (lane_id() == 0) out[w] = sum;
+  for (int k = y; k < 32; k += 8) {
+    const int row = i0 + k, col = j0 + x;
+    if (row >= c.to_rows || col >= c.to_width) continue;
+    T v;
+    if constexpr (kTranspose) v = tile[x][k];
+    else v = row < c.rows && col < c.width ? from[row * c.ld_from + col] : static_cast<T>(0.0f);
+    to[row * c.ld_to + col] = v;
+  }
+}
+
+template <typename T, bool kTranspose>
+lipcache_status ad_copy(const AdCopy& c, hipStream_t s) {
+  const int64_t blocks = ceil_div(c.to_width, 32) * ceil_div(c.to_rows, 32) * c.stack;
+  if (blocks <= 0) return LIPCACHE_OK;
+  if (blocks > 0x7fffffff) return LIPCACHE_EUNSUPPORTED;
+  ad_copy_kernel<T, kTranspose><<<static_cast<unsigned>(blocks), 256, 0, s>>>(c);
+  LC_LAUNCHED();
+  return LIPCACHE_OK;
+}
+
+// ------------------------------------------------------------ thin products
+// out[row][rho] = F_a[rho] . x[row] for the up to 32 sorted rows of one tile
+// of the table: F is [S][r][ldf].  Both operands come straight from global
+// memory in 16-byte vectors: lane l holds row l % 32 of x and of F, and half
+// l / 32 of each 128 bytes of the contraction, so a row's four vectors are one
+// half of a cache line.  The eight waves share the contraction and their sums
+// are added in LDS in order.  Bound by the latency and bandwidth of x's rows.
+template <class E, int NR>
+__global__ __launch_bounds__(512) void ad_thin_kernel(const E* __restrict__ x, int64_t ldx, int width,
+                                                      const E* __restrict__ F, int64_t ldf, int r, AdGroups g,
+                                                      float* __restrict__ out) {
+  constexpr int kV = Vec16<E>::kCount, kBlock = 8 * kV, kWaves = 8;
+  typedef typename Vec16<E>::type V;
+  __shared__ f32x4 part[kWaves][4][kWave];
+  const int t = static_cast<int>(blockIdx.x);
+  if (static_cast<uint32_t>(t) >= static_cast<uint32_t>(*g.tiles)) return;
+  const int a = g.tile_pair[t], row0 = g.tile_row[t];
+  if (row0 < 0) return;
+  const int end = g.start[a + 1] - row0, rows = end < kThinRows ? end : kThinRows;
+  if (rows <= 0) return;
+  const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+  const int li = lane & 31, half = lane >> 5;
+  const int row = g.order[row0 + (li < rows ? li : rows - 1)];
+  const E* px = x + row * ldx + half * (4 * kV);
+  const E* pf[NR];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const int rho = 32 * n + li < r ? 32 * n + li : r - 1;
+    pf[n] = F + (static_cast<int64_t>(a) * r + rho) * ldf + half * (4 * kV);
+  }
+  f32x16 acc[NR] = {};
+  for (int k = wave * kBlock; k < width; k += kWaves * kBlock) {
+    V vx[4], vf[NR][4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const bool in = k + half * (4 * kV) + c * kV < width;
+      vx[c] = in ? *reinterpret_cast<const V*>(px + k + c * kV) : V{};
+#pragma unroll
+      for (int n = 0; n < NR; ++n) vf[n][c] = in ? *reinterpret_cast<const V*>(pf[n] + k + c * kV) : V{};
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int n = 0; n < NR; ++n) acc[n] = MfmaType<E>::mul(vx[c], vf[n][c], acc[n]);
+  }
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    if (n > 0) __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      part[wave][q][lane] = f32x4{acc[n][4 * q], acc[n][4 * q + 1], acc[n][4 * q + 2], acc[n][4 * q + 3]};
+    __syncthreads();
+    // 4 x 64 vectors of four rows: one for each thread of the first four waves
+    if (wave < 4) {
+      f32x4 v = part[0][wave][lane];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) {
+        const f32x4 u = part[w][wave][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += u[e];
+      }
+      const int rho = 32 * n + li;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = 8 * wave + 4 * half + e;
+        if (i < rows && rho < r) out[static_cast<int64_t>(g.order[row0 + i]) * r + rho] = v[e];
+      }
+    }
+  }
+}
+
+// Rows without a pair: zeros.
+__global__ __launch_bounds__(256) void ad_zero_rows_kernel(AdGroups g, int S, int T, int r, float* __restrict__ out) {
+  const int first = g.start[S];
+  const int64_t all = static_cast<int64_t>(T - first) * r;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += 256 * static_cast<int64_t>(gridDim.x))
+    out[static_cast<int64_t>(g.order[first + i / r]) * r + i % r] = 0.0f;
+}
+
+// ------------------------------------------------------------- main product
+// The fragment (one 16-byte vector) of lane's row or column from `p`, the
+// `count` valid elements of which start at p (others 0); whole vectors where `wide`.
+template <class E>
+__device__ __forceinline__ typename Vec16<E>::type load_some(const E* p, int count, bool wide) {
+  typedef typename Vec16<E>::type V;
+  constexpr int kV = Vec16<E>::kCount;
+  if (wide && count >= kV) return *reinterpret_cast<const V*>(p);
+  V v{};
+#pragma unroll
+  for (int e = 0; e < kV; ++e)
+    if (e < count) v[e] = p[e];
+  return v;
+}
+
+struct AdLow {
+  const void* F;       // [S][width][ldf]: B (forward) or A transposed (backward)
+  int64_t ldf;         // elements between its rows
+  const float* v;      // [T][r]
+  const float* scale;  // [S]
+  int r, S, width;
+  int wide;            // F's rows and r allow whole vectors
+  int wide_v;          // v's
+};
+
+// acc += scale_a F_a v for the tile's rows of every pair among them.
+template <class S, class E>
+__device__ __forceinline__ void add_low_rank(const AdLow& low, const AdGroups& g, int i0, int rows, int j0,
+                                             f32x16 (&acc)[S::TM][S::TN]) {
+  constexpr int kV = Vec16<E>::kCount;
+  typedef typename Vec16<E>::type V;
+  const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+  const int wm = wave / S::WN, wn = wave % S::WN;
+  const int li = lane & 31, half = lane >> 5;
+  const E* F = static_cast<const E*>(low.F);
+  for (int at = 0; at < rows;) {
+    const int a = uniform(g.pair[i0 + at]);
+    if (a >= low.S) break;  // rows without a pair come last
+    const int next = uniform(g.start[a + 1]) - i0, end = next < rows ? next : rows;
+    if (end <= at) break;
+    const float scale = low.scale[a];
+#pragma unroll
+    for (int tm = 0; tm < S::TM; ++tm) {
+      const int m0 = (wm * S::TM + tm) * 32;  // the 32 rows of this accumulator
+      if (m0 >= end || m0 + 32 <= at) continue;
+      const bool mine = m0 + li >= at && m0 + li < end;
+      const float* v = low.v + static_cast<int64_t>(g.order[i0 + (mine ? m0 + li : at)]) * low.r;
+#pragma unroll
+      for (int tn = 0; tn < S::TN; ++tn) {
+        const int j = j0 + (wn * S::TN + tn) * 32 + li;
+        const E* f = F + (static_cast<int64_t>(a) * low.width + (j < low.width ? j : low.width - 1)) * low.ldf;
+        f32x16 sum = {};
+#pragma unroll 1
+        for (int k = 0; k < low.r; k += 2 * kV) {
+          const int at_k = k + half * kV, left = low.r - at_k;
+          const V vf = load_some<E>(f + at_k, left, low.wide != 0);
+          float w[kV];
+#pragma unroll
+          for (int e = 0; e < kV; e += 4) {
+            const f32x4 u = load_some<float>(v + at_k + e, mine ? left - e : 0, low.wide_v != 0);
+#pragma unroll
+            for (int o = 0; o < 4; ++o) w[e + o] = mine ? scale * u[o] : 0.0f;
+          }
+          if constexpr (std::is_same_v<E, float>) {
+            sum = MfmaType<E>::mul(V{w[0], w[1], w[2], w[3]}, vf, sum);
+          } else {
+            V first, second;
+#pragma unroll
+            for (int e = 0; e < kV; ++e) {
+              E p, q;
+              two_parts(w[e], p, q);
+              first[e] = p;
+              second[e] = q;
+            }
+            sum = MfmaType<E>::mul(second, vf, sum);
+            sum = MfmaType<E>::mul(first, vf, sum);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int i = m0 + acc_row(e) + 4 * half;
+          if (i >= at && i < end) acc[tm][tn][e] += sum[e];
+        }
+      }
+    }
+    at = end;
+  }
+}
+
+// out[row] = P[row] Q^T + bias + the low-rank part, for the sorted rows of this tile.
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void ad_main_kernel(const typename S::E* __restrict__ P, int64_t ldp,
+                                                              const typename S::E* __restrict__ Q, int64_t ldq, int T,
+                                                              int width, int K, const float* __restrict__ bias,
+                                                              AdLow low, AdGroups g, typename S::E* __restrict__ out,
+                                                              int64_t ldo) {
+  typedef typename S::E E;
+  __shared__ __align__(16) char lds[S::kLds];
+  int bi, bj;
+  tile_of(static_cast<int>(ceil_div(T, S::BM)), static_cast<int>(ceil_div(width, S::BN)), bi, bj);
+  const int i0 = bi * S::BM, j0 = bj * S::BN;
+  Side p{}, q{};
+  p.p = P;
+  p.ld = ldp * sizeof(E);
+  p.rows = T - i0 < S::BM ? T - i0 : S::BM;
+  p.pick = g.order + i0;
+  q.p = Q + (S::QCOL ? static_cast<int64_t>(j0) : j0 * ldq);
+  q.ld = ldq * sizeof(E);
+  q.rows = width - j0 < S::BN ? width - j0 : S::BN;
+  f32x16 acc[S::TM][S::TN] = {};
+  tile_products<S>(p, q, K, lds, acc);
+  if (low.S > 0) add_low_rank<S, E>(low, g, i0, p.rows, j0, acc);
+  tile_store<S>(acc, [&](int i, int j, const f32x16& v) {
+    j += j0;
+    if (j >= width) return;
+    const float b = bias ? bias[j] : 0.0f;
+    int row[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) row[e] = g.order[i0 + (i + acc_row(e) < p.rows ? i + acc_row(e) : p.rows - 1)];
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (i + acc_row(e) < p.rows) out[row[e] * ldo + j] = static_cast<E>(v[e] + b);
+  });
+}
+
+// Tile size by the number of 128 x 128 tiles, as the CUs fill (256 of them).
+template <class E, bool kCol>
+lipcache_status ad_main(const void* P, int64_t ldp, const void* Q, int64_t ldq, int T, int width, int K,
+                        const float* bias, const AdLow& low, const AdGroups& g, void* out, int64_t ldo, hipStream_t s) {
+  auto run = [&](auto shape) {
+    typedef decltype(shape) S;
+    const int64_t tiles = ceil_div(T, S::BM) * ceil_div(width, S::BN);
+    ad_main_kernel<S><<<static_cast<unsigned>(tiles), S::kThreads, 0, s>>>(
+        static_cast<const E*>(P), ldp, static_cast<const E*>(Q), ldq, T, width, K, bias, low, g, static_cast<E*>(out), ldo);
+    return hipGetLastError() == hipSuccess ? LIPCACHE_OK : LIPCACHE_EHIP;
+  };
+  const int64_t t128 = ceil_div(T, 128) * ceil_div(width, 128), t256 = ceil_div(T, 256) * ceil_div(width, 256);
+  if (t128 < 128) return run(TileShape<E, 64, 64, 2, 2, 1, 3, 1, false, kCol>{});
+  if constexpr (sizeof(E) == 2)
+    if (5 * t256 >= 4 * 256 * ceil_div(t256, 256)) return run(TileShape<E, 256, 256, 2, 4, 1, 2, 1, false, kCol>{});
+  if (t128 < 320) return run(TileShape<E, 128, 128, 2, 4, 1, 4, 1, false, kCol>{});
+  return run(TileShape<E, 128, 128, 2, 2, 1, 2, 1, false, kCol>{});
+}
+
+// -------------------------------------------------------- gradients of pairs
+// D_a[rho][c] = scale_a sum over pair a's rows t of f[t][rho] z[t][c]: dA with
+// f = u, z = x, and dB (transposed) with f = v, z = dy.  One workgroup takes
+// 128 columns of one pair (and one of `splits` shares of its rows); z's rows
+// come gathered into LDS, 64 (float32: 32) at a time through a ring of three
+// buffers, and are read across (the contraction runs over the rows); f comes
+// straight to registers as two 16-bit parts.  Bound by reading x and dy once.
+template <class E>
+struct AdGradSide {
+  const E* z;
+  int64_t ldz;
+  const float* f;
+  E* out;          // dA: [S][r][width];  dB: [S][width][r]
+  float* part;     // [splits][S][r][width] where splits > 1
+  int width, blocks;
+  bool across;     // dB's layout
+};
+
+template <class E, int NR>
+__global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSide<E> B, int r, int S, int splits,
+                                                      const float* __restrict__ scale, AdGroups g) {
+  typedef TileOf<E, 128, true, 4> Tile;
+  constexpr int kV = Vec16<E>::kCount, kPart = Tile::kPart, kStages = 3;
+  typedef typename Vec16<E>::type V;
+  __shared__ __align__(16) char lds[kStages * Tile::kBytes];
+  const int per = (A.blocks + B.blocks) * splits;
+  const int a = static_cast<int>(blockIdx.x) / per;
+  int in = static_cast<int>(blockIdx.x) % per;
+  const int share = in % splits;
+  in /= splits;
+  const bool second = in >= A.blocks;
+  const AdGradSide<E>& d = second ? B : A;
+  const int c0 = (second ? in - A.blocks : in) * 128;
+  const int begin0 = g.start[a], end0 = g.start[a + 1];
+  // shares in whole parts
+  const int parts = end0 > begin0 ? (end0 - begin0 + kPart - 1) / kPart : 0, each = (parts + splits - 1) / splits;
+  const int begin = begin0 + share * each * kPart;
+  const int stop = begin + each * kPart < end0 ? begin + each * kPart : end0;
+  const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+  const int li = lane & 31, half = lane >> 5;
+  const uint32_t base = lds_address(lds);
+
+  auto copy = [&](int t0, int pos) {
+#pragma unroll
+    for (int c = 0; c < Tile::kCopies; ++c) {
+      const int n = (wave * Tile::kCopies + c) * 64 + lane;
+      const int row = n / Tile::kSlots, chunk = (n % Tile::kSlots) ^ Tile::swz(row);
+      const int col = c0 + chunk * kV;
+      const void* p = g.zeros;  // rows past the share and columns past the matrix
+      if (t0 + row < stop && col < d.width) p = d.z + g.order[t0 + row] * d.ldz + col;
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p),
+                   "s"(uniform(static_cast<int>(base + pos * Tile::kBytes + (wave * Tile::kCopies + c) * 1024)))
+                   : "memory", "m0");
+    }
+  };
+  f32x16 acc[NR] = {};
+  uint32_t read[Tile::kGroups];
+#pragma unroll
+  for (int n = 0; n < Tile::kGroups; ++n) read[n] = Tile::row_offset(Tile::read_offset(n, 0), wave);
+  const int steps = stop > begin ? (stop - begin + kPart - 1) / kPart : 0;
+  int copied = 0;
+  for (; copied < kStages - 1 && copied < steps; ++copied) copy(begin + copied * kPart, copied);
+  for (int step = 0; step < steps; ++step) {
+    // f of this step: lane's rank, kV rows of the group and half
+    V f1[Tile::kGroups][NR], f2[Tile::kGroups][NR];
+#pragma unroll
+    for (int n = 0; n < Tile::kGroups; ++n)
+#pragma unroll
+      for (int e = 0; e < kV; ++e) {
+        const int t = begin + step * kPart + (2 * n + half) * kV + e;
+        const float* p = d.f + static_cast<int64_t>(g.order[t < stop ? t : stop - 1]) * r;
+#pragma unroll
+        for (int m = 0; m < NR; ++m) {
+          const float v = t < stop && 32 * m + li < r ? p[32 * m + li] : 0.0f;
+          if constexpr (std::is_same_v<E, float>) {
+            f1[n][m][e] = v;
+          } else {
+            E x, y;
+            two_parts(v, x, y);
+            f1[n][m][e] = x;
+            f2[n][m][e] = y;
+          }
+        }
+      }
+    copies_left<0>();
+    __syncthreads();
+    if (copied < steps) {
+      copy(begin + copied * kPart, copied % kStages);
+      ++copied;
+    }
+    const char* at = lds + (step % kStages) * Tile::kBytes;
+#pragma unroll
+    for (int n = 0; n < Tile::kGroups; ++n) {
+      const V z = __builtin_bit_cast(V, Tile::read16(at + read[n]));
+#pragma unroll
+      for (int m = 0; m < NR; ++m) {
+        if constexpr (!std::is_same_v<E, float>) acc[m] = MfmaType<E>::mul(f2[n][m], z, acc[m]);
+        acc[m] = MfmaType<E>::mul(f1[n][m], z, acc[m]);
+      }
+    }
+  }
+  const int col = c0 + wave * 32 + li;
+  if (col >= d.width) return;
+  const float sc = scale[a];
+#pragma unroll
+  for (int m = 0; m < NR; ++m)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int rho = 32 * m + acc_row(e) + 4 * half;
+      if (rho >= r) continue;
+      if (splits > 1) {
+        d.part[((static_cast<int64_t>(share) * S + a) * r + rho) * d.width + col] = acc[m][e];
+      } else {
+        const int64_t to = d.across ? (static_cast<int64_t>(a) * d.width + col) * r + rho
+                                    : (static_cast<int64_t>(a) * r + rho) * d.width + col;
+        d.out[to] = static_cast<E>(begin0 < end0 ? sc * acc[m][e] : 0.0f);
+      }
+    }
+}
+
+// Adds the shares in order.
+template <class E>
+__global__ __launch_bounds__(256) void ad_join_kernel(AdGradSide<E> A, AdGradSide<E> B, int r, int S, int splits,
+                                                      const float* __restrict__ scale, AdGroups g) {
+  const AdGradSide<E>& d = blockIdx.y ? B : A;
+  const int64_t size = static_cast<int64_t>(S) * r * d.width;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= size) return;
+  float sum = 0.0f;
+  for (int k = 0; k < splits; ++k) sum += d.part[k * size + i];
+  const int col = static_cast<int>(i % d.width), rho = static_cast<int>(i / d.width % r);
+  const int64_t a = i / d.width / r;
+  const int64_t to = d.across ? (a * d.width + col) * r + rho : i;
+  d.out[to] = static_cast<E>(g.start[a] < g.start[a + 1] ? scale[a] * sum : 0.0f);
+}
+
+// ------------------------------------------------------------------ the calls
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+inline size_t ad_size(int32_t dtype) { return dtype == LIPCACHE_F32 ? 4 : 2; }
+
+// The workspace, in order of use.  Sizes only: `at` NULL gives the sum.
+struct AdSpace {
+  char* at;
+  size_t used = 0;
+  template <class P>
+  P* take(size_t count) {
+    P* p = reinterpret_cast<P*>(at ? at + used : nullptr);
+    used += align_up(count * sizeof(P), 256);
+    return p;
+  }
+};
+
+AdGroups ad_groups(AdSpace& ws, int64_t T, int S) {
+  AdGroups g;
+  g.order = ws.take<int32_t>(T);
+  g.pair = ws.take<int32_t>(T);
+  g.start = ws.take<int32_t>(S + 2);
+  g.tile_pair = ws.take<int32_t>(ad_tiles(T, S) + 1);
+  g.tile_row = ws.take<int32_t>(ad_tiles(T, S) + 1);
+  g.tiles = ws.take<int32_t>(1);
+  g.zeros = ws.take<uint32_t>(4);
+  return g;
+}
+
+lipcache_status ad_group(int64_t t0, int64_t T, const lipcache_adapters& ad, const AdGroups& g, hipStream_t s) {
+  ad_group_kernel<<<ad.S + 1, 256, (ad.S + 1 + 512) * 4, s>>>(t0, static_cast<int>(T), ad.offsets, ad.adapter, ad.R, ad.S, g);
+  LC_LAUNCHED();
+  return LIPCACHE_OK;
+}
+
+// A matrix whose rows are read as 16-byte vectors: itself, or its copy in the workspace.
+template <class E>
+struct AdRows {
+  const E* p;
+  int64_t ld;
+};
+
+template <class E>
+lipcache_status ad_rows(const void* from, int64_t ld, int64_t rows, int width, E* room, AdRows<E>& out, hipStream_t s) {
+  constexpr int kV = Vec16<E>::kCount;
+  const E* p = static_cast<const E*>(from);
+  if (aligned16(from) && ld % kV == 0 && width % kV == 0 && ld * sizeof(E) <= (4u << 20)) {
+    out = {p, ld};
+    return LIPCACHE_OK;
+  }
+  const int64_t to = round_up(width, kV);
+  out = {room, to};
+  // at most 2^31 - 1 tiles a launch
+  for (int64_t r0 = 0; r0 < rows; r0 += 1 << 20) {
+    const int n = static_cast<int>(rows - r0 < (1 << 20) ? rows - r0 : 1 << 20);
+    const AdCopy c{p + r0 * ld, room + r0 * to, ld, to, 0, 0, n, width, n, static_cast<int>(to), 1};
+    if (lipcache_status st = ad_copy<E, false>(c, s); st != LIPCACHE_OK) return st;
+  }
+  return LIPCACHE_OK;
+}
+
+template <class E>
+lipcache_status ad_thin(const AdRows<E>& x, int width, const E* F, int64_t ldf, int64_t T, const lipcache_adapters& ad,
+                        const AdGroups& g, float* out, hipStream_t s) {
+  const unsigned tiles = static_cast<unsigned>(ad_tiles(T, ad.S));
+  if (ad.S > 0 && tiles > 0) {
+    if (ad.r <= 32) ad_thin_kernel<E, 1><<<tiles, 512, 0, s>>>(x.p, x.ld, width, F, ldf, ad.r, g, out);
+    else if (ad.r <= 64) ad_thin_kernel<E, 2><<<tiles, 512, 0, s>>>(x.p, x.ld, width, F, ldf, ad.r, g, out);
+    else ad_thin_kernel<E, 4><<<tiles, 512, 0, s>>>(x.p, x.ld, width, F, ldf, ad.r, g, out);
+    LC_LAUNCHED();
+  }
+  return LIPCACHE_OK;
 }
 
 struct AdArgs {
@@ -59,93 +663,156 @@ struct AdArgs {
   lipcache_adapters ad;
 };
 
-template <typename T>
-lipcache_status ad_forward(const AdArgs& g, const float* bias, void* y_, int64_t ldy, float* v, int32_t* pair,
-                           hipStream_t s) {
-  const T *x = static_cast<const T*>(g.x), *W = static_cast<const T*>(g.W), *A = static_cast<const T*>(g.ad.A),
-          *B = static_cast<const T*>(g.ad.B);
-  const float* scale = g.ad.scale;
-  T* y = static_cast<T*>(y_);
-  const int64_t ldx = g.ldx, ldw = g.ldw, N = g.N;
-  const int r = g.ad.r;
-  ad_pairs_kernel<<<static_cast<unsigned>((g.T + 255) / 256), 256, 0, s>>>(g.T, g.ad.offsets, g.ad.adapter, g.ad.R,
-                                                                          g.ad.S, pair);
-  LC_LAUNCHED();
-  ad_shrink_kernel<T, false><<<static_cast<unsigned>((g.T * r + 3) / 4), 256, 0, s>>>(g.T, x, ldx, g.K, A, r, pair, v);
-  LC_LAUNCHED();
-  LC_HIP(tile_product(
-      g.T, N, g.K, 1, [=] __device__(int, int64_t i, int64_t k) { return load_f32(x + i * ldx + k); },
-      [=] __device__(int, int64_t j, int64_t k) { return load_f32(W + j * ldw + k); },
-      [=] __device__(int, int64_t i, int64_t j, float sum) {
-        const int a = pair[i];
-        if (bias) sum += bias[j];
-        if (a >= 0) {
-          const T* b = B + (static_cast<int64_t>(a) * N + j) * r;
-          float low = 0.0f;
-          for (int rho = 0; rho < r; ++rho) low = fmaf(v[i * r + rho], load_f32(b + rho), low);
-          sum = fmaf(scale[a], low, sum);
-        }
-        y[i * ldy + j] = round_to<T>(sum);
-      },
-      s));
+// Rows of one pass of the main product: their offsets stay below 2^31 bytes.
+inline int64_t ad_chunk(int64_t ld, size_t size) {
+  const int64_t rows = ((1ll << 31) - (8ll << 20)) / (ld * static_cast<int64_t>(size));
+  return rows / 256 * 256 > 0 ? rows / 256 * 256 : 256;
+}
+
+template <class E>
+struct AdForwardSpace {
+  AdGroups g;
+  float* v;
+  E *x, *W, *A, *B;
+  AdForwardSpace(AdSpace& ws, int64_t T, int K, int N, int r, int S) {
+    constexpr int kV = Vec16<E>::kCount;
+    g = ad_groups(ws, T, S);
+    v = ws.take<float>(static_cast<size_t>(T) * r);
+    x = ws.take<E>(static_cast<size_t>(T) * round_up(K, kV));
+    W = ws.take<E>(static_cast<size_t>(N) * round_up(K, kV));
+    A = ws.take<E>(static_cast<size_t>(S) * r * round_up(K, kV));
+  }
+};
+
+template <class E>
+lipcache_status ad_forward(const AdArgs& a, const float* bias, void* y, int64_t ldy, float* v, void* ws_, hipStream_t s) {
+  constexpr int kV = Vec16<E>::kCount;
+  AdSpace space{static_cast<char*>(ws_)};
+  const AdForwardSpace<E> ws(space, a.T, a.K, a.N, a.ad.r, a.ad.S);
+  AdRows<E> x, W, A;
+  lipcache_status st;
+  if ((st = ad_rows<E>(a.x, a.ldx, a.T, a.K, ws.x, x, s)) != LIPCACHE_OK) return st;
+  if ((st = ad_rows<E>(a.W, a.ldw, a.N, a.K, ws.W, W, s)) != LIPCACHE_OK) return st;
+  if ((st = ad_rows<E>(a.ad.A, a.K, static_cast<int64_t>(a.ad.S) * a.ad.r, a.K, ws.A, A, s)) != LIPCACHE_OK) return st;
+  const bool keep = v != nullptr;
+  if (!keep) v = ws.v;
+  const AdLow low{a.ad.B, a.ad.r, v, a.ad.scale, a.ad.r, a.ad.S, a.N, aligned16(a.ad.B) && a.ad.r % kV == 0,
+                  aligned16(v) && a.ad.r % 4 == 0};
+  const int64_t chunk = ad_chunk(x.ld, sizeof(E));
+  for (int64_t t0 = 0; t0 < a.T; t0 += chunk) {
+    const int T = static_cast<int>(a.T - t0 < chunk ? a.T - t0 : chunk);
+    const AdRows<E> xc{x.p + t0 * x.ld, x.ld};
+    AdLow lc = low;
+    lc.v = v + t0 * a.ad.r;
+    if ((st = ad_group(t0, T, a.ad, ws.g, s)) != LIPCACHE_OK) return st;
+    if ((st = ad_thin<E>(xc, a.K, A.p, A.ld, T, a.ad, ws.g, v + t0 * a.ad.r, s)) != LIPCACHE_OK) return st;
+    if (keep) {
+      ad_zero_rows_kernel<<<static_cast<unsigned>(ceil_div(T, 64) < 1024 ? ceil_div(T, 64) : 1024), 256, 0, s>>>(
+          ws.g, a.ad.S, T, a.ad.r, v + t0 * a.ad.r);
+      LC_LAUNCHED();
+    }
+    if ((st = ad_main<E, false>(xc.p, xc.ld, W.p, W.ld, T, a.N, a.K, bias, lc, ws.g, static_cast<E*>(y) + t0 * ldy, ldy, s)) !=
+        LIPCACHE_OK)
+      return st;
+  }
   return LIPCACHE_OK;
 }
 
-template <typename T>
-lipcache_status ad_backward(const AdArgs& g, const float* v_in, void* dx_, int64_t lddx, void* dA_, void* dB_,
-                            int32_t* pair, float* u, float* v_ws, hipStream_t s) {
-  const T *x = static_cast<const T*>(g.x), *W = static_cast<const T*>(g.W), *A = static_cast<const T*>(g.ad.A),
-          *B = static_cast<const T*>(g.ad.B), *dy = static_cast<const T*>(g.dy);
-  const float* scale = g.ad.scale;
-  T *dx = static_cast<T*>(dx_), *dA = static_cast<T*>(dA_), *dB = static_cast<T*>(dB_);
-  const int64_t ldx = g.ldx, ldw = g.ldw, lddy = g.lddy, N = g.N, K = g.K;
-  const int r = g.ad.r, S = g.ad.S;
-  if (g.T > 0) {
-    ad_pairs_kernel<<<static_cast<unsigned>((g.T + 255) / 256), 256, 0, s>>>(g.T, g.ad.offsets, g.ad.adapter, g.ad.R, S,
-                                                                            pair);
-    LC_LAUNCHED();
-    const unsigned waves = static_cast<unsigned>((g.T * r + 3) / 4);
-    ad_shrink_kernel<T, true><<<waves, 256, 0, s>>>(g.T, dy, lddy, g.N, B, r, pair, u);
-    LC_LAUNCHED();
+// Shares of a pair's rows, so that few pairs still fill the chip: about 512 workgroups, at least 512 rows each.
+inline int ad_splits(int64_t T, int K, int N, int S) {
+  const int64_t blocks = (ceil_div(K, 128) + ceil_div(N, 128)) * (S > 0 ? S : 1);
+  int64_t n = 512 / blocks;
+  const int64_t most = T / (S > 0 ? S : 1) / 512;
+  if (n > most) n = most;
+  return n < 1 ? 1 : n > 16 ? 16 : static_cast<int>(n);
+}
+
+template <class E>
+struct AdBackwardSpace {
+  AdGroups g;
+  float *u, *v, *part_a, *part_b;
+  E *x, *W, *dy, *A, *At, *Bt;
+  AdBackwardSpace(AdSpace& ws, int64_t T, int K, int N, int r, int S) {
+    constexpr int kV = Vec16<E>::kCount;
+    const size_t K8 = round_up(K, kV), N8 = round_up(N, kV), n = S;
+    g = ad_groups(ws, T, S);
+    u = ws.take<float>(static_cast<size_t>(T) * r);
+    v = ws.take<float>(static_cast<size_t>(T) * r);
+    At = ws.take<E>(n * K * round_up(r, kV));
+    Bt = ws.take<E>(n * r * N8);
+    const int splits = ad_splits(T, K, N, S);
+    part_a = ws.take<float>(splits > 1 ? splits * n * r * K : 0);
+    part_b = ws.take<float>(splits > 1 ? splits * n * r * N : 0);
+    x = ws.take<E>(static_cast<size_t>(T) * K8);
+    W = ws.take<E>(static_cast<size_t>(N) * K8);
+    dy = ws.take<E>(static_cast<size_t>(T) * N8);
+    A = ws.take<E>(n * r * K8);
+  }
+};
+
+template <class E>
+lipcache_status ad_backward(const AdArgs& a, const float* v_in, void* dx, int64_t lddx, void* dA, void* dB, void* ws_,
+                            hipStream_t s) {
+  constexpr int kV = Vec16<E>::kCount;
+  AdSpace space{static_cast<char*>(ws_)};
+  const AdBackwardSpace<E> ws(space, a.T, a.K, a.N, a.ad.r, a.ad.S);
+  const int r = a.ad.r, S = a.ad.S, K = a.K, N = a.N;
+  AdRows<E> x{}, W{}, dy{}, A{};
+  lipcache_status st;
+  if ((st = ad_rows<E>(a.dy, a.lddy, a.T, N, ws.dy, dy, s)) != LIPCACHE_OK) return st;
+  if (dA && (st = ad_rows<E>(a.x, a.ldx, a.T, K, ws.x, x, s)) != LIPCACHE_OK) return st;
+  const int64_t r8 = round_up(r, kV), N8 = round_up(N, kV);
+  const AdCopy bt{a.ad.B, ws.Bt, r, N8, static_cast<int64_t>(N) * r, r * N8, N, r, r, static_cast<int>(N8), S};
+  if ((st = ad_copy<E, true>(bt, s)) != LIPCACHE_OK) return st;
+  if ((st = ad_group(0, a.T, a.ad, ws.g, s)) != LIPCACHE_OK) return st;
+  if ((st = ad_thin<E>(dy, N, ws.Bt, N8, a.T, a.ad, ws.g, ws.u, s)) != LIPCACHE_OK) return st;
+  if (dA && S > 0) {
     if (!v_in) {
-      ad_shrink_kernel<T, false><<<waves, 256, 0, s>>>(g.T, x, ldx, g.K, A, r, pair, v_ws);
+      if ((st = ad_rows<E>(a.ad.A, K, static_cast<int64_t>(S) * r, K, ws.A, A, s)) != LIPCACHE_OK) return st;
+      if ((st = ad_thin<E>(x, K, A.p, A.ld, a.T, a.ad, ws.g, ws.v, s)) != LIPCACHE_OK) return st;
+      v_in = ws.v;
+    }
+    const int splits = ad_splits(a.T, K, N, S);
+    const AdGradSide<E> ga{x.p, x.ld, ws.u, static_cast<E*>(dA), ws.part_a, K, static_cast<int>(ceil_div(K, 128)), false};
+    const AdGradSide<E> gb{dy.p, dy.ld, v_in, static_cast<E*>(dB), ws.part_b, N, static_cast<int>(ceil_div(N, 128)), true};
+    const unsigned blocks = static_cast<unsigned>((ga.blocks + gb.blocks) * splits) * S;
+    if (r <= 32) ad_grad_kernel<E, 1><<<blocks, 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g);
+    else if (r <= 64) ad_grad_kernel<E, 2><<<blocks, 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g);
+    else ad_grad_kernel<E, 4><<<blocks, 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g);
+    LC_LAUNCHED();
+    if (splits > 1) {
+      const int64_t most = static_cast<int64_t>(S) * r * (K > N ? K : N);
+      ad_join_kernel<E><<<dim3(static_cast<unsigned>(ceil_div(most, 256)), 2), 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g);
       LC_LAUNCHED();
-      v_in = v_ws;
     }
   }
-  if (dx)
-    LC_HIP(tile_product(
-        g.T, K, N, 1, [=] __device__(int, int64_t i, int64_t k) { return load_f32(dy + i * lddy + k); },
-        [=] __device__(int, int64_t j, int64_t k) { return load_f32(W + k * ldw + j); },
-        [=] __device__(int, int64_t i, int64_t j, float sum) {
-          const int a = pair[i];
-          if (a >= 0) {
-            const T* f = A + static_cast<int64_t>(a) * r * K + j;
-            float low = 0.0f;
-            for (int rho = 0; rho < r; ++rho) low = fmaf(u[i * r + rho], load_f32(f + rho * K), low);
-            sum = fmaf(scale[a], low, sum);
-          }
-          dx[i * lddx + j] = round_to<T>(sum);
-        },
-        s));
-  if (dA && S > 0) {
-    LC_HIP(tile_product(
-        r, K, g.T, S, [=] __device__(int z, int64_t i, int64_t t) { return pair[t] == z ? u[t * r + i] : 0.0f; },
-        [=] __device__(int z, int64_t j, int64_t t) { return pair[t] == z ? load_f32(x + t * ldx + j) : 0.0f; },
-        [=] __device__(int z, int64_t i, int64_t j, float sum) {
-          dA[(static_cast<int64_t>(z) * r + i) * K + j] = round_to<T>(scale[z] * sum);
-        },
-        s));
-    LC_HIP(tile_product(
-        N, r, g.T, S,
-        [=] __device__(int z, int64_t i, int64_t t) { return pair[t] == z ? load_f32(dy + t * lddy + i) : 0.0f; },
-        [=] __device__(int z, int64_t j, int64_t t) { return pair[t] == z ? v_in[t * r + j] : 0.0f; },
-        [=] __device__(int z, int64_t i, int64_t j, float sum) {
-          dB[(static_cast<int64_t>(z) * N + i) * r + j] = round_to<T>(scale[z] * sum);
-        },
-        s));
+  if (dx && a.T > 0) {
+    if ((st = ad_rows<E>(a.W, a.ldw, N, K, ws.W, W, s)) != LIPCACHE_OK) return st;
+    const AdCopy at{a.ad.A, ws.At, K, r8, static_cast<int64_t>(r) * K, K * r8, r, K, K, static_cast<int>(r8), S};
+    if ((st = ad_copy<E, true>(at, s)) != LIPCACHE_OK) return st;
+    const int64_t chunk = ad_chunk(dy.ld, sizeof(E));
+    for (int64_t t0 = 0; t0 < a.T; t0 += chunk) {
+      const int T = static_cast<int>(a.T - t0 < chunk ? a.T - t0 : chunk);
+      if (a.T > chunk && (st = ad_group(t0, T, a.ad, ws.g, s)) != LIPCACHE_OK) return st;
+      const AdLow low{ws.At, r8, ws.u + t0 * r, a.ad.scale, r, S, K, true, aligned16(ws.u + t0 * r) && r % 4 == 0};
+      if ((st = ad_main<E, true>(dy.p + t0 * dy.ld, dy.ld, W.p, W.ld, T, K, N, nullptr, low, ws.g,
+                                 static_cast<E*>(dx) + t0 * lddx, lddx, s)) != LIPCACHE_OK)
+        return st;
+    }
   }
   return LIPCACHE_OK;
+}
+
+template <class E>
+size_t ad_workspace(bool backward, int64_t T, int K, int N, int r, int S) {
+  AdSpace space{nullptr};
+  if (backward) AdBackwardSpace<E>(space, T, K, N, r, S);
+  else AdForwardSpace<E>(space, T, K, N, r, S);
+  return space.used;
+}
+
+size_t ad_workspace(bool backward, int64_t T, int K, int N, int r, int S, int32_t dtype) {
+  return dtype == LIPCACHE_F32 ? ad_workspace<float>(backward, T, K, N, r, S) : ad_workspace<__bf16>(backward, T, K, N, r, S);
 }
 
 // ------------------------------------------------------------- validation
@@ -166,7 +833,7 @@ lipcache_status ad_check(const lipcache_adapters* ad, int64_t T, int32_t K, int3
   if (ad->R > 0 && (!ad->offsets || !ad->adapter || ad_unaligned(ad->offsets, LIPCACHE_F32) ||
                     ad_unaligned(ad->adapter, LIPCACHE_F32)))
     return LIPCACHE_EINVAL;
-  if (ad->r > kAdMaxRank || K > kAdMaxWidth || N > kAdMaxWidth || T > 0x7fffffff || ad->S > 65535)
+  if (ad->r > kAdMaxRank || K > kAdMaxWidth || N > kAdMaxWidth || T > 0x7fffffff || ad->S > kAdMaxPairs)
     return LIPCACHE_EUNSUPPORTED;
   return LIPCACHE_OK;
 }
@@ -178,7 +845,7 @@ using namespace lc;
 extern "C" size_t lipcache_adapter_forward_workspace_bytes(int64_t T, int32_t K, int32_t N, int32_t r, int32_t S,
                                                            int32_t dtype) {
   if (ad_sizes_bad(T, K, N, dtype) || r < 1 || S < 0) return 0;
-  return align_up(static_cast<size_t>(T) * 4, 256) + align_up(static_cast<size_t>(T) * r * 4, 256);
+  return ad_workspace(false, T, K, N, r, S, dtype);
 }
 
 extern "C" lipcache_status lipcache_adapter_forward(const void* x, int64_t ldx, int64_t T, const void* W, int64_t ldw,
@@ -194,22 +861,18 @@ extern "C" lipcache_status lipcache_adapter_forward(const void* x, int64_t ldx, 
   if (!ws || !aligned256(ws) || ws_bytes < lipcache_adapter_forward_workspace_bytes(T, K, N, ad->r, ad->S, dtype))
     return LIPCACHE_EWORKSPACE;
   if (T == 0) return LIPCACHE_OK;
-  char* p = static_cast<char*>(ws);
-  int32_t* pair = reinterpret_cast<int32_t*>(p);
-  p += align_up(static_cast<size_t>(T) * 4, 256);
-  if (!v) v = reinterpret_cast<float*>(p);
   AdArgs g{x, W, nullptr, ldx, ldw, 0, T, K, N, *ad};
   switch (dtype) {
-    case LIPCACHE_F32: return ad_forward<float>(g, bias, y, ldy, v, pair, stream);
-    case LIPCACHE_BF16: return ad_forward<__bf16>(g, bias, y, ldy, v, pair, stream);
-    default: return ad_forward<_Float16>(g, bias, y, ldy, v, pair, stream);
+    case LIPCACHE_F32: return ad_forward<float>(g, bias, y, ldy, v, ws, stream);
+    case LIPCACHE_BF16: return ad_forward<__bf16>(g, bias, y, ldy, v, ws, stream);
+    default: return ad_forward<_Float16>(g, bias, y, ldy, v, ws, stream);
   }
 }
 
 extern "C" size_t lipcache_adapter_backward_workspace_bytes(int64_t T, int32_t K, int32_t N, int32_t r, int32_t S,
                                                             int32_t dtype) {
   if (ad_sizes_bad(T, K, N, dtype) || r < 1 || S < 0) return 0;
-  return align_up(static_cast<size_t>(T) * 4, 256) + 2 * align_up(static_cast<size_t>(T) * r * 4, 256);
+  return ad_workspace(true, T, K, N, r, S, dtype);
 }
 
 extern "C" lipcache_status lipcache_adapter_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, int64_t T,
@@ -225,15 +888,10 @@ extern "C" lipcache_status lipcache_adapter_backward(const void* dy, int64_t ldd
     return LIPCACHE_EINVAL;
   if (!ws || !aligned256(ws) || ws_bytes < lipcache_adapter_backward_workspace_bytes(T, K, N, ad->r, ad->S, dtype))
     return LIPCACHE_EWORKSPACE;
-  char* p = static_cast<char*>(ws);
-  int32_t* pair = reinterpret_cast<int32_t*>(p);
-  p += align_up(static_cast<size_t>(T) * 4, 256);
-  float* u = reinterpret_cast<float*>(p);
-  float* v_ws = reinterpret_cast<float*>(p + align_up(static_cast<size_t>(T) * ad->r * 4, 256));
   AdArgs g{x, W, dy, ldx, ldw, lddy, T, K, N, *ad};
   switch (dtype) {
-    case LIPCACHE_F32: return ad_backward<float>(g, v, dx, lddx, dA, dB, pair, u, v_ws, stream);
-    case LIPCACHE_BF16: return ad_backward<__bf16>(g, v, dx, lddx, dA, dB, pair, u, v_ws, stream);
-    default: return ad_backward<_Float16>(g, v, dx, lddx, dA, dB, pair, u, v_ws, stream);
+    case LIPCACHE_F32: return ad_backward<float>(g, v, dx, lddx, dA, dB, ws, stream);
+    case LIPCACHE_BF16: return ad_backward<__bf16>(g, v, dx, lddx, dA, dB, ws, stream);
+    default: return ad_backward<_Float16>(g, v, dx, lddx, dA, dB, ws, stream);
   }
 }

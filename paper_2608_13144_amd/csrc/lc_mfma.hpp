@@ -38,12 +38,12 @@ typedef __attribute__((address_space(3))) char lds_char;
 
 constexpr uint32_t kNoRow = 0x80000000u;  // a copy offset past every buffer (their sizes stay below 2^31): reads zero
 
-// Buffer descriptor of `bytes` bytes at p (raw 32-bit format, no stride).
+// Buffer descriptor of `bytes` bytes at p (wave-uniform; raw 32-bit format, no stride).
 __device__ __forceinline__ i32x4 buffer_of(const void* p, uint32_t bytes) {
   const uint64_t a = reinterpret_cast<uint64_t>(p);
   i32x4 r;
-  r[0] = static_cast<int32_t>(static_cast<uint32_t>(a));
-  r[1] = static_cast<int32_t>(static_cast<uint32_t>(a >> 32) & 0xffffu);
+  r[0] = uniform(static_cast<int32_t>(static_cast<uint32_t>(a)));
+  r[1] = uniform(static_cast<int32_t>(static_cast<uint32_t>(a >> 32) & 0xffffu));
   r[2] = static_cast<int32_t>(bytes);
   r[3] = 0x00027000;
   return r;

@@ -143,6 +143,49 @@ def test_output_rows_apart(dtype):
     assert bool((wide[:, :5] == 7).all()) and bool((wide[:, 205:] == 7).all())
 
 
+# Every tile size of the main product, and a pair's rows in several shares.
+LARGE = [(2100, 136, 1040, 5, 20, 40), (2600, 72, 2100, 3, 8, 9), (4200, 72, 3300, 2, 24, 30), (4200, 136, 72, 2, 16, 7),
+         (5000, 64, 200, 1, 40, 3), (1300, 2100, 72, 40, 8, 600), (4200, 3300, 72, 4, 72, 12)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("size", LARGE, ids=lambda s: "x".join(map(str, s)))
+def test_large(size, dtype):
+    T, K, N, S, r, R_ = size
+    b = make(sum(size), T, K, N, S, r, R_, dtype)
+    out = check_forward(b, dtype, f"large {size} {dtype}")
+    check_backward(b, dtype, f"large {size} {dtype}", out.v)
+
+
+def test_rows_past_31_bits():
+    """Rows 4 MiB apart: offsets of x and dy pass 2^31 bytes inside one batch."""
+    b = make(15, 600, 64, 48, 3, 8, 7, "f16")
+    ref = check_forward(b, "f16", "rows close together")
+    gref = check_backward(b, "f16", "rows close together", ref.v)
+    for name in ("x", "dy"):
+        wide = torch.empty(600, 1 << 21, dtype=torch.float16, device=DEV)
+        view = wide[:, 32:32 + b[name].shape[1]]
+        view.copy_(b[name])
+        b[name] = view
+    out = check_forward(b, "f16", "rows 4 MiB apart")
+    g = check_backward(b, "f16", "rows 4 MiB apart", ref.v)
+    assert torch.equal(out.y, ref.y) and torch.equal(out.v, ref.v)
+    assert torch.equal(g.dx, gref.dx) and torch.equal(g.dA, gref.dA) and torch.equal(g.dB, gref.dB)
+
+
+def test_offsets_that_decrease_stay_inside():
+    """Not a valid batch: rows land anywhere, but every output is written from inside the arrays and the call ends."""
+    for T in (20, 400):
+        b = make(16, T, 64, 48, 3, 8, 6, "bf16")
+        for offs in ([9, 3, T, 0, T, 2, T], [T, T, 5, 0, 0, 0, 0], [-(1 << 31), (1 << 31) - 1, 0, T, -9, T, 1]):
+            b["offsets"] = torch.tensor(offs, dtype=torch.int64).to(torch.int32).to(DEV)
+            out = api.adapter_forward(*[b[k] for k in ("x", "W", "bias", "A", "B", "scale", "offsets", "adapter")], keep=True)
+            api.adapter_backward(*[b[k] for k in ("dy", "x", "W", "A", "B", "scale", "offsets", "adapter")], v=out.v)
+            torch.cuda.synchronize()
+    b = make(16, 400, 64, 48, 3, 8, 6, "bf16")
+    check_forward(b, "bf16", "after them")
+
+
 @pytest.mark.parametrize("T", [3, 200])
 def test_no_pairs_no_requests_no_bias(T):
     for S, R_, none in ((2, 3, 1.0), (2, 0, 0.0), (0, 3, 0.0)):
