@@ -34,48 +34,70 @@ struct AdGroups {
   int32_t* start;      // [S + 2] first place of each pair, of none, and T
   int32_t* tile_pair;  // [tiles]
   int32_t* tile_row;   // [tiles] first sorted place
-  int32_t* tiles;      // number of tiles
+  int32_t* tile_start; // [S + 1] first tile of each pair, and the number of tiles
   uint32_t* zeros;     // 16 bytes of zero
 };
 
 __host__ __device__ inline int64_t ad_tiles(int64_t T, int S) { return T / kThinRows + (S < T ? S : T); }
 
+constexpr int kGroupThreads = 1024;
+
+// Inclusive sums over the workgroup's threads, in LDS (`sums`, one word a
+// thread; `waves`, one a wave).  Ends with a barrier.
+__device__ __forceinline__ void group_scan(int v, int32_t* sums, int32_t* waves) {
+  const int tid = static_cast<int>(threadIdx.x), lane = lane_id(), wave = tid / kWave;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int u = __shfl_up(v, o, kWave);
+    if (lane >= o) v += u;
+  }
+  if (lane == kWave - 1) waves[wave] = v;
+  __syncthreads();
+  int before = 0;
+  for (int w = 0; w < wave; ++w) before += waves[w];
+  sums[tid] = before + v;
+  __syncthreads();
+}
+
 // Workgroup s places the rows of pair s.  Every workgroup counts all pairs'
 // rows (integer sums in LDS: any order gives the same), then walks the
-// requests in order, 256 at a time.  Request -1 is the rows before the first
+// requests in order, 1024 at a time.  Request -1 is the rows before the first
 // offset, request R those after the last.  Offsets that decrease place rows
 // wrongly or not at all; every index is checked, and places left over hold row
-// 0 without a pair, so whatever they are no access leaves the arrays.
-__global__ __launch_bounds__(256) void ad_group_kernel(int64_t t0, int T, const int32_t* __restrict__ offsets,
-                                                       const int32_t* __restrict__ adapter, int R, int S, AdGroups g) {
-  extern __shared__ int32_t count[];  // [S + 1] rows of each pair, then scratch
-  int32_t* sum = count + S + 1;       // [256]
-  int32_t* first = sum + 256;         // [256]
-  __shared__ uint32_t base_rows, base_tiles;
+// 0 without a pair, so whatever they are no access leaves the arrays.  Bound
+// by the latency of three dependent steps of loads: 4 us for 1024 requests.
+__global__ __launch_bounds__(kGroupThreads) void ad_group_kernel(int64_t t0, int T, const int32_t* __restrict__ offsets,
+                                                                 const int32_t* __restrict__ adapter, int R, int S,
+                                                                 AdGroups g) {
+  extern __shared__ int32_t count[];        // [S + 1] rows of each pair, then scratch
+  int32_t* sums = count + S + 1;            // [kGroupThreads]
+  int32_t* first = sums + kGroupThreads;    // [kGroupThreads]
+  int32_t* waves = first + kGroupThreads;   // [kGroupThreads / kWave]
+  __shared__ unsigned long long base_rows, base_tiles;
   const int tid = static_cast<int>(threadIdx.x), s = static_cast<int>(blockIdx.x);
-  for (int i = tid; i <= S; i += 256) count[i] = 0;
-  if (tid == 0) base_rows = base_tiles = 0;
-  __syncthreads();
   auto request = [&](int i, int& lo, int& key) {  // i in [-1, R]; returns its rows
     const int64_t a = i < 0 ? t0 : R > 0 ? offsets[i] : t0, b = i < 0 ? (R > 0 ? offsets[0] : t0) : i < R ? offsets[i + 1] : t0 + T;
+    const int p = i >= 0 && i < R ? adapter[i] : -1;
     const int64_t l = a < t0 ? t0 : a, h = b > t0 + T ? t0 + T : b;
     lo = static_cast<int>(l - t0);
-    key = S;
-    if (i >= 0 && i < R) {
-      const int p = adapter[i];
-      if (p >= 0 && p < S) key = p;
-    }
+    key = p >= 0 && p < S ? p : S;
     return h > l ? static_cast<int>(h - l) : 0;
   };
-  for (int i = tid - 1; i <= R; i += 256) {
+  int lo0 = 0, key0 = S, n0 = 0;  // this thread's request among the first 1024
+  if (tid - 1 <= R) n0 = request(tid - 1, lo0, key0);
+  for (int i = tid; i <= S; i += kGroupThreads) count[i] = 0;
+  if (tid == 0) base_rows = base_tiles = 0;
+  __syncthreads();
+  if (n0 > 0) atomicAdd(&count[key0], n0);
+  for (int i = tid - 1 + kGroupThreads; i <= R; i += kGroupThreads) {
     int lo, key;
     const int n = request(i, lo, key);
     if (n > 0) atomicAdd(&count[key], n);
   }
   __syncthreads();
-  uint32_t rows = 0, tiles = 0;
-  const uint32_t all = static_cast<uint32_t>(T);
-  for (int i = tid; i < s; i += 256) {
+  unsigned long long rows = 0, tiles = 0;
+  const uint32_t all = static_cast<uint32_t>(T), last = static_cast<uint32_t>(ad_tiles(T, S));
+  for (int i = tid; i < s; i += kGroupThreads) {
     const uint32_t n = static_cast<uint32_t>(count[i]);
     rows += n;
     tiles += ((n < all ? n : all) + kThinRows - 1) / kThinRows;  // as many as the pair writes below
@@ -85,59 +107,48 @@ __global__ __launch_bounds__(256) void ad_group_kernel(int64_t t0, int T, const 
     atomicAdd(&base_tiles, tiles);
   }
   __syncthreads();
-  const uint32_t place0 = base_rows, mine = static_cast<uint32_t>(count[s]);
+  const uint64_t place0 = base_rows;
+  const uint32_t mine = static_cast<uint32_t>(count[s]);
   if (tid == 0) {
     g.start[s] = static_cast<int32_t>(place0 < all ? place0 : all);
-    if (s == S) {
-      g.start[S + 1] = T;
-      *g.tiles = static_cast<int32_t>(base_tiles);
-    }
+    g.tile_start[s] = static_cast<int32_t>(base_tiles < last ? base_tiles : last);
+    if (s == S) g.start[S + 1] = T;
   }
   if (s == S && tid < 4) g.zeros[tid] = 0;
   if (s < S) {
-    const uint32_t last = static_cast<uint32_t>(ad_tiles(T, S));
-    for (uint32_t i = tid; i * kThinRows < (mine < all ? mine : all); i += 256) {
-      const uint32_t at = base_tiles + i;
+    for (uint64_t i = tid; i * kThinRows < (mine < all ? mine : all); i += kGroupThreads) {
+      const uint64_t at = base_tiles + i, row = place0 + i * kThinRows;
       if (at < last) {
         g.tile_pair[at] = s;
-        g.tile_row[at] = static_cast<int32_t>(place0 + i * kThinRows);
+        g.tile_row[at] = static_cast<int32_t>(row < all ? row : all);
       }
     }
   }
-  uint32_t place = place0;
-  for (int i0 = -1; i0 <= R && mine > 0 && place < all; i0 += 256) {
-    int lo = 0, key = S, n = 0;
-    if (i0 + tid <= R) {
-      n = request(i0 + tid, lo, key);
-      if (key != s) n = 0;
+  uint64_t place = place0;
+  for (int i0 = -1; i0 <= R && mine > 0 && place < all; i0 += kGroupThreads) {
+    if (i0 >= 0) {
+      n0 = 0;
+      if (i0 + tid <= R) n0 = request(i0 + tid, lo0, key0);
+      __syncthreads();  // the last round's readers of sums and first are done
     }
-    // exclusive sums of n over the 256 requests
-    __syncthreads();
-    sum[tid] = n;
-    first[tid] = lo;
-    __syncthreads();
-    for (int o = 1; o < 256; o <<= 1) {
-      const int v = tid >= o ? sum[tid - o] : 0;
-      __syncthreads();
-      sum[tid] += v;
-      __syncthreads();
-    }
-    const int total = sum[255];
-    for (int p = tid; p < total && place + p < all; p += 256) {
-      int a = 0, b = 255;  // the request that holds the p-th row: the first whose sum passes p
+    first[tid] = lo0;
+    group_scan(key0 == s ? n0 : 0, sums, waves);
+    const int total = sums[kGroupThreads - 1];
+    for (int p = tid; p < total && place + p < all; p += kGroupThreads) {
+      int a = 0, b = kGroupThreads - 1;  // the request that holds the p-th row: the first whose sum passes p
       while (a < b) {
         const int mid = (a + b) >> 1;
-        if (sum[mid] > p) b = mid; else a = mid + 1;
+        if (sums[mid] > p) b = mid; else a = mid + 1;
       }
-      const int before = a > 0 ? sum[a - 1] : 0;
+      const int before = a > 0 ? sums[a - 1] : 0;
       const uint32_t row = static_cast<uint32_t>(first[a] + p - before);
       g.order[place + p] = row < all ? static_cast<int32_t>(row) : 0;
       g.pair[place + p] = s;
     }
-    place += static_cast<uint32_t>(total);
+    place += total > 0 ? total : 0;
   }
   if (s == S)
-    for (uint64_t p = static_cast<uint64_t>(place) + tid; p < all; p += 256) {
+    for (uint64_t p = place + tid; p < all; p += kGroupThreads) {
       g.order[p] = 0;
       g.pair[p] = S;
     }
@@ -184,13 +195,19 @@ struct AdCopy {
   int stack;
 };
 
+// The first `blocks` workgroups copy c, the others d.
 template <typename T, bool kTranspose>
-__global__ __launch_bounds__(256) void ad_copy_kernel(AdCopy c) {
+__global__ __launch_bounds__(256) void ad_copy_kernel(AdCopy c, AdCopy d, int blocks) {
   __shared__ T tile[32][33];
   const int x = static_cast<int>(threadIdx.x) & 31, y = static_cast<int>(threadIdx.x) >> 5;
+  int block = static_cast<int>(blockIdx.x);
+  if (block >= blocks) {
+    block -= blocks;
+    c = d;
+  }
   // tiles of the result
   const int64_t tiles_w = ceil_div(c.to_width, 32), tiles = tiles_w * ceil_div(c.to_rows, 32);
-  const int64_t z = blockIdx.x / tiles, t = blockIdx.x % tiles;
+  const int64_t z = block / tiles, t = block % tiles;
   const int i0 = static_cast<int>(t / tiles_w) * 32, j0 = static_cast<int>(t % tiles_w) * 32;
   const T* from = static_cast<const T*>(c.from) + z * c.from_next;
   T* to = static_cast<T*>(c.to) + z * c.to_next;
@@ -213,93 +230,57 @@ __global__ __launch_bounds__(256) void ad_copy_kernel(AdCopy c) {
   }
 }
 
+inline int64_t ad_copy_blocks(const AdCopy& c) { return ceil_div(c.to_width, 32) * ceil_div(c.to_rows, 32) * c.stack; }
+
 template <typename T, bool kTranspose>
-lipcache_status ad_copy(const AdCopy& c, hipStream_t s) {
-  const int64_t blocks = ceil_div(c.to_width, 32) * ceil_div(c.to_rows, 32) * c.stack;
-  if (blocks <= 0) return LIPCACHE_OK;
-  if (blocks > 0x7fffffff) return LIPCACHE_EUNSUPPORTED;
-  ad_copy_kernel<T, kTranspose><<<static_cast<unsigned>(blocks), 256, 0, s>>>(c);
+lipcache_status ad_copy(const AdCopy& c, const AdCopy& d, hipStream_t s) {
+  const int64_t blocks = ad_copy_blocks(c), more = ad_copy_blocks(d);
+  if (blocks + more <= 0) return LIPCACHE_OK;
+  if (blocks + more > 0x7fffffff) return LIPCACHE_EUNSUPPORTED;
+  ad_copy_kernel<T, kTranspose><<<static_cast<unsigned>(blocks + more), 256, 0, s>>>(c, d, static_cast<int>(blocks));
   LC_LAUNCHED();
   return LIPCACHE_OK;
 }
 
 // ------------------------------------------------------------ thin products
 // out[row][rho] = F_a[rho] . x[row] for the up to 32 sorted rows of one tile
-// of the table: F is [S][r][ldf].  Both operands come straight from global
-// memory in 16-byte vectors: lane l holds row l % 32 of x and of F, and half
-// l / 32 of each 128 bytes of the contraction, so a row's four vectors are one
-// half of a cache line.  The eight waves share the contraction and their sums
-// are added in LDS in order.  Bound by the latency and bandwidth of x's rows.
-template <class E, int NR>
-__global__ __launch_bounds__(512) void ad_thin_kernel(const E* __restrict__ x, int64_t ldx, int width,
-                                                      const E* __restrict__ F, int64_t ldf, int r, AdGroups g,
-                                                      float* __restrict__ out) {
-  constexpr int kV = Vec16<E>::kCount, kBlock = 8 * kV, kWaves = 8;
-  typedef typename Vec16<E>::type V;
-  __shared__ f32x4 part[kWaves][4][kWave];
-  const int t = static_cast<int>(blockIdx.x);
-  if (static_cast<uint32_t>(t) >= static_cast<uint32_t>(*g.tiles)) return;
+// of the table (F is [S][r][ldf]), the contraction shared by four waves.  The
+// workgroups past the table write zeros to the rows without a pair.  Bound by
+// reading x once, and F_a once a tile.
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void ad_thin_kernel(const typename S::E* __restrict__ x, int64_t ldx, int width,
+                                                              const typename S::E* __restrict__ F, int64_t ldf, int r,
+                                                              int pairs, int T, AdGroups g, float* __restrict__ out) {
+  typedef typename S::E E;
+  __shared__ __align__(16) char lds[S::kLds];
+  const int t = static_cast<int>(blockIdx.x), table = static_cast<int>(ad_tiles(T, pairs));
+  if (t >= table) {
+    const int first = g.start[pairs];
+    const int64_t all = static_cast<int64_t>(T - first) * r, step = static_cast<int64_t>(gridDim.x - table) * S::kThreads;
+    for (int64_t i = static_cast<int64_t>(t - table) * S::kThreads + threadIdx.x; i < all; i += step)
+      out[static_cast<int64_t>(g.order[first + i / r]) * r + i % r] = 0.0f;
+    return;
+  }
+  if (static_cast<uint32_t>(t) >= static_cast<uint32_t>(g.tile_start[pairs])) return;
   const int a = g.tile_pair[t], row0 = g.tile_row[t];
-  if (row0 < 0) return;
   const int end = g.start[a + 1] - row0, rows = end < kThinRows ? end : kThinRows;
   if (rows <= 0) return;
-  const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
-  const int li = lane & 31, half = lane >> 5;
-  const int row = g.order[row0 + (li < rows ? li : rows - 1)];
-  const E* px = x + row * ldx + half * (4 * kV);
-  const E* pf[NR];
+  Side p{}, q{};
+  p.p = x;
+  p.ld = ldx * sizeof(E);
+  p.rows = rows;
+  p.pick = g.order + row0;
+  q.p = F + static_cast<int64_t>(a) * r * ldf;
+  q.ld = ldf * sizeof(E);
+  q.rows = r;
+  f32x16 acc[S::TM][S::TN] = {};
+  tile_products<S>(p, q, width, lds, acc);
+  tile_store<S>(acc, [&](int i, int j, const f32x16& v) {
+    if (j >= r) return;
 #pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    const int rho = 32 * n + li < r ? 32 * n + li : r - 1;
-    pf[n] = F + (static_cast<int64_t>(a) * r + rho) * ldf + half * (4 * kV);
-  }
-  f32x16 acc[NR] = {};
-  for (int k = wave * kBlock; k < width; k += kWaves * kBlock) {
-    V vx[4], vf[NR][4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const bool in = k + half * (4 * kV) + c * kV < width;
-      vx[c] = in ? *reinterpret_cast<const V*>(px + k + c * kV) : V{};
-#pragma unroll
-      for (int n = 0; n < NR; ++n) vf[n][c] = in ? *reinterpret_cast<const V*>(pf[n] + k + c * kV) : V{};
-    }
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-      for (int n = 0; n < NR; ++n) acc[n] = MfmaType<E>::mul(vx[c], vf[n][c], acc[n]);
-  }
-#pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    if (n > 0) __syncthreads();
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      part[wave][q][lane] = f32x4{acc[n][4 * q], acc[n][4 * q + 1], acc[n][4 * q + 2], acc[n][4 * q + 3]};
-    __syncthreads();
-    // 4 x 64 vectors of four rows: one for each thread of the first four waves
-    if (wave < 4) {
-      f32x4 v = part[0][wave][lane];
-#pragma unroll
-      for (int w = 1; w < kWaves; ++w) {
-        const f32x4 u = part[w][wave][lane];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += u[e];
-      }
-      const int rho = 32 * n + li;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int i = 8 * wave + 4 * half + e;
-        if (i < rows && rho < r) out[static_cast<int64_t>(g.order[row0 + i]) * r + rho] = v[e];
-      }
-    }
-  }
-}
-
-// Rows without a pair: zeros.
-__global__ __launch_bounds__(256) void ad_zero_rows_kernel(AdGroups g, int S, int T, int r, float* __restrict__ out) {
-  const int first = g.start[S];
-  const int64_t all = static_cast<int64_t>(T - first) * r;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += 256 * static_cast<int64_t>(gridDim.x))
-    out[static_cast<int64_t>(g.order[first + i / r]) * r + i % r] = 0.0f;
+    for (int e = 0; e < 16; ++e)
+      if (i + acc_row(e) < rows) out[static_cast<int64_t>(g.order[row0 + i + acc_row(e)]) * r + j] = v[e];
+  });
 }
 
 // ------------------------------------------------------------- main product
@@ -327,28 +308,44 @@ struct AdLow {
   int wide_v;          // v's
 };
 
-// acc += scale_a F_a v for the tile's rows of every pair among them.
+// The rows of a wave's accumulators: lane l has row l % 32 of each 32, loaded before the main loop.
+template <class S>
+struct AdTileRows {
+  int pair[S::TM], row[S::TM];
+  __device__ __forceinline__ void load(const AdGroups& g, int pairs, int i0, int rows) {
+    const int wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+    const int wm = wave % (S::WM * S::WN) / S::WN;
+#pragma unroll
+    for (int tm = 0; tm < S::TM; ++tm) {
+      const int i = (wm * S::TM + tm) * 32 + (lane_id() & 31);
+      const bool in = i < rows;
+      pair[tm] = in ? g.pair[i0 + i] : pairs;
+      row[tm] = g.order[i0 + (in ? i : 0)];
+    }
+  }
+};
+
+// acc += scale_a F_a v for the tile's rows of every pair among them: one pair
+// of a 32-row accumulator at a time, its rows a mask.
 template <class S, class E>
-__device__ __forceinline__ void add_low_rank(const AdLow& low, const AdGroups& g, int i0, int rows, int j0,
+__device__ __forceinline__ void add_low_rank(const AdLow& low, const AdTileRows<S>& rows, int j0,
                                              f32x16 (&acc)[S::TM][S::TN]) {
   constexpr int kV = Vec16<E>::kCount;
   typedef typename Vec16<E>::type V;
   const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
-  const int wm = wave / S::WN, wn = wave % S::WN;
+  const int wn = wave % S::WN;
   const int li = lane & 31, half = lane >> 5;
   const E* F = static_cast<const E*>(low.F);
-  for (int at = 0; at < rows;) {
-    const int a = uniform(g.pair[i0 + at]);
-    if (a >= low.S) break;  // rows without a pair come last
-    const int next = uniform(g.start[a + 1]) - i0, end = next < rows ? next : rows;
-    if (end <= at) break;
-    const float scale = low.scale[a];
 #pragma unroll
-    for (int tm = 0; tm < S::TM; ++tm) {
-      const int m0 = (wm * S::TM + tm) * 32;  // the 32 rows of this accumulator
-      if (m0 >= end || m0 + 32 <= at) continue;
-      const bool mine = m0 + li >= at && m0 + li < end;
-      const float* v = low.v + static_cast<int64_t>(g.order[i0 + (mine ? m0 + li : at)]) * low.r;
+  for (int tm = 0; tm < S::TM; ++tm) {
+    uint32_t todo = static_cast<uint32_t>(__ballot(rows.pair[tm] < low.S));
+    const float* v = low.v + static_cast<int64_t>(rows.row[tm]) * low.r;
+    while (todo) {
+      const int a = __builtin_amdgcn_readlane(rows.pair[tm], __builtin_ctz(todo));
+      const bool mine = rows.pair[tm] == a;
+      const uint32_t mask = static_cast<uint32_t>(__ballot(mine));
+      todo &= ~mask;
+      const float scale = low.scale[a];
 #pragma unroll
       for (int tn = 0; tn < S::TN; ++tn) {
         const int j = j0 + (wn * S::TN + tn) * 32 + li;
@@ -381,13 +378,10 @@ __device__ __forceinline__ void add_low_rank(const AdLow& low, const AdGroups& g
           }
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int i = m0 + acc_row(e) + 4 * half;
-          if (i >= at && i < end) acc[tm][tn][e] += sum[e];
-        }
+        for (int e = 0; e < 16; ++e)
+          if (mask >> (acc_row(e) + 4 * half) & 1) acc[tm][tn][e] += sum[e];
       }
     }
-    at = end;
   }
 }
 
@@ -411,9 +405,11 @@ __global__ __launch_bounds__(S::kThreads) void ad_main_kernel(const typename S::
   q.p = Q + (S::QCOL ? static_cast<int64_t>(j0) : j0 * ldq);
   q.ld = ldq * sizeof(E);
   q.rows = width - j0 < S::BN ? width - j0 : S::BN;
+  AdTileRows<S> rows;
+  rows.load(g, low.S, i0, p.rows);
   f32x16 acc[S::TM][S::TN] = {};
   tile_products<S>(p, q, K, lds, acc);
-  if (low.S > 0) add_low_rank<S, E>(low, g, i0, p.rows, j0, acc);
+  add_low_rank<S, E>(low, rows, j0, acc);
   tile_store<S>(acc, [&](int i, int j, const f32x16& v) {
     j += j0;
     if (j >= width) return;
@@ -447,17 +443,53 @@ lipcache_status ad_main(const void* P, int64_t ldp, const void* Q, int64_t ldq, 
 }
 
 // -------------------------------------------------------- gradients of pairs
+// The factors u and v as the gradient kernel's operand: for each tile of the
+// table a block of r rows of 128 bytes, row rho the tile's 32 values f[row][rho]
+// as float32, or as 32 first and 32 second 16-bit parts; zeros past its rows.
+template <class E>
+__global__ __launch_bounds__(256) void ad_factor_kernel(const float* __restrict__ u, const float* __restrict__ v, int r,
+                                                        int pairs, AdGroups g, E* __restrict__ to_u, E* __restrict__ to_v) {
+  __shared__ float tile[32][33];
+  const int t = static_cast<int>(blockIdx.x);
+  if (static_cast<uint32_t>(t) >= static_cast<uint32_t>(g.tile_start[pairs])) return;
+  const float* f = blockIdx.y ? v : u;
+  E* to = (blockIdx.y ? to_v : to_u) + static_cast<int64_t>(t) * r * (128 / sizeof(E));
+  const int row0 = g.tile_row[t];
+  const int rows = g.start[g.tile_pair[t] + 1] - row0;
+  const int x = static_cast<int>(threadIdx.x) & 31, y = static_cast<int>(threadIdx.x) >> 5;
+  for (int rho0 = 0; rho0 < r; rho0 += 32) {
+    __syncthreads();
+#pragma unroll
+    for (int i = y; i < 32; i += 8)
+      tile[i][x] = i < rows && rho0 + x < r ? f[static_cast<int64_t>(g.order[row0 + i]) * r + rho0 + x] : 0.0f;
+    __syncthreads();
+#pragma unroll
+    for (int k = y; k < 32; k += 8) {
+      const int rho = rho0 + k;
+      if (rho >= r) continue;
+      const float w = tile[x][k];
+      E* p = to + rho * (128 / sizeof(E)) + x;
+      if constexpr (std::is_same_v<E, float>) {
+        *p = w;
+      } else {
+        two_parts(w, p[0], p[32]);
+      }
+    }
+  }
+}
+
 // D_a[rho][c] = scale_a sum over pair a's rows t of f[t][rho] z[t][c]: dA with
 // f = u, z = x, and dB (transposed) with f = v, z = dy.  One workgroup takes
-// 128 columns of one pair (and one of `splits` shares of its rows); z's rows
-// come gathered into LDS, 64 (float32: 32) at a time through a ring of three
-// buffers, and are read across (the contraction runs over the rows); f comes
-// straight to registers as two 16-bit parts.  Bound by reading x and dy once.
+// 128 columns of one pair (and one of `splits` shares of its tiles); a tile's 32
+// rows of z come gathered into LDS through a ring of buffers, two tiles a step,
+// and are read across (the contraction runs over the rows); their row numbers
+// come by scalar loads, which vmcnt does not count, so the ring's waits are
+// exact.  Bound by reading x and dy once.
 template <class E>
 struct AdGradSide {
   const E* z;
   int64_t ldz;
-  const float* f;
+  const E* f;      // ad_factor_kernel's
   E* out;          // dA: [S][r][width];  dB: [S][width][r]
   float* part;     // [splits][S][r][width] where splits > 1
   int width, blocks;
@@ -466,11 +498,21 @@ struct AdGradSide {
 
 template <class E, int NR>
 __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSide<E> B, int r, int S, int splits,
-                                                      const float* __restrict__ scale, AdGroups g) {
-  typedef TileOf<E, 128, true, 4> Tile;
-  constexpr int kV = Vec16<E>::kCount, kPart = Tile::kPart, kStages = 3;
+                                                      const float* __restrict__ scale, const int32_t* __restrict__ order,
+                                                      const int32_t* __restrict__ start,
+                                                      const int32_t* __restrict__ tile_start,
+                                                      const int32_t* __restrict__ tile_row, const void* zeros) {
+  constexpr bool kF32 = std::is_same_v<E, float>;
+  constexpr int kV = Vec16<E>::kCount, kSize = static_cast<int>(sizeof(E));
   typedef typename Vec16<E>::type V;
-  __shared__ __align__(16) char lds[kStages * Tile::kBytes];
+  typedef TileOf<E, 128, true, 4> TileZ;                                       // rows of it, as many as there are
+  typedef TileOf<std::conditional_t<kF32, float, Split>, 32 * NR, false, 4> TileF;
+  constexpr int kZ = 32 * 128 * kSize, kF = NR * 4096, kTile = kZ + kF;        // LDS bytes of a tile
+  constexpr int kSub = 2, kStages = NR == 1 ? 3 : 2;
+  constexpr int kZCopies = kZ / 4096, kFCopies = NR;                           // of a wave and tile
+  constexpr int kRowsCopy = 64 / TileZ::kSlots;                                // rows of z a copy takes: 4 or 2
+  constexpr int kGroups = kF32 ? 4 : 2, kParts = kF32 ? 1 : 2;
+  __shared__ __align__(16) char lds[kStages * kSub * kTile];
   const int per = (A.blocks + B.blocks) * splits;
   const int a = static_cast<int>(blockIdx.x) / per;
   int in = static_cast<int>(blockIdx.x) % per;
@@ -479,71 +521,76 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
   const bool second = in >= A.blocks;
   const AdGradSide<E>& d = second ? B : A;
   const int c0 = (second ? in - A.blocks : in) * 128;
-  const int begin0 = g.start[a], end0 = g.start[a + 1];
-  // shares in whole parts
-  const int parts = end0 > begin0 ? (end0 - begin0 + kPart - 1) / kPart : 0, each = (parts + splits - 1) / splits;
-  const int begin = begin0 + share * each * kPart;
-  const int stop = begin + each * kPart < end0 ? begin + each * kPart : end0;
+  const int end = start[a + 1], all = tile_start[a + 1] - tile_start[a];
+  const int each = (all + splits - 1) / splits;
+  const int tile0 = tile_start[a] + share * each;
+  const int tiles = all - share * each < each ? all - share * each : each;
   const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
   const int li = lane & 31, half = lane >> 5;
   const uint32_t base = lds_address(lds);
 
-  auto copy = [&](int t0, int pos) {
+  auto copy = [&](const void* p, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(uniform(static_cast<int>(to)))
+                 : "memory", "m0");
+  };
+  auto copy_tile = [&](int n, uint32_t to) {  // tile n of the share; zeros past the last
+    const bool some = n < tiles;
+    const int t = uniform(tile0 + (some ? n : 0));
+    const int row0 = some ? uniform(tile_row[t]) : end;
 #pragma unroll
-    for (int c = 0; c < Tile::kCopies; ++c) {
-      const int n = (wave * Tile::kCopies + c) * 64 + lane;
-      const int row = n / Tile::kSlots, chunk = (n % Tile::kSlots) ^ Tile::swz(row);
+    for (int c = 0; c < kZCopies; ++c) {
+      const int first = (wave * kZCopies + c) * kRowsCopy;
+      typedef int32_t rows_t __attribute__((ext_vector_type(kRowsCopy), aligned(4)));
+      const rows_t rows = *reinterpret_cast<const rows_t*>(order + (some ? row0 : 0) + first);
+      const int mine = lane / TileZ::kSlots;
+      int row = rows[0];
+#pragma unroll
+      for (int e = 1; e < kRowsCopy; ++e) row = mine == e ? rows[e] : row;
+      const int chunk = (lane % TileZ::kSlots) ^ TileZ::swz(first + mine);
       const int col = c0 + chunk * kV;
-      const void* p = g.zeros;  // rows past the share and columns past the matrix
-      if (t0 + row < stop && col < d.width) p = d.z + g.order[t0 + row] * d.ldz + col;
-      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p),
-                   "s"(uniform(static_cast<int>(base + pos * Tile::kBytes + (wave * Tile::kCopies + c) * 1024)))
-                   : "memory", "m0");
+      const void* p = zeros;  // rows past the pair's and columns past the matrix
+      if (row0 + first + mine < end && col < d.width) p = d.z + row * d.ldz + col;
+      copy(p, to + (wave * kZCopies + c) * 1024);
+    }
+    const char* f = reinterpret_cast<const char*>(d.f) + static_cast<int64_t>(t) * r * 128;
+#pragma unroll
+    for (int c = 0; c < kFCopies; ++c) {
+      const int n8 = (wave * kFCopies + c) * 64 + lane, rho = n8 / 8, chunk = (n8 % 8) ^ TileF::swz(rho);
+      copy(some && rho < r ? f + rho * 128 + chunk * 16 : static_cast<const char*>(zeros),
+           to + kZ + (wave * kFCopies + c) * 1024);
     }
   };
   f32x16 acc[NR] = {};
-  uint32_t read[Tile::kGroups];
+  uint32_t rz[kGroups], rf[kGroups][kParts];
 #pragma unroll
-  for (int n = 0; n < Tile::kGroups; ++n) read[n] = Tile::row_offset(Tile::read_offset(n, 0), wave);
-  const int steps = stop > begin ? (stop - begin + kPart - 1) / kPart : 0;
-  int copied = 0;
-  for (; copied < kStages - 1 && copied < steps; ++copied) copy(begin + copied * kPart, copied);
+  for (int n = 0; n < kGroups; ++n) {
+    rz[n] = TileZ::row_offset(TileZ::read_offset(n, 0), wave);
+#pragma unroll
+    for (int h = 0; h < kParts; ++h) rf[n][h] = kZ + TileF::read_offset(n, h);
+  }
+  const int steps = tiles > 0 ? (tiles + kSub - 1) / kSub : 0;
+  constexpr int kCopies = kSub * (kZCopies + kFCopies);
+  auto copy_step = [&](int step) {
+#pragma unroll
+    for (int u = 0; u < kSub; ++u) copy_tile(step * kSub + u, base + (step % kStages * kSub + u) * kTile);
+  };
+  for (int step = 0; step < kStages - 1 && step < steps; ++step) copy_step(step);
   for (int step = 0; step < steps; ++step) {
-    // f of this step: lane's rank, kV rows of the group and half
-    V f1[Tile::kGroups][NR], f2[Tile::kGroups][NR];
-#pragma unroll
-    for (int n = 0; n < Tile::kGroups; ++n)
-#pragma unroll
-      for (int e = 0; e < kV; ++e) {
-        const int t = begin + step * kPart + (2 * n + half) * kV + e;
-        const float* p = d.f + static_cast<int64_t>(g.order[t < stop ? t : stop - 1]) * r;
-#pragma unroll
-        for (int m = 0; m < NR; ++m) {
-          const float v = t < stop && 32 * m + li < r ? p[32 * m + li] : 0.0f;
-          if constexpr (std::is_same_v<E, float>) {
-            f1[n][m][e] = v;
-          } else {
-            E x, y;
-            two_parts(v, x, y);
-            f1[n][m][e] = x;
-            f2[n][m][e] = y;
-          }
-        }
-      }
-    copies_left<0>();
+    if (kStages > 2 && step + 1 < steps) copies_left<(kStages - 2) * kCopies>();
+    else copies_left<0>();
     __syncthreads();
-    if (copied < steps) {
-      copy(begin + copied * kPart, copied % kStages);
-      ++copied;
-    }
-    const char* at = lds + (step % kStages) * Tile::kBytes;
+    if (step + kStages - 1 < steps) copy_step(step + kStages - 1);
 #pragma unroll
-    for (int n = 0; n < Tile::kGroups; ++n) {
-      const V z = __builtin_bit_cast(V, Tile::read16(at + read[n]));
+    for (int u = 0; u < kSub; ++u) {
+      const char* at = lds + (step % kStages * kSub + u) * kTile;
 #pragma unroll
-      for (int m = 0; m < NR; ++m) {
-        if constexpr (!std::is_same_v<E, float>) acc[m] = MfmaType<E>::mul(f2[n][m], z, acc[m]);
-        acc[m] = MfmaType<E>::mul(f1[n][m], z, acc[m]);
+      for (int n = 0; n < kGroups; ++n) {
+        const V z = __builtin_bit_cast(V, TileZ::read16(at + rz[n]));
+#pragma unroll
+        for (int m = 0; m < NR; ++m)
+#pragma unroll
+          for (int h = kParts - 1; h >= 0; --h)
+            acc[m] = MfmaType<E>::mul(__builtin_bit_cast(V, TileF::read16(at + TileF::row_offset(rf[n][h], m))), z, acc[m]);
       }
     }
   }
@@ -561,7 +608,7 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
       } else {
         const int64_t to = d.across ? (static_cast<int64_t>(a) * d.width + col) * r + rho
                                     : (static_cast<int64_t>(a) * r + rho) * d.width + col;
-        d.out[to] = static_cast<E>(begin0 < end0 ? sc * acc[m][e] : 0.0f);
+        d.out[to] = static_cast<E>(all > 0 ? sc * acc[m][e] : 0.0f);
       }
     }
 }
@@ -579,7 +626,7 @@ __global__ __launch_bounds__(256) void ad_join_kernel(AdGradSide<E> A, AdGradSid
   const int col = static_cast<int>(i % d.width), rho = static_cast<int>(i / d.width % r);
   const int64_t a = i / d.width / r;
   const int64_t to = d.across ? (a * d.width + col) * r + rho : i;
-  d.out[to] = static_cast<E>(g.start[a] < g.start[a + 1] ? scale[a] * sum : 0.0f);
+  d.out[to] = static_cast<E>(g.tile_start[a] < g.tile_start[a + 1] ? scale[a] * sum : 0.0f);
 }
 
 // ------------------------------------------------------------------ the calls
@@ -601,18 +648,18 @@ struct AdSpace {
 
 AdGroups ad_groups(AdSpace& ws, int64_t T, int S) {
   AdGroups g;
-  g.order = ws.take<int32_t>(T);
+  g.order = ws.take<int32_t>(T + 64);  // scalar loads read whole vectors
   g.pair = ws.take<int32_t>(T);
   g.start = ws.take<int32_t>(S + 2);
   g.tile_pair = ws.take<int32_t>(ad_tiles(T, S) + 1);
   g.tile_row = ws.take<int32_t>(ad_tiles(T, S) + 1);
-  g.tiles = ws.take<int32_t>(1);
+  g.tile_start = ws.take<int32_t>(S + 1);
   g.zeros = ws.take<uint32_t>(4);
   return g;
 }
 
 lipcache_status ad_group(int64_t t0, int64_t T, const lipcache_adapters& ad, const AdGroups& g, hipStream_t s) {
-  ad_group_kernel<<<ad.S + 1, 256, (ad.S + 1 + 512) * 4, s>>>(t0, static_cast<int>(T), ad.offsets, ad.adapter, ad.R, ad.S, g);
+  ad_group_kernel<<<ad.S + 1, kGroupThreads, (ad.S + 1 + 2 * kGroupThreads + kGroupThreads / kWave) * 4, s>>>(t0, static_cast<int>(T), ad.offsets, ad.adapter, ad.R, ad.S, g);
   LC_LAUNCHED();
   return LIPCACHE_OK;
 }
@@ -638,22 +685,26 @@ lipcache_status ad_rows(const void* from, int64_t ld, int64_t rows, int width, E
   for (int64_t r0 = 0; r0 < rows; r0 += 1 << 20) {
     const int n = static_cast<int>(rows - r0 < (1 << 20) ? rows - r0 : 1 << 20);
     const AdCopy c{p + r0 * ld, room + r0 * to, ld, to, 0, 0, n, width, n, static_cast<int>(to), 1};
-    if (lipcache_status st = ad_copy<E, false>(c, s); st != LIPCACHE_OK) return st;
+    if (lipcache_status st = ad_copy<E, false>(c, AdCopy{}, s); st != LIPCACHE_OK) return st;
   }
   return LIPCACHE_OK;
 }
 
+// v (u) of every row; rows without a pair are written (zeros) where `all_rows`.
 template <class E>
-lipcache_status ad_thin(const AdRows<E>& x, int width, const E* F, int64_t ldf, int64_t T, const lipcache_adapters& ad,
-                        const AdGroups& g, float* out, hipStream_t s) {
-  const unsigned tiles = static_cast<unsigned>(ad_tiles(T, ad.S));
-  if (ad.S > 0 && tiles > 0) {
-    if (ad.r <= 32) ad_thin_kernel<E, 1><<<tiles, 512, 0, s>>>(x.p, x.ld, width, F, ldf, ad.r, g, out);
-    else if (ad.r <= 64) ad_thin_kernel<E, 2><<<tiles, 512, 0, s>>>(x.p, x.ld, width, F, ldf, ad.r, g, out);
-    else ad_thin_kernel<E, 4><<<tiles, 512, 0, s>>>(x.p, x.ld, width, F, ldf, ad.r, g, out);
-    LC_LAUNCHED();
-  }
-  return LIPCACHE_OK;
+lipcache_status ad_thin(const AdRows<E>& x, int width, const E* F, int64_t ldf, int T, const lipcache_adapters& ad,
+                        const AdGroups& g, float* out, bool all_rows, hipStream_t s) {
+  const int64_t table = ad_tiles(T, ad.S), more = all_rows ? ceil_div(T, 256) : 0;
+  const unsigned blocks = static_cast<unsigned>(table + (more < 256 ? more : 256));
+  if (blocks == 0) return LIPCACHE_OK;
+  auto run = [&](auto shape) {
+    typedef decltype(shape) S;
+    ad_thin_kernel<S><<<blocks, S::kThreads, 0, s>>>(x.p, x.ld, width, F, ldf, ad.r, ad.S, T, g, out);
+    return hipGetLastError() == hipSuccess ? LIPCACHE_OK : LIPCACHE_EHIP;
+  };
+  if (ad.r <= 32) return run(TileShape<E, 32, 32, 1, 1, 4, 4, 2, false, false>{});
+  if (ad.r <= 64) return run(TileShape<E, 32, 64, 1, 1, 4, 3, 2, false, false>{});
+  return run(TileShape<E, 32, 128, 1, 1, 4, 3, 1, false, false>{});
 }
 
 struct AdArgs {
@@ -705,12 +756,7 @@ lipcache_status ad_forward(const AdArgs& a, const float* bias, void* y, int64_t 
     AdLow lc = low;
     lc.v = v + t0 * a.ad.r;
     if ((st = ad_group(t0, T, a.ad, ws.g, s)) != LIPCACHE_OK) return st;
-    if ((st = ad_thin<E>(xc, a.K, A.p, A.ld, T, a.ad, ws.g, v + t0 * a.ad.r, s)) != LIPCACHE_OK) return st;
-    if (keep) {
-      ad_zero_rows_kernel<<<static_cast<unsigned>(ceil_div(T, 64) < 1024 ? ceil_div(T, 64) : 1024), 256, 0, s>>>(
-          ws.g, a.ad.S, T, a.ad.r, v + t0 * a.ad.r);
-      LC_LAUNCHED();
-    }
+    if ((st = ad_thin<E>(xc, a.K, A.p, A.ld, T, a.ad, ws.g, v + t0 * a.ad.r, keep, s)) != LIPCACHE_OK) return st;
     if ((st = ad_main<E, false>(xc.p, xc.ld, W.p, W.ld, T, a.N, a.K, bias, lc, ws.g, static_cast<E*>(y) + t0 * ldy, ldy, s)) !=
         LIPCACHE_OK)
       return st;
@@ -731,7 +777,7 @@ template <class E>
 struct AdBackwardSpace {
   AdGroups g;
   float *u, *v, *part_a, *part_b;
-  E *x, *W, *dy, *A, *At, *Bt;
+  E *x, *W, *dy, *A, *At, *Bt, *fu, *fv;
   AdBackwardSpace(AdSpace& ws, int64_t T, int K, int N, int r, int S) {
     constexpr int kV = Vec16<E>::kCount;
     const size_t K8 = round_up(K, kV), N8 = round_up(N, kV), n = S;
@@ -740,6 +786,9 @@ struct AdBackwardSpace {
     v = ws.take<float>(static_cast<size_t>(T) * r);
     At = ws.take<E>(n * K * round_up(r, kV));
     Bt = ws.take<E>(n * r * N8);
+    const size_t factors = static_cast<size_t>(ad_tiles(T, S)) * r * (128 / sizeof(E));
+    fu = ws.take<E>(factors);
+    fv = ws.take<E>(factors);
     const int splits = ad_splits(T, K, N, S);
     part_a = ws.take<float>(splits > 1 ? splits * n * r * K : 0);
     part_b = ws.take<float>(splits > 1 ? splits * n * r * N : 0);
@@ -763,42 +812,51 @@ lipcache_status ad_backward(const AdArgs& a, const float* v_in, void* dx, int64_
   if (dA && (st = ad_rows<E>(a.x, a.ldx, a.T, K, ws.x, x, s)) != LIPCACHE_OK) return st;
   const int64_t r8 = round_up(r, kV), N8 = round_up(N, kV);
   const AdCopy bt{a.ad.B, ws.Bt, r, N8, static_cast<int64_t>(N) * r, r * N8, N, r, r, static_cast<int>(N8), S};
-  if ((st = ad_copy<E, true>(bt, s)) != LIPCACHE_OK) return st;
-  if ((st = ad_group(0, a.T, a.ad, ws.g, s)) != LIPCACHE_OK) return st;
-  if ((st = ad_thin<E>(dy, N, ws.Bt, N8, a.T, a.ad, ws.g, ws.u, s)) != LIPCACHE_OK) return st;
-  if (dA && S > 0) {
-    if (!v_in) {
-      if ((st = ad_rows<E>(a.ad.A, K, static_cast<int64_t>(S) * r, K, ws.A, A, s)) != LIPCACHE_OK) return st;
-      if ((st = ad_thin<E>(x, K, A.p, A.ld, a.T, a.ad, ws.g, ws.v, s)) != LIPCACHE_OK) return st;
-      v_in = ws.v;
-    }
-    const int splits = ad_splits(a.T, K, N, S);
-    const AdGradSide<E> ga{x.p, x.ld, ws.u, static_cast<E*>(dA), ws.part_a, K, static_cast<int>(ceil_div(K, 128)), false};
-    const AdGradSide<E> gb{dy.p, dy.ld, v_in, static_cast<E*>(dB), ws.part_b, N, static_cast<int>(ceil_div(N, 128)), true};
-    const unsigned blocks = static_cast<unsigned>((ga.blocks + gb.blocks) * splits) * S;
-    if (r <= 32) ad_grad_kernel<E, 1><<<blocks, 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g);
-    else if (r <= 64) ad_grad_kernel<E, 2><<<blocks, 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g);
-    else ad_grad_kernel<E, 4><<<blocks, 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g);
-    LC_LAUNCHED();
-    if (splits > 1) {
-      const int64_t most = static_cast<int64_t>(S) * r * (K > N ? K : N);
-      ad_join_kernel<E><<<dim3(static_cast<unsigned>(ceil_div(most, 256)), 2), 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g);
-      LC_LAUNCHED();
-    }
-  }
-  if (dx && a.T > 0) {
-    if ((st = ad_rows<E>(a.W, a.ldw, N, K, ws.W, W, s)) != LIPCACHE_OK) return st;
-    const AdCopy at{a.ad.A, ws.At, K, r8, static_cast<int64_t>(r) * K, K * r8, r, K, K, static_cast<int>(r8), S};
-    if ((st = ad_copy<E, true>(at, s)) != LIPCACHE_OK) return st;
-    const int64_t chunk = ad_chunk(dy.ld, sizeof(E));
-    for (int64_t t0 = 0; t0 < a.T; t0 += chunk) {
-      const int T = static_cast<int>(a.T - t0 < chunk ? a.T - t0 : chunk);
-      if (a.T > chunk && (st = ad_group(t0, T, a.ad, ws.g, s)) != LIPCACHE_OK) return st;
+  const AdCopy at{a.ad.A, ws.At, K, r8, static_cast<int64_t>(r) * K, K * r8, r, K, K, static_cast<int>(r8), dx ? S : 0};
+  if ((st = ad_copy<E, true>(bt, at, s)) != LIPCACHE_OK) return st;
+  // u and, if it did not come, v of all rows; a pass for each chunk of rows whose offsets stay below 2^31 bytes
+  const bool need_v = dA && !v_in && S > 0;
+  if (need_v && (st = ad_rows<E>(a.ad.A, K, static_cast<int64_t>(S) * r, K, ws.A, A, s)) != LIPCACHE_OK) return st;
+  if (dx && (st = ad_rows<E>(a.W, a.ldw, N, K, ws.W, W, s)) != LIPCACHE_OK) return st;
+  const int64_t chunk_dy = ad_chunk(dy.ld, sizeof(E)), chunk_x = need_v ? ad_chunk(x.ld, sizeof(E)) : chunk_dy;
+  const int64_t chunk = chunk_dy < chunk_x ? chunk_dy : chunk_x;
+  for (int64_t t0 = 0; t0 < a.T; t0 += chunk) {
+    const int T = static_cast<int>(a.T - t0 < chunk ? a.T - t0 : chunk);
+    const AdRows<E> dyc{dy.p + t0 * dy.ld, dy.ld};
+    if ((st = ad_group(t0, T, a.ad, ws.g, s)) != LIPCACHE_OK) return st;
+    if ((st = ad_thin<E>(dyc, N, ws.Bt, N8, T, a.ad, ws.g, ws.u + t0 * r, false, s)) != LIPCACHE_OK) return st;
+    if (need_v &&
+        (st = ad_thin<E>({x.p + t0 * x.ld, x.ld}, K, A.p, A.ld, T, a.ad, ws.g, ws.v + t0 * r, false, s)) != LIPCACHE_OK)
+      return st;
+    if (dx) {
       const AdLow low{ws.At, r8, ws.u + t0 * r, a.ad.scale, r, S, K, true, aligned16(ws.u + t0 * r) && r % 4 == 0};
-      if ((st = ad_main<E, true>(dy.p + t0 * dy.ld, dy.ld, W.p, W.ld, T, K, N, nullptr, low, ws.g,
+      if ((st = ad_main<E, true>(dyc.p, dyc.ld, W.p, W.ld, T, K, N, nullptr, low, ws.g,
                                  static_cast<E*>(dx) + t0 * lddx, lddx, s)) != LIPCACHE_OK)
         return st;
     }
+  }
+  if (!dA || S == 0) return LIPCACHE_OK;
+  if ((a.T == 0 || a.T > chunk) && (st = ad_group(0, a.T, a.ad, ws.g, s)) != LIPCACHE_OK) return st;
+  if (const int64_t tiles = ad_tiles(a.T, S); tiles > 0) {
+    ad_factor_kernel<E><<<dim3(static_cast<unsigned>(tiles), 2), 256, 0, s>>>(ws.u, need_v ? ws.v : v_in, r, S, ws.g, ws.fu, ws.fv);
+    LC_LAUNCHED();
+  }
+  const int splits = ad_splits(a.T, K, N, S);
+  const AdGradSide<E> ga{x.p, x.ld, ws.fu, static_cast<E*>(dA), ws.part_a, K, static_cast<int>(ceil_div(K, 128)), false};
+  const AdGradSide<E> gb{dy.p, dy.ld, ws.fv, static_cast<E*>(dB), ws.part_b, N, static_cast<int>(ceil_div(N, 128)), true};
+  const unsigned blocks = static_cast<unsigned>((ga.blocks + gb.blocks) * splits) * S;
+  auto grad = [&](auto ranks) {
+    ad_grad_kernel<E, decltype(ranks)::value><<<blocks, 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g.order, ws.g.start,
+                                                                    ws.g.tile_start, ws.g.tile_row, ws.g.zeros);
+  };
+  if (r <= 32) grad(std::integral_constant<int, 1>{});
+  else if (r <= 64) grad(std::integral_constant<int, 2>{});
+  else grad(std::integral_constant<int, 4>{});
+  LC_LAUNCHED();
+  if (splits > 1) {
+    const int64_t most = static_cast<int64_t>(S) * r * (K > N ? K : N);
+    ad_join_kernel<E><<<dim3(static_cast<unsigned>(ceil_div(most, 256)), 2), 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g);
+    LC_LAUNCHED();
   }
   return LIPCACHE_OK;
 }
