@@ -173,6 +173,13 @@ struct Vec16<_Float16> {
   typedef f16x8 type;
 };
 
+// A matrix whose rows are read as 16-byte vectors: itself, or its copy in the workspace.
+template <class E>
+struct AdRows {
+  const E* p;
+  int64_t ld;
+};
+
 // A float32 factor as what the matrix cores take: itself, or the sum of two
 // 16-bit numbers (each product then takes two instructions; 16 or 22 bits).
 template <class E>
@@ -442,6 +449,158 @@ lipcache_status ad_main(const void* P, int64_t ldp, const void* Q, int64_t ldq, 
   return run(TileShape<E, 128, 128, 2, 2, 1, 2, 1, false, kCol>{});
 }
 
+// ------------------------------------------------------------- few rows
+// Up to 64 rows (a decode batch) are bound by reading W once.  They are not
+// sorted: a first kernel finds each row's pair and A_a x, one wave a row and
+// rank; the second takes 16 columns of W a workgroup, all rows at once, its
+// eight waves sharing the contraction, W and x straight to registers (16 rows
+// of 64 bytes a load), and adds the low-rank part of each output as a dot
+// product of r before it stores it.
+constexpr int kFewRows = 64;
+
+// The pair of row t (-1: none), by the whole wave: 64 offsets a round.
+__device__ __forceinline__ int pair_of_row(int64_t t, const int32_t* __restrict__ offsets,
+                                           const int32_t* __restrict__ adapter, int R, int S) {
+  int lo = 0, n = R + 1;  // the first offset past t lies in [lo, lo + n]
+  while (n > 0) {
+    const int step = (n + kWave - 1) / kWave, at = lo + (lane_id() + 1) * step - 1;
+    const bool before = at < lo + n && offsets[at] <= t;
+    const int passed = __builtin_popcountll(__ballot(before));
+    lo += passed * step;
+    n = step > 1 ? (n - passed * step < step ? n - passed * step : step - 1) : 0;
+  }
+  if (lo < 1 || lo > R) return -1;
+  const int a = adapter[lo - 1];
+  return a >= 0 && a < S ? a : -1;
+}
+
+template <class E>
+__global__ __launch_bounds__(256) void ad_few_low_kernel(const E* __restrict__ x, int64_t ldx, int T, int K,
+                                                         const E* __restrict__ A, int64_t lda, int r,
+                                                         const int32_t* __restrict__ offsets,
+                                                         const int32_t* __restrict__ adapter, int R, int S,
+                                                         int32_t* __restrict__ pair, float* __restrict__ v) {
+  constexpr int kV = Vec16<E>::kCount;
+  typedef typename Vec16<E>::type V;
+  const int w = uniform(static_cast<int>(blockIdx.x * 4 + threadIdx.x / kWave));
+  if (w >= T * r) return;
+  const int t = w / r, rho = w % r, lane = lane_id();
+  const int a = R > 0 ? uniform(pair_of_row(t, offsets, adapter, R, S)) : -1;
+  float sum = 0.0f;
+  if (a >= 0) {
+    const E* px = x + t * ldx;
+    const E* pa = A + (static_cast<int64_t>(a) * r + rho) * lda;
+#pragma unroll 4
+    for (int k = lane * kV; k < K; k += kWave * kV) {
+      const V vx = *reinterpret_cast<const V*>(px + k), va = *reinterpret_cast<const V*>(pa + k);
+#pragma unroll
+      for (int e = 0; e < kV; ++e)
+        sum = fmaf(k + e < K ? static_cast<float>(vx[e]) : 0.0f, k + e < K ? static_cast<float>(va[e]) : 0.0f, sum);
+    }
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+  if (lane == 0) {
+    v[w] = sum;
+    if (rho == 0) pair[t] = a;
+  }
+}
+
+// 16 x 16 products of 16-byte fragments: lane l holds row l % 16 and quarter l / 16 of 64 bytes of the contraction,
+// and ends with rows 4 (l / 16) .. + 3 of column l % 16.
+__device__ __forceinline__ f32x4 mul16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mul16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mul16(f32x4 a, f32x4 b, f32x4 c) {
+  c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[0], b[0], c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[1], b[1], c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[2], b[2], c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a[3], b[3], c, 0, 0, 0);
+}
+
+template <class E, int TT>
+__global__ __launch_bounds__(512) void ad_few_main_kernel(const E* __restrict__ x, int64_t ldx, int T,
+                                                          const E* __restrict__ W, int64_t ldw, int K, int N,
+                                                          const float* __restrict__ bias, AdLow low,
+                                                          const int32_t* __restrict__ pair, E* __restrict__ y,
+                                                          int64_t ldy) {
+  constexpr int kV = Vec16<E>::kCount, kWaves = 8, kStep = 4 * kV, kUnroll = 4;
+  typedef typename Vec16<E>::type V;
+  __shared__ __align__(16) float part[kWaves][TT * 256];
+  const int n0 = static_cast<int>(blockIdx.x) * 16;
+  const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+  const int li = lane & 15, quarter = lane >> 4;
+  const E* pw = W + (n0 + li < N ? n0 + li : N - 1) * ldw + quarter * kV;
+  const E* px[TT];
+#pragma unroll
+  for (int m = 0; m < TT; ++m) px[m] = x + (16 * m + li < T ? 16 * m + li : T - 1) * ldx + quarter * kV;
+  f32x4 acc[TT] = {};
+  // whole blocks of kUnroll steps, then the rest step by step
+  int k = wave * (kUnroll * kStep);
+  for (; k + kUnroll * kStep <= K; k += kWaves * kUnroll * kStep) {
+    V w[kUnroll], f[kUnroll][TT];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      w[u] = *reinterpret_cast<const V*>(pw + k + u * kStep);
+#pragma unroll
+      for (int m = 0; m < TT; ++m) f[u][m] = *reinterpret_cast<const V*>(px[m] + k + u * kStep);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int m = 0; m < TT; ++m) acc[m] = mul16(w[u], f[u][m], acc[m]);
+  }
+  for (int stop = k + kUnroll * kStep; k < K && k < stop; k += kStep) {
+    const bool in = k + quarter * kV < K;
+    const V w = in ? *reinterpret_cast<const V*>(pw + k) : V{};
+#pragma unroll
+    for (int m = 0; m < TT; ++m) acc[m] = mul16(w, in ? *reinterpret_cast<const V*>(px[m] + k) : V{}, acc[m]);
+  }
+#pragma unroll
+  for (int m = 0; m < TT; ++m) *reinterpret_cast<f32x4*>(&part[wave][(m * 64 + lane) * 4]) = acc[m];
+  __syncthreads();
+  const E* F = static_cast<const E*>(low.F);
+  for (int i = static_cast<int>(threadIdx.x); i < TT * 256; i += 512) {
+    const int n = n0 + 4 * ((i >> 6) & 3) + (i & 3), t = (i >> 8) * 16 + ((i >> 2) & 15);
+    if (n >= N || t >= T) continue;
+    float sum = part[0][i];
+#pragma unroll
+    for (int u = 1; u < kWaves; ++u) sum += part[u][i];
+    if (bias) sum += bias[n];
+    const int a = low.S > 0 ? pair[t] : -1;
+    if (a >= 0) {
+      const E* f = F + (static_cast<int64_t>(a) * N + n) * low.ldf;
+      const float* v = low.v + t * low.r;
+      float dot = 0.0f;
+      for (int rho = 0; rho < low.r; rho += kV) {
+        const V b = load_some<E>(f + rho, low.r - rho, low.wide != 0);
+#pragma unroll
+        for (int e = 0; e < kV; e += 4) {
+          const f32x4 u = load_some<float>(v + rho + e, low.r - rho - e, low.wide_v != 0);
+#pragma unroll
+          for (int o = 0; o < 4; ++o) dot = fmaf(u[o], static_cast<float>(b[e + o]), dot);
+        }
+      }
+      sum = fmaf(low.scale[a], dot, sum);
+    }
+    y[t * ldy + n] = static_cast<E>(sum);
+  }
+}
+
+template <class E>
+lipcache_status ad_few(const AdRows<E>& x, int T, const AdRows<E>& W, int K, int N, const float* bias,
+                       const AdRows<E>& A, const lipcache_adapters& ad, const AdLow& low, int32_t* pair, float* v,
+                       E* y, int64_t ldy, hipStream_t s) {
+  ad_few_low_kernel<E><<<static_cast<unsigned>(ceil_div(static_cast<int64_t>(T) * ad.r, 4)), 256, 0, s>>>(
+      x.p, x.ld, T, K, A.p, A.ld, ad.r, ad.offsets, ad.adapter, ad.R, ad.S, pair, v);
+  LC_LAUNCHED();
+  const unsigned blocks = static_cast<unsigned>(ceil_div(N, 16));
+  if (T <= 16) ad_few_main_kernel<E, 1><<<blocks, 512, 0, s>>>(x.p, x.ld, T, W.p, W.ld, K, N, bias, low, pair, y, ldy);
+  else if (T <= 32) ad_few_main_kernel<E, 2><<<blocks, 512, 0, s>>>(x.p, x.ld, T, W.p, W.ld, K, N, bias, low, pair, y, ldy);
+  else ad_few_main_kernel<E, 4><<<blocks, 512, 0, s>>>(x.p, x.ld, T, W.p, W.ld, K, N, bias, low, pair, y, ldy);
+  LC_LAUNCHED();
+  return LIPCACHE_OK;
+}
+
 // -------------------------------------------------------- gradients of pairs
 // The factors u and v as the gradient kernel's operand: for each tile of the
 // table a block of r rows of 128 bytes, row rho the tile's 32 values f[row][rho]
@@ -664,13 +823,6 @@ lipcache_status ad_group(int64_t t0, int64_t T, const lipcache_adapters& ad, con
   return LIPCACHE_OK;
 }
 
-// A matrix whose rows are read as 16-byte vectors: itself, or its copy in the workspace.
-template <class E>
-struct AdRows {
-  const E* p;
-  int64_t ld;
-};
-
 template <class E>
 lipcache_status ad_rows(const void* from, int64_t ld, int64_t rows, int width, E* room, AdRows<E>& out, hipStream_t s) {
   constexpr int kV = Vec16<E>::kCount;
@@ -749,6 +901,8 @@ lipcache_status ad_forward(const AdArgs& a, const float* bias, void* y, int64_t 
   if (!keep) v = ws.v;
   const AdLow low{a.ad.B, a.ad.r, v, a.ad.scale, a.ad.r, a.ad.S, a.N, aligned16(a.ad.B) && a.ad.r % kV == 0,
                   aligned16(v) && a.ad.r % 4 == 0};
+  if (a.T <= kFewRows)
+    return ad_few<E>(x, static_cast<int>(a.T), W, a.K, a.N, bias, A, a.ad, low, ws.g.pair, v, static_cast<E*>(y), ldy, s);
   const int64_t chunk = ad_chunk(x.ld, sizeof(E));
   for (int64_t t0 = 0; t0 < a.T; t0 += chunk) {
     const int T = static_cast<int>(a.T - t0 < chunk ? a.T - t0 : chunk);
