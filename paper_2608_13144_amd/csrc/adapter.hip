@@ -24,6 +24,7 @@ constexpr int64_t kAdMaxWidth = 1 << 20;
 constexpr int kThinRows = 32;  // sorted rows of one pair that a workgroup of the thin products takes
 
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // ---------------------------------------------------------------- grouping
 // Rows sorted by pair (rows without one last), and the table of the thin
@@ -451,11 +452,12 @@ lipcache_status ad_main(const void* P, int64_t ldp, const void* Q, int64_t ldq, 
 
 // ------------------------------------------------------------- few rows
 // Up to 64 rows (a decode batch) are bound by reading W once.  They are not
-// sorted: a first kernel finds each row's pair and A_a x, one wave a row and
-// rank; the second takes 16 columns of W a workgroup, all rows at once, its
-// eight waves sharing the contraction, W and x straight to registers (16 rows
-// of 64 bytes a load), and adds the low-rank part of each output as a dot
-// product of r before it stores it.
+// sorted.  One launch does two independent things: some workgroups multiply all
+// rows with 64 rows of W over a share of the contraction each (so that W comes
+// through all CUs, and x, which every one of them needs, in shares), the others
+// find each row's pair and A_a x, one wave a row and rank.  A second launch adds
+// the shares in order, the bias and scale_a B_a v, a dot product of r an output.
+// 32 MiB of W: 8 us for one row, where one launch after another took 13.
 constexpr int kFewRows = 64;
 
 // The pair of row t (-1: none), by the whole wave: 64 offsets a round.
@@ -474,22 +476,19 @@ __device__ __forceinline__ int pair_of_row(int64_t t, const int32_t* __restrict_
   return a >= 0 && a < S ? a : -1;
 }
 
+// A_a x of row t at one rank, by one wave.
 template <class E>
-__global__ __launch_bounds__(256) void ad_few_low_kernel(const E* __restrict__ x, int64_t ldx, int T, int K,
-                                                         const E* __restrict__ A, int64_t lda, int r,
-                                                         const int32_t* __restrict__ offsets,
-                                                         const int32_t* __restrict__ adapter, int R, int S,
-                                                         int32_t* __restrict__ pair, float* __restrict__ v) {
+__device__ __forceinline__ void few_low(int w, const E* __restrict__ x, int64_t ldx, int K, const E* __restrict__ A,
+                                        int64_t lda, const lipcache_adapters& ad, int32_t* __restrict__ pair,
+                                        float* __restrict__ v) {
   constexpr int kV = Vec16<E>::kCount;
   typedef typename Vec16<E>::type V;
-  const int w = uniform(static_cast<int>(blockIdx.x * 4 + threadIdx.x / kWave));
-  if (w >= T * r) return;
-  const int t = w / r, rho = w % r, lane = lane_id();
-  const int a = R > 0 ? uniform(pair_of_row(t, offsets, adapter, R, S)) : -1;
+  const int t = w / ad.r, rho = w % ad.r, lane = lane_id();
+  const int a = ad.R > 0 ? uniform(pair_of_row(t, ad.offsets, ad.adapter, ad.R, ad.S)) : -1;
   float sum = 0.0f;
   if (a >= 0) {
     const E* px = x + t * ldx;
-    const E* pa = A + (static_cast<int64_t>(a) * r + rho) * lda;
+    const E* pa = A + (static_cast<int64_t>(a) * ad.r + rho) * lda;
 #pragma unroll 4
     for (int k = lane * kV; k < K; k += kWave * kV) {
       const V vx = *reinterpret_cast<const V*>(px + k), va = *reinterpret_cast<const V*>(pa + k);
@@ -506,97 +505,99 @@ __global__ __launch_bounds__(256) void ad_few_low_kernel(const E* __restrict__ x
   }
 }
 
-// 16 x 16 products of 16-byte fragments: lane l holds row l % 16 and quarter l / 16 of 64 bytes of the contraction,
-// and ends with rows 4 (l / 16) .. + 3 of column l % 16.
-__device__ __forceinline__ f32x4 mul16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x4 mul16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x4 mul16(f32x4 a, f32x4 b, f32x4 c) {
-  c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[0], b[0], c, 0, 0, 0);
-  c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[1], b[1], c, 0, 0, 0);
-  c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[2], b[2], c, 0, 0, 0);
-  return __builtin_amdgcn_mfma_f32_16x16x4f32(a[3], b[3], c, 0, 0, 0);
+// Workgroups [0, tiles * shares): part[share][t][j] of the projection; the others: v and the pairs.
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void ad_few_kernel(const typename S::E* __restrict__ x, int64_t ldx, int T,
+                                                             const typename S::E* __restrict__ W, int64_t ldw, int K,
+                                                             int N, int tiles, int shares, int each,
+                                                             float* __restrict__ part,
+                                                             const typename S::E* __restrict__ A, int64_t lda,
+                                                             lipcache_adapters ad, int32_t* __restrict__ pair,
+                                                             float* __restrict__ v) {
+  typedef typename S::E E;
+  __shared__ __align__(16) char lds[S::kLds];
+  const int block = static_cast<int>(blockIdx.x);
+  if (block >= tiles * shares) {
+    const int w = uniform((block - tiles * shares) * S::kWaves + static_cast<int>(threadIdx.x) / kWave);
+    if (w < T * ad.r) few_low<E>(w, x, ldx, K, A, lda, ad, pair, v);
+    return;
+  }
+  const int share = block / tiles, j0 = block % tiles * S::BN, k0 = share * each;
+  const int count = K - k0 < each ? K - k0 : each;
+  Side p{}, q{};
+  p.p = x + k0;
+  p.ld = ldx * sizeof(E);
+  p.rows = T;
+  q.p = W + j0 * ldw + k0;
+  q.ld = ldw * sizeof(E);
+  q.rows = N - j0 < S::BN ? N - j0 : S::BN;
+  f32x16 acc[S::TM][S::TN] = {};
+  tile_products<S>(p, q, count, lds, acc);
+  tile_store<S>(acc, [&](int i, int j, const f32x16& u) {
+    j += j0;
+    if (j >= N) return;
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (i + acc_row(e) < T) part[(static_cast<int64_t>(share) * T + i + acc_row(e)) * N + j] = u[e];
+  });
 }
 
-template <class E, int TT>
-__global__ __launch_bounds__(512) void ad_few_main_kernel(const E* __restrict__ x, int64_t ldx, int T,
-                                                          const E* __restrict__ W, int64_t ldw, int K, int N,
+template <class E>
+__global__ __launch_bounds__(256) void ad_few_join_kernel(int T, int N, int shares, const float* __restrict__ part,
                                                           const float* __restrict__ bias, AdLow low,
                                                           const int32_t* __restrict__ pair, E* __restrict__ y,
                                                           int64_t ldy) {
-  constexpr int kV = Vec16<E>::kCount, kWaves = 8, kStep = 4 * kV, kUnroll = 4;
+  constexpr int kV = Vec16<E>::kCount;
   typedef typename Vec16<E>::type V;
-  __shared__ __align__(16) float part[kWaves][TT * 256];
-  const int n0 = static_cast<int>(blockIdx.x) * 16;
-  const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
-  const int li = lane & 15, quarter = lane >> 4;
-  const E* pw = W + (n0 + li < N ? n0 + li : N - 1) * ldw + quarter * kV;
-  const E* px[TT];
+  const int n = static_cast<int>(blockIdx.x) * 256 + static_cast<int>(threadIdx.x), t = static_cast<int>(blockIdx.y);
+  if (n >= N) return;
+  const int a = pair[t];
+  float sum = 0.0f;
+  for (int k = 0; k < shares; ++k) sum += part[(static_cast<int64_t>(k) * T + t) * N + n];
+  if (bias) sum += bias[n];
+  if (a >= 0) {
+    const E* f = static_cast<const E*>(low.F) + (static_cast<int64_t>(a) * N + n) * low.ldf;
+    const float* v = low.v + t * low.r;
+    float dot = 0.0f;
+#pragma unroll 2
+    for (int rho = 0; rho < low.r; rho += kV) {
+      const V b = load_some<E>(f + rho, low.r - rho, low.wide != 0);
 #pragma unroll
-  for (int m = 0; m < TT; ++m) px[m] = x + (16 * m + li < T ? 16 * m + li : T - 1) * ldx + quarter * kV;
-  f32x4 acc[TT] = {};
-  // whole blocks of kUnroll steps, then the rest step by step
-  int k = wave * (kUnroll * kStep);
-  for (; k + kUnroll * kStep <= K; k += kWaves * kUnroll * kStep) {
-    V w[kUnroll], f[kUnroll][TT];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      w[u] = *reinterpret_cast<const V*>(pw + k + u * kStep);
-#pragma unroll
-      for (int m = 0; m < TT; ++m) f[u][m] = *reinterpret_cast<const V*>(px[m] + k + u * kStep);
+      for (int e = 0; e < kV; ++e)
+        dot = fmaf(rho + e < low.r ? v[rho + e] : 0.0f, static_cast<float>(b[e]), dot);
     }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-      for (int m = 0; m < TT; ++m) acc[m] = mul16(w[u], f[u][m], acc[m]);
+    sum = fmaf(low.scale[a], dot, sum);
   }
-  for (int stop = k + kUnroll * kStep; k < K && k < stop; k += kStep) {
-    const bool in = k + quarter * kV < K;
-    const V w = in ? *reinterpret_cast<const V*>(pw + k) : V{};
-#pragma unroll
-    for (int m = 0; m < TT; ++m) acc[m] = mul16(w, in ? *reinterpret_cast<const V*>(px[m] + k) : V{}, acc[m]);
-  }
-#pragma unroll
-  for (int m = 0; m < TT; ++m) *reinterpret_cast<f32x4*>(&part[wave][(m * 64 + lane) * 4]) = acc[m];
-  __syncthreads();
-  const E* F = static_cast<const E*>(low.F);
-  for (int i = static_cast<int>(threadIdx.x); i < TT * 256; i += 512) {
-    const int n = n0 + 4 * ((i >> 6) & 3) + (i & 3), t = (i >> 8) * 16 + ((i >> 2) & 15);
-    if (n >= N || t >= T) continue;
-    float sum = part[0][i];
-#pragma unroll
-    for (int u = 1; u < kWaves; ++u) sum += part[u][i];
-    if (bias) sum += bias[n];
-    const int a = low.S > 0 ? pair[t] : -1;
-    if (a >= 0) {
-      const E* f = F + (static_cast<int64_t>(a) * N + n) * low.ldf;
-      const float* v = low.v + t * low.r;
-      float dot = 0.0f;
-      for (int rho = 0; rho < low.r; rho += kV) {
-        const V b = load_some<E>(f + rho, low.r - rho, low.wide != 0);
-#pragma unroll
-        for (int e = 0; e < kV; e += 4) {
-          const f32x4 u = load_some<float>(v + rho + e, low.r - rho - e, low.wide_v != 0);
-#pragma unroll
-          for (int o = 0; o < 4; ++o) dot = fmaf(u[o], static_cast<float>(b[e + o]), dot);
-        }
-      }
-      sum = fmaf(low.scale[a], dot, sum);
-    }
-    y[t * ldy + n] = static_cast<E>(sum);
-  }
+  y[t * ldy + n] = static_cast<E>(sum);
+}
+
+// Shares of the contraction: about 256 workgroups, at least 512 bytes of a row each.
+inline int few_shares(int K, int N, size_t size) {
+  const int64_t tiles = ceil_div(N, 64), most = ceil_div(K * static_cast<int64_t>(size), 512);
+  int64_t n = 256 / tiles;
+  if (n > most) n = most;
+  return n < 1 ? 1 : n > 16 ? 16 : static_cast<int>(n);
 }
 
 template <class E>
 lipcache_status ad_few(const AdRows<E>& x, int T, const AdRows<E>& W, int K, int N, const float* bias,
-                       const AdRows<E>& A, const lipcache_adapters& ad, const AdLow& low, int32_t* pair, float* v,
-                       E* y, int64_t ldy, hipStream_t s) {
-  ad_few_low_kernel<E><<<static_cast<unsigned>(ceil_div(static_cast<int64_t>(T) * ad.r, 4)), 256, 0, s>>>(
-      x.p, x.ld, T, K, A.p, A.ld, ad.r, ad.offsets, ad.adapter, ad.R, ad.S, pair, v);
+                       const AdRows<E>& A, const lipcache_adapters& ad, const AdLow& low, int32_t* pair, float* part,
+                       float* v, E* y, int64_t ldy, hipStream_t s) {
+  const int tiles = static_cast<int>(ceil_div(N, 64)), wanted = few_shares(K, N, sizeof(E));
+  const int each = static_cast<int>(round_up(ceil_div(K, wanted), 128 / sizeof(E)));
+  const int shares = static_cast<int>(ceil_div(K, each));
+  const unsigned blocks = static_cast<unsigned>(tiles * shares + ceil_div(T * ad.r, 4));
+  auto run = [&](auto shape) {
+    typedef decltype(shape) S;
+    static_assert(S::kWaves == 4, "four rows and ranks a workgroup");
+    ad_few_kernel<S><<<blocks, S::kThreads, 0, s>>>(x.p, x.ld, T, W.p, W.ld, K, N, tiles, shares, each, part, A.p, A.ld,
+                                                    ad, pair, v);
+  };
+  if (T <= 32) run(TileShape<E, 32, 64, 1, 2, 2, 4, 1, false, false>{});
+  else run(TileShape<E, 64, 64, 2, 2, 1, 3, 1, false, false>{});
   LC_LAUNCHED();
-  const unsigned blocks = static_cast<unsigned>(ceil_div(N, 16));
-  if (T <= 16) ad_few_main_kernel<E, 1><<<blocks, 512, 0, s>>>(x.p, x.ld, T, W.p, W.ld, K, N, bias, low, pair, y, ldy);
-  else if (T <= 32) ad_few_main_kernel<E, 2><<<blocks, 512, 0, s>>>(x.p, x.ld, T, W.p, W.ld, K, N, bias, low, pair, y, ldy);
-  else ad_few_main_kernel<E, 4><<<blocks, 512, 0, s>>>(x.p, x.ld, T, W.p, W.ld, K, N, bias, low, pair, y, ldy);
+  ad_few_join_kernel<E><<<dim3(static_cast<unsigned>(ceil_div(N, 256)), static_cast<unsigned>(T)), 256, 0, s>>>(
+      T, N, shares, part, bias, low, pair, y, ldy);
   LC_LAUNCHED();
   return LIPCACHE_OK;
 }
@@ -790,7 +791,6 @@ __global__ __launch_bounds__(256) void ad_join_kernel(AdGradSide<E> A, AdGradSid
 
 // ------------------------------------------------------------------ the calls
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 inline size_t ad_size(int32_t dtype) { return dtype == LIPCACHE_F32 ? 4 : 2; }
 
 // The workspace, in order of use.  Sizes only: `at` NULL gives the sum.
@@ -875,12 +875,13 @@ inline int64_t ad_chunk(int64_t ld, size_t size) {
 template <class E>
 struct AdForwardSpace {
   AdGroups g;
-  float* v;
-  E *x, *W, *A, *B;
+  float *v, *part;
+  E *x, *W, *A;
   AdForwardSpace(AdSpace& ws, int64_t T, int K, int N, int r, int S) {
     constexpr int kV = Vec16<E>::kCount;
     g = ad_groups(ws, T, S);
     v = ws.take<float>(static_cast<size_t>(T) * r);
+    part = ws.take<float>(T <= kFewRows ? static_cast<size_t>(T) * N * few_shares(K, N, sizeof(E)) : 0);
     x = ws.take<E>(static_cast<size_t>(T) * round_up(K, kV));
     W = ws.take<E>(static_cast<size_t>(N) * round_up(K, kV));
     A = ws.take<E>(static_cast<size_t>(S) * r * round_up(K, kV));
@@ -902,7 +903,7 @@ lipcache_status ad_forward(const AdArgs& a, const float* bias, void* y, int64_t 
   const AdLow low{a.ad.B, a.ad.r, v, a.ad.scale, a.ad.r, a.ad.S, a.N, aligned16(a.ad.B) && a.ad.r % kV == 0,
                   aligned16(v) && a.ad.r % 4 == 0};
   if (a.T <= kFewRows)
-    return ad_few<E>(x, static_cast<int>(a.T), W, a.K, a.N, bias, A, a.ad, low, ws.g.pair, v, static_cast<E*>(y), ldy, s);
+    return ad_few<E>(x, static_cast<int>(a.T), W, a.K, a.N, bias, A, a.ad, low, ws.g.pair, ws.part, v, static_cast<E*>(y), ldy, s);
   const int64_t chunk = ad_chunk(x.ld, sizeof(E));
   for (int64_t t0 = 0; t0 < a.T; t0 += chunk) {
     const int T = static_cast<int>(a.T - t0 < chunk ? a.T - t0 : chunk);
