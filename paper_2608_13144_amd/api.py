@@ -396,39 +396,52 @@ def _dtype(t: torch.Tensor, name: str) -> int:
     return code
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(device: torch.device) -> int:
+    """The current stream's handle; torch.cuda.current_stream builds an object around it (2 us a call)."""
+    if _raw_stream is None:
+        return torch.cuda.current_stream(device).cuda_stream
+    return _raw_stream(device.index if device.index is not None else torch.cuda.current_device())
+
+
 def _need_rows(t: torch.Tensor, name: str, dtype: torch.dtype, device: torch.device, rows: int, width: int) -> int:
     """Checks a [rows, width] matrix whose rows may lie apart; returns their distance in elements."""
-    if not isinstance(t, torch.Tensor) or t.device != device:
+    if t.dtype is dtype and t.device == device and t.shape == (rows, width):
+        if t.is_contiguous():
+            return width
+        if (width == 1 or t.stride(1) == 1) and (rows == 1 or t.stride(0) >= width):
+            return t.stride(0) if rows > 1 else width
+        raise ValueError(f"{name} must have contiguous, non-overlapping rows")
+    if t.device != device:
         raise ValueError(f"{name} must be on {device}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width:
-        raise ValueError(f"{name} must be [{rows}, {width}], got {list(t.shape)}")
-    if (width > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < width):
-        raise ValueError(f"{name} must have contiguous, non-overlapping rows")
-    return t.stride(0) if rows > 1 else width
+    raise ValueError(f"{name} must be [{rows}, {width}], got {list(t.shape)}")
 
 
 def _need_shape(t: torch.Tensor, name: str, dtype: torch.dtype, device: torch.device, shape: tuple) -> None:
-    if not isinstance(t, torch.Tensor) or t.device != device:
+    if t.dtype is dtype and t.device == device and t.shape == shape and t.is_contiguous():
+        return
+    if t.device != device:
         raise ValueError(f"{name} must be on {device}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _adapters(A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor, offsets: torch.Tensor, adapter: torch.Tensor,
               dtype: torch.dtype, device: torch.device, K: int, N: int) -> L.LipcacheAdapters:
-    if not isinstance(A, torch.Tensor) or A.dim() != 3:
+    if A.dim() != 3:
         raise ValueError("A must be [S, r, K]")
-    S, r = A.shape[0], A.shape[1]
+    S, r, _ = A.shape
     _need_shape(A, "A", dtype, device, (S, r, K))
     _need_shape(B, "B", dtype, device, (S, N, r))
     _need_shape(scale, "scale", torch.float32, device, (S,))
-    if not isinstance(adapter, torch.Tensor) or adapter.dim() != 1:
+    if adapter.dim() != 1:
         raise ValueError("adapter must be [R]")
     R = adapter.shape[0]
     _need_shape(adapter, "adapter", torch.int32, device, (R,))
@@ -455,7 +468,7 @@ def adapter_forward(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None,
     also returns v, which the backward pass takes."""
     code = _dtype(x, "x")
     dev, dt = x.device, x.dtype
-    if x.dim() != 2 or not isinstance(W, torch.Tensor) or W.dim() != 2:
+    if x.dim() != 2 or W.dim() != 2:
         raise ValueError("x must be [T, K] and W [N, K]")
     T, K = x.shape
     N = W.shape[0]
@@ -465,17 +478,19 @@ def adapter_forward(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None,
         _need_shape(bias, "bias", torch.float32, dev, (N,))
     ad = _adapters(A, B, scale, offsets, adapter, dt, dev, K, N)
     if out is None:
-        out = AdapterOutput(torch.empty((T, N), dtype=dt, device=dev),
+        out = AdapterOutput(x.new_empty((T, N)),
                             torch.empty((T, ad.r), dtype=torch.float32, device=dev) if keep else None)
-    ldy = _need_rows(out.y, "out.y", dt, dev, T, N)
-    if out.v is not None:
-        _need_shape(out.v, "out.v", torch.float32, dev, (T, ad.r))
+        ldy = N
+    else:
+        ldy = _need_rows(out.y, "out.y", dt, dev, T, N)
+        if out.v is not None:
+            _need_shape(out.v, "out.v", torch.float32, dev, (T, ad.r))
     lib = L.load()
     ws = workspace(lib.lipcache_adapter_forward_workspace_bytes(T, K, N, ad.r, ad.S, code), dev)
     st = lib.lipcache_adapter_forward(x.data_ptr(), ldx, T, W.data_ptr(), ldw, None if bias is None else bias.data_ptr(),
                                       K, N, ctypes.byref(ad), code, out.y.data_ptr(), ldy,
                                       None if out.v is None else out.v.data_ptr(), ws.data_ptr(), ws.numel(),
-                                      torch.cuda.current_stream(dev).cuda_stream)
+                                      _stream_of(dev))
     L.check("lipcache_adapter_forward", st)
     return out
 
@@ -496,7 +511,7 @@ def adapter_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, A: torc
     again when None); the others are the forward pass's arguments."""
     code = _dtype(x, "x")
     dev, dt = x.device, x.dtype
-    if x.dim() != 2 or not isinstance(W, torch.Tensor) or W.dim() != 2:
+    if x.dim() != 2 or W.dim() != 2:
         raise ValueError("x must be [T, K] and W [N, K]")
     T, K = x.shape
     N = W.shape[0]
@@ -506,7 +521,7 @@ def adapter_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, A: torc
     ad = _adapters(A, B, scale, offsets, adapter, dt, dev, K, N)
     if v is not None:
         _need_shape(v, "v", torch.float32, dev, (T, ad.r))
-    g = AdapterGradients(torch.empty((T, K), dtype=dt, device=dev) if want_dx else None,
+    g = AdapterGradients(x.new_empty((T, K)) if want_dx else None,
                          torch.empty_like(A) if want_pairs else None, torch.empty_like(B) if want_pairs else None)
     lib = L.load()
     ws = workspace(lib.lipcache_adapter_backward_workspace_bytes(T, K, N, ad.r, ad.S, code), dev)
@@ -514,7 +529,7 @@ def adapter_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, A: torc
                                        ctypes.byref(ad), code, None if v is None else v.data_ptr(),
                                        g.dx.data_ptr() if want_dx else None, K, g.dA.data_ptr() if want_pairs else None,
                                        g.dB.data_ptr() if want_pairs else None, ws.data_ptr(), ws.numel(),
-                                       torch.cuda.current_stream(dev).cuda_stream)
+                                       _stream_of(dev))
     L.check("lipcache_adapter_backward", st)
     return g
 
@@ -555,7 +570,7 @@ def orthogonalise(G: torch.Tensor, steps: int = 5, coefficients=NEWTON_SCHULZ, e
     lib = L.load()
     ws = workspace(lib.lipcache_orthogonalise_workspace_bytes(b, m, n, code), G.device)
     st = lib.lipcache_orthogonalise(G.data_ptr(), b, m, n, code, int(steps), coef, float(eps), out.data_ptr(),
-                                    ws.data_ptr(), ws.numel(), torch.cuda.current_stream(G.device).cuda_stream)
+                                    ws.data_ptr(), ws.numel(), _stream_of(G.device))
     L.check("lipcache_orthogonalise", st)
     return out
 
@@ -579,5 +594,5 @@ def muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, lr: float, mome
     lib = L.load()
     ws = workspace(lib.lipcache_muon_step_workspace_bytes(b, m, n, code), W.device)
     st = lib.lipcache_muon_step(W.data_ptr(), G.data_ptr(), M.data_ptr(), b, m, n, code, ctypes.byref(opt),
-                                ws.data_ptr(), ws.numel(), torch.cuda.current_stream(W.device).cuda_stream)
+                                ws.data_ptr(), ws.numel(), _stream_of(W.device))
     L.check("lipcache_muon_step", st)
