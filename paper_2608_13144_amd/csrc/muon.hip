@@ -327,6 +327,268 @@ __global__ __launch_bounds__(S::kThreads) void ns_apply_kernel(const _Float16* _
   });
 }
 
+// ------------------------------------------------------------ short matrices
+// With the shorter side p <= 64 the iteration runs on the p x p Gram matrix:
+// X_k = P_k X_0 with P_k a polynomial of A_0 = X_0 X_0^T, so the long side is
+// read twice and written once, whatever the number of steps:
+//   A <- Q A Q, P <- Q P with Q = a I + b A + c A^2   (all commute, all symmetric).
+// A_0 squares the singular values, so everything here is float64: small ones
+// relative to the largest keep the digits that float32 products of X would
+// give them.  Three launches: the Gram matrix in shares of the long side (and
+// the momentum), the polynomial (one workgroup a matrix, in LDS), the product
+// P U.  Bound by reading and writing the long matrices: 64 of 16 x 4096.
+constexpr int kShortMost = 64;
+constexpr int kShortBlock = 256;  // of the long side, in LDS at a time
+
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+
+// A block of U in LDS as float32: element (k, c) of the short and the long index at k * sk + c * sc.
+template <typename T, bool kStep>
+struct ShortU {
+  const T* G;
+  float* M;
+  int m, n;
+  float mu;
+  int nesterov;
+  int wide;  // vectors of eight
+
+  __device__ __forceinline__ int p() const { return m < n ? m : n; }
+  __device__ __forceinline__ int q() const { return m < n ? n : m; }
+  // wide matrices (m <= n) lie [k][c], tall ones [c][k] (odd strides keep the banks apart)
+  __device__ __forceinline__ int sk() const { return m <= n ? kShortBlock + 4 : 1; }
+  __device__ __forceinline__ int sc() const { return m <= n ? 1 : (n | 1); }
+  static int room(int p, bool wide) { return wide ? p * (kShortBlock + 4) : kShortBlock * (p | 1); }
+
+  // f(element index in the matrix, k, c, count) for groups of up to eight neighbours along a row
+  template <class F>
+  __device__ __forceinline__ void each(int c0, int count, F f) const {
+    if (m <= n) {
+      const int groups = (count + 7) / 8;
+      for (int i = threadIdx.x; i < groups * m; i += 256) {
+        const int k = i / groups, c = i % groups * 8;
+        f(static_cast<int64_t>(k) * n + c0 + c, k, c, count - c < 8 ? count - c : 8);
+      }
+    } else {
+      const int groups = (n + 7) / 8;
+      for (int i = threadIdx.x; i < groups * count; i += 256) {
+        const int c = i / groups, k = i % groups * 8;
+        f(static_cast<int64_t>(c0 + c) * n + k, k, c, n - k < 8 ? n - k : 8);
+      }
+    }
+  }
+
+  template <bool kUpdate>
+  __device__ __forceinline__ void load(int64_t z, int c0, int count, float* lds) const {
+    const int64_t base = z * m * static_cast<int64_t>(n);
+    const int ek = m <= n ? 0 : sk(), ec = m <= n ? sc() : 0;  // along a row
+    each(c0, count, [&](int64_t at, int k, int c, int some) {
+      float u[8];
+      ns_direction8<T, kStep, kUpdate>(G, M, base + at, some, wide != 0, mu, nesterov, u);
+      float* to = lds + k * sk() + c * sc();
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < some) to[e * (ek + ec)] = u[e];
+    });
+  }
+};
+
+// part[z][share] = sum over the share's c of U(:, c) U(:, c)^T, N x N tiles of 16 (the lower ones; zeros past p).
+template <int N, typename T, bool kStep>
+__global__ __launch_bounds__(256) void ns_short_gram_kernel(ShortU<T, kStep> U, int shares, double* __restrict__ part) {
+  constexpr int kTiles = N * (N + 1) / 2;
+  extern __shared__ __align__(16) float lds[];
+  __shared__ double join[4][256];
+  const int64_t z = blockIdx.y;
+  const int p = U.p(), q = U.q(), sk = U.sk(), sc = U.sc();
+  const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+  const int row = lane & 15, quarter = lane >> 4;
+  f64x4 acc[kTiles] = {};
+  for (int c0 = static_cast<int>(blockIdx.x) * kShortBlock; c0 < q; c0 += shares * kShortBlock) {
+    const int count = q - c0 < kShortBlock ? q - c0 : kShortBlock;
+    __syncthreads();
+    U.template load<true>(z, c0, count, lds);
+    __syncthreads();
+    for (int c = wave * 4; c < count; c += 16) {
+      double f[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        f[i] = 16 * i + row < p && c + quarter < count ? static_cast<double>(lds[(16 * i + row) * sk + (c + quarter) * sc]) : 0.0;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j <= i; ++j)
+          acc[i * (i + 1) / 2 + j] = __builtin_amdgcn_mfma_f64_16x16x4f64(f[i], f[j], acc[i * (i + 1) / 2 + j], 0, 0, 0);
+    }
+  }
+  // the waves' sums, in order
+  double* out = part + (z * shares + blockIdx.x) * (kTiles * 256);
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < 4; ++v) join[wave][v * 64 + lane] = acc[t][v];
+    __syncthreads();
+    const int i = static_cast<int>(threadIdx.x);
+    out[t * 256 + i] = ((join[0][i] + join[1][i]) + join[2][i]) + join[3][i];
+  }
+}
+
+struct ShortCoefficients {
+  float c[3 * 32];
+};
+
+// P [z][16 N][16 N], with the 1 / (||U||_F + eps) of X_0 in it.
+template <int N>
+__global__ __launch_bounds__(64 * N * N) void ns_short_poly_kernel(const double* __restrict__ part, int shares, float eps,
+                                                                   int steps, ShortCoefficients coef,
+                                                                   double* __restrict__ out) {
+  constexpr int kTiles = N * (N + 1) / 2, kSide = 16 * N, kLd = kSide + 2;
+  __shared__ double A[kSide * kLd], Q[kSide * kLd], P[kSide * kLd], B[N > 3 ? 1 : kSide * kLd];
+  extern __shared__ __align__(16) double more[];
+  double* R = N > 3 ? more : B;  // four of them pass the static limit at N = 4
+  __shared__ double scale;
+  const int64_t z = blockIdx.x;
+  const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+  const int ti = wave / N, tj = wave % N;  // the wave's 16 x 16 tile
+  const int row = lane & 15, quarter = lane >> 4;
+  // rows 4 v + quarter, column `row` of the tile
+  auto at = [&](int v) { return (16 * ti + 4 * v + quarter) * kLd + 16 * tj + row; };
+  {
+    const int i = ti > tj ? ti : tj, j = ti > tj ? tj : ti;
+    const double* from = part + z * shares * (kTiles * 256) + (i * (i + 1) / 2 + j) * 256;
+    int slot[4];
+    double sum[4] = {};
+#pragma unroll
+    for (int v = 0; v < 4; ++v)  // element (r, c) of the tile, or (c, r) of its mirror image: slot (r / 4) * 64 + (r % 4) * 16 + c
+      slot[v] = ti >= tj ? v * 64 + lane : (row >> 2) * 64 + (row & 3) * 16 + 4 * v + quarter;
+    for (int s = 0; s < shares; s += 8) {
+      double in[8][4];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          in[u][v] = from[static_cast<int64_t>(s + u < shares ? s + u : s) * (kTiles * 256) + slot[v]];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) sum[v] += s + u < shares ? in[u][v] : 0.0;
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) A[at(v)] = sum[v];
+  }
+  __syncthreads();
+  if (wave == 0) {
+    double t = lane < kSide ? A[lane * kLd + lane] : 0.0;
+    t = wave_sum(t);
+    if (lane == 0) {
+      const double f = sqrt(t) + static_cast<double>(eps);
+      scale = f > 0.0 || f != f ? 1.0 / f : 0.0;
+    }
+  }
+  __syncthreads();
+  const double s = scale;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    A[at(v)] *= s * s;
+    P[at(v)] = 16 * ti + 4 * v + quarter == 16 * tj + row ? s : 0.0;
+  }
+  __syncthreads();
+  // the wave's tile of X Y, Y symmetric
+  auto product = [&](const double* X, const double* Y) {
+    f64x4 acc = {};
+#pragma unroll
+    for (int k = 0; k < kSide; k += 4)
+      acc = __builtin_amdgcn_mfma_f64_16x16x4f64(X[(16 * ti + row) * kLd + k + quarter], Y[(16 * tj + row) * kLd + k + quarter], acc, 0, 0, 0);
+    return acc;
+  };
+  for (int k = 0; k < steps; ++k) {
+    const double a = coef.c[3 * k], b = coef.c[3 * k + 1], c = coef.c[3 * k + 2];
+    const f64x4 square = product(A, A);
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+      Q[at(v)] = c * square[v] + b * A[at(v)] + (16 * ti + 4 * v + quarter == 16 * tj + row ? a : 0.0);
+    __syncthreads();
+    const f64x4 p = product(P, Q), qa = product(A, Q);
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      P[at(v)] = p[v];
+      R[at(v)] = qa[v];
+    }
+    __syncthreads();
+    const f64x4 next = product(R, Q);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) A[at(v)] = next[v];
+    __syncthreads();
+  }
+#pragma unroll
+  for (int v = 0; v < 4; ++v)
+    out[(z * kSide + 16 * ti + 4 * v + quarter) * kSide + 16 * tj + row] = P[at(v)];
+}
+
+// O(:, c) = P U(:, c) for 256 c, stored or subtracted from W.
+template <int N, typename T, bool kStep>
+__global__ __launch_bounds__(256) void ns_short_apply_kernel(ShortU<T, kStep> U, const double* __restrict__ P, float keep,
+                                                             float gain, T* out) {
+  constexpr int kSide = 16 * N;
+  extern __shared__ __align__(16) float lds[];
+  const int64_t z = blockIdx.y;
+  const int p = U.p(), q = U.q(), sk = U.sk(), sc = U.sc();
+  const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+  const int row = lane & 15, quarter = lane >> 4;
+  const int c0 = static_cast<int>(blockIdx.x) * kShortBlock, count = q - c0 < kShortBlock ? q - c0 : kShortBlock;
+  U.template load<false>(z, c0, count, lds);
+  __syncthreads();
+  const double* pz = P + z * kSide * kSide;
+  for (int c = wave * 16; c < count; c += 64) {
+    f64x4 acc[N] = {};
+    const bool in = c + row < count;
+#pragma unroll 4
+    for (int k = 0; k < kSide; k += 4) {
+      const double u = in && k + quarter < p ? static_cast<double>(lds[(k + quarter) * sk + (c + row) * sc]) : 0.0;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        acc[i] = __builtin_amdgcn_mfma_f64_16x16x4f64(pz[(16 * i + row) * kSide + k + quarter], u, acc[i], 0, 0, 0);
+    }
+    // over the columns of U that only this wave has read
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int k = 16 * i + 4 * v + quarter;
+        if (in && k < p) lds[k * sk + (c + row) * sc] = static_cast<float>(acc[i][v]);
+      }
+  }
+  __syncthreads();
+  const int step = U.m <= U.n ? sc : sk;
+  T* oz = out + z * U.m * static_cast<int64_t>(U.n);
+  U.each(c0, count, [&](int64_t at, int k, int c, int some) {
+    typedef T vec __attribute__((ext_vector_type(8)));
+    const float* from = lds + k * sk + c * sc;
+    if (U.wide) {
+      vec w{};
+      if constexpr (kStep) w = *reinterpret_cast<const vec*>(oz + at);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        w[e] = static_cast<T>(kStep ? fmaf(keep, static_cast<float>(w[e]), -gain * from[e * step]) : from[e * step]);
+      *reinterpret_cast<vec*>(oz + at) = w;
+    } else {
+      for (int e = 0; e < some; ++e)
+        oz[at + e] = static_cast<T>(kStep ? fmaf(keep, static_cast<float>(oz[at + e]), -gain * from[e * step]) : from[e * step]);
+    }
+  });
+}
+
+// Shares of the long side of one matrix: blocks of 256, up to 256 shares and about 2048 workgroups.
+inline int ns_short_shares(int64_t batch, int q) {
+  int64_t n = (q + kShortBlock - 1) / kShortBlock, most = 2048 / batch;
+  if (most < 1) most = 1;
+  if (most > 256) most = 256;
+  return static_cast<int>(n < most ? n : most);
+}
+
+inline bool ns_short(int m, int n) { return (m < n ? m : n) <= kShortMost; }
+
 struct NsArgs {
   int64_t batch;
   int m, n, steps;
@@ -345,6 +607,11 @@ inline int round_up(int v, int to) { return (v + to - 1) / to * to; }
 inline bool ns_split(int32_t dtype, bool step) { return !step || dtype == LIPCACHE_F32; }
 
 size_t ns_workspace(int64_t batch, int32_t m, int32_t n, bool split) {
+  if (ns_short(m, n)) {
+    const size_t tiles = ((m < n ? m : n) + 15) / 16, b = static_cast<size_t>(batch);
+    return align_up(b * ns_short_shares(batch > 0 ? batch : 1, m < n ? n : m) * (tiles * (tiles + 1) / 2) * 2048, 256) +
+           align_up(b * tiles * tiles * 2048, 256);
+  }
   const int pad = split ? 32 : 8;
   const size_t b = static_cast<size_t>(batch), mp = round_up(m, pad), np = round_up(n, pad), p = mp < np ? mp : np,
                e = split ? 4 : 2;
@@ -459,11 +726,44 @@ lipcache_status ns_products(const NsArgs& g, double sx, _Float16* X, _Float16* X
   return LIPCACHE_OK;
 }
 
+template <int N, typename T, bool kStep>
+lipcache_status ns_short_run(const NsArgs& g, const T* G, float* M, float mu, int nesterov, float keep, float gain, T* out,
+                             void* ws, hipStream_t s) {
+  const bool across = g.m <= g.n;
+  const int p = across ? g.m : g.n, q = across ? g.n : g.m, shares = ns_short_shares(g.batch, q);
+  // eight neighbours of a row stay in it
+  const int wide = g.n % 8 == 0 && aligned16(G) && aligned16(out) && (!kStep || aligned16(M));
+  const ShortU<T, kStep> U{G, M, g.m, g.n, mu, nesterov, wide};
+  const unsigned nb = static_cast<unsigned>(g.batch);
+  const size_t lds = static_cast<size_t>(ShortU<T, kStep>::room(p, across)) * 4;
+  double* part = static_cast<double*>(ws);
+  double* P = reinterpret_cast<double*>(static_cast<char*>(ws) +
+                                        align_up(static_cast<size_t>(g.batch) * shares * (N * (N + 1) / 2) * 2048, 256));
+  ShortCoefficients coef{};
+  for (int i = 0; i < 3 * g.steps; ++i) coef.c[i] = g.coef[i];
+  ns_short_gram_kernel<N, T, kStep><<<dim3(shares, nb), 256, lds, s>>>(U, shares, part);
+  LC_LAUNCHED();
+  constexpr size_t kMore = N > 3 ? 16 * N * (16 * N + 2) * 8 : 0;
+  ns_short_poly_kernel<N><<<nb, 64 * N * N, kMore, s>>>(part, shares, g.eps, g.steps, coef, P);
+  LC_LAUNCHED();
+  ns_short_apply_kernel<N, T, kStep><<<dim3(static_cast<unsigned>((q + kShortBlock - 1) / kShortBlock), nb), 256, lds, s>>>(
+      U, P, keep, gain, out);
+  LC_LAUNCHED();
+  return LIPCACHE_OK;
+}
+
 template <class E, typename T, bool kStep>
 lipcache_status ns_run(const NsArgs& g, const void* G_, float* M, float mu, int nesterov, float keep, float gain,
                        void* out_, void* ws, hipStream_t s) {
   const T* G = static_cast<const T*>(G_);
   T* out = static_cast<T*>(out_);
+  if (ns_short(g.m, g.n)) {
+    const int tiles = ((g.m < g.n ? g.m : g.n) + 15) / 16;
+    if (tiles == 1) return ns_short_run<1, T, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
+    if (tiles == 2) return ns_short_run<2, T, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
+    if (tiles == 3) return ns_short_run<3, T, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
+    return ns_short_run<4, T, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
+  }
   const int m8 = round_up(g.m, NsAt<E>::kPad), n8 = round_up(g.n, NsAt<E>::kPad);
   const size_t b = static_cast<size_t>(g.batch), p8 = m8 < n8 ? m8 : n8;
   const int64_t size = static_cast<int64_t>(g.m) * g.n, room = static_cast<int64_t>(m8) * n8;

@@ -132,6 +132,20 @@ def test_muon_step(shape, dtype, nesterov):
     assert np.linalg.norm(n64(W) - ref) <= lim, (shape, dtype)
 
 
+@pytest.mark.parametrize("shape", [(1, 3, 70000), (1, 66000, 5), (3, 64, 5000), (2, 4099, 50), (300, 16, 24), (2, 33, 2048),
+                                   (70, 48, 520)], ids=lambda s: "x".join(map(str, s)))
+def test_short_matrices_with_long_sides(shape):
+    for dtype in ("f32", "bf16"):
+        say("short", shape, dtype)
+        for kind in ("random", "strong"):
+            G = matrices(40, *shape, dtype, kind)
+            assert far(api.orthogonalise(G), R.newton_schulz(n64(G), 5, NS5, 1e-7)) <= R.NS_TOL[dtype]
+        W, M = torch.zeros_like(G), matrices(41, *shape, "f32")
+        U = 0.25 * n64(M) + 1.5 * n64(G)
+        api.muon_step(W, G, M, lr=1.0, momentum=0.5, scale=1.0)
+        assert far(W, -R.newton_schulz(U, 5, NS5, 1e-7)) <= R.NS_TOL[dtype]
+
+
 # Large and many matrices: every tile size of the products, wide and tall.
 LARGE = [("ortho", (1, 2080, 2050), "f32"), ("ortho", (1, 2050, 2080), "f16"), ("ortho", (5, 1100, 1030), "f32"),
          ("ortho", (5, 1030, 1100), "bf16"), ("ortho", (40, 500, 520), "f32"), ("ortho", (40, 520, 500), "f16"),
