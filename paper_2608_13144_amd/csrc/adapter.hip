@@ -190,6 +190,26 @@ __device__ __forceinline__ void two_parts(float v, E& first, E& second) {
   second = static_cast<E>(v - static_cast<float>(first));
 }
 
+// float16 ends at 65504 and loses digits below 2^-14, where A_a x and B_a^T dy
+// may lie (gradients of a mean over many rows, outliers of a wide sum).  Such
+// factors go to the matrix cores times 2^e, which brings the largest finite one
+// of a tile to [2^14, 2^15), and what comes out is taken back by 2^-e in float32.
+// bfloat16 has float32's range and takes them as they are.
+template <class E>
+inline constexpr bool kScaledFactors = std::is_same_v<E, _Float16>;
+__device__ __forceinline__ float finite_size(float v) {
+  const float a = fabsf(v);
+  return a < __builtin_huge_valf() ? a : 0.0f;
+}
+__device__ __forceinline__ int factor_exponent(float peak) {  // of a peak > 0
+  return 15 - __builtin_amdgcn_frexp_expf(peak);
+}
+template <class E>
+__device__ __forceinline__ float two_to(float v, int e) {
+  if constexpr (kScaledFactors<E>) return __builtin_amdgcn_ldexpf(v, e);
+  else return v;
+}
+
 // ------------------------------------------------------- copies and transposes
 // Rows moved into the workspace: padded with zeros to a width of whole 16-byte
 // vectors, as they are or transposed.
@@ -253,12 +273,14 @@ lipcache_status ad_copy(const AdCopy& c, const AdCopy& d, hipStream_t s) {
 // ------------------------------------------------------------ thin products
 // out[row][rho] = F_a[rho] . x[row] for the up to 32 sorted rows of one tile
 // of the table (F is [S][r][ldf]), the contraction shared by four waves.  The
-// workgroups past the table write zeros to the rows without a pair.  Bound by
-// reading x once, and F_a once a tile.
+// workgroups past the table write zeros to the rows without a pair.  peak[row]
+// (or NULL): the largest finite |out| of a row with one.  Bound by reading x
+// once, and F_a once a tile.
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void ad_thin_kernel(const typename S::E* __restrict__ x, int64_t ldx, int width,
                                                               const typename S::E* __restrict__ F, int64_t ldf, int r,
-                                                              int pairs, int T, AdGroups g, float* __restrict__ out) {
+                                                              int pairs, int T, AdGroups g, float* __restrict__ out,
+                                                              float* __restrict__ peak) {
   typedef typename S::E E;
   __shared__ __align__(16) char lds[S::kLds];
   const int t = static_cast<int>(blockIdx.x), table = static_cast<int>(ad_tiles(T, pairs));
@@ -283,12 +305,32 @@ __global__ __launch_bounds__(S::kThreads) void ad_thin_kernel(const typename S::
   q.rows = r;
   f32x16 acc[S::TM][S::TN] = {};
   tile_products<S>(p, q, width, lds, acc);
+  float size[16] = {};
   tile_store<S>(acc, [&](int i, int j, const f32x16& v) {
     if (j >= r) return;
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
+    for (int e = 0; e < 16; ++e) {
       if (i + acc_row(e) < rows) out[static_cast<int64_t>(g.order[row0 + i + acc_row(e)]) * r + j] = v[e];
+      if constexpr (kScaledFactors<E>) size[e] = fmaxf(size[e], finite_size(v[e]));
+    }
   });
+  if constexpr (kScaledFactors<E>) {
+    // each lane has a column of 16 rows: halve the rows and double the columns, four times
+    if (!peak || threadIdx.x >= kWave) return;  // the first wave has the sums
+    const int lane = lane_id();
+#pragma unroll
+    for (int b = 0, n = 8; b < 4; ++b, n >>= 1)
+#pragma unroll
+      for (int e = 0; e < n; ++e) {
+        const bool upper = (lane >> b & 1) != 0;
+        const float mine = upper ? size[e + n] : size[e], other = upper ? size[e] : size[e + n];
+        size[e] = fmaxf(mine, __shfl_xor(other, 1 << b, kWave));
+      }
+    const float top = fmaxf(size[0], __shfl_xor(size[0], 16, kWave));
+    const int e = (lane & 1) << 3 | (lane & 2) << 1 | (lane & 4) >> 1 | (lane & 8) >> 3;
+    const int i = acc_row(e) + 4 * (lane >> 5);
+    if ((lane & 16) == 0 && i < rows) peak[g.order[row0 + i]] = top;
+  }
 }
 
 // ------------------------------------------------------------- main product
@@ -310,6 +352,7 @@ struct AdLow {
   const void* F;       // [S][width][ldf]: B (forward) or A transposed (backward)
   int64_t ldf;         // elements between its rows
   const float* v;      // [T][r]
+  const float* peak;   // [T]: the thin product's (float16 only)
   const float* scale;  // [S]
   int r, S, width;
   int wide;            // F's rows and r allow whole vectors
@@ -320,15 +363,17 @@ struct AdLow {
 template <class S>
 struct AdTileRows {
   int pair[S::TM], row[S::TM];
-  __device__ __forceinline__ void load(const AdGroups& g, int pairs, int i0, int rows) {
+  float peak[S::TM];
+  __device__ __forceinline__ void load(const AdGroups& g, const AdLow& low, int i0, int rows) {
     const int wave = uniform(static_cast<int>(threadIdx.x) / kWave);
     const int wm = wave % (S::WM * S::WN) / S::WN;
 #pragma unroll
     for (int tm = 0; tm < S::TM; ++tm) {
       const int i = (wm * S::TM + tm) * 32 + (lane_id() & 31);
       const bool in = i < rows;
-      pair[tm] = in ? g.pair[i0 + i] : pairs;
+      pair[tm] = in ? g.pair[i0 + i] : low.S;
       row[tm] = g.order[i0 + (in ? i : 0)];
+      if constexpr (kScaledFactors<typename S::E>) peak[tm] = pair[tm] < low.S ? low.peak[row[tm]] : 0.0f;
     }
   }
 };
@@ -354,6 +399,13 @@ __device__ __forceinline__ void add_low_rank(const AdLow& low, const AdTileRows<
       const uint32_t mask = static_cast<uint32_t>(__ballot(mine));
       todo &= ~mask;
       const float scale = low.scale[a];
+      int up = 0;
+      if constexpr (kScaledFactors<E>) {
+        float top = mine ? finite_size(scale * rows.peak[tm]) : 0.0f;
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+        up = top > 0.0f ? factor_exponent(top) : 0;
+      }
 #pragma unroll
       for (int tn = 0; tn < S::TN; ++tn) {
         const int j = j0 + (wn * S::TN + tn) * 32 + li;
@@ -368,7 +420,7 @@ __device__ __forceinline__ void add_low_rank(const AdLow& low, const AdTileRows<
           for (int e = 0; e < kV; e += 4) {
             const f32x4 u = load_some<float>(v + at_k + e, mine ? left - e : 0, low.wide_v != 0);
 #pragma unroll
-            for (int o = 0; o < 4; ++o) w[e + o] = mine ? scale * u[o] : 0.0f;
+            for (int o = 0; o < 4; ++o) w[e + o] = mine ? two_to<E>(scale * u[o], up) : 0.0f;
           }
           if constexpr (std::is_same_v<E, float>) {
             sum = MfmaType<E>::mul(V{w[0], w[1], w[2], w[3]}, vf, sum);
@@ -387,7 +439,7 @@ __device__ __forceinline__ void add_low_rank(const AdLow& low, const AdTileRows<
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (mask >> (acc_row(e) + 4 * half) & 1) acc[tm][tn][e] += sum[e];
+          if (mask >> (acc_row(e) + 4 * half) & 1) acc[tm][tn][e] += two_to<E>(sum[e], -up);
       }
     }
   }
@@ -414,7 +466,7 @@ __global__ __launch_bounds__(S::kThreads) void ad_main_kernel(const typename S::
   q.ld = ldq * sizeof(E);
   q.rows = width - j0 < S::BN ? width - j0 : S::BN;
   AdTileRows<S> rows;
-  rows.load(g, low.S, i0, p.rows);
+  rows.load(g, low, i0, p.rows);
   f32x16 acc[S::TM][S::TN] = {};
   tile_products<S>(p, q, K, lds, acc);
   add_low_rank<S, E>(low, rows, j0, acc);
@@ -606,10 +658,16 @@ lipcache_status ad_few(const AdRows<E>& x, int T, const AdRows<E>& W, int K, int
 // The factors u and v as the gradient kernel's operand: for each tile of the
 // table a block of r rows of 128 bytes, row rho the tile's 32 values f[row][rho]
 // as float32, or as 32 first and 32 second 16-bit parts; zeros past its rows.
+// float16: times 2^exponent[tile], a multiple of 4 (so that the sums, which
+// follow it, seldom change) up to 40 (float16 gradients are zero from there).
+constexpr int kNoExponent = -1000;  // a tile of zeros
+
 template <class E>
 __global__ __launch_bounds__(256) void ad_factor_kernel(const float* __restrict__ u, const float* __restrict__ v, int r,
-                                                        int pairs, AdGroups g, E* __restrict__ to_u, E* __restrict__ to_v) {
-  __shared__ float tile[32][33];
+                                                        int pairs, AdGroups g, E* __restrict__ to_u, E* __restrict__ to_v,
+                                                        int32_t* __restrict__ exps_u, int32_t* __restrict__ exps_v) {
+  __shared__ float tile[32][kAdMaxRank + 1];
+  __shared__ float wave_top[256 / kWave];
   const int t = static_cast<int>(blockIdx.x);
   if (static_cast<uint32_t>(t) >= static_cast<uint32_t>(g.tile_start[pairs])) return;
   const float* f = blockIdx.y ? v : u;
@@ -617,24 +675,34 @@ __global__ __launch_bounds__(256) void ad_factor_kernel(const float* __restrict_
   const int row0 = g.tile_row[t];
   const int rows = g.start[g.tile_pair[t] + 1] - row0;
   const int x = static_cast<int>(threadIdx.x) & 31, y = static_cast<int>(threadIdx.x) >> 5;
-  for (int rho0 = 0; rho0 < r; rho0 += 32) {
-    __syncthreads();
+  float top = 0.0f;
 #pragma unroll
-    for (int i = y; i < 32; i += 8)
-      tile[i][x] = i < rows && rho0 + x < r ? f[static_cast<int64_t>(g.order[row0 + i]) * r + rho0 + x] : 0.0f;
-    __syncthreads();
-#pragma unroll
-    for (int k = y; k < 32; k += 8) {
-      const int rho = rho0 + k;
-      if (rho >= r) continue;
-      const float w = tile[x][k];
-      E* p = to + rho * (128 / sizeof(E)) + x;
-      if constexpr (std::is_same_v<E, float>) {
-        *p = w;
-      } else {
-        two_parts(w, p[0], p[32]);
-      }
+  for (int i = y; i < 32; i += 8) {
+    const float* from = f + static_cast<int64_t>(g.order[row0 + (i < rows ? i : 0)]) * r;
+    for (int rho = x; rho < r; rho += 32) {
+      const float w = i < rows ? from[rho] : 0.0f;
+      tile[i][rho] = w;
+      if constexpr (kScaledFactors<E>) top = fmaxf(top, finite_size(w));
     }
+  }
+  if constexpr (kScaledFactors<E>) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+    if (lane_id() == 0) wave_top[threadIdx.x / kWave] = top;
+  }
+  __syncthreads();
+  int up = 0;
+  if constexpr (kScaledFactors<E>) {
+    top = fmaxf(fmaxf(wave_top[0], wave_top[1]), fmaxf(wave_top[2], wave_top[3]));
+    if (top > 0.0f) up = factor_exponent(top) & ~3;
+    if (up > 40) up = 40;
+    if (threadIdx.x == 0) (blockIdx.y ? exps_v : exps_u)[t] = top > 0.0f ? up : kNoExponent;
+  }
+  for (int rho = y; rho < r; rho += 8) {
+    const float w = two_to<E>(tile[x][rho], up);
+    E* p = to + rho * (128 / sizeof(E)) + x;
+    if constexpr (std::is_same_v<E, float>) *p = w;
+    else two_parts(w, p[0], p[32]);
   }
 }
 
@@ -661,7 +729,9 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
                                                       const float* __restrict__ scale, const int32_t* __restrict__ order,
                                                       const int32_t* __restrict__ start,
                                                       const int32_t* __restrict__ tile_start,
-                                                      const int32_t* __restrict__ tile_row, const void* zeros) {
+                                                      const int32_t* __restrict__ tile_row,
+                                                      const int32_t* __restrict__ exps_a,
+                                                      const int32_t* __restrict__ exps_b, const void* zeros) {
   constexpr bool kF32 = std::is_same_v<E, float>;
   constexpr int kV = Vec16<E>::kCount, kSize = static_cast<int>(sizeof(E));
   typedef typename Vec16<E>::type V;
@@ -735,7 +805,16 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
     for (int u = 0; u < kSub; ++u) copy_tile(step * kSub + u, base + (step % kStages * kSub + u) * kTile);
   };
   for (int step = 0; step < kStages - 1 && step < steps; ++step) copy_step(step);
+  int up = 0;  // the sums are times 2^up
   for (int step = 0; step < steps; ++step) {
+    int exps[kSub];
+    if constexpr (kScaledFactors<E>) {
+#pragma unroll
+      for (int u = 0; u < kSub; ++u) {
+        const int n = step * kSub + u;
+        exps[u] = n < tiles ? uniform((second ? exps_b : exps_a)[uniform(tile0 + n)]) : kNoExponent;
+      }
+    }
     if (kStages > 2 && step + 1 < steps) copies_left<(kStages - 2) * kCopies>();
     else copies_left<0>();
     __syncthreads();
@@ -743,6 +822,15 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
 #pragma unroll
     for (int u = 0; u < kSub; ++u) {
       const char* at = lds + (step % kStages * kSub + u) * kTile;
+      if constexpr (kScaledFactors<E>) {
+        if (exps[u] != kNoExponent && exps[u] != up) {
+#pragma unroll
+          for (int m = 0; m < NR; ++m)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[m][e] = two_to<E>(acc[m][e], exps[u] - up);
+          up = exps[u];
+        }
+      }
 #pragma unroll
       for (int n = 0; n < kGroups; ++n) {
         const V z = __builtin_bit_cast(V, TileZ::read16(at + rz[n]));
@@ -763,12 +851,13 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
     for (int e = 0; e < 16; ++e) {
       const int rho = 32 * m + acc_row(e) + 4 * half;
       if (rho >= r) continue;
+      const float sum = two_to<E>(acc[m][e], -up);
       if (splits > 1) {
-        d.part[((static_cast<int64_t>(share) * S + a) * r + rho) * d.width + col] = acc[m][e];
+        d.part[((static_cast<int64_t>(share) * S + a) * r + rho) * d.width + col] = sum;
       } else {
         const int64_t to = d.across ? (static_cast<int64_t>(a) * d.width + col) * r + rho
                                     : (static_cast<int64_t>(a) * r + rho) * d.width + col;
-        d.out[to] = static_cast<E>(all > 0 ? sc * acc[m][e] : 0.0f);
+        d.out[to] = static_cast<E>(all > 0 ? sc * sum : 0.0f);
       }
     }
 }
@@ -845,13 +934,13 @@ lipcache_status ad_rows(const void* from, int64_t ld, int64_t rows, int width, E
 // v (u) of every row; rows without a pair are written (zeros) where `all_rows`.
 template <class E>
 lipcache_status ad_thin(const AdRows<E>& x, int width, const E* F, int64_t ldf, int T, const lipcache_adapters& ad,
-                        const AdGroups& g, float* out, bool all_rows, hipStream_t s) {
+                        const AdGroups& g, float* out, float* peak, bool all_rows, hipStream_t s) {
   const int64_t table = ad_tiles(T, ad.S), more = all_rows ? ceil_div(T, 256) : 0;
   const unsigned blocks = static_cast<unsigned>(table + (more < 256 ? more : 256));
   if (blocks == 0) return LIPCACHE_OK;
   auto run = [&](auto shape) {
     typedef decltype(shape) S;
-    ad_thin_kernel<S><<<blocks, S::kThreads, 0, s>>>(x.p, x.ld, width, F, ldf, ad.r, ad.S, T, g, out);
+    ad_thin_kernel<S><<<blocks, S::kThreads, 0, s>>>(x.p, x.ld, width, F, ldf, ad.r, ad.S, T, g, out, peak);
     return hipGetLastError() == hipSuccess ? LIPCACHE_OK : LIPCACHE_EHIP;
   };
   if (ad.r <= 32) return run(TileShape<E, 32, 32, 1, 1, 4, 4, 2, false, false>{});
@@ -875,12 +964,13 @@ inline int64_t ad_chunk(int64_t ld, size_t size) {
 template <class E>
 struct AdForwardSpace {
   AdGroups g;
-  float *v, *part;
+  float *v, *peak, *part;
   E *x, *W, *A;
   AdForwardSpace(AdSpace& ws, int64_t T, int K, int N, int r, int S) {
     constexpr int kV = Vec16<E>::kCount;
     g = ad_groups(ws, T, S);
     v = ws.take<float>(static_cast<size_t>(T) * r);
+    peak = ws.take<float>(T);
     part = ws.take<float>(T <= kFewRows ? static_cast<size_t>(T) * N * few_shares(K, N, sizeof(E)) : 0);
     x = ws.take<E>(static_cast<size_t>(T) * round_up(K, kV));
     W = ws.take<E>(static_cast<size_t>(N) * round_up(K, kV));
@@ -900,7 +990,7 @@ lipcache_status ad_forward(const AdArgs& a, const float* bias, void* y, int64_t 
   if ((st = ad_rows<E>(a.ad.A, a.K, static_cast<int64_t>(a.ad.S) * a.ad.r, a.K, ws.A, A, s)) != LIPCACHE_OK) return st;
   const bool keep = v != nullptr;
   if (!keep) v = ws.v;
-  const AdLow low{a.ad.B, a.ad.r, v, a.ad.scale, a.ad.r, a.ad.S, a.N, aligned16(a.ad.B) && a.ad.r % kV == 0,
+  const AdLow low{a.ad.B, a.ad.r, v, ws.peak, a.ad.scale, a.ad.r, a.ad.S, a.N, aligned16(a.ad.B) && a.ad.r % kV == 0,
                   aligned16(v) && a.ad.r % 4 == 0};
   if (a.T <= kFewRows)
     return ad_few<E>(x, static_cast<int>(a.T), W, a.K, a.N, bias, A, a.ad, low, ws.g.pair, ws.part, v, static_cast<E*>(y), ldy, s);
@@ -911,7 +1001,7 @@ lipcache_status ad_forward(const AdArgs& a, const float* bias, void* y, int64_t 
     AdLow lc = low;
     lc.v = v + t0 * a.ad.r;
     if ((st = ad_group(t0, T, a.ad, ws.g, s)) != LIPCACHE_OK) return st;
-    if ((st = ad_thin<E>(xc, a.K, A.p, A.ld, T, a.ad, ws.g, v + t0 * a.ad.r, keep, s)) != LIPCACHE_OK) return st;
+    if ((st = ad_thin<E>(xc, a.K, A.p, A.ld, T, a.ad, ws.g, v + t0 * a.ad.r, ws.peak, keep, s)) != LIPCACHE_OK) return st;
     if ((st = ad_main<E, false>(xc.p, xc.ld, W.p, W.ld, T, a.N, a.K, bias, lc, ws.g, static_cast<E*>(y) + t0 * ldy, ldy, s)) !=
         LIPCACHE_OK)
       return st;
@@ -931,7 +1021,8 @@ inline int ad_splits(int64_t T, int K, int N, int S) {
 template <class E>
 struct AdBackwardSpace {
   AdGroups g;
-  float *u, *v, *part_a, *part_b;
+  float *u, *v, *peak, *part_a, *part_b;
+  int32_t *exps_u, *exps_v;
   E *x, *W, *dy, *A, *At, *Bt, *fu, *fv;
   AdBackwardSpace(AdSpace& ws, int64_t T, int K, int N, int r, int S) {
     constexpr int kV = Vec16<E>::kCount;
@@ -939,6 +1030,9 @@ struct AdBackwardSpace {
     g = ad_groups(ws, T, S);
     u = ws.take<float>(static_cast<size_t>(T) * r);
     v = ws.take<float>(static_cast<size_t>(T) * r);
+    peak = ws.take<float>(T);
+    exps_u = ws.take<int32_t>(ad_tiles(T, S));
+    exps_v = ws.take<int32_t>(ad_tiles(T, S));
     At = ws.take<E>(n * K * round_up(r, kV));
     Bt = ws.take<E>(n * r * N8);
     const size_t factors = static_cast<size_t>(ad_tiles(T, S)) * r * (128 / sizeof(E));
@@ -979,12 +1073,12 @@ lipcache_status ad_backward(const AdArgs& a, const float* v_in, void* dx, int64_
     const int T = static_cast<int>(a.T - t0 < chunk ? a.T - t0 : chunk);
     const AdRows<E> dyc{dy.p + t0 * dy.ld, dy.ld};
     if ((st = ad_group(t0, T, a.ad, ws.g, s)) != LIPCACHE_OK) return st;
-    if ((st = ad_thin<E>(dyc, N, ws.Bt, N8, T, a.ad, ws.g, ws.u + t0 * r, false, s)) != LIPCACHE_OK) return st;
+    if ((st = ad_thin<E>(dyc, N, ws.Bt, N8, T, a.ad, ws.g, ws.u + t0 * r, ws.peak, false, s)) != LIPCACHE_OK) return st;
     if (need_v &&
-        (st = ad_thin<E>({x.p + t0 * x.ld, x.ld}, K, A.p, A.ld, T, a.ad, ws.g, ws.v + t0 * r, false, s)) != LIPCACHE_OK)
+        (st = ad_thin<E>({x.p + t0 * x.ld, x.ld}, K, A.p, A.ld, T, a.ad, ws.g, ws.v + t0 * r, nullptr, false, s)) != LIPCACHE_OK)
       return st;
     if (dx) {
-      const AdLow low{ws.At, r8, ws.u + t0 * r, a.ad.scale, r, S, K, true, aligned16(ws.u + t0 * r) && r % 4 == 0};
+      const AdLow low{ws.At, r8, ws.u + t0 * r, ws.peak, a.ad.scale, r, S, K, true, aligned16(ws.u + t0 * r) && r % 4 == 0};
       if ((st = ad_main<E, true>(dyc.p, dyc.ld, W.p, W.ld, T, K, N, nullptr, low, ws.g,
                                  static_cast<E*>(dx) + t0 * lddx, lddx, s)) != LIPCACHE_OK)
         return st;
@@ -993,7 +1087,8 @@ lipcache_status ad_backward(const AdArgs& a, const float* v_in, void* dx, int64_
   if (!dA || S == 0) return LIPCACHE_OK;
   if ((a.T == 0 || a.T > chunk) && (st = ad_group(0, a.T, a.ad, ws.g, s)) != LIPCACHE_OK) return st;
   if (const int64_t tiles = ad_tiles(a.T, S); tiles > 0) {
-    ad_factor_kernel<E><<<dim3(static_cast<unsigned>(tiles), 2), 256, 0, s>>>(ws.u, need_v ? ws.v : v_in, r, S, ws.g, ws.fu, ws.fv);
+    ad_factor_kernel<E><<<dim3(static_cast<unsigned>(tiles), 2), 256, 0, s>>>(ws.u, need_v ? ws.v : v_in, r, S, ws.g, ws.fu, ws.fv,
+                                                                                           ws.exps_u, ws.exps_v);
     LC_LAUNCHED();
   }
   const int splits = ad_splits(a.T, K, N, S);
@@ -1002,7 +1097,7 @@ lipcache_status ad_backward(const AdArgs& a, const float* v_in, void* dx, int64_
   const unsigned blocks = static_cast<unsigned>((ga.blocks + gb.blocks) * splits) * S;
   auto grad = [&](auto ranks) {
     ad_grad_kernel<E, decltype(ranks)::value><<<blocks, 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g.order, ws.g.start,
-                                                                    ws.g.tile_start, ws.g.tile_row, ws.g.zeros);
+                                                                    ws.g.tile_start, ws.g.tile_row, ws.exps_u, ws.exps_v, ws.g.zeros);
   };
   if (r <= 32) grad(std::integral_constant<int, 1>{});
   else if (r <= 64) grad(std::integral_constant<int, 2>{});

@@ -250,6 +250,31 @@ def test_values_that_are_not_finite_stay_in_their_request(dtype, T, lengths):
         assert torch.equal(g.dA[a], gclean.dA[a]) and torch.equal(g.dB[a], gclean.dB[a]), a
 
 
+@pytest.mark.parametrize("T", [12, 190, 700])
+@pytest.mark.parametrize("r", [8, 40])
+def test_float16_factors_outside_its_range(T, r):
+    """A_a x past 65504 and B_a^T dy below 2^-14 keep their digits; rows 2^10 apart in size share a tile."""
+    b = make(18, T, 256, 200, 3, r, 7, "f16")
+    b["x"].mul_(1e4 / 256)
+    b["x"][::3] *= 256
+    b["A"].mul_(16)
+    b["B"].mul_(1e-3)
+    assert float(b["x"].abs().max()) < 65504
+    out = check_forward(b, "f16", f"large A x, T {T}")
+    if T > 100:
+        assert float(out.v.abs().max()) > 65504
+    b = make(19, T, 256, 200, 3, r, 7, "f16")
+    b["B"].mul_(1e-2)
+    b["x"].mul_(16)
+    b["dy"].mul_(2e-5)
+    b["dy"][::5] *= 64
+    v = check_forward(b, "f16", f"before small gradients, T {T}").v
+    check_backward(b, "f16", f"small gradients, T {T}", v)
+    b["dy"].zero_()
+    b["dy"][T // 2] = 1e-6
+    check_backward(b, "f16", f"one row of gradients, T {T}")
+
+
 @pytest.mark.parametrize("T", [12, 190])
 def test_gradients_against_differences(T):
     """L = sum(dy * y) is linear in x, in A and in B apart, so a wide difference quotient is exact but for rounding."""
