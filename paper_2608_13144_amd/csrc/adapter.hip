@@ -35,6 +35,7 @@ struct AdGroups {
   int32_t* start;      // [S + 2] first place of each pair, of none, and T
   int32_t* tile_pair;  // [tiles]
   int32_t* tile_row;   // [tiles] first sorted place
+  int32_t* tile_rows;  // [tiles] rows
   int32_t* tile_start; // [S + 1] first tile of each pair, and the number of tiles
   uint32_t* zeros;     // 16 bytes of zero
 };
@@ -42,6 +43,7 @@ struct AdGroups {
 __host__ __device__ inline int64_t ad_tiles(int64_t T, int S) { return T / kThinRows + (S < T ? S : T); }
 
 constexpr int kGroupThreads = 1024;
+constexpr int kGroupRound = 2 * kGroupThreads;  // requests that the workgroup takes at a time
 
 // Inclusive sums over the workgroup's threads, in LDS (`sums`, one word a
 // thread; `waves`, one a wave).  Ends with a barrier.
@@ -55,45 +57,62 @@ __device__ __forceinline__ void group_scan(int v, int32_t* sums, int32_t* waves)
   if (lane == kWave - 1) waves[wave] = v;
   __syncthreads();
   int before = 0;
-  for (int w = 0; w < wave; ++w) before += waves[w];
+#pragma unroll
+  for (int w = 0; w < kGroupThreads / kWave; ++w) before += w < wave ? waves[w] : 0;
   sums[tid] = before + v;
   __syncthreads();
 }
 
 // Workgroup s places the rows of pair s.  Every workgroup counts all pairs'
 // rows (integer sums in LDS: any order gives the same), then walks the
-// requests in order, 1024 at a time.  Request -1 is the rows before the first
-// offset, request R those after the last.  Offsets that decrease place rows
+// requests in order, 2048 at a time, two neighbours a thread (whose loads go
+// out together).  Request -1 is the rows before the first offset, request R
+// those after the last.  Offsets that decrease place rows
 // wrongly or not at all; every index is checked, and places left over hold row
 // 0 without a pair, so whatever they are no access leaves the arrays.  Bound
-// by the latency of three dependent steps of loads: 4 us for 1024 requests.
+// by latency (one round of loads, then scans and a search in LDS): 6 us for 64 pairs and 1024 requests, 9 us for four
+// pairs of 2048 rows each.
 __global__ __launch_bounds__(kGroupThreads) void ad_group_kernel(int64_t t0, int T, const int32_t* __restrict__ offsets,
                                                                  const int32_t* __restrict__ adapter, int R, int S,
                                                                  AdGroups g) {
   extern __shared__ int32_t count[];        // [S + 1] rows of each pair, then scratch
   int32_t* sums = count + S + 1;            // [kGroupThreads]
-  int32_t* first = sums + kGroupThreads;    // [kGroupThreads]
-  int32_t* waves = first + kGroupThreads;   // [kGroupThreads / kWave]
+  int32_t* first = sums + kGroupThreads;    // [kGroupRound]
+  int32_t* some = first + kGroupRound;      // [kGroupThreads] rows of a thread's first request
+  int32_t* waves = some + kGroupThreads;    // [kGroupThreads / kWave]
   __shared__ unsigned long long base_rows, base_tiles;
   const int tid = static_cast<int>(threadIdx.x), s = static_cast<int>(blockIdx.x);
-  auto request = [&](int i, int& lo, int& key) {  // i in [-1, R]; returns its rows
-    const int64_t a = i < 0 ? t0 : R > 0 ? offsets[i] : t0, b = i < 0 ? (R > 0 ? offsets[0] : t0) : i < R ? offsets[i + 1] : t0 + T;
-    const int p = i >= 0 && i < R ? adapter[i] : -1;
+  // rows of request i >= -1 (none past R).  Three loads that wait for nothing, least of all each other.
+  auto request = [&](int i, int& lo, int& key) {
+    int64_t a = t0, b = t0 + T;
+    int p = -1;
+    if (R > 0) {
+      const int at = i < 0 ? 0 : i < R ? i : R, next = i + 1 < R ? i + 1 : R;
+      const int32_t begin = offsets[at], end = offsets[next], named = adapter[at < R ? at : R - 1];
+      if (i >= 0) a = begin;
+      if (i < R) b = end;
+      if (i >= 0 && i < R) p = named;
+    } else if (i < 0) {
+      b = t0;
+    }
     const int64_t l = a < t0 ? t0 : a, h = b > t0 + T ? t0 + T : b;
     lo = static_cast<int>(l - t0);
     key = p >= 0 && p < S ? p : S;
-    return h > l ? static_cast<int>(h - l) : 0;
+    return i <= R && h > l ? static_cast<int>(h - l) : 0;
   };
-  int lo0 = 0, key0 = S, n0 = 0;  // this thread's request among the first 1024
-  if (tid - 1 <= R) n0 = request(tid - 1, lo0, key0);
+  int lo[2], key[2], n[2];  // this thread's requests among the first 2048
+#pragma unroll
+  for (int e = 0; e < 2; ++e) n[e] = request(2 * tid + e - 1, lo[e], key[e]);
   for (int i = tid; i <= S; i += kGroupThreads) count[i] = 0;
   if (tid == 0) base_rows = base_tiles = 0;
   __syncthreads();
-  if (n0 > 0) atomicAdd(&count[key0], n0);
-  for (int i = tid - 1 + kGroupThreads; i <= R; i += kGroupThreads) {
-    int lo, key;
-    const int n = request(i, lo, key);
-    if (n > 0) atomicAdd(&count[key], n);
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    if (n[e] > 0) atomicAdd(&count[key[e]], n[e]);
+  for (int i = tid - 1 + kGroupRound; i <= R; i += kGroupThreads) {
+    int l, k;
+    const int rows = request(i, l, k);
+    if (rows > 0) atomicAdd(&count[k], rows);
   }
   __syncthreads();
   unsigned long long rows = 0, tiles = 0;
@@ -103,9 +122,16 @@ __global__ __launch_bounds__(kGroupThreads) void ad_group_kernel(int64_t t0, int
     rows += n;
     tiles += ((n < all ? n : all) + kThinRows - 1) / kThinRows;  // as many as the pair writes below
   }
-  if (rows > 0) {
-    atomicAdd(&base_rows, rows);
-    atomicAdd(&base_tiles, tiles);
+  if (uniform(tid / kWave) * kWave < s) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+      rows += __shfl_xor(rows, o, kWave);
+      tiles += __shfl_xor(tiles, o, kWave);
+    }
+    if (lane_id() == 0 && rows > 0) {
+      atomicAdd(&base_rows, rows);
+      atomicAdd(&base_tiles, tiles);
+    }
   }
   __syncthreads();
   const uint64_t place0 = base_rows;
@@ -122,27 +148,32 @@ __global__ __launch_bounds__(kGroupThreads) void ad_group_kernel(int64_t t0, int
       if (at < last) {
         g.tile_pair[at] = s;
         g.tile_row[at] = static_cast<int32_t>(row < all ? row : all);
+        const uint64_t end = place0 + mine < all ? place0 + mine : all, left = row < end ? end - row : 0;
+        g.tile_rows[at] = static_cast<int32_t>(left < kThinRows ? left : kThinRows);
       }
     }
   }
   uint64_t place = place0;
-  for (int i0 = -1; i0 <= R && mine > 0 && place < all; i0 += kGroupThreads) {
+  for (int i0 = -1; i0 <= R && mine > 0 && place < all; i0 += kGroupRound) {
     if (i0 >= 0) {
-      n0 = 0;
-      if (i0 + tid <= R) n0 = request(i0 + tid, lo0, key0);
-      __syncthreads();  // the last round's readers of sums and first are done
+#pragma unroll
+      for (int e = 0; e < 2; ++e) n[e] = request(i0 + 2 * tid + e, lo[e], key[e]);
+      __syncthreads();  // the last round's readers are done
     }
-    first[tid] = lo0;
-    group_scan(key0 == s ? n0 : 0, sums, waves);
+    const int n0 = key[0] == s ? n[0] : 0, n1 = key[1] == s ? n[1] : 0;
+    first[2 * tid] = lo[0];
+    first[2 * tid + 1] = lo[1];
+    some[tid] = n0;
+    group_scan(n0 + n1, sums, waves);
     const int total = sums[kGroupThreads - 1];
     for (int p = tid; p < total && place + p < all; p += kGroupThreads) {
-      int a = 0, b = kGroupThreads - 1;  // the request that holds the p-th row: the first whose sum passes p
+      int a = 0, b = kGroupThreads - 1;  // the thread whose requests hold the p-th row: the first whose sum passes p
       while (a < b) {
         const int mid = (a + b) >> 1;
         if (sums[mid] > p) b = mid; else a = mid + 1;
       }
-      const int before = a > 0 ? sums[a - 1] : 0;
-      const uint32_t row = static_cast<uint32_t>(first[a] + p - before);
+      const int in = p - (a > 0 ? sums[a - 1] : 0), n_a = some[a];
+      const uint32_t row = static_cast<uint32_t>(in < n_a ? first[2 * a] + in : first[2 * a + 1] + in - n_a);
       g.order[place + p] = row < all ? static_cast<int32_t>(row) : 0;
       g.pair[place + p] = s;
     }
@@ -291,10 +322,9 @@ __global__ __launch_bounds__(S::kThreads) void ad_thin_kernel(const typename S::
       out[static_cast<int64_t>(g.order[first + i / r]) * r + i % r] = 0.0f;
     return;
   }
-  if (static_cast<uint32_t>(t) >= static_cast<uint32_t>(g.tile_start[pairs])) return;
-  const int a = g.tile_pair[t], row0 = g.tile_row[t];
-  const int end = g.start[a + 1] - row0, rows = end < kThinRows ? end : kThinRows;
-  if (rows <= 0) return;
+  // together: past the last tile they are not used
+  const int last = g.tile_start[pairs], a = g.tile_pair[t], row0 = g.tile_row[t], rows = g.tile_rows[t];
+  if (static_cast<uint32_t>(t) >= static_cast<uint32_t>(last) || rows <= 0) return;
   Side p{}, q{};
   p.p = x;
   p.ld = ldx * sizeof(E);
@@ -363,7 +393,7 @@ struct AdLow {
 template <class S>
 struct AdTileRows {
   int pair[S::TM], row[S::TM];
-  float peak[S::TM];
+  float peak[S::TM], scale[S::TM];
   __device__ __forceinline__ void load(const AdGroups& g, const AdLow& low, int i0, int rows) {
     const int wave = uniform(static_cast<int>(threadIdx.x) / kWave);
     const int wm = wave % (S::WM * S::WN) / S::WN;
@@ -373,6 +403,7 @@ struct AdTileRows {
       const bool in = i < rows;
       pair[tm] = in ? g.pair[i0 + i] : low.S;
       row[tm] = g.order[i0 + (in ? i : 0)];
+      scale[tm] = pair[tm] < low.S ? low.scale[pair[tm]] : 0.0f;
       if constexpr (kScaledFactors<typename S::E>) peak[tm] = pair[tm] < low.S ? low.peak[row[tm]] : 0.0f;
     }
   }
@@ -398,7 +429,7 @@ __device__ __forceinline__ void add_low_rank(const AdLow& low, const AdTileRows<
       const bool mine = rows.pair[tm] == a;
       const uint32_t mask = static_cast<uint32_t>(__ballot(mine));
       todo &= ~mask;
-      const float scale = low.scale[a];
+      const float scale = rows.scale[tm];  // of this lane's row: its own where `mine`
       int up = 0;
       if constexpr (kScaledFactors<E>) {
         float top = mine ? finite_size(scale * rows.peak[tm]) : 0.0f;
@@ -469,6 +500,7 @@ __global__ __launch_bounds__(S::kThreads) void ad_main_kernel(const typename S::
   rows.load(g, low, i0, p.rows);
   f32x16 acc[S::TM][S::TN] = {};
   tile_products<S>(p, q, K, lds, acc);
+  if (S::WK > 1 && static_cast<int>(threadIdx.x) / kWave >= S::WM * S::WN) return;  // their sums are added
   add_low_rank<S, E>(low, rows, j0, acc);
   tile_store<S>(acc, [&](int i, int j, const f32x16& v) {
     j += j0;
@@ -495,6 +527,10 @@ lipcache_status ad_main(const void* P, int64_t ldp, const void* Q, int64_t ldq, 
     return hipGetLastError() == hipSuccess ? LIPCACHE_OK : LIPCACHE_EHIP;
   };
   const int64_t t128 = ceil_div(T, 128) * ceil_div(width, 128), t256 = ceil_div(T, 256) * ceil_div(width, 256);
+  // float32 products of one wave's 32 x 32 tile take 3.4 us at K = 256: two waves share them where workgroups are few
+  // (1024 x 256 -> 200: 13.0 -> 10.9 us; with 256 tiles of 64 x 64 the larger tile is ahead, 12.4 to 14.0)
+  if constexpr (sizeof(E) == 4)
+    if (ceil_div(T, 64) * ceil_div(width, 64) <= 128) return run(TileShape<E, 32, 64, 1, 2, 2, 4, 1, false, kCol>{});
   if (t128 < 128) return run(TileShape<E, 64, 64, 2, 2, 1, 3, 1, false, kCol>{});
   if constexpr (sizeof(E) == 2)
     if (5 * t256 >= 4 * 256 * ceil_div(t256, 256)) return run(TileShape<E, 256, 256, 2, 4, 1, 2, 1, false, kCol>{});
@@ -669,11 +705,10 @@ __global__ __launch_bounds__(256) void ad_factor_kernel(const float* __restrict_
   __shared__ float tile[32][kAdMaxRank + 1];
   __shared__ float wave_top[256 / kWave];
   const int t = static_cast<int>(blockIdx.x);
-  if (static_cast<uint32_t>(t) >= static_cast<uint32_t>(g.tile_start[pairs])) return;
+  const int last = g.tile_start[pairs], row0 = g.tile_row[t], rows = g.tile_rows[t];
+  if (static_cast<uint32_t>(t) >= static_cast<uint32_t>(last)) return;
   const float* f = blockIdx.y ? v : u;
   E* to = (blockIdx.y ? to_v : to_u) + static_cast<int64_t>(t) * r * (128 / sizeof(E));
-  const int row0 = g.tile_row[t];
-  const int rows = g.start[g.tile_pair[t] + 1] - row0;
   const int x = static_cast<int>(threadIdx.x) & 31, y = static_cast<int>(threadIdx.x) >> 5;
   float top = 0.0f;
 #pragma unroll
@@ -729,7 +764,6 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
                                                       const float* __restrict__ scale, const int32_t* __restrict__ order,
                                                       const int32_t* __restrict__ start,
                                                       const int32_t* __restrict__ tile_start,
-                                                      const int32_t* __restrict__ tile_row,
                                                       const int32_t* __restrict__ exps_a,
                                                       const int32_t* __restrict__ exps_b, const void* zeros) {
   constexpr bool kF32 = std::is_same_v<E, float>;
@@ -763,15 +797,32 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(uniform(static_cast<int>(to)))
                  : "memory", "m0");
   };
-  auto copy_tile = [&](int n, uint32_t to) {  // tile n of the share; zeros past the last
+  // a pair's tiles are neighbours, so the places of its rows are known; the rows there come a step ahead of the copies
+  // (offsets that decrease may put a tile past the pair's end: it reads as empty)
+  const int64_t place0 = uniform(start[a]) + static_cast<int64_t>(share) * each * kThinRows;
+  auto place = [&](int n) {
+    const int64_t at = place0 + static_cast<int64_t>(n) * kThinRows;
+    return n < tiles && at < end ? static_cast<int>(at) : end;
+  };
+  typedef int32_t rows_t __attribute__((ext_vector_type(kRowsCopy), aligned(4)));
+  rows_t ahead[kSub][kZCopies];
+  auto rows_of_step = [&](int step) {
+#pragma unroll
+    for (int u = 0; u < kSub; ++u) {
+      const int n = step * kSub + u;
+#pragma unroll
+      for (int c = 0; c < kZCopies; ++c)
+        ahead[u][c] = *reinterpret_cast<const rows_t*>(order + uniform(place(n)) + (wave * kZCopies + c) * kRowsCopy);
+    }
+  };
+  auto copy_tile = [&](int n, const rows_t (&row_of)[kZCopies], uint32_t to) {  // tile n of the share; zeros past the last
     const bool some = n < tiles;
     const int t = uniform(tile0 + (some ? n : 0));
-    const int row0 = some ? uniform(tile_row[t]) : end;
+    const int row0 = place(n);
 #pragma unroll
     for (int c = 0; c < kZCopies; ++c) {
       const int first = (wave * kZCopies + c) * kRowsCopy;
-      typedef int32_t rows_t __attribute__((ext_vector_type(kRowsCopy), aligned(4)));
-      const rows_t rows = *reinterpret_cast<const rows_t*>(order + (some ? row0 : 0) + first);
+      const rows_t rows = row_of[c];
       const int mine = lane / TileZ::kSlots;
       int row = rows[0];
 #pragma unroll
@@ -779,7 +830,7 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
       const int chunk = (lane % TileZ::kSlots) ^ TileZ::swz(first + mine);
       const int col = c0 + chunk * kV;
       const void* p = zeros;  // rows past the pair's and columns past the matrix
-      if (row0 + first + mine < end && col < d.width) p = d.z + row * d.ldz + col;
+      if (first + mine < end - row0 && col < d.width) p = d.z + row * d.ldz + col;
       copy(p, to + (wave * kZCopies + c) * 1024);
     }
     const char* f = reinterpret_cast<const char*>(d.f) + static_cast<int64_t>(t) * r * 128;
@@ -802,8 +853,11 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
   constexpr int kCopies = kSub * (kZCopies + kFCopies);
   auto copy_step = [&](int step) {
 #pragma unroll
-    for (int u = 0; u < kSub; ++u) copy_tile(step * kSub + u, base + (step % kStages * kSub + u) * kTile);
+    for (int u = 0; u < kSub; ++u)
+      copy_tile(step * kSub + u, ahead[u], base + (step % kStages * kSub + u) * kTile);
+    rows_of_step(step + 1);
   };
+  rows_of_step(0);
   for (int step = 0; step < kStages - 1 && step < steps; ++step) copy_step(step);
   int up = 0;  // the sums are times 2^up
   for (int step = 0; step < steps; ++step) {
@@ -901,13 +955,15 @@ AdGroups ad_groups(AdSpace& ws, int64_t T, int S) {
   g.start = ws.take<int32_t>(S + 2);
   g.tile_pair = ws.take<int32_t>(ad_tiles(T, S) + 1);
   g.tile_row = ws.take<int32_t>(ad_tiles(T, S) + 1);
+  g.tile_rows = ws.take<int32_t>(ad_tiles(T, S) + 1);
   g.tile_start = ws.take<int32_t>(S + 1);
   g.zeros = ws.take<uint32_t>(4);
   return g;
 }
 
 lipcache_status ad_group(int64_t t0, int64_t T, const lipcache_adapters& ad, const AdGroups& g, hipStream_t s) {
-  ad_group_kernel<<<ad.S + 1, kGroupThreads, (ad.S + 1 + 2 * kGroupThreads + kGroupThreads / kWave) * 4, s>>>(t0, static_cast<int>(T), ad.offsets, ad.adapter, ad.R, ad.S, g);
+  ad_group_kernel<<<ad.S + 1, kGroupThreads, (ad.S + 1 + 2 * kGroupThreads + kGroupRound + kGroupThreads / kWave) * 4, s>>>(
+      t0, static_cast<int>(T), ad.offsets, ad.adapter, ad.R, ad.S, g);
   LC_LAUNCHED();
   return LIPCACHE_OK;
 }
@@ -1009,11 +1065,13 @@ lipcache_status ad_forward(const AdArgs& a, const float* bias, void* y, int64_t 
   return LIPCACHE_OK;
 }
 
-// Shares of a pair's rows, so that few pairs still fill the chip: about 512 workgroups, at least 512 rows each.
+// Shares of a pair's rows, so that few pairs still fill the chip: about 1024 workgroups, at least 128 rows each.
+// 8192 rows of four pairs, 4096 wide: 70 us with 256 workgroups, 42 + 8 (the join) with 512, 30 + 9 with 1024; 4096
+// rows of 16 pairs, 256 wide: 19 us with 64, 12 + 4 with 128.
 inline int ad_splits(int64_t T, int K, int N, int S) {
   const int64_t blocks = (ceil_div(K, 128) + ceil_div(N, 128)) * (S > 0 ? S : 1);
-  int64_t n = 512 / blocks;
-  const int64_t most = T / (S > 0 ? S : 1) / 512;
+  int64_t n = 1024 / blocks;
+  const int64_t most = T / (S > 0 ? S : 1) / 128;
   if (n > most) n = most;
   return n < 1 ? 1 : n > 16 ? 16 : static_cast<int>(n);
 }
@@ -1097,7 +1155,7 @@ lipcache_status ad_backward(const AdArgs& a, const float* v_in, void* dx, int64_
   const unsigned blocks = static_cast<unsigned>((ga.blocks + gb.blocks) * splits) * S;
   auto grad = [&](auto ranks) {
     ad_grad_kernel<E, decltype(ranks)::value><<<blocks, 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g.order, ws.g.start,
-                                                                    ws.g.tile_start, ws.g.tile_row, ws.exps_u, ws.exps_v, ws.g.zeros);
+                                                                    ws.g.tile_start, ws.exps_u, ws.exps_v, ws.g.zeros);
   };
   if (r <= 32) grad(std::integral_constant<int, 1>{});
   else if (r <= 64) grad(std::integral_constant<int, 2>{});
