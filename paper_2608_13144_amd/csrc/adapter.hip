@@ -539,14 +539,23 @@ lipcache_status ad_main(const void* P, int64_t ldp, const void* Q, int64_t ldq, 
 }
 
 // ------------------------------------------------------------- few rows
-// Up to 64 rows (a decode batch) are bound by reading W once.  They are not
-// sorted.  One launch does two independent things: some workgroups multiply all
-// rows with 64 rows of W over a share of the contraction each (so that W comes
-// through all CUs, and x, which every one of them needs, in shares), the others
-// find each row's pair and A_a x, one wave a row and rank.  A second launch adds
-// the shares in order, the bias and scale_a B_a v, a dot product of r an output.
-// 32 MiB of W: 8 us for one row, where one launch after another took 13.
+// A decode batch is bound by reading W once, a batch of single queries of a
+// small head by launches.  Neither is sorted.  One launch does two independent
+// things: some workgroups multiply a tile of rows with 64 rows of W over a share
+// of the contraction each (so that W comes through all CUs, and x in shares), the
+// others find each row's pair and A_a x, a wave a row and one or four ranks.  A
+// second launch adds the shares in order, the bias and scale_a B_a v, a dot
+// product of r an output.  32 MiB of W: 8 us for one row, where one launch after
+// another took 13.
 constexpr int kFewRows = 64;
+
+// Up to 64 rows always; up to 2048 where what every row reads of its pair for itself (sorted rows share it) and the
+// projection's float32 shares stay below 16 MiB each.
+inline bool few_rows(int64_t T, int64_t K, int64_t N, int r, size_t size) {
+  if (T <= kFewRows) return true;
+  constexpr int64_t most = 16 << 20;
+  return T <= 2048 && T * r * K * static_cast<int64_t>(size) <= most && T * N * (r * static_cast<int64_t>(size) + 8) <= most;
+}
 
 // The pair of row t (-1: none), by the whole wave: 64 offsets a round.
 __device__ __forceinline__ int pair_of_row(int64_t t, const int32_t* __restrict__ offsets,
@@ -564,40 +573,49 @@ __device__ __forceinline__ int pair_of_row(int64_t t, const int32_t* __restrict_
   return a >= 0 && a < S ? a : -1;
 }
 
-// A_a x of row t at one rank, by one wave.
-template <class E>
+// A_a x of a row at kRanks ranks, by one wave.
+template <class E, int kRanks>
 __device__ __forceinline__ void few_low(int w, const E* __restrict__ x, int64_t ldx, int K, const E* __restrict__ A,
                                         int64_t lda, const lipcache_adapters& ad, int32_t* __restrict__ pair,
                                         float* __restrict__ v) {
   constexpr int kV = Vec16<E>::kCount;
   typedef typename Vec16<E>::type V;
-  const int t = w / ad.r, rho = w % ad.r, lane = lane_id();
+  const int groups = (ad.r + kRanks - 1) / kRanks;
+  const int t = w / groups, rho = w % groups * kRanks, lane = lane_id();
   const int a = ad.R > 0 ? uniform(pair_of_row(t, ad.offsets, ad.adapter, ad.R, ad.S)) : -1;
-  float sum = 0.0f;
+  float sum[kRanks] = {};
   if (a >= 0) {
     const E* px = x + t * ldx;
-    const E* pa = A + (static_cast<int64_t>(a) * ad.r + rho) * lda;
-#pragma unroll 4
-    for (int k = lane * kV; k < K; k += kWave * kV) {
-      const V vx = *reinterpret_cast<const V*>(px + k), va = *reinterpret_cast<const V*>(pa + k);
+    const E* pa[kRanks];
 #pragma unroll
-      for (int e = 0; e < kV; ++e)
-        sum = fmaf(k + e < K ? static_cast<float>(vx[e]) : 0.0f, k + e < K ? static_cast<float>(va[e]) : 0.0f, sum);
+    for (int i = 0; i < kRanks; ++i)
+      pa[i] = A + (static_cast<int64_t>(a) * ad.r + (rho + i < ad.r ? rho + i : ad.r - 1)) * lda;
+#pragma unroll(kRanks > 1 ? 2 : 4)
+    for (int k = lane * kV; k < K; k += kWave * kV) {
+      const V vx = *reinterpret_cast<const V*>(px + k);
+#pragma unroll
+      for (int i = 0; i < kRanks; ++i) {
+        const V va = *reinterpret_cast<const V*>(pa[i] + k);
+#pragma unroll
+        for (int e = 0; e < kV; ++e)
+          sum[i] = fmaf(k + e < K ? static_cast<float>(vx[e]) : 0.0f, k + e < K ? static_cast<float>(va[e]) : 0.0f, sum[i]);
+      }
     }
   }
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, kWave);
-  if (lane == 0) {
-    v[w] = sum;
-    if (rho == 0) pair[t] = a;
+  for (int i = 0; i < kRanks; ++i) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) sum[i] += __shfl_xor(sum[i], o, kWave);
+    if (lane == 0 && rho + i < ad.r) v[static_cast<int64_t>(t) * ad.r + rho + i] = sum[i];
   }
+  if (lane == 0 && rho == 0) pair[t] = a;
 }
 
-// Workgroups [0, tiles * shares): part[share][t][j] of the projection; the others: v and the pairs.
-template <class S>
+// The first `products` workgroups: part[share][t][j] of the projection; the others: v and the pairs.
+template <class S, int kRanks>
 __global__ __launch_bounds__(S::kThreads) void ad_few_kernel(const typename S::E* __restrict__ x, int64_t ldx, int T,
                                                              const typename S::E* __restrict__ W, int64_t ldw, int K,
-                                                             int N, int tiles, int shares, int each,
+                                                             int N, int row_tiles, int tiles, int products, int each,
                                                              float* __restrict__ part,
                                                              const typename S::E* __restrict__ A, int64_t lda,
                                                              lipcache_adapters ad, int32_t* __restrict__ pair,
@@ -605,23 +623,24 @@ __global__ __launch_bounds__(S::kThreads) void ad_few_kernel(const typename S::E
   typedef typename S::E E;
   __shared__ __align__(16) char lds[S::kLds];
   const int block = static_cast<int>(blockIdx.x);
-  if (block >= tiles * shares) {
-    const int w = uniform((block - tiles * shares) * S::kWaves + static_cast<int>(threadIdx.x) / kWave);
-    if (w < T * ad.r) few_low<E>(w, x, ldx, K, A, lda, ad, pair, v);
+  if (block >= products) {
+    const int w = uniform((block - products) * S::kWaves + static_cast<int>(threadIdx.x) / kWave);
+    if (w < T * ((ad.r + kRanks - 1) / kRanks)) few_low<E, kRanks>(w, x, ldx, K, A, lda, ad, pair, v);
     return;
   }
-  const int share = block / tiles, j0 = block % tiles * S::BN, k0 = share * each;
-  const int count = K - k0 < each ? K - k0 : each;
+  const int share = block / tiles, tile = block % tiles, i0 = tile % row_tiles * S::BM, j0 = tile / row_tiles * S::BN;
+  const int k0 = share * each, count = K - k0 < each ? K - k0 : each;
   Side p{}, q{};
-  p.p = x + k0;
+  p.p = x + i0 * ldx + k0;
   p.ld = ldx * sizeof(E);
-  p.rows = T;
+  p.rows = T - i0 < S::BM ? T - i0 : S::BM;
   q.p = W + j0 * ldw + k0;
   q.ld = ldw * sizeof(E);
   q.rows = N - j0 < S::BN ? N - j0 : S::BN;
   f32x16 acc[S::TM][S::TN] = {};
   tile_products<S>(p, q, count, lds, acc);
   tile_store<S>(acc, [&](int i, int j, const f32x16& u) {
+    i += i0;
     j += j0;
     if (j >= N) return;
 #pragma unroll
@@ -637,15 +656,16 @@ __global__ __launch_bounds__(256) void ad_few_join_kernel(int T, int N, int shar
                                                           int64_t ldy) {
   constexpr int kV = Vec16<E>::kCount;
   typedef typename Vec16<E>::type V;
-  const int n = static_cast<int>(blockIdx.x) * 256 + static_cast<int>(threadIdx.x), t = static_cast<int>(blockIdx.y);
-  if (n >= N) return;
+  const uint32_t i = blockIdx.x * 256 + threadIdx.x, size = static_cast<uint32_t>(T) * static_cast<uint32_t>(N);
+  if (i >= size) return;
+  const int t = static_cast<int>(i / static_cast<uint32_t>(N)), n = static_cast<int>(i % static_cast<uint32_t>(N));
   const int a = pair[t];
   float sum = 0.0f;
-  for (int k = 0; k < shares; ++k) sum += part[(static_cast<int64_t>(k) * T + t) * N + n];
+  for (int k = 0; k < shares; ++k) sum += part[static_cast<int64_t>(k) * size + i];
   if (bias) sum += bias[n];
   if (a >= 0) {
     const E* f = static_cast<const E*>(low.F) + (static_cast<int64_t>(a) * N + n) * low.ldf;
-    const float* v = low.v + t * low.r;
+    const float* v = low.v + static_cast<int64_t>(t) * low.r;
     float dot = 0.0f;
 #pragma unroll 2
     for (int rho = 0; rho < low.r; rho += kV) {
@@ -659,10 +679,13 @@ __global__ __launch_bounds__(256) void ad_few_join_kernel(int T, int N, int shar
   y[t * ldy + n] = static_cast<E>(sum);
 }
 
+// Rows of x that a workgroup of the projection takes.  float32 products are slow enough that two waves share them.
+inline int few_tile_rows(int64_t T, size_t size) { return T <= 32 || size == 4 && T > kFewRows ? 32 : 64; }
+
 // Shares of the contraction: about 256 workgroups, at least 512 bytes of a row each.
-inline int few_shares(int K, int N, size_t size) {
-  const int64_t tiles = ceil_div(N, 64), most = ceil_div(K * static_cast<int64_t>(size), 512);
-  int64_t n = 256 / tiles;
+inline int few_shares(int64_t T, int K, int N, size_t size) {
+  const int64_t tiles = ceil_div(N, 64) * ceil_div(T, few_tile_rows(T, size)), most = ceil_div(K * static_cast<int64_t>(size), 512);
+  int64_t n = tiles > 0 ? 256 / tiles : 1;  // no rows: none
   if (n > most) n = most;
   return n < 1 ? 1 : n > 16 ? 16 : static_cast<int>(n);
 }
@@ -671,20 +694,27 @@ template <class E>
 lipcache_status ad_few(const AdRows<E>& x, int T, const AdRows<E>& W, int K, int N, const float* bias,
                        const AdRows<E>& A, const lipcache_adapters& ad, const AdLow& low, int32_t* pair, float* part,
                        float* v, E* y, int64_t ldy, hipStream_t s) {
-  const int tiles = static_cast<int>(ceil_div(N, 64)), wanted = few_shares(K, N, sizeof(E));
+  const int rows = few_tile_rows(T, sizeof(E)), row_tiles = static_cast<int>(ceil_div(T, rows));
+  const int tiles = static_cast<int>(ceil_div(N, 64)) * row_tiles, wanted = few_shares(T, K, N, sizeof(E));
   const int each = static_cast<int>(round_up(ceil_div(K, wanted), 128 / sizeof(E)));
   const int shares = static_cast<int>(ceil_div(K, each));
-  const unsigned blocks = static_cast<unsigned>(tiles * shares + ceil_div(T * ad.r, 4));
-  auto run = [&](auto shape) {
+  auto run = [&](auto shape, auto ranks) {
     typedef decltype(shape) S;
+    constexpr int kRanks = decltype(ranks)::value;
     static_assert(S::kWaves == 4, "four rows and ranks a workgroup");
-    ad_few_kernel<S><<<blocks, S::kThreads, 0, s>>>(x.p, x.ld, T, W.p, W.ld, K, N, tiles, shares, each, part, A.p, A.ld,
-                                                    ad, pair, v);
+    const unsigned blocks = static_cast<unsigned>(tiles * shares + ceil_div(T * ceil_div(ad.r, kRanks), 4));
+    ad_few_kernel<S, kRanks><<<blocks, S::kThreads, 0, s>>>(x.p, x.ld, T, W.p, W.ld, K, N, row_tiles, tiles,
+                                                            tiles * shares, each, part, A.p, A.ld, ad, pair, v);
   };
-  if (T <= 32) run(TileShape<E, 32, 64, 1, 2, 2, 4, 1, false, false>{});
-  else run(TileShape<E, 64, 64, 2, 2, 1, 3, 1, false, false>{});
+  typedef TileShape<E, 32, 64, 1, 2, 2, 4, 1, false, false> Low;
+  typedef TileShape<E, 64, 64, 2, 2, 1, 3, 1, false, false> High;
+  // one rank a wave where the batch is a few rows (latency), four where its rows fill the chip
+  if (T <= 32) run(Low{}, std::integral_constant<int, 1>{});
+  else if (T <= kFewRows) run(High{}, std::integral_constant<int, 1>{});
+  else if constexpr (sizeof(E) == 4) run(Low{}, std::integral_constant<int, 4>{});
+  else run(High{}, std::integral_constant<int, 4>{});
   LC_LAUNCHED();
-  ad_few_join_kernel<E><<<dim3(static_cast<unsigned>(ceil_div(N, 256)), static_cast<unsigned>(T)), 256, 0, s>>>(
+  ad_few_join_kernel<E><<<static_cast<unsigned>(ceil_div(static_cast<int64_t>(T) * N, 256)), 256, 0, s>>>(
       T, N, shares, part, bias, low, pair, y, ldy);
   LC_LAUNCHED();
   return LIPCACHE_OK;
@@ -1027,7 +1057,7 @@ struct AdForwardSpace {
     g = ad_groups(ws, T, S);
     v = ws.take<float>(static_cast<size_t>(T) * r);
     peak = ws.take<float>(T);
-    part = ws.take<float>(T <= kFewRows ? static_cast<size_t>(T) * N * few_shares(K, N, sizeof(E)) : 0);
+    part = ws.take<float>(few_rows(T, K, N, r, sizeof(E)) ? static_cast<size_t>(T) * N * few_shares(T, K, N, sizeof(E)) : 0);
     x = ws.take<E>(static_cast<size_t>(T) * round_up(K, kV));
     W = ws.take<E>(static_cast<size_t>(N) * round_up(K, kV));
     A = ws.take<E>(static_cast<size_t>(S) * r * round_up(K, kV));
@@ -1048,7 +1078,7 @@ lipcache_status ad_forward(const AdArgs& a, const float* bias, void* y, int64_t 
   if (!keep) v = ws.v;
   const AdLow low{a.ad.B, a.ad.r, v, ws.peak, a.ad.scale, a.ad.r, a.ad.S, a.N, aligned16(a.ad.B) && a.ad.r % kV == 0,
                   aligned16(v) && a.ad.r % 4 == 0};
-  if (a.T <= kFewRows)
+  if (few_rows(a.T, a.K, a.N, a.ad.r, sizeof(E)))
     return ad_few<E>(x, static_cast<int>(a.T), W, a.K, a.N, bias, A, a.ad, low, ws.g.pair, ws.part, v, static_cast<E*>(y), ldy, s);
   const int64_t chunk = ad_chunk(x.ld, sizeof(E));
   for (int64_t t0 = 0; t0 < a.T; t0 += chunk) {

@@ -359,3 +359,28 @@ def test_binding_refuses():
     with pytest.raises(ValueError):
         api.adapter_backward(b["dy"], *[b[k] for k in ("x", "W", "A", "B", "scale", "offsets", "adapter")],
                              v=torch.zeros(20, 4, dtype=torch.bfloat16, device=DEV))
+
+
+# Past 2048 rows the forward pass sorts them by pair; up to there (small products) each row finds its pair by itself.
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_many_rows_and_values_that_are_not_finite(dtype):
+    test_values_that_are_not_finite_stay_in_their_request(dtype, 2100, "ragged")
+
+
+def test_many_rows_and_strange_offsets():
+    test_offsets_that_reach_past_the_rows(2100)
+    test_no_pairs_no_requests_no_bias(2100)
+
+
+@pytest.mark.parametrize("r", [8, 40])
+def test_many_rows_and_float16_factors(r):
+    test_float16_factors_outside_its_range(2100, r)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("size", [(2048, 64, 40, 9, 4, 2048), (2049, 64, 40, 9, 4, 300), (1500, 257, 131, 40, 8, 1500),
+                                  (333, 1000, 77, 5, 30, 333), (2000, 40, 11, 3, 1, 5)], ids=lambda s: "x".join(map(str, s)))
+def test_single_queries_and_their_limit(size, dtype):
+    T, K, N, S, r, R_ = size
+    b = make(sum(size), T, K, N, S, r, R_, dtype, "one" if R_ == T else "ragged", pad=8)
+    check_forward(b, dtype, f"single queries {size} {dtype}")
