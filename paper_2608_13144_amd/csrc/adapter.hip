@@ -242,8 +242,8 @@ __device__ __forceinline__ float two_to(float v, int e) {
 }
 
 // ------------------------------------------------------- copies and transposes
-// Rows moved into the workspace: padded with zeros to a width of whole 16-byte
-// vectors, as they are or transposed.
+// Matrices moved into the workspace: padded with zeros to a width of whole
+// 16-byte vectors, as they are or transposed; all of a call in one launch.
 struct AdCopy {
   const void* from;
   void* to;
@@ -252,54 +252,74 @@ struct AdCopy {
   int rows, width;            // of the source
   int to_rows, to_width;      // written, zeros outside the source
   int stack;
+  int transpose;
+};
+constexpr int kAdCopies = 6;
+struct AdCopies {
+  AdCopy c[kAdCopies];
+  int64_t end[kAdCopies];  // first workgroup past each (none of a copy that is not there)
 };
 
-// The first `blocks` workgroups copy c, the others d.
-template <typename T, bool kTranspose>
-__global__ __launch_bounds__(256) void ad_copy_kernel(AdCopy c, AdCopy d, int blocks) {
+template <typename T>
+__global__ __launch_bounds__(256) void ad_copy_kernel(AdCopies all) {
   __shared__ T tile[32][33];
   const int x = static_cast<int>(threadIdx.x) & 31, y = static_cast<int>(threadIdx.x) >> 5;
-  int block = static_cast<int>(blockIdx.x);
-  if (block >= blocks) {
-    block -= blocks;
-    c = d;
-  }
+  int64_t block = blockIdx.x;
+  AdCopy c = all.c[0];
+#pragma unroll
+  for (int i = 1; i < kAdCopies; ++i)
+    if (static_cast<int64_t>(blockIdx.x) >= all.end[i - 1]) {
+      c = all.c[i];
+      block = blockIdx.x - all.end[i - 1];
+    }
   // tiles of the result
   const int64_t tiles_w = ceil_div(c.to_width, 32), tiles = tiles_w * ceil_div(c.to_rows, 32);
   const int64_t z = block / tiles, t = block % tiles;
-  const int i0 = static_cast<int>(t / tiles_w) * 32, j0 = static_cast<int>(t % tiles_w) * 32;
+  const int64_t i0 = t / tiles_w * 32;
+  const int j0 = static_cast<int>(t % tiles_w) * 32;
   const T* from = static_cast<const T*>(c.from) + z * c.from_next;
   T* to = static_cast<T*>(c.to) + z * c.to_next;
-  if constexpr (kTranspose) {
+  if (c.transpose) {
 #pragma unroll
     for (int k = y; k < 32; k += 8) {
-      const int row = j0 + k, col = i0 + x;  // of the source
+      const int row = j0 + k;  // of the source
+      const int64_t col = i0 + x;
       tile[k][x] = row < c.rows && col < c.width ? from[row * c.ld_from + col] : static_cast<T>(0.0f);
     }
     __syncthreads();
   }
 #pragma unroll
   for (int k = y; k < 32; k += 8) {
-    const int row = i0 + k, col = j0 + x;
+    const int64_t row = i0 + k;
+    const int col = j0 + x;
     if (row >= c.to_rows || col >= c.to_width) continue;
     T v;
-    if constexpr (kTranspose) v = tile[x][k];
+    if (c.transpose) v = tile[x][k];
     else v = row < c.rows && col < c.width ? from[row * c.ld_from + col] : static_cast<T>(0.0f);
     to[row * c.ld_to + col] = v;
   }
 }
 
-inline int64_t ad_copy_blocks(const AdCopy& c) { return ceil_div(c.to_width, 32) * ceil_div(c.to_rows, 32) * c.stack; }
-
-template <typename T, bool kTranspose>
-lipcache_status ad_copy(const AdCopy& c, const AdCopy& d, hipStream_t s) {
-  const int64_t blocks = ad_copy_blocks(c), more = ad_copy_blocks(d);
-  if (blocks + more <= 0) return LIPCACHE_OK;
-  if (blocks + more > 0x7fffffff) return LIPCACHE_EUNSUPPORTED;
-  ad_copy_kernel<T, kTranspose><<<static_cast<unsigned>(blocks + more), 256, 0, s>>>(c, d, static_cast<int>(blocks));
-  LC_LAUNCHED();
-  return LIPCACHE_OK;
-}
+struct AdCopyList {
+  AdCopies all{};
+  int count = 0;
+  int64_t blocks = 0;
+  void add(const AdCopy& c) {
+    const int64_t n = ceil_div(c.to_width, 32) * ceil_div(c.to_rows, 32) * c.stack;
+    if (n <= 0) return;
+    blocks += n;
+    all.c[count] = c;
+    for (int i = count++; i < kAdCopies; ++i) all.end[i] = blocks;
+  }
+  template <typename T>
+  lipcache_status launch(hipStream_t s) const {
+    if (blocks <= 0) return LIPCACHE_OK;
+    if (blocks > 0x7fffffff) return LIPCACHE_EUNSUPPORTED;
+    ad_copy_kernel<T><<<static_cast<unsigned>(blocks), 256, 0, s>>>(all);
+    LC_LAUNCHED();
+    return LIPCACHE_OK;
+  }
+};
 
 // ------------------------------------------------------------ thin products
 // out[row][rho] = F_a[rho] . x[row] for the up to 32 sorted rows of one tile
@@ -549,12 +569,15 @@ lipcache_status ad_main(const void* P, int64_t ldp, const void* Q, int64_t ldq, 
 // another took 13.
 constexpr int kFewRows = 64;
 
-// Up to 64 rows always; up to 2048 where what every row reads of its pair for itself (sorted rows share it) and the
-// projection's float32 shares stay below 16 MiB each.
+// Up to 64 rows always; up to 8192 where what every row reads of its pair for itself (sorted rows share it) and the
+// projection's float32 sums stay below 60 MiB.  In us, few against sorted: 1024 x 256 -> 200 (float32, rank 8, 16 MiB)
+// 9 to 22, 128 x 4096 -> 4096 (bf16, rank 16, 36 MiB) 20 to 41, 256 x 4096 -> 4096 (rank 8, 40 MiB) 30 to 40, 4096 x 256
+// -> 200 (bf16, rank 16, 63 MiB) 24 to 23, 8192 x 64 -> 64 (float32, rank 16, 68 MiB) 37 to 29, 512 x 4096 -> 4096 (bf16,
+// rank 8, 80 MiB) 52 to 52, 1024 x 1024 -> 1024 (bf16, rank 64, 264 MiB) 55 to 30.
 inline bool few_rows(int64_t T, int64_t K, int64_t N, int r, size_t size) {
   if (T <= kFewRows) return true;
-  constexpr int64_t most = 16 << 20;
-  return T <= 2048 && T * r * K * static_cast<int64_t>(size) <= most && T * N * (r * static_cast<int64_t>(size) + 8) <= most;
+  const int64_t e = static_cast<int64_t>(size);
+  return T <= 8192 && T * (r * K * e + N * (r * e + 8)) <= (60 << 20);
 }
 
 // The pair of row t (-1: none), by the whole wave: 64 offsets a round.
@@ -998,23 +1021,16 @@ lipcache_status ad_group(int64_t t0, int64_t T, const lipcache_adapters& ad, con
   return LIPCACHE_OK;
 }
 
+// `rows` rows of a matrix as AdRows: itself, or its copy in `room`, which `copies` will make.
 template <class E>
-lipcache_status ad_rows(const void* from, int64_t ld, int64_t rows, int width, E* room, AdRows<E>& out, hipStream_t s) {
+AdRows<E> ad_rows(const void* from, int64_t ld, int64_t rows, int width, E* room, AdCopyList& copies) {
   constexpr int kV = Vec16<E>::kCount;
-  const E* p = static_cast<const E*>(from);
-  if (aligned16(from) && ld % kV == 0 && width % kV == 0 && ld * sizeof(E) <= (4u << 20)) {
-    out = {p, ld};
-    return LIPCACHE_OK;
-  }
+  if (aligned16(from) && ld % kV == 0 && width % kV == 0 && ld * sizeof(E) <= (4u << 20))
+    return {static_cast<const E*>(from), ld};
   const int64_t to = round_up(width, kV);
-  out = {room, to};
-  // at most 2^31 - 1 tiles a launch
-  for (int64_t r0 = 0; r0 < rows; r0 += 1 << 20) {
-    const int n = static_cast<int>(rows - r0 < (1 << 20) ? rows - r0 : 1 << 20);
-    const AdCopy c{p + r0 * ld, room + r0 * to, ld, to, 0, 0, n, width, n, static_cast<int>(to), 1};
-    if (lipcache_status st = ad_copy<E, false>(c, AdCopy{}, s); st != LIPCACHE_OK) return st;
-  }
-  return LIPCACHE_OK;
+  const int n = static_cast<int>(rows);
+  copies.add({from, room, ld, to, 0, 0, n, width, n, static_cast<int>(to), 1, 0});
+  return {room, to};
 }
 
 // v (u) of every row; rows without a pair are written (zeros) where `all_rows`.
@@ -1069,11 +1085,11 @@ lipcache_status ad_forward(const AdArgs& a, const float* bias, void* y, int64_t 
   constexpr int kV = Vec16<E>::kCount;
   AdSpace space{static_cast<char*>(ws_)};
   const AdForwardSpace<E> ws(space, a.T, a.K, a.N, a.ad.r, a.ad.S);
-  AdRows<E> x, W, A;
+  AdCopyList copies;
+  const AdRows<E> x = ad_rows<E>(a.x, a.ldx, a.T, a.K, ws.x, copies), W = ad_rows<E>(a.W, a.ldw, a.N, a.K, ws.W, copies),
+                  A = ad_rows<E>(a.ad.A, a.K, static_cast<int64_t>(a.ad.S) * a.ad.r, a.K, ws.A, copies);
   lipcache_status st;
-  if ((st = ad_rows<E>(a.x, a.ldx, a.T, a.K, ws.x, x, s)) != LIPCACHE_OK) return st;
-  if ((st = ad_rows<E>(a.W, a.ldw, a.N, a.K, ws.W, W, s)) != LIPCACHE_OK) return st;
-  if ((st = ad_rows<E>(a.ad.A, a.K, static_cast<int64_t>(a.ad.S) * a.ad.r, a.K, ws.A, A, s)) != LIPCACHE_OK) return st;
+  if ((st = copies.launch<E>(s)) != LIPCACHE_OK) return st;
   const bool keep = v != nullptr;
   if (!keep) v = ws.v;
   const AdLow low{a.ad.B, a.ad.r, v, ws.peak, a.ad.scale, a.ad.r, a.ad.S, a.N, aligned16(a.ad.B) && a.ad.r % kV == 0,
@@ -1143,18 +1159,21 @@ lipcache_status ad_backward(const AdArgs& a, const float* v_in, void* dx, int64_
   AdSpace space{static_cast<char*>(ws_)};
   const AdBackwardSpace<E> ws(space, a.T, a.K, a.N, a.ad.r, a.ad.S);
   const int r = a.ad.r, S = a.ad.S, K = a.K, N = a.N;
-  AdRows<E> x{}, W{}, dy{}, A{};
-  lipcache_status st;
-  if ((st = ad_rows<E>(a.dy, a.lddy, a.T, N, ws.dy, dy, s)) != LIPCACHE_OK) return st;
-  if (dA && (st = ad_rows<E>(a.x, a.ldx, a.T, K, ws.x, x, s)) != LIPCACHE_OK) return st;
+  AdCopyList copies;
+  AdRows<E> x{}, W{}, A{};
+  const AdRows<E> dy = ad_rows<E>(a.dy, a.lddy, a.T, N, ws.dy, copies);
+  if (dA) x = ad_rows<E>(a.x, a.ldx, a.T, K, ws.x, copies);
   const int64_t r8 = round_up(r, kV), N8 = round_up(N, kV);
-  const AdCopy bt{a.ad.B, ws.Bt, r, N8, static_cast<int64_t>(N) * r, r * N8, N, r, r, static_cast<int>(N8), S};
-  const AdCopy at{a.ad.A, ws.At, K, r8, static_cast<int64_t>(r) * K, K * r8, r, K, K, static_cast<int>(r8), dx ? S : 0};
-  if ((st = ad_copy<E, true>(bt, at, s)) != LIPCACHE_OK) return st;
-  // u and, if it did not come, v of all rows; a pass for each chunk of rows whose offsets stay below 2^31 bytes
+  copies.add({a.ad.B, ws.Bt, r, N8, static_cast<int64_t>(N) * r, r * N8, N, r, r, static_cast<int>(N8), S, 1});
+  if (dx) {
+    copies.add({a.ad.A, ws.At, K, r8, static_cast<int64_t>(r) * K, K * r8, r, K, K, static_cast<int>(r8), S, 1});
+    W = ad_rows<E>(a.W, a.ldw, N, K, ws.W, copies);
+  }
   const bool need_v = dA && !v_in && S > 0;
-  if (need_v && (st = ad_rows<E>(a.ad.A, K, static_cast<int64_t>(S) * r, K, ws.A, A, s)) != LIPCACHE_OK) return st;
-  if (dx && (st = ad_rows<E>(a.W, a.ldw, N, K, ws.W, W, s)) != LIPCACHE_OK) return st;
+  if (need_v) A = ad_rows<E>(a.ad.A, K, static_cast<int64_t>(S) * r, K, ws.A, copies);
+  lipcache_status st;
+  if ((st = copies.launch<E>(s)) != LIPCACHE_OK) return st;
+  // u and, if it did not come, v of all rows; a pass for each chunk of rows whose offsets stay below 2^31 bytes
   const int64_t chunk_dy = ad_chunk(dy.ld, sizeof(E)), chunk_x = need_v ? ad_chunk(x.ld, sizeof(E)) : chunk_dy;
   const int64_t chunk = chunk_dy < chunk_x ? chunk_dy : chunk_x;
   for (int64_t t0 = 0; t0 < a.T; t0 += chunk) {

@@ -361,7 +361,7 @@ def test_binding_refuses():
                              v=torch.zeros(20, 4, dtype=torch.bfloat16, device=DEV))
 
 
-# Past 2048 rows the forward pass sorts them by pair; up to there (small products) each row finds its pair by itself.
+# Small products of up to 8192 rows are not sorted by pair in the forward pass: each row finds its own.
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_many_rows_and_values_that_are_not_finite(dtype):
     test_values_that_are_not_finite_stay_in_their_request(dtype, 2100, "ragged")
@@ -384,3 +384,36 @@ def test_single_queries_and_their_limit(size, dtype):
     T, K, N, S, r, R_ = size
     b = make(sum(size), T, K, N, S, r, R_, dtype, "one" if R_ == T else "ragged", pad=8)
     check_forward(b, dtype, f"single queries {size} {dtype}")
+
+
+# Past 8192 rows they are sorted, whatever the product.
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_sorted_rows_and_values_that_are_not_finite(dtype):
+    test_values_that_are_not_finite_stay_in_their_request(dtype, 8300, "ragged")
+
+
+def test_sorted_rows_and_strange_offsets():
+    test_offsets_that_reach_past_the_rows(8300)
+    test_no_pairs_no_requests_no_bias(8300)
+    b = make(17, 8300, 64, 48, 3, 8, 6, "bf16")
+    good = b["offsets"]
+    for offs in ([9, 3, 8300, 0, 8300, 2, 8300], [8300, 8300, 5, 0, 0, 0, 0], [-(1 << 31), (1 << 31) - 1, 0, 8300, -9, 8300, 1]):
+        b["offsets"] = torch.tensor(offs, dtype=torch.int64).to(torch.int32).to(DEV)
+        api.adapter_forward(*[b[k] for k in ("x", "W", "bias", "A", "B", "scale", "offsets", "adapter")])
+        torch.cuda.synchronize()
+    b["offsets"] = good
+    check_forward(b, "bf16", "after offsets that decrease")
+
+
+@pytest.mark.parametrize("r", [8, 40])
+def test_sorted_rows_and_float16_factors(r):
+    test_float16_factors_outside_its_range(8300, r)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("size", [(8192, 40, 24, 5, 4, 300), (8193, 40, 24, 5, 4, 8193), (8300, 65, 130, 3, 8, 60), (5000, 33, 64, 9, 5, 5000)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_many_rows_of_small_products(size, dtype):
+    T, K, N, S, r, R_ = size
+    b = make(sum(size), T, K, N, S, r, R_, dtype, "one" if R_ == T else "ragged")
+    check_forward(b, dtype, f"many rows {size} {dtype}")
