@@ -512,6 +512,13 @@ __global__ __launch_bounds__(64 * N * N) void ns_short_poly_kernel(const double*
     for (int v = 0; v < 4; ++v)
       Q[at(v)] = c * square[v] + b * A[at(v)] + (16 * ti + 4 * v + quarter == 16 * tj + row ? a : 0.0);
     __syncthreads();
+    if (k + 1 == steps) {  // nobody asks for the next A
+      const f64x4 p = product(P, Q);
+      __syncthreads();
+#pragma unroll
+      for (int v = 0; v < 4; ++v) P[at(v)] = p[v];
+      break;
+    }
     const f64x4 p = product(P, Q), qa = product(A, Q);
     __syncthreads();
 #pragma unroll
