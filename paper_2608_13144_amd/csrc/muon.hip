@@ -639,7 +639,7 @@ inline int64_t tiles_of(int rows, int side) { return (rows + side - 1) / side; }
 //   192, 256  one workgroup a CU, where their tiles fill at least 4/5 of the rounds of 256 CUs
 // One step of a square matrix in us (P, P^2, X'; 22-bit operands): 1536 wide 26 + 27 + 39 with 64, 32 + 35 + 35
 // with 128d, 40 + 43 + 43 with 128; 2048 wide 48 + 49 + 67, 46 + 47 + 53, 51 + 54 + 61; four of 2048: 140 + 141 + 243,
-// 135 + 139 + 200, 131 + 135 + 189.  4096 wide (11 bits): P 81 with 192, X' 133 with 256, against 100 and 150 with 128.
+// 135 + 139 + 200, 131 + 135 + 189.  4096 wide (11 bits): P 85 with 192 against 100 with 128, X' 152 with 256 against 165.
 enum NsTile { kNs64, kNs128Deep, kNs128, kNs192, kNs256 };
 
 inline bool fills_chip(int64_t tiles) { return 5 * tiles >= 4 * 256 * ((tiles + 255) / 256); }
