@@ -90,6 +90,8 @@ class LipcacheMuon(ctypes.Structure):
     ]
 
 
+MUON_SHORT_OPERANDS = 2  # beside nesterov
+
 _PADAPTERS = ctypes.POINTER(LipcacheAdapters)
 _PMUON = ctypes.POINTER(LipcacheMuon)
 _f32, _pf32 = ctypes.c_float, ctypes.POINTER(ctypes.c_float)

@@ -577,11 +577,14 @@ def orthogonalise(G: torch.Tensor, steps: int = 5, coefficients=NEWTON_SCHULZ, e
 
 def muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, lr: float, momentum: float = 0.95,
               weight_decay: float = 0.0, nesterov: bool = True, scale: float | None = None, steps: int = 5,
-              coefficients=NEWTON_SCHULZ, eps: float = 1e-7) -> None:
+              coefficients=NEWTON_SCHULZ, eps: float = 1e-7, short_operands: bool = False) -> None:
     """lipcache_muon_step: one step along the orthogonalised momentum, W and M in place (async).
 
     W and G [m, n] or [b, m, n] of one type, M float32 of the same shape.
-    ``scale``: the update's factor, sqrt(max(1, m / n)) when None."""
+    ``scale``: the update's factor, sqrt(max(1, m / n)) when None.
+    ``short_operands`` (16-bit W): products of 11-bit operands in place of
+    22-bit ones, 2.5 times as fast on large matrices; the update is then 2e-3 to 4e-3
+    of its norm off."""
     code = _dtype(W, "W")
     b, m, n = _stack(W, "W")
     _need_shape(G, "G", W.dtype, W.device, tuple(W.shape))
@@ -589,8 +592,8 @@ def muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, lr: float, mome
     if scale is None:
         scale = max(1.0, m / max(n, 1)) ** 0.5
     coef = _coefficients(steps, coefficients)
-    opt = L.LipcacheMuon(float(lr), float(momentum), float(weight_decay), float(scale), float(eps), int(bool(nesterov)),
-                         int(steps), ctypes.cast(coef, ctypes.POINTER(ctypes.c_float)))
+    opt = L.LipcacheMuon(float(lr), float(momentum), float(weight_decay), float(scale), float(eps),
+                         int(bool(nesterov)) | (L.MUON_SHORT_OPERANDS if short_operands else 0), int(steps), ctypes.cast(coef, ctypes.POINTER(ctypes.c_float)))
     lib = L.load()
     ws = workspace(lib.lipcache_muon_step_workspace_bytes(b, m, n, code), W.device)
     st = lib.lipcache_muon_step(W.data_ptr(), G.data_ptr(), M.data_ptr(), b, m, n, code, ctypes.byref(opt),

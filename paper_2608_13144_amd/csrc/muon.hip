@@ -7,12 +7,12 @@
 
 namespace lc {
 
-// X, P = X X^T (or X^T X) and B = b P + c P^2 go to the matrix cores as float16
-// numbers, or as sums of two (22 bits), each times a power of two that keeps
-// the largest possible entry below 2^15; the sums of the products are float32.
+// X, P = X X^T (or X^T X) and B = b P + c P^2 go to the matrix cores as sums of
+// two float16 numbers (22 bits), each times a power of two that keeps the
+// largest possible entry below 2^15; the sums of the products are float32.
 //
-// Where they are single float16 numbers, X's rounding is kept in a second array
-// and comes in with the term a X.  Small singular values grow by a = 3.4 a step
+// A step may ask for single float16 numbers (LIPCACHE_MUON_SHORT_OPERANDS).  X's
+// rounding is then kept in a second array and comes in with the term a X.  Small singular values grow by a = 3.4 a step
 // through that term alone, and what is lost of X there is lost of them: 2e-2
 // of the result for a matrix of a few strong directions over noise, 5e-4 with
 // the second array.
@@ -612,11 +612,6 @@ double ns_bound(double a, double b, double c, double h);
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline int round_up(int v, int to) { return (v + to - 1) / to * to; }
 
-// A step takes its orthogonalised direction with 11-bit operands where W has 16 bits: the direction's relative
-// error, 2e-3 (measured against float64), is below W's own rounding unless the step is as large as W.  Results that
-// are the direction itself, and float32 parameters, take 22-bit operands.
-inline bool ns_split(int32_t dtype, bool step) { return !step || dtype == LIPCACHE_F32; }
-
 size_t ns_workspace(int64_t batch, int32_t m, int32_t n, bool split) {
   if (ns_short(m, n)) {
     const size_t tiles = ((m < n ? m : n) + 15) / 16, b = static_cast<size_t>(batch);
@@ -628,6 +623,12 @@ size_t ns_workspace(int64_t batch, int32_t m, int32_t n, bool split) {
                e = split ? 4 : 2;
   return align_up(b * ns_chunks(static_cast<int64_t>(m) * n) * 8, 256) + 2 * align_up(b * mp * np * e, 256) + (split ? 0 : 2 * align_up(b * mp * np * 2, 256)) +
          2 * align_up(b * p * p * e, 256);
+}
+
+// A step's: for either kind of operands.
+size_t ns_step_workspace(int64_t batch, int32_t m, int32_t n) {
+  const size_t a = ns_workspace(batch, m, n, true), b = ns_workspace(batch, m, n, false);
+  return a > b ? a : b;
 }
 
 inline int64_t tiles_of(int rows, int side) { return (rows + side - 1) / side; }
@@ -860,23 +861,13 @@ bool ns_unaligned(const void* p, int32_t dtype) {
   return !p || (reinterpret_cast<uintptr_t>(p) & (dtype == LIPCACHE_F32 ? 3u : 1u)) != 0;
 }
 
-template <bool kStep>
-struct NsOperand {
-  typedef Split E;
-};
-template <>
-struct NsOperand<true> {
-  typedef _Float16 E;
-};
-
-template <bool kStep>
+template <class E, bool kStep>
 lipcache_status ns_dispatch(const NsArgs& g, int32_t dtype, const void* G, float* M, float mu, int nesterov, float keep,
                             float gain, void* out, void* ws, hipStream_t s) {
-  typedef typename NsOperand<kStep>::E E16;  // as ns_split() says
   switch (dtype) {
     case LIPCACHE_F32: return ns_run<Split, float, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
-    case LIPCACHE_BF16: return ns_run<E16, __bf16, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
-    default: return ns_run<E16, _Float16, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
+    case LIPCACHE_BF16: return ns_run<E, __bf16, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
+    default: return ns_run<E, _Float16, kStep>(g, G, M, mu, nesterov, keep, gain, out, ws, s);
   }
 }
 
@@ -886,7 +877,7 @@ using namespace lc;
 
 extern "C" size_t lipcache_orthogonalise_workspace_bytes(int64_t batch, int32_t m, int32_t n, int32_t dtype) {
   if (batch < 0 || m < 1 || n < 1 || dtype < LIPCACHE_F32 || dtype > LIPCACHE_F16) return 0;
-  return ns_workspace(batch, m, n, ns_split(dtype, false));
+  return ns_workspace(batch, m, n, true);
 }
 
 extern "C" lipcache_status lipcache_orthogonalise(const void* G, int64_t batch, int32_t m, int32_t n, int32_t dtype,
@@ -894,16 +885,15 @@ extern "C" lipcache_status lipcache_orthogonalise(const void* G, int64_t batch, 
                                                   size_t ws_bytes, lipcache_stream_t stream) {
   if (lipcache_status st = ns_check(batch, m, n, dtype, steps, coef, eps); st != LIPCACHE_OK) return st;
   if (batch > 0 && (ns_unaligned(G, dtype) || ns_unaligned(out, dtype))) return LIPCACHE_EINVAL;
-  if (!ws || !aligned256(ws) || ws_bytes < ns_workspace(batch, m, n, ns_split(dtype, false)))
-    return LIPCACHE_EWORKSPACE;
+  if (!ws || !aligned256(ws) || ws_bytes < ns_workspace(batch, m, n, true)) return LIPCACHE_EWORKSPACE;
   if (batch == 0) return LIPCACHE_OK;
   const NsArgs g{batch, m, n, steps, coef, eps};
-  return ns_dispatch<false>(g, dtype, G, nullptr, 0.0f, 0, 0.0f, 0.0f, out, ws, stream);
+  return ns_dispatch<Split, false>(g, dtype, G, nullptr, 0.0f, 0, 0.0f, 0.0f, out, ws, stream);
 }
 
 extern "C" size_t lipcache_muon_step_workspace_bytes(int64_t batch, int32_t m, int32_t n, int32_t dtype) {
   if (batch < 0 || m < 1 || n < 1 || dtype < LIPCACHE_F32 || dtype > LIPCACHE_F16) return 0;
-  return ns_workspace(batch, m, n, ns_split(dtype, true));
+  return ns_step_workspace(batch, m, n);
 }
 
 extern "C" lipcache_status lipcache_muon_step(void* W, const void* G, float* M, int64_t batch, int32_t m, int32_t n,
@@ -913,12 +903,15 @@ extern "C" lipcache_status lipcache_muon_step(void* W, const void* G, float* M, 
   if (lipcache_status st = ns_check(batch, m, n, dtype, opt->steps, opt->coef, opt->eps); st != LIPCACHE_OK) return st;
   if (!isfinite(opt->lr) || !isfinite(opt->momentum) || !isfinite(opt->weight_decay) || !isfinite(opt->scale))
     return LIPCACHE_EINVAL;
+  const bool nesterov = (opt->nesterov & 1) != 0, few_bits = (opt->nesterov & LIPCACHE_MUON_SHORT_OPERANDS) != 0;
+  if ((opt->nesterov & ~(1 | LIPCACHE_MUON_SHORT_OPERANDS)) != 0 || (few_bits && dtype == LIPCACHE_F32)) return LIPCACHE_EINVAL;
   if (batch > 0 && (ns_unaligned(W, dtype) || ns_unaligned(G, dtype) || ns_unaligned(M, LIPCACHE_F32)))
     return LIPCACHE_EINVAL;
-  if (!ws || !aligned256(ws) || ws_bytes < ns_workspace(batch, m, n, ns_split(dtype, true))) return LIPCACHE_EWORKSPACE;
+  if (!ws || !aligned256(ws) || ws_bytes < ns_step_workspace(batch, m, n)) return LIPCACHE_EWORKSPACE;
   if (batch == 0) return LIPCACHE_OK;
   const NsArgs g{batch, m, n, opt->steps, opt->coef, opt->eps};
   const float keep = static_cast<float>(1.0 - static_cast<double>(opt->lr) * opt->weight_decay);
   const float gain = static_cast<float>(static_cast<double>(opt->lr) * opt->scale);
-  return ns_dispatch<true>(g, dtype, G, M, opt->momentum, opt->nesterov != 0, keep, gain, W, ws, stream);
+  if (few_bits) return ns_dispatch<_Float16, true>(g, dtype, G, M, opt->momentum, nesterov, keep, gain, W, ws, stream);
+  return ns_dispatch<Split, true>(g, dtype, G, M, opt->momentum, nesterov, keep, gain, W, ws, stream);
 }
