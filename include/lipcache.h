@@ -480,9 +480,8 @@ typedef struct lipcache_adapters {
  * every row t of a request with pair a
  *   v_t = A_a x_t,    y_t = W x_t + bias + scale_a B_a v_t,
  * and y_t = W x_t + bias, v_t = 0 for rows without one.  Sums are held in
- * float32; v is never rounded to 16 bits in one piece (the product B_a v_t
- * takes it as float32 or as a sum of two such numbers, for float16 times a
- * power of two, so that its range is float32's), y is rounded once.  A value that is
+ * float32; v is not rounded for the product B_a v_t (for float16 to 22 bits,
+ * times a power of two, so that its range is float32's), y is rounded once.  A value that is
  * not finite stays in its own request's rows (in W or bias: in its outputs).
  *
  *  x [T][K] (ldx), W [N][K] (ldw), bias [N] float or NULL

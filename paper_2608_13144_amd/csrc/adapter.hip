@@ -212,13 +212,20 @@ struct AdRows {
   int64_t ld;
 };
 
-// A float32 factor as what the matrix cores take: itself, or the sum of two
-// 16-bit numbers (each product then takes two instructions; 16 or 22 bits).
+// A float32 factor as what the matrix cores take: itself, or a sum of 16-bit
+// numbers, an instruction each: three bfloat16 (all 24 bits) or two float16 (22).
+// What is not finite, or rounds to infinity, is the first part alone.
 template <class E>
-__device__ __forceinline__ void two_parts(float v, E& first, E& second) {
-  asm("" : "+v"(v));
-  first = static_cast<E>(v);
-  second = static_cast<E>(v - static_cast<float>(first));
+inline constexpr int kFactorParts = std::is_same_v<E, float> ? 1 : std::is_same_v<E, __bf16> ? 3 : 2;
+template <class E>
+__device__ __forceinline__ void factor_parts(float v, E (&part)[kFactorParts<E>]) {
+#pragma unroll
+  for (int h = 0; h < kFactorParts<E>; ++h) {
+    asm("" : "+v"(v));
+    part[h] = static_cast<E>(v);
+    v -= static_cast<float>(part[h]);
+    v = fabsf(v) < __builtin_huge_valf() ? v : 0.0f;
+  }
 }
 
 // float16 ends at 65504 and loses digits below 2^-14, where A_a x and B_a^T dy
@@ -477,16 +484,16 @@ __device__ __forceinline__ void add_low_rank(const AdLow& low, const AdTileRows<
           if constexpr (std::is_same_v<E, float>) {
             sum = MfmaType<E>::mul(V{w[0], w[1], w[2], w[3]}, vf, sum);
           } else {
-            V first, second;
+            V part[kFactorParts<E>];
 #pragma unroll
             for (int e = 0; e < kV; ++e) {
-              E p, q;
-              two_parts(w[e], p, q);
-              first[e] = p;
-              second[e] = q;
+              E p[kFactorParts<E>];
+              factor_parts(w[e], p);
+#pragma unroll
+              for (int h = 0; h < kFactorParts<E>; ++h) part[h][e] = p[h];
             }
-            sum = MfmaType<E>::mul(second, vf, sum);
-            sum = MfmaType<E>::mul(first, vf, sum);
+#pragma unroll
+            for (int h = kFactorParts<E> - 1; h >= 0; --h) sum = MfmaType<E>::mul(part[h], vf, sum);
           }
         }
 #pragma unroll
@@ -749,9 +756,12 @@ lipcache_status ad_few(const AdRows<E>& x, int T, const AdRows<E>& W, int K, int
 // The factors u and v as the gradient kernel's operand: for each tile of the
 // table a block of r rows of 128 bytes, row rho the tile's 32 values f[row][rho]
 // as float32, or as 32 first and 32 second 16-bit parts; zeros past its rows.
+// bfloat16's third parts follow as r rows of 64 bytes.
 // float16: times 2^exponent[tile], a multiple of 4 (so that the sums, which
 // follow it, seldom change) up to 40 (float16 gradients are zero from there).
 constexpr int kNoExponent = -1000;  // a tile of zeros
+template <class E>
+inline constexpr int kFactorRow = kFactorParts<E> == 3 ? 192 : 128;  // bytes a rank and tile
 
 template <class E>
 __global__ __launch_bounds__(256) void ad_factor_kernel(const float* __restrict__ u, const float* __restrict__ v, int r,
@@ -763,7 +773,7 @@ __global__ __launch_bounds__(256) void ad_factor_kernel(const float* __restrict_
   const int last = g.tile_start[pairs], row0 = g.tile_row[t], rows = g.tile_rows[t];
   if (static_cast<uint32_t>(t) >= static_cast<uint32_t>(last)) return;
   const float* f = blockIdx.y ? v : u;
-  E* to = (blockIdx.y ? to_v : to_u) + static_cast<int64_t>(t) * r * (128 / sizeof(E));
+  E* to = (blockIdx.y ? to_v : to_u) + static_cast<int64_t>(t) * r * (kFactorRow<E> / sizeof(E));
   const int x = static_cast<int>(threadIdx.x) & 31, y = static_cast<int>(threadIdx.x) >> 5;
   float top = 0.0f;
 #pragma unroll
@@ -791,8 +801,12 @@ __global__ __launch_bounds__(256) void ad_factor_kernel(const float* __restrict_
   for (int rho = y; rho < r; rho += 8) {
     const float w = two_to<E>(tile[x][rho], up);
     E* p = to + rho * (128 / sizeof(E)) + x;
-    if constexpr (std::is_same_v<E, float>) *p = w;
-    else two_parts(w, p[0], p[32]);
+    E part[kFactorParts<E>];
+    if constexpr (std::is_same_v<E, float>) part[0] = w;
+    else factor_parts(w, part);
+    p[0] = part[0];
+    if constexpr (kFactorParts<E> > 1) p[32] = part[1];
+    if constexpr (kFactorParts<E> > 2) to[r * 64 + rho * 32 + x] = part[2];
   }
 }
 
@@ -827,9 +841,14 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
   typedef typename Vec16<E>::type V;
   typedef TileOf<E, 128, true, 4> TileZ;                                       // rows of it, as many as there are
   typedef TileOf<std::conditional_t<kF32, float, Split>, 32 * NR, false, 4> TileF;
-  constexpr int kZ = 32 * 128 * kSize, kF = NR * 4096, kTile = kZ + kF;        // LDS bytes of a tile
-  constexpr int kSub = 2, kStages = NR == 1 ? 3 : 2;
-  constexpr int kZCopies = kZ / 4096, kFCopies = NR;                           // of a wave and tile
+  // third parts: ranks rho and rho + 16 of 32 share a row of 128 bytes, swizzled as the others
+  constexpr bool kThird = kFactorParts<E> == 3;
+  constexpr int kZ = 32 * 128 * kSize, kF = NR * 4096, kT = kThird ? NR * 2048 : 0, kTile = kZ + kF + kT;  // LDS bytes of a tile
+  // A third stage only where two workgroups share a CU all the same: with it bfloat16's (86 KB) took the
+  // backward pass of 8192 x 4096 -> 4096, rank 32, from 350 to 364 us
+  constexpr int kSub = 2, kStages = NR == 1 && !kThird ? 3 : 2;
+  constexpr int kZCopies = kZ / 4096, kFCopies = NR, kTCopies = kThird ? (NR + 1) / 2 : 0;  // of a wave and tile
+  constexpr int kTLanes = NR == 1 ? 32 : 64;                                   // of a copy of third parts
   constexpr int kRowsCopy = 64 / TileZ::kSlots;                                // rows of z a copy takes: 4 or 2
   constexpr int kGroups = kF32 ? 4 : 2, kParts = kF32 ? 1 : 2;
   __shared__ __align__(16) char lds[kStages * kSub * kTile];
@@ -889,24 +908,33 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
       if (first + mine < end - row0 && col < d.width) p = d.z + row * d.ldz + col;
       copy(p, to + (wave * kZCopies + c) * 1024);
     }
-    const char* f = reinterpret_cast<const char*>(d.f) + static_cast<int64_t>(t) * r * 128;
+    const char* f = reinterpret_cast<const char*>(d.f) + static_cast<int64_t>(t) * r * kFactorRow<E>;
 #pragma unroll
     for (int c = 0; c < kFCopies; ++c) {
       const int n8 = (wave * kFCopies + c) * 64 + lane, rho = n8 / 8, chunk = (n8 % 8) ^ TileF::swz(rho);
       copy(some && rho < r ? f + rho * 128 + chunk * 16 : static_cast<const char*>(zeros),
            to + kZ + (wave * kFCopies + c) * 1024);
     }
+#pragma unroll
+    for (int c = 0; c < kTCopies; ++c) {
+      const int n8 = (wave * kTCopies + c) * kTLanes + lane, at = n8 / 8, chunk = (n8 % 8) ^ TileF::swz(at);
+      const int rho = at / 16 * 32 + at % 16 + chunk / 4 * 16;
+      if (lane < kTLanes)
+        copy(some && rho < r ? f + r * 128 + rho * 64 + chunk % 4 * 16 : static_cast<const char*>(zeros),
+             to + kZ + kF + (wave * kTCopies + c) * (kTLanes * 16));
+    }
   };
   f32x16 acc[NR] = {};
-  uint32_t rz[kGroups], rf[kGroups][kParts];
+  uint32_t rz[kGroups], rf[kGroups][kParts], rt[kGroups];
 #pragma unroll
   for (int n = 0; n < kGroups; ++n) {
     rz[n] = TileZ::row_offset(TileZ::read_offset(n, 0), wave);
 #pragma unroll
     for (int h = 0; h < kParts; ++h) rf[n][h] = kZ + TileF::read_offset(n, h);
+    rt[n] = kZ + kF + (li & 15) * 128 + (((2 * n + half + (li >> 4) * 4) ^ TileF::swz(li & 15)) * 16);
   }
   const int steps = tiles > 0 ? (tiles + kSub - 1) / kSub : 0;
-  constexpr int kCopies = kSub * (kZCopies + kFCopies);
+  constexpr int kCopies = kSub * (kZCopies + kFCopies + kTCopies);
   auto copy_step = [&](int step) {
 #pragma unroll
     for (int u = 0; u < kSub; ++u)
@@ -945,10 +973,13 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
       for (int n = 0; n < kGroups; ++n) {
         const V z = __builtin_bit_cast(V, TileZ::read16(at + rz[n]));
 #pragma unroll
-        for (int m = 0; m < NR; ++m)
+        for (int m = 0; m < NR; ++m) {
+          if constexpr (kThird)
+            acc[m] = MfmaType<E>::mul(__builtin_bit_cast(V, TileF::read16(at + rt[n] + m * 2048)), z, acc[m]);
 #pragma unroll
           for (int h = kParts - 1; h >= 0; --h)
             acc[m] = MfmaType<E>::mul(__builtin_bit_cast(V, TileF::read16(at + TileF::row_offset(rf[n][h], m))), z, acc[m]);
+        }
       }
     }
   }
@@ -1142,7 +1173,7 @@ struct AdBackwardSpace {
     exps_v = ws.take<int32_t>(ad_tiles(T, S));
     At = ws.take<E>(n * K * round_up(r, kV));
     Bt = ws.take<E>(n * r * N8);
-    const size_t factors = static_cast<size_t>(ad_tiles(T, S)) * r * (128 / sizeof(E));
+    const size_t factors = static_cast<size_t>(ad_tiles(T, S)) * r * (kFactorRow<E> / sizeof(E));
     fu = ws.take<E>(factors);
     fv = ws.take<E>(factors);
     const int splits = ad_splits(T, K, N, S);
@@ -1230,7 +1261,8 @@ size_t ad_workspace(bool backward, int64_t T, int K, int N, int r, int S) {
 }
 
 size_t ad_workspace(bool backward, int64_t T, int K, int N, int r, int S, int32_t dtype) {
-  return dtype == LIPCACHE_F32 ? ad_workspace<float>(backward, T, K, N, r, S) : ad_workspace<__bf16>(backward, T, K, N, r, S);
+  if (dtype == LIPCACHE_F32) return ad_workspace<float>(backward, T, K, N, r, S);
+  return dtype == LIPCACHE_BF16 ? ad_workspace<__bf16>(backward, T, K, N, r, S) : ad_workspace<_Float16>(backward, T, K, N, r, S);
 }
 
 // ------------------------------------------------------------- validation

@@ -1,0 +1,87 @@
+"""Adapters at their edges: what the passes work out in between keeps float32's digits, requests keep apart."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_helpers import say
+from paper_2608_13144_amd import api
+from test_gpu_adapter import DEV, DT, n64
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(g, lo, hi, *shape):
+    return torch.randint(lo, hi + 1, shape, generator=g).float()
+
+
+def one_hot(width, at):
+    return torch.nn.functional.one_hot(at % width, width).float()
+
+
+def batch(T, S, g, dtype, x, W, A, B):
+    cuts = torch.randint(0, T + 1, (6,), generator=g).sort().values
+    offsets = torch.cat([torch.zeros(1, dtype=torch.int64), cuts, torch.full((1,), T)])
+    adapter = torch.arange(7) % S
+    cast = lambda t: t.to(DT[dtype]).to(DEV)  # noqa: E731
+    for t in (x, W, A, B):
+        assert torch.equal(t.to(DT[dtype]).float(), t)
+    return dict(x=cast(x), W=cast(W), A=cast(A), B=cast(B), scale=torch.ones(S, device=DEV), offsets=offsets.int().to(DEV),
+                adapter=adapter.int().to(DEV)), torch.repeat_interleave(adapter, offsets[1:] - offsets[:-1])
+
+
+# Whole numbers whose sums stay below 2^24 are exact in float32, whatever the order.  A x and B^T dy take 17 to 21 bits here
+# and nearly cancel against W's part, or in pairs of rows, so that a digit lost in between is whole units of the result.
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T", [50, 8300])
+def test_forward_keeps_every_digit_of_what_lies_between(dtype, T):
+    say("digits of v", T, dtype)
+    g = torch.Generator().manual_seed(T)
+    S, r, K, N = 2, 3, 64, 48
+    A = ints(g, 0, 100, r, K).expand(S, r, K).contiguous()
+    rho = torch.arange(N) % r
+    B = one_hot(r, rho).expand(S, N, r).contiguous()
+    keep = torch.arange(N) % K
+    W = one_hot(K, keep) - A[0][rho]  # y = x[keep]
+    x = ints(g, 0, 255, T, K)
+    b, _ = batch(T, S, g, dtype, x, W, A, B)
+    y = api.adapter_forward(b["x"], b["W"], None, b["A"], b["B"], b["scale"], b["offsets"], b["adapter"]).y
+    assert torch.equal(y.float().cpu(), x[:, keep])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,r", [(50, 3), (700, 3), (700, 20), (700, 40), (700, 100)])
+def test_backward_keeps_every_digit_of_what_lies_between(dtype, T, r):
+    say("digits of u and v", T, r, dtype)
+    g = torch.Generator().manual_seed(T + r)
+    S, K, N = 2, 64, 512
+    # ranks past the third are zeros in A and small in B, so that the sums stay exact
+    A = torch.zeros(S, r, K)
+    A[:, -3:] = ints(g, 0, 7, 3, K)
+    rho = torch.arange(N) % 3
+    B = torch.zeros(S, N, r)
+    B[:, :, -3:] = one_hot(3, rho) * ints(g, 1, 15, N, 1)
+    W = one_hot(K, torch.arange(N)) - B[0] @ A[0]  # dx: the sums of dy over the n of each column
+    dy = ints(g, 0, 127, T, N)
+    n0 = torch.randint(0, N, (T // 2,), generator=g)
+    dy[1::2] = -dy[0::2]
+    dy[1::2] += one_hot(N, n0)
+    x = ints(g, 0, 3, T // 2, K).repeat_interleave(2, 0)
+    v = ints(g, -(1 << 20), 1 << 20, T // 2, r).repeat_interleave(2, 0)
+    b, pair = batch(T, S, g, dtype, x, W, A, B)
+    b["offsets"] = (b["offsets"] // 2 * 2).int()  # pairs of rows stay in one request
+    pair = torch.repeat_interleave(b["adapter"].cpu().long(), (b["offsets"][1:] - b["offsets"][:-1]).cpu().long())
+    args = [b[k] for k in ("x", "W", "A", "B", "scale", "offsets", "adapter")]
+    out = api.adapter_backward(dy.to(DT[dtype]).to(DEV), *args, v=v.to(DEV))
+    exact = lambda t: t.to(DT[dtype]).double()  # noqa: E731  (rounded once)
+    dx = dy.double() @ one_hot(K, torch.arange(N)).double()
+    assert torch.equal(out.dx.double().cpu(), exact(dx))
+    u = dy.double() @ B[0].double()
+    dA = torch.stack([u[pair == a].T @ x[pair == a].double() for a in range(S)])
+    assert torch.equal(out.dA.double().cpu(), exact(dA))
+    # dB: a second row's v is minus the first's, and a little
+    v[1::2] = -v[0::2] + ints(g, 0, 3, T // 2, r)
+    dz = ints(g, -1, 1, T // 2, N).repeat_interleave(2, 0)
+    out = api.adapter_backward(dz.to(DT[dtype]).to(DEV), *args, v=v.to(DEV), want_dx=False)
+    dB = torch.stack([dz[pair == a].double().T @ v[pair == a].double() for a in range(S)])
+    assert torch.equal(out.dB.double().cpu(), exact(dB))
+    assert np.isfinite(n64(out.dB)).all()
