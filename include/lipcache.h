@@ -533,6 +533,10 @@ size_t lipcache_adapter_backward_workspace_bytes(int64_t T, int32_t K, int32_t N
  * sum of two float16 numbers (22 bits).  Operands are scaled by powers of two
  * that no value can overflow: the bound of the singular values, worked out
  * from the coefficients on the host, must stay below 16 (else EUNSUPPORTED).
+ * With a shorter side of at most 64 they run in float64 on the Gram matrix, in
+ * rounds of as many steps as float64 bears (7 of the coefficients above).
+ * Rounding grows by up to max |a + b s + c s^2| a step in directions that G
+ * lacks, as in any form of the iteration, up to the last step's bound.
  *
  *  G, out [batch][m][n] contiguous, batch >= 0, 1 <= m, n, min(m, n) <= 16384,
  *         m n <= 2^30; out may be G

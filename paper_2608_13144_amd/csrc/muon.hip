@@ -338,7 +338,15 @@ __global__ __launch_bounds__(S::kThreads) void ns_apply_kernel(const _Float16* _
 // relative to the largest keep the digits that float32 products of X would
 // give them.  Three launches: the Gram matrix in shares of the long side (and
 // the momentum), the polynomial (one workgroup a matrix, in LDS), the product
-// P U.  Bound by reading and writing the long matrices, and by the chain of
+// P U.
+//
+// Rounding leaves A eigenvalues of about -2^-53, which no X X^T has, and a step
+// multiplies them by up to g^2, g the largest |a + b s + c s^2| on the spectrum;
+// near -1 they would explode.  So before A's errors have grown by 2^24 (7 steps
+// of the usual coefficients) a round ends: X = P U is formed in float64, and the
+// next round starts from its Gram matrix, whose eigenvalues are squares again.
+//
+// Bound by reading and writing the long matrices, and by the chain of
 // small products between: 64 of 16 x 4096 (bf16, with the momentum) 12 + 8 + 12 us
 // for 84 MB.
 constexpr int kShortMost = 64;
@@ -396,6 +404,21 @@ struct ShortU {
   }
 };
 
+// The tiles of a Gram matrix: the four waves' sums, added in order.
+template <int N>
+__device__ __forceinline__ void short_gram_store(const f64x4 (&acc)[N * (N + 1) / 2], double (&join)[4][256], double* out) {
+  const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+#pragma unroll
+  for (int t = 0; t < N * (N + 1) / 2; ++t) {
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < 4; ++v) join[wave][v * 64 + lane] = acc[t][v];
+    __syncthreads();
+    const int i = static_cast<int>(threadIdx.x);
+    out[t * 256 + i] = ((join[0][i] + join[1][i]) + join[2][i]) + join[3][i];
+  }
+}
+
 // part[z][share] = sum over the share's c of U(:, c) U(:, c)^T, N x N tiles of 16 (the lower ones; zeros past p).
 template <int N, typename T, bool kStep>
 __global__ __launch_bounds__(256) void ns_short_gram_kernel(ShortU<T, kStep> U, int shares, double* __restrict__ part) {
@@ -424,27 +447,45 @@ __global__ __launch_bounds__(256) void ns_short_gram_kernel(ShortU<T, kStep> U, 
           acc[i * (i + 1) / 2 + j] = __builtin_amdgcn_mfma_f64_16x16x4f64(f[i], f[j], acc[i * (i + 1) / 2 + j], 0, 0, 0);
     }
   }
-  // the waves' sums, in order
-  double* out = part + (z * shares + blockIdx.x) * (kTiles * 256);
+  short_gram_store<N>(acc, join, part + (z * shares + blockIdx.x) * (kTiles * 256));
+}
+
+// The same for a round's X [z][q][p].
+template <int N>
+__global__ __launch_bounds__(256) void ns_short_regram_kernel(const double* __restrict__ X, int p, int q, int shares,
+                                                              double* __restrict__ part) {
+  constexpr int kTiles = N * (N + 1) / 2;
+  __shared__ double join[4][256];
+  const int64_t z = blockIdx.y;
+  const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+  const int row = lane & 15, quarter = lane >> 4;
+  const double* x = X + z * q * p;
+  f64x4 acc[kTiles] = {};
+  for (int c0 = static_cast<int>(blockIdx.x) * kShortBlock; c0 < q; c0 += shares * kShortBlock) {
+    const int count = q - c0 < kShortBlock ? q - c0 : kShortBlock;
+    for (int c = wave * 4; c < count; c += 16) {
+      double f[N];
 #pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
-    __syncthreads();
+      for (int i = 0; i < N; ++i)
+        f[i] = 16 * i + row < p && c + quarter < count ? x[static_cast<int64_t>(c0 + c + quarter) * p + 16 * i + row] : 0.0;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) join[wave][v * 64 + lane] = acc[t][v];
-    __syncthreads();
-    const int i = static_cast<int>(threadIdx.x);
-    out[t * 256 + i] = ((join[0][i] + join[1][i]) + join[2][i]) + join[3][i];
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j <= i; ++j)
+          acc[i * (i + 1) / 2 + j] = __builtin_amdgcn_mfma_f64_16x16x4f64(f[i], f[j], acc[i * (i + 1) / 2 + j], 0, 0, 0);
+    }
   }
+  short_gram_store<N>(acc, join, part + (z * shares + blockIdx.x) * (kTiles * 256));
 }
 
 struct ShortCoefficients {
   float c[3 * 32];
 };
 
-// P [z][16 N][16 N], with the 1 / (||U||_F + eps) of X_0 in it.
+// P [z][16 N][16 N] of a round's steps, in the first with the 1 / (||U||_F + eps) of X_0 in it.
 template <int N>
 __global__ __launch_bounds__(64 * N * N) void ns_short_poly_kernel(const double* __restrict__ part, int shares, float eps,
-                                                                   int steps, ShortCoefficients coef,
+                                                                   int first, int steps, ShortCoefficients coef,
                                                                    double* __restrict__ out) {
   constexpr int kTiles = N * (N + 1) / 2, kSide = 16 * N, kLd = kSide + 2;
   __shared__ double A[kSide * kLd], Q[kSide * kLd], P[kSide * kLd], B[N > 3 ? 1 : kSide * kLd];
@@ -486,7 +527,7 @@ __global__ __launch_bounds__(64 * N * N) void ns_short_poly_kernel(const double*
     t = wave_sum(t);
     if (lane == 0) {
       const double f = sqrt(t) + static_cast<double>(eps);
-      scale = f > 0.0 || f != f ? 1.0 / f : 0.0;
+      scale = !first ? 1.0 : f > 0.0 || f != f ? 1.0 / f : 0.0;
     }
   }
   __syncthreads();
@@ -537,10 +578,10 @@ __global__ __launch_bounds__(64 * N * N) void ns_short_poly_kernel(const double*
     out[(z * kSide + 16 * ti + 4 * v + quarter) * kSide + 16 * tj + row] = P[at(v)];
 }
 
-// O(:, c) = P U(:, c) for 256 c, stored or subtracted from W.
-template <int N, typename T, bool kStep>
+// O(:, c) = P U(:, c) for 256 c, stored or subtracted from W; before the last round (kLast false) X [z][q][p] is stored.
+template <int N, typename T, bool kStep, bool kLast>
 __global__ __launch_bounds__(256) void ns_short_apply_kernel(ShortU<T, kStep> U, const double* __restrict__ P, float keep,
-                                                             float gain, T* out) {
+                                                             float gain, T* out, double* __restrict__ X) {
   constexpr int kSide = 16 * N;
   extern __shared__ __align__(16) float lds[];
   const int64_t z = blockIdx.y;
@@ -567,9 +608,12 @@ __global__ __launch_bounds__(256) void ns_short_apply_kernel(ShortU<T, kStep> U,
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         const int k = 16 * i + 4 * v + quarter;
-        if (in && k < p) lds[k * sk + (c + row) * sc] = static_cast<float>(acc[i][v]);
+        if (!in || k >= p) continue;
+        if constexpr (kLast) lds[k * sk + (c + row) * sc] = static_cast<float>(acc[i][v]);
+        else X[(z * q + c0 + c + row) * p + k] = acc[i][v];
       }
   }
+  if constexpr (!kLast) return;
   __syncthreads();
   const int step = U.m <= U.n ? sc : sk;
   T* oz = out + z * U.m * static_cast<int64_t>(U.n);
@@ -588,6 +632,46 @@ __global__ __launch_bounds__(256) void ns_short_apply_kernel(ShortU<T, kStep> U,
         oz[at + e] = static_cast<T>(kStep ? fmaf(keep, static_cast<float>(oz[at + e]), -gain * from[e * step]) : from[e * step]);
     }
   });
+}
+
+// A later round's P X: X again (in place: a wave reads all of its columns before it writes them), or the result.
+template <int N, typename T, bool kStep, bool kLast>
+__global__ __launch_bounds__(256) void ns_short_reapply_kernel(double* X, const double* __restrict__ P, int m, int n, float keep,
+                                                               float gain, T* __restrict__ out) {
+  constexpr int kSide = 16 * N;
+  const int64_t z = blockIdx.y;
+  const int p = m < n ? m : n, q = m < n ? n : m;
+  const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+  const int row = lane & 15, quarter = lane >> 4;
+  const int c0 = static_cast<int>(blockIdx.x) * kShortBlock, count = q - c0 < kShortBlock ? q - c0 : kShortBlock;
+  const double* pz = P + z * kSide * kSide;
+  for (int c = wave * 16; c < count; c += 64) {
+    f64x4 acc[N] = {};
+    const bool in = c + row < count;
+    double* x = X + (z * q + c0 + c + (in ? row : 0)) * p;
+#pragma unroll 4
+    for (int k = 0; k < kSide; k += 4) {
+      const double u = in && k + quarter < p ? x[k + quarter] : 0.0;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        acc[i] = __builtin_amdgcn_mfma_f64_16x16x4f64(pz[(16 * i + row) * kSide + k + quarter], u, acc[i], 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int k = 16 * i + 4 * v + quarter;
+        if (!in || k >= p) continue;
+        if constexpr (kLast) {
+          const float o = static_cast<float>(acc[i][v]);
+          const int64_t at = m <= n ? static_cast<int64_t>(k) * n + c0 + c + row : static_cast<int64_t>(c0 + c + row) * n + k;
+          T* to = out + z * m * static_cast<int64_t>(n) + at;
+          *to = static_cast<T>(kStep ? fmaf(keep, static_cast<float>(*to), -gain * o) : o);
+        } else {
+          x[k] = acc[i][v];
+        }
+      }
+  }
 }
 
 // Shares of the long side of one matrix: blocks of 256, up to 256 shares and about 2048 workgroups.
@@ -609,6 +693,22 @@ struct NsArgs {
 
 double ns_bound(double a, double b, double c, double h);
 
+// The end of the round that starts with step k; h, the bound of the singular values, moves along.
+constexpr double kShortGrowth = 1 << 24;
+inline int ns_short_round(const NsArgs& g, int k, double& h) {
+  double grown = 1.0;
+  const int from = k;
+  for (; k < g.steps && (k == from || grown <= kShortGrowth); ++k) {
+    const double a = g.coef[3 * k], b = g.coef[3 * k + 1], c = g.coef[3 * k + 2];
+    auto q = [&](double s) { return fabs(a + s * (b + s * c)); };
+    double top = fmax(q(0.0), q(h * h));
+    if (c != 0.0 && -b / (2.0 * c) > 0.0 && -b / (2.0 * c) < h * h) top = fmax(top, q(-b / (2.0 * c)));
+    grown *= fmax(1.0, top * top);
+    h = ns_bound(a, b, c, h);
+  }
+  return k;
+}
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline int round_up(int v, int to) { return (v + to - 1) / to * to; }
 
@@ -616,7 +716,7 @@ size_t ns_workspace(int64_t batch, int32_t m, int32_t n, bool split) {
   if (ns_short(m, n)) {
     const size_t tiles = ((m < n ? m : n) + 15) / 16, b = static_cast<size_t>(batch);
     return align_up(b * ns_short_shares(batch > 0 ? batch : 1, m < n ? n : m) * (tiles * (tiles + 1) / 2) * 2048, 256) +
-           align_up(b * tiles * tiles * 2048, 256);
+           align_up(b * tiles * tiles * 2048, 256) + align_up(b * m * n * 8, 256);
   }
   const int pad = split ? 32 : 8;
   const size_t b = static_cast<size_t>(batch), mp = round_up(m, pad), np = round_up(n, pad), p = mp < np ? mp : np,
@@ -751,17 +851,28 @@ lipcache_status ns_short_run(const NsArgs& g, const T* G, float* M, float mu, in
   double* part = static_cast<double*>(ws);
   double* P = reinterpret_cast<double*>(static_cast<char*>(ws) +
                                         align_up(static_cast<size_t>(g.batch) * shares * (N * (N + 1) / 2) * 2048, 256));
-  ShortCoefficients coef{};
-  for (int i = 0; i < 3 * g.steps; ++i) coef.c[i] = g.coef[i];
-  ns_short_gram_kernel<N, T, kStep><<<dim3(shares, nb), 256, lds, s>>>(U, shares, part);
-  LC_LAUNCHED();
+  double* X = reinterpret_cast<double*>(reinterpret_cast<char*>(P) + align_up(static_cast<size_t>(g.batch) * N * N * 2048, 256));
   constexpr size_t kMore = N > 3 ? 16 * N * (16 * N + 2) * 8 : 0;
-  ns_short_poly_kernel<N><<<nb, 64 * N * N, kMore, s>>>(part, shares, g.eps, g.steps, coef, P);
-  LC_LAUNCHED();
-  ns_short_apply_kernel<N, T, kStep><<<dim3(static_cast<unsigned>((q + kShortBlock - 1) / kShortBlock), nb), 256, lds, s>>>(
-      U, P, keep, gain, out);
-  LC_LAUNCHED();
-  return LIPCACHE_OK;
+  const dim3 blocks(static_cast<unsigned>((q + kShortBlock - 1) / kShortBlock), nb);
+  double h = 1.0;
+  for (int k = 0, first = 1;; first = 0) {
+    const int end = ns_short_round(g, k, h);
+    const bool last = end == g.steps;
+    ShortCoefficients coef{};
+    for (int i = 0; i < 3 * (end - k); ++i) coef.c[i] = g.coef[3 * k + i];
+    if (first) ns_short_gram_kernel<N, T, kStep><<<dim3(shares, nb), 256, lds, s>>>(U, shares, part);
+    else ns_short_regram_kernel<N><<<dim3(shares, nb), 256, 0, s>>>(X, p, q, shares, part);
+    LC_LAUNCHED();
+    ns_short_poly_kernel<N><<<nb, 64 * N * N, kMore, s>>>(part, shares, g.eps, first, end - k, coef, P);
+    LC_LAUNCHED();
+    if (first && last) ns_short_apply_kernel<N, T, kStep, true><<<blocks, 256, lds, s>>>(U, P, keep, gain, out, X);
+    else if (first) ns_short_apply_kernel<N, T, kStep, false><<<blocks, 256, lds, s>>>(U, P, keep, gain, out, X);
+    else if (last) ns_short_reapply_kernel<N, T, kStep, true><<<blocks, 256, 0, s>>>(X, P, g.m, g.n, keep, gain, out);
+    else ns_short_reapply_kernel<N, T, kStep, false><<<blocks, 256, 0, s>>>(X, P, g.m, g.n, keep, gain, out);
+    LC_LAUNCHED();
+    if (last) return LIPCACHE_OK;
+    k = end;
+  }
 }
 
 template <class E, typename T, bool kStep>

@@ -32,3 +32,83 @@ def test_steps_on_16_bits_lose_only_the_rounding_of_the_result(shape, dtype):
         again = torch.zeros_like(G)
         api.muon_step(again, G, torch.zeros(shape, device=DEV), lr=1.0, momentum=0.5, scale=1.0, short_operands=short)
         assert torch.equal(W, again), "two calls differ"
+
+
+CUBIC = (15 / 8, -10 / 8, 3 / 8)
+
+
+def deficient(seed, kind, b, m, n, dtype):
+    """Matrices of whole numbers with an exact null space: rank 1, rank 4, equal halves, rows of zero; or full rank."""
+    g = torch.Generator().manual_seed(seed)
+    p = min(m, n)
+    ints = lambda *s: torch.randint(-3, 4, s, generator=g).float()  # noqa: E731
+    if kind in ("rank 1", "rank 4"):
+        k = min(1 if kind == "rank 1" else 4, p)
+        G = ints(b, m, k) @ ints(b, k, n)
+    else:
+        G = ints(b, p, max(m, n)) + torch.eye(p, max(m, n))
+        if kind == "halves":
+            G[:, p // 2:2 * (p // 2)] = G[:, :p // 2]
+        elif kind == "zeros":
+            G[:, 1::3] = 0
+        G = G if m <= n else G.transpose(1, 2).contiguous()
+    out = G.to({"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[dtype])
+    assert torch.equal(out.float(), G) and bool((G.abs().sum((1, 2)) > 0).all())
+    return out.to(DEV)
+
+
+def by_singular_values(G, coefficients, eps):
+    """The iteration on the singular values, in float64: what is zero stays zero.  Also the projector on G's columns."""
+    u, s, vt = np.linalg.svd(G, full_matrices=False)
+    s = np.where(s > 1e-9 * s[:, :1], s, 0.0)
+    t = s / (np.sqrt(np.sum(s * s, axis=1, keepdims=True)) + eps)
+    for a, b, c in coefficients:
+        t = t * (a + t * t * (b + c * t * t))
+    u1 = u * (s > 0)[:, None, :]
+    return (u * t[:, None, :]) @ vt, u1 @ u1.transpose(0, 2, 1)
+
+
+def amplified(coefficients):
+    """What the steps make of float64's rounding, 2^-53, in directions that G does not have."""
+    return 2.0 ** -53 * float(np.prod([max(1.0, abs(c[0])) for c in coefficients]))
+
+
+@pytest.mark.parametrize("kind", ["rank 1", "rank 4", "halves", "zeros", "full"])
+@pytest.mark.parametrize("shape", [(2, 8, 256), (3, 16, 40), (1, 300, 30), (2, 33, 500), (1, 64, 256), (1, 256, 64), (1, 1, 9)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_short_matrices_and_many_steps(shape, kind):
+    """Singular values stay below the last step's bound, and the result is the float64 one, also on a null space."""
+    for dtype in ("f32", "bf16"):
+        G = deficient(sum(shape), kind, *shape, dtype)
+        for name, one, counts in (("usual", api.NEWTON_SCHULZ, (7, 8, 12, 16, 20, 32)), ("cubic", CUBIC, (12, 24, 32))):
+            one = tuple(float(np.float32(c)) for c in one)
+            for steps in counts:
+                say("many steps", shape, kind, dtype, name, steps)
+                O = n64(api.orthogonalise(G, steps=steps, coefficients=one))
+                assert np.isfinite(O).all()
+                # rounding to bfloat16 moves a singular value by at most 2^-8 of the Frobenius norm
+                slack = 1e-5 + (2.0 ** -8 * np.sqrt(min(shape[1:])) if dtype == "bf16" else 0.0)
+                assert np.linalg.svd(O, compute_uv=False).max() <= 1.21 + slack
+                ref, columns = by_singular_values(n64(G), [one] * steps, float(np.float32(1e-7)))
+                grown = 64 * amplified([one] * steps)
+                off = O - ref if grown < 1e-5 else columns @ (O - ref)  # what rounding makes of nothing is no error
+                tol = R.NS_TOL["f32"] + (R.U["bf16"] if dtype == "bf16" else 0.0) + min(1e-5, grown)
+                assert np.linalg.norm(off) <= tol * np.linalg.norm(ref), np.linalg.norm(off) / np.linalg.norm(ref)
+        G = deficient(sum(shape), kind, *shape, dtype)
+        W, M = torch.zeros_like(G), torch.zeros(shape, device=DEV)
+        api.muon_step(W, G, M, lr=1.0, momentum=0.5, nesterov=False, scale=1.0, steps=16)
+        assert np.array_equal(n64(M), n64(G))
+        ref, _ = by_singular_values(n64(G), [tuple(float(np.float32(c)) for c in api.NEWTON_SCHULZ)] * 16, float(np.float32(1e-7)))
+        assert far(W, -ref) <= R.NS_TOL["f32"] + (R.U["bf16"] if dtype == "bf16" else 0.0) + 1e-5
+
+
+@pytest.mark.parametrize("kind", ["rank 1", "halves", "full"])
+@pytest.mark.parametrize("shape", [(2, 72, 200), (1, 150, 70)], ids=lambda s: "x".join(map(str, s)))
+def test_other_matrices_and_many_steps(shape, kind):
+    """Shorter sides above 64 iterate on X itself: singular values stay bounded whatever the steps."""
+    for dtype in ("f32", "f16"):
+        G = deficient(sum(shape), kind, *shape, dtype)
+        for steps in (8, 16, 32):
+            say("many steps", shape, kind, dtype, steps)
+            s = np.linalg.svd(n64(api.orthogonalise(G, steps=steps)), compute_uv=False)
+            assert s.max() <= 1.21 + 1e-3  # float16: 2^-11 of a norm of at most 9 at random angles
