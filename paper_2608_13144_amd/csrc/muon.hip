@@ -751,6 +751,14 @@ inline NsTile ns_tile(int64_t tiles128, int64_t large, NsTile large_tile) {
   return tiles128 < 320 ? kNs128Deep : kNs128;
 }
 
+constexpr int tile_side(NsTile t) { return t == kNs64 ? 64 : t == kNs192 ? 192 : t == kNs256 ? 256 : 128; }
+
+// A tile's copies reach offsets below 2^31 bytes.  Rows along the long side of a wide matrix take smaller tiles where they
+// would pass that; parts of the contraction that run across such rows (32 of 22-bit operands, 64 of 11-bit ones) do not.
+constexpr int64_t kLongest = (1ll << 30) / (kShortMost + 1) + 32;  // elements, padded
+static_assert(31 * 4 * kLongest + 4096 < (1ll << 31) && 63 * 2 * kLongest + 4096 < (1ll << 31), "offsets of a tile's copies");
+inline bool rows_fit(int rows, int64_t ld) { return (rows - 1) * ld + 128 <= 0x7fffffff; }
+
 struct NsPlan {
   int m8, n8;
   unsigned nb;
@@ -768,7 +776,13 @@ struct NsPlan {
   void square(const _Float16* F, int k8, int width, const _Float16* in, double f_sum, double f_in, _Float16* out) const {
     const int p8 = m8 < n8 ? m8 : n8;
     const int64_t t128 = tiles_of(p8, 128), t192 = tiles_of(p8, 192);
-    switch (ns_tile(t128 * (t128 + 1) / 2 * nb, kCol ? 0 : t192 * (t192 + 1) / 2 * nb, kNs192)) {
+    NsTile tile = ns_tile(t128 * (t128 + 1) / 2 * nb, kCol ? 0 : t192 * (t192 + 1) / 2 * nb, kNs192);
+    if constexpr (!kCol) {
+      const int64_t ld = static_cast<int64_t>(width) * static_cast<int64_t>(sizeof(E));
+      if (!rows_fit(tile_side(tile), ld)) tile = kNs64;
+      if (!rows_fit(64, ld)) return square_with<TileShape<E, 32, 32, 1, 1, 4, 4, 2, false, false>>(F, k8, width, in, f_sum, f_in, out);
+    }
+    switch (tile) {
       case kNs64: return square_with<TileShape<E, 64, 64, 2, 2, 1, 3, 1, kCol, kCol>>(F, k8, width, in, f_sum, f_in, out);
       case kNs128Deep: return square_with<TileShape<E, 128, 128, 2, 4, 1, 4, 1, kCol, kCol>>(F, k8, width, in, f_sum, f_in, out);
       case kNs192:

@@ -112,3 +112,35 @@ def test_other_matrices_and_many_steps(shape, kind):
             say("many steps", shape, kind, dtype, steps)
             s = np.linalg.svd(n64(api.orthogonalise(G, steps=steps)), compute_uv=False)
             assert s.max() <= 1.21 + 1e-3  # float16: 2^-11 of a norm of at most 9 at random angles
+
+
+@pytest.mark.parametrize("n,what", [(8_600_000, "f32"), (16_519_104, "bf16"), (16_519_104, "step"), (16_519_104, "short step")])
+def test_rows_past_31_bits(n, what):
+    """65 rows so long that a tile of 64 of them passes 2^31 bytes; one step, against float64 in pieces."""
+    m, coef = 65, tuple(float(np.float32(c)) for c in api.NEWTON_SCHULZ)
+    say("long rows", n, what)
+    g = torch.Generator(device=DEV).manual_seed(n)
+    G = torch.randn(m, n, generator=g, device=DEV, dtype=torch.float32 if what == "f32" else torch.bfloat16)
+    if what in ("f32", "bf16"):
+        O = api.orthogonalise(G, steps=1, eps=0.0)
+        sign = 1.0
+    else:
+        O, M, sign = torch.zeros_like(G), torch.zeros(m, n, device=DEV), -1.0
+        api.muon_step(O, G, M, lr=1.0, momentum=0.5, nesterov=False, scale=1.0, steps=1, eps=0.0, short_operands=what == "short step")
+        del M
+    pieces = [slice(c, min(c + (1 << 20), n)) for c in range(0, n, 1 << 20)]
+    P = torch.zeros(m, m, dtype=torch.float64, device=DEV)
+    for c in pieces:
+        x = G[:, c].double()
+        P += x @ x.t().contiguous()
+    size = P.trace()
+    P /= size
+    B = coef[0] * torch.eye(m, dtype=torch.float64, device=DEV) + coef[1] * P + coef[2] * (P @ P)
+    wrong = ref2 = 0.0
+    for c in pieces:
+        ref = sign * (B @ (G[:, c].double() / size.sqrt()))
+        wrong += float(((O[:, c].double() - ref) ** 2).sum())
+        ref2 += float((ref ** 2).sum())
+    # one step: float32's error is below a step's share of five; 11-bit operands as in NS_TOL
+    own = 0.0 if what == "f32" else R.U["bf16"]
+    assert (wrong / ref2) ** 0.5 <= own + R.NS_TOL["f32"] + (2.6e-3 if what == "short step" else 0.0)
