@@ -14,6 +14,7 @@
 #include <type_traits>
 
 #include "lc_common.hpp"
+#include "lc_group.hpp"
 #include "lc_mfma.hpp"
 
 namespace lc {
@@ -45,21 +46,21 @@ __host__ __device__ inline int64_t ad_tiles(int64_t T, int S) { return T / kThin
 constexpr int kGroupThreads = 1024;
 constexpr int kGroupRound = 2 * kGroupThreads;  // requests that the workgroup takes at a time
 
-// Inclusive sums over the workgroup's threads, in LDS (`sums`, one word a
+// Inclusive sums over the workgroup's threads, at most T, in LDS (`sums`, one word a
 // thread; `waves`, one a wave).  Ends with a barrier.
-__device__ __forceinline__ void group_scan(int v, int32_t* sums, int32_t* waves) {
+__device__ __forceinline__ void group_scan(uint32_t v, uint32_t T, uint32_t* sums, uint32_t* waves) {
   const int tid = static_cast<int>(threadIdx.x), lane = lane_id(), wave = tid / kWave;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
-    const int u = __shfl_up(v, o, kWave);
-    if (lane >= o) v += u;
+    const uint32_t u = __shfl_up(v, o, kWave);
+    if (lane >= o) v = group_add(v, u, T);
   }
   if (lane == kWave - 1) waves[wave] = v;
   __syncthreads();
-  int before = 0;
+  uint32_t before = 0;
 #pragma unroll
-  for (int w = 0; w < kGroupThreads / kWave; ++w) before += w < wave ? waves[w] : 0;
-  sums[tid] = before + v;
+  for (int w = 0; w < kGroupThreads / kWave; ++w) before = group_add(before, w < wave ? waves[w] : 0, T);
+  sums[tid] = group_add(before, v, T);
   __syncthreads();
 }
 
@@ -68,22 +69,23 @@ __device__ __forceinline__ void group_scan(int v, int32_t* sums, int32_t* waves)
 // requests in order, 2048 at a time, two neighbours a thread (whose loads go
 // out together).  Request -1 is the rows before the first offset, request R
 // those after the last.  Offsets that decrease place rows
-// wrongly or not at all; every index is checked, and places left over hold row
-// 0 without a pair, so whatever they are no access leaves the arrays.  Bound
+// wrongly or not at all: counts may wrap and pairs' places overlap, but a pair fills at least the places up to the next one's
+// first, the last workgroup the rest, with rows below T (sums stop there), so whatever they are no access leaves the arrays.  Bound
 // by latency (one round of loads, then scans and a search in LDS): 6 us for 64 pairs and 1024 requests, 9 us for four
 // pairs of 2048 rows each.
 __global__ __launch_bounds__(kGroupThreads) void ad_group_kernel(int64_t t0, int T, const int32_t* __restrict__ offsets,
                                                                  const int32_t* __restrict__ adapter, int R, int S,
                                                                  AdGroups g) {
-  extern __shared__ int32_t count[];        // [S + 1] rows of each pair, then scratch
-  int32_t* sums = count + S + 1;            // [kGroupThreads]
-  int32_t* first = sums + kGroupThreads;    // [kGroupRound]
-  int32_t* some = first + kGroupRound;      // [kGroupThreads] rows of a thread's first request
-  int32_t* waves = some + kGroupThreads;    // [kGroupThreads / kWave]
+  extern __shared__ uint32_t count[];       // [S + 1] rows of each pair, then scratch
+  uint32_t* sums = count + S + 1;           // [kGroupThreads]
+  uint32_t* first = sums + kGroupThreads;   // [kGroupRound]
+  uint32_t* some = first + kGroupRound;     // [kGroupThreads] rows of a thread's first request
+  uint32_t* waves = some + kGroupThreads;   // [kGroupThreads / kWave]
   __shared__ unsigned long long base_rows, base_tiles;
   const int tid = static_cast<int>(threadIdx.x), s = static_cast<int>(blockIdx.x);
+  const uint32_t all = static_cast<uint32_t>(T), last = static_cast<uint32_t>(ad_tiles(T, S));
   // rows of request i >= -1 (none past R).  Three loads that wait for nothing, least of all each other.
-  auto request = [&](int i, int& lo, int& key) {
+  auto request = [&](int i, uint32_t& lo, int& key) {
     int64_t a = t0, b = t0 + T;
     int p = -1;
     if (R > 0) {
@@ -95,12 +97,13 @@ __global__ __launch_bounds__(kGroupThreads) void ad_group_kernel(int64_t t0, int
     } else if (i < 0) {
       b = t0;
     }
-    const int64_t l = a < t0 ? t0 : a, h = b > t0 + T ? t0 + T : b;
-    lo = static_cast<int>(l - t0);
+    const GroupRows rows = group_clamp(a, b, t0, all);
+    lo = rows.first;
     key = p >= 0 && p < S ? p : S;
-    return i <= R && h > l ? static_cast<int>(h - l) : 0;
+    return i <= R ? rows.count : 0;
   };
-  int lo[2], key[2], n[2];  // this thread's requests among the first 2048
+  int key[2];
+  uint32_t lo[2], n[2];  // this thread's requests among the first 2048
 #pragma unroll
   for (int e = 0; e < 2; ++e) n[e] = request(2 * tid + e - 1, lo[e], key[e]);
   for (int i = tid; i <= S; i += kGroupThreads) count[i] = 0;
@@ -110,15 +113,15 @@ __global__ __launch_bounds__(kGroupThreads) void ad_group_kernel(int64_t t0, int
   for (int e = 0; e < 2; ++e)
     if (n[e] > 0) atomicAdd(&count[key[e]], n[e]);
   for (int i = tid - 1 + kGroupRound; i <= R; i += kGroupThreads) {
-    int l, k;
-    const int rows = request(i, l, k);
+    int k;
+    uint32_t l;
+    const uint32_t rows = request(i, l, k);
     if (rows > 0) atomicAdd(&count[k], rows);
   }
   __syncthreads();
   unsigned long long rows = 0, tiles = 0;
-  const uint32_t all = static_cast<uint32_t>(T), last = static_cast<uint32_t>(ad_tiles(T, S));
   for (int i = tid; i < s; i += kGroupThreads) {
-    const uint32_t n = static_cast<uint32_t>(count[i]);
+    const uint32_t n = count[i];
     rows += n;
     tiles += ((n < all ? n : all) + kThinRows - 1) / kThinRows;  // as many as the pair writes below
   }
@@ -135,7 +138,7 @@ __global__ __launch_bounds__(kGroupThreads) void ad_group_kernel(int64_t t0, int
   }
   __syncthreads();
   const uint64_t place0 = base_rows;
-  const uint32_t mine = static_cast<uint32_t>(count[s]);
+  const uint32_t mine = count[s];
   if (tid == 0) {
     g.start[s] = static_cast<int32_t>(place0 < all ? place0 : all);
     g.tile_start[s] = static_cast<int32_t>(base_tiles < last ? base_tiles : last);
@@ -160,24 +163,17 @@ __global__ __launch_bounds__(kGroupThreads) void ad_group_kernel(int64_t t0, int
       for (int e = 0; e < 2; ++e) n[e] = request(i0 + 2 * tid + e, lo[e], key[e]);
       __syncthreads();  // the last round's readers are done
     }
-    const int n0 = key[0] == s ? n[0] : 0, n1 = key[1] == s ? n[1] : 0;
+    const uint32_t n0 = key[0] == s ? n[0] : 0, n1 = key[1] == s ? n[1] : 0;
     first[2 * tid] = lo[0];
     first[2 * tid + 1] = lo[1];
     some[tid] = n0;
-    group_scan(n0 + n1, sums, waves);
-    const int total = sums[kGroupThreads - 1];
-    for (int p = tid; p < total && place + p < all; p += kGroupThreads) {
-      int a = 0, b = kGroupThreads - 1;  // the thread whose requests hold the p-th row: the first whose sum passes p
-      while (a < b) {
-        const int mid = (a + b) >> 1;
-        if (sums[mid] > p) b = mid; else a = mid + 1;
-      }
-      const int in = p - (a > 0 ? sums[a - 1] : 0), n_a = some[a];
-      const uint32_t row = static_cast<uint32_t>(in < n_a ? first[2 * a] + in : first[2 * a + 1] + in - n_a);
-      g.order[place + p] = row < all ? static_cast<int32_t>(row) : 0;
+    group_scan(group_add(n0, n1, all), all, sums, waves);
+    const uint32_t total = sums[kGroupThreads - 1];
+    for (uint32_t p = tid; p < total && place + p < all; p += kGroupThreads) {
+      g.order[place + p] = static_cast<int32_t>(group_row(sums, some, first, kGroupThreads, p, all));
       g.pair[place + p] = s;
     }
-    place += total > 0 ? total : 0;
+    place += total;
   }
   if (s == S)
     for (uint64_t p = place + tid; p < all; p += kGroupThreads) {
