@@ -164,25 +164,24 @@ __global__ __launch_bounds__(256) void ns_start_kernel(const T* __restrict__ G, 
                                                        _Float16* __restrict__ Xlow) {
   __shared__ double lds;
   const int64_t z = blockIdx.y, size = static_cast<int64_t>(m) * n, groups = static_cast<int64_t>(m8) * n8 / 8;
-  const float f = static_cast<float>(ns_inverse(part + z * chunks, chunks, eps, &lds) * scale);
+  // as mantissa and exponent: the factor itself may pass float32's range where U is tiny (or huge) and eps 0
+  int up;
+  const float f = static_cast<float>(frexp(ns_inverse(part + z * chunks, chunks, eps, &lds) * scale, &up));
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < groups; i += 256 * static_cast<int64_t>(gridDim.x)) {
     const int row = static_cast<int>(i / (n8 / 8)), col = static_cast<int>(i % (n8 / 8)) * 8;
     float u[8] = {};
     if (row < m && col < n)
       ns_direction8<T, kStep, false>(G, M, z * size + static_cast<int64_t>(row) * n + col, n - col, wide != 0, mu, nesterov, u);
-    f32x4 lo, hi;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      lo[e] = f * u[e];
-      hi[e] = f * u[e + 4];
-    }
+    for (int e = 0; e < 8; ++e) u[e] = f * ldexpf(u[e], up);
+    const f32x4 lo = {u[0], u[1], u[2], u[3]}, hi = {u[4], u[5], u[6], u[7]};
     const int64_t at = NsAt<E>::at(z * m8 + row, col, n8);
     if constexpr (NsAt<E>::kLow) {
       f16x8 first, second;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         _Float16 p, r;
-        split_f16(f * u[e], p, r);
+        split_f16(u[e], p, r);
         first[e] = p;
         second[e] = r;
       }

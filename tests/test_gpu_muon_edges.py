@@ -144,3 +144,19 @@ def test_rows_past_31_bits(n, what):
     # one step: float32's error is below a step's share of five; 11-bit operands as in NS_TOL
     own = 0.0 if what == "f32" else R.U["bf16"]
     assert (wrong / ref2) ** 0.5 <= own + R.NS_TOL["f32"] + (2.6e-3 if what == "short step" else 0.0)
+
+
+@pytest.mark.parametrize("shape", [(2, 12, 50), (2, 150, 140), (1, 90, 300)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype,size", [("f32", 1e-37), ("f32", 3e-41), ("f32", 6e37), ("bf16", 1e-37), ("bf16", 6e37), ("f16", 1e-6)])
+def test_matrices_near_the_ends_of_the_range(shape, dtype, size):
+    """No eps: 1 / ||G|| and its multiples pass float32's range, the result does not."""
+    say("ends of the range", shape, dtype, size)
+    H = matrices(50, *shape, dtype, size=size)
+    assert bool(H.isfinite().all()) and bool((H != 0).any())
+    ref = R.newton_schulz(n64(H), 5, NS5, 0.0)
+    O = api.orthogonalise(H, eps=0.0)
+    assert far(O, ref) <= R.NS_TOL[dtype], far(O, ref)
+    W, M = torch.zeros_like(H), H.float() / 4
+    api.muon_step(W, torch.zeros_like(H), M, lr=1.0, momentum=2.0, nesterov=False, scale=1.0, eps=0.0)
+    ref = R.newton_schulz(n64(M), 5, NS5, 0.0)
+    assert far(W, -ref) <= R.NS_TOL[dtype], far(W, -ref)
