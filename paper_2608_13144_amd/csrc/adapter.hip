@@ -227,7 +227,8 @@ __device__ __forceinline__ void factor_parts(float v, E (&part)[kFactorParts<E>]
 // float16 ends at 65504 and loses digits below 2^-14, where A_a x and B_a^T dy
 // may lie (gradients of a mean over many rows, outliers of a wide sum).  Such
 // factors go to the matrix cores times 2^e, which brings the largest finite one
-// of a tile to [2^14, 2^15), and what comes out is taken back by 2^-e in float32.
+// of a row (in the pairs' gradients, of a tile) to [2^14, 2^15), and what comes out is taken back by 2^-e in float32.
+// Rows keep exponents of their own, so that one request's size costs another's rows no digits.
 // bfloat16 has float32's range and takes them as they are.
 template <class E>
 inline constexpr bool kScaledFactors = std::is_same_v<E, _Float16>;
@@ -454,12 +455,12 @@ __device__ __forceinline__ void add_low_rank(const AdLow& low, const AdTileRows<
       const uint32_t mask = static_cast<uint32_t>(__ballot(mine));
       todo &= ~mask;
       const float scale = rows.scale[tm];  // of this lane's row: its own where `mine`
-      int up = 0;
+      int up = 0, up_of[16];  // of this lane's row; of the accumulators' rows
       if constexpr (kScaledFactors<E>) {
-        float top = mine ? finite_size(scale * rows.peak[tm]) : 0.0f;
-#pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+        const float top = mine ? finite_size(scale * rows.peak[tm]) : 0.0f;
         up = top > 0.0f ? factor_exponent(top) : 0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) up_of[e] = __shfl(up, acc_row(e) + 4 * half, kWave);
       }
 #pragma unroll
       for (int tn = 0; tn < S::TN; ++tn) {
@@ -494,7 +495,7 @@ __device__ __forceinline__ void add_low_rank(const AdLow& low, const AdTileRows<
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (mask >> (acc_row(e) + 4 * half) & 1) acc[tm][tn][e] += two_to<E>(sum[e], -up);
+          if (mask >> (acc_row(e) + 4 * half) & 1) acc[tm][tn][e] += two_to<E>(sum[e], kScaledFactors<E> ? -up_of[e] : 0);
       }
     }
   }

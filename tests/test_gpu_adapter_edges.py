@@ -85,3 +85,40 @@ def test_backward_keeps_every_digit_of_what_lies_between(dtype, T, r):
     dB = torch.stack([dz[pair == a].double().T @ v[pair == a].double() for a in range(S)])
     assert torch.equal(out.dB.double().cpu(), exact(dB))
     assert np.isfinite(n64(out.dB)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T", [64, 700, 8300])
+def test_rows_of_other_requests_cost_no_digits(dtype, T):
+    """Every fifth row's A x (B^T dy) is 2^35, the others' below 2^12 with eight digits after the point: none of them is lost."""
+    say("rows of different size", T, dtype)
+    g = torch.Generator().manual_seed(T)
+    S, r, K, N = 1, 3, 64, 64
+    rho = torch.arange(N) % r
+    big = torch.zeros(T, dtype=torch.bool)
+    big[::5] = True
+
+    def rows(top):  # whole numbers / 256 in the first half of the columns, or 2^15 in the second
+        x = torch.zeros(T, 64)
+        x[:, :32] = ints(g, 0, top, T, 32) / 256
+        x[big, :32] = 0
+        x[big, 32:] = 32768
+        return x
+    half = torch.zeros(64)
+    half[:32] = 1
+    A = ints(g, 0, 100, S, r, K) * half + 32768 * (1 - half)
+    B = one_hot(r, rho).expand(S, N, r).contiguous()
+    keep = torch.arange(N) % 32
+    W = one_hot(K, keep) - A[0][rho]  # y = x[keep]
+    x = rows(255)
+    b, _ = batch(T, S, g, dtype, x, W, A, B)
+    y = api.adapter_forward(b["x"], b["W"], None, b["A"], b["B"], b["scale"], b["offsets"], b["adapter"]).y
+    assert torch.equal(y.float().cpu(), x[:, keep])
+    # backward: dx = dy in the first half, zero in the second
+    A = ints(g, 0, 1, S, r, K)
+    B = (one_hot(r, rho) * (ints(g, 1, 100, N, 1) * half[:, None] + 32768 * (1 - half[:, None]))).expand(S, N, r).contiguous()
+    W = torch.diag(half) - B[0] @ A[0]
+    dy = rows(255)
+    b, _ = batch(T, S, g, dtype, x, W, A, B)
+    out = api.adapter_backward(dy.to(DT[dtype]).to(DEV), *[b[k] for k in ("x", "W", "A", "B", "scale", "offsets", "adapter")])
+    assert torch.equal(out.dx.float().cpu(), dy * half)
