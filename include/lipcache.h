@@ -485,7 +485,8 @@ typedef struct lipcache_adapters {
  * not finite stays in its own request's rows (in W or bias: in its outputs).
  *
  *  x [T][K] (ldx), W [N][K] (ldw), bias [N] float or NULL
- *  y [T][N] (ldy) out;  v [T][r] float out, or NULL (the backward pass takes it)
+ *  y [T][N] (ldy) out;  v [T][r] float out, or NULL (the backward pass takes it);
+ *  neither overlaps an input
  *  ws lipcache_adapter_forward_workspace_bytes(T, K, N, r, S, dtype) bytes
  * T = 0 is valid and does nothing. (async)
  */
@@ -508,7 +509,7 @@ size_t lipcache_adapter_forward_workspace_bytes(int64_t T, int32_t K, int32_t N,
  *  dy [T][N] (lddy), x [T][K] (ldx), W [N][K] (ldw)
  *  v  [T][r] float of the forward pass, or NULL (computed again)
  *  dx [T][K] (lddx) out, or NULL;  dA [S][r][K], dB [S][N][r] out, both or
- *  neither NULL
+ *  neither NULL;  none overlaps an input
  *  ws lipcache_adapter_backward_workspace_bytes(T, K, N, r, S, dtype) bytes
  * T = 0 writes zeros to dA and dB. (async)
  */

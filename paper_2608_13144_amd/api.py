@@ -465,7 +465,8 @@ def adapter_forward(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None,
     lie apart), bias float32 [N] or None, A [S, r, K], B [S, N, r], scale
     float32 [S]; request i owns the rows offsets[i]:offsets[i + 1] (int32,
     R + 1 of them) and names the pair adapter[i] (int32, -1: none).  ``keep``
-    also returns v, which the backward pass takes."""
+    also returns v, which the backward pass takes; ``out.v``, if it is there, is
+    written without it.  ``out`` must not overlap what is read."""
     code = _dtype(x, "x")
     dev, dt = x.device, x.dtype
     if x.dim() != 2 or W.dim() != 2:
@@ -483,7 +484,9 @@ def adapter_forward(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None,
         ldy = N
     else:
         ldy = _need_rows(out.y, "out.y", dt, dev, T, N)
-        if out.v is not None:
+        if out.v is None and keep:
+            out.v = torch.empty((T, ad.r), dtype=torch.float32, device=dev)
+        elif out.v is not None:
             _need_shape(out.v, "out.v", torch.float32, dev, (T, ad.r))
     lib = L.load()
     ws = workspace(lib.lipcache_adapter_forward_workspace_bytes(T, K, N, ad.r, ad.S, code), dev)

@@ -122,3 +122,20 @@ def test_rows_of_other_requests_cost_no_digits(dtype, T):
     b, _ = batch(T, S, g, dtype, x, W, A, B)
     out = api.adapter_backward(dy.to(DT[dtype]).to(DEV), *[b[k] for k in ("x", "W", "A", "B", "scale", "offsets", "adapter")])
     assert torch.equal(out.dx.float().cpu(), dy * half)
+
+
+@pytest.mark.parametrize("T", [40, 300])
+def test_keep_with_an_output_of_the_callers(T):
+    g = torch.Generator().manual_seed(T)
+    b, _ = batch(T, 2, g, "f32", ints(g, -9, 9, T, 96), ints(g, -9, 9, 40, 96), ints(g, -9, 9, 2, 4, 96), ints(g, -9, 9, 2, 40, 4))
+    args = [b["x"], b["W"], None] + [b[k] for k in ("A", "B", "scale", "offsets", "adapter")]
+    ref = api.adapter_forward(*args, keep=True)
+    out = api.AdapterOutput(torch.empty_like(ref.y), None)
+    y = out.y
+    assert api.adapter_forward(*args, keep=True, out=out) is out and out.y is y
+    assert out.v is not None and torch.equal(out.v, ref.v) and torch.equal(out.y, ref.y)
+    out = api.AdapterOutput(torch.empty_like(ref.y), None)
+    assert api.adapter_forward(*args, out=out).v is None and torch.equal(out.y, ref.y)
+    out = api.AdapterOutput(torch.empty_like(ref.y), torch.empty_like(ref.v))
+    v = out.v
+    assert api.adapter_forward(*args, out=out).v is v and torch.equal(v, ref.v)
