@@ -450,7 +450,7 @@ lipcache_status lipcache_lookup_filter_dump(const lipcache_cache* c, const float
  * sites share.  Their matrices take float32, bfloat16 or float16 (`dtype`),
  * any sizes >= 1, and rows at a stride where an `ld*` argument is given (in
  * elements, at least the row's width).  Widths reach 2^20, rows 2^31 - 1,
- * pairs 8,192 and stacks 65,535 (beyond: EUNSUPPORTED).  16-bit rows that start on 16-byte
+ * pairs 8,192, requests 2^30 and stacks 65,535 (beyond: EUNSUPPORTED).  16-bit rows that start on 16-byte
  * boundaries are read in place; others are first copied into the workspace.
  * A workspace may be reused by the next call on the same stream.
  */

@@ -21,11 +21,23 @@ namespace lc {
 
 constexpr int kAdMaxRank = 128;
 constexpr int kAdMaxPairs = 8192;
+constexpr int kAdMaxRequests = 1 << 30;
 constexpr int64_t kAdMaxWidth = 1 << 20;
 constexpr int kThinRows = 32;  // sorted rows of one pair that a workgroup of the thin products takes
 
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// A launch holds fewer than 2^32 threads.  Kernels whose workgroups may be more take the first one's number, a pass after another.
+constexpr int64_t kMostBlocks = 1 << 23;
+template <class F>
+lipcache_status in_passes(int64_t blocks, F launch) {
+  for (int64_t first = 0; first < blocks; first += kMostBlocks) {
+    launch(first, static_cast<unsigned>(blocks - first < kMostBlocks ? blocks - first : kMostBlocks));
+    LC_LAUNCHED();
+  }
+  return LIPCACHE_OK;
+}
 
 // ---------------------------------------------------------------- grouping
 // Rows sorted by pair (rows without one last), and the table of the thin
@@ -265,16 +277,17 @@ struct AdCopies {
 };
 
 template <typename T>
-__global__ __launch_bounds__(256) void ad_copy_kernel(AdCopies all) {
+__global__ __launch_bounds__(256) void ad_copy_kernel(AdCopies all, int64_t first) {
   __shared__ T tile[32][33];
   const int x = static_cast<int>(threadIdx.x) & 31, y = static_cast<int>(threadIdx.x) >> 5;
-  int64_t block = blockIdx.x;
+  const int64_t number = first + blockIdx.x;
+  int64_t block = number;
   AdCopy c = all.c[0];
 #pragma unroll
   for (int i = 1; i < kAdCopies; ++i)
-    if (static_cast<int64_t>(blockIdx.x) >= all.end[i - 1]) {
+    if (number >= all.end[i - 1]) {
       c = all.c[i];
-      block = blockIdx.x - all.end[i - 1];
+      block = number - all.end[i - 1];
     }
   // tiles of the result
   const int64_t tiles_w = ceil_div(c.to_width, 32), tiles = tiles_w * ceil_div(c.to_rows, 32);
@@ -317,11 +330,7 @@ struct AdCopyList {
   }
   template <typename T>
   lipcache_status launch(hipStream_t s) const {
-    if (blocks <= 0) return LIPCACHE_OK;
-    if (blocks > 0x7fffffff) return LIPCACHE_EUNSUPPORTED;
-    ad_copy_kernel<T><<<static_cast<unsigned>(blocks), 256, 0, s>>>(all);
-    LC_LAUNCHED();
-    return LIPCACHE_OK;
+    return in_passes(blocks, [&](int64_t first, unsigned n) { ad_copy_kernel<T><<<n, 256, 0, s>>>(all, first); });
   }
 };
 
@@ -763,10 +772,11 @@ inline constexpr int kFactorRow = kFactorParts<E> == 3 ? 192 : 128;  // bytes a 
 template <class E>
 __global__ __launch_bounds__(256) void ad_factor_kernel(const float* __restrict__ u, const float* __restrict__ v, int r,
                                                         int pairs, AdGroups g, E* __restrict__ to_u, E* __restrict__ to_v,
-                                                        int32_t* __restrict__ exps_u, int32_t* __restrict__ exps_v) {
+                                                        int32_t* __restrict__ exps_u, int32_t* __restrict__ exps_v,
+                                                        int64_t first) {
   __shared__ float tile[32][kAdMaxRank + 1];
   __shared__ float wave_top[256 / kWave];
-  const int t = static_cast<int>(blockIdx.x);
+  const int t = static_cast<int>(first + blockIdx.x);
   const int last = g.tile_start[pairs], row0 = g.tile_row[t], rows = g.tile_rows[t];
   if (static_cast<uint32_t>(t) >= static_cast<uint32_t>(last)) return;
   const float* f = blockIdx.y ? v : u;
@@ -832,7 +842,7 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
                                                       const int32_t* __restrict__ start,
                                                       const int32_t* __restrict__ tile_start,
                                                       const int32_t* __restrict__ exps_a,
-                                                      const int32_t* __restrict__ exps_b, const void* zeros) {
+                                                      const int32_t* __restrict__ exps_b, const void* zeros, int64_t first) {
   constexpr bool kF32 = std::is_same_v<E, float>;
   constexpr int kV = Vec16<E>::kCount, kSize = static_cast<int>(sizeof(E));
   typedef typename Vec16<E>::type V;
@@ -850,8 +860,8 @@ __global__ __launch_bounds__(256) void ad_grad_kernel(AdGradSide<E> A, AdGradSid
   constexpr int kGroups = kF32 ? 4 : 2, kParts = kF32 ? 1 : 2;
   __shared__ __align__(16) char lds[kStages * kSub * kTile];
   const int per = (A.blocks + B.blocks) * splits;
-  const int a = static_cast<int>(blockIdx.x) / per;
-  int in = static_cast<int>(blockIdx.x) % per;
+  const int number = static_cast<int>(first + blockIdx.x), a = number / per;
+  int in = number % per;
   const int share = in % splits;
   in /= splits;
   const bool second = in >= A.blocks;
@@ -1225,22 +1235,24 @@ lipcache_status ad_backward(const AdArgs& a, const float* v_in, void* dx, int64_
   if (!dA || S == 0) return LIPCACHE_OK;
   if ((a.T == 0 || a.T > chunk) && (st = ad_group(0, a.T, a.ad, ws.g, s)) != LIPCACHE_OK) return st;
   if (const int64_t tiles = ad_tiles(a.T, S); tiles > 0) {
-    ad_factor_kernel<E><<<dim3(static_cast<unsigned>(tiles), 2), 256, 0, s>>>(ws.u, need_v ? ws.v : v_in, r, S, ws.g, ws.fu, ws.fv,
-                                                                                           ws.exps_u, ws.exps_v);
-    LC_LAUNCHED();
+    st = in_passes(tiles, [&](int64_t first, unsigned n) {
+      ad_factor_kernel<E><<<dim3(n, 2), 256, 0, s>>>(ws.u, need_v ? ws.v : v_in, r, S, ws.g, ws.fu, ws.fv, ws.exps_u, ws.exps_v, first);
+    });
+    if (st != LIPCACHE_OK) return st;
   }
   const int splits = ad_splits(a.T, K, N, S);
   const AdGradSide<E> ga{x.p, x.ld, ws.fu, static_cast<E*>(dA), ws.part_a, K, static_cast<int>(ceil_div(K, 128)), false};
   const AdGradSide<E> gb{dy.p, dy.ld, ws.fv, static_cast<E*>(dB), ws.part_b, N, static_cast<int>(ceil_div(N, 128)), true};
-  const unsigned blocks = static_cast<unsigned>((ga.blocks + gb.blocks) * splits) * S;
   auto grad = [&](auto ranks) {
-    ad_grad_kernel<E, decltype(ranks)::value><<<blocks, 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g.order, ws.g.start,
-                                                                    ws.g.tile_start, ws.exps_u, ws.exps_v, ws.g.zeros);
+    return in_passes(static_cast<int64_t>(ga.blocks + gb.blocks) * splits * S, [&](int64_t first, unsigned n) {
+      ad_grad_kernel<E, decltype(ranks)::value><<<n, 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g.order, ws.g.start,
+                                                                 ws.g.tile_start, ws.exps_u, ws.exps_v, ws.g.zeros, first);
+    });
   };
-  if (r <= 32) grad(std::integral_constant<int, 1>{});
-  else if (r <= 64) grad(std::integral_constant<int, 2>{});
-  else grad(std::integral_constant<int, 4>{});
-  LC_LAUNCHED();
+  if (r <= 32) st = grad(std::integral_constant<int, 1>{});
+  else if (r <= 64) st = grad(std::integral_constant<int, 2>{});
+  else st = grad(std::integral_constant<int, 4>{});
+  if (st != LIPCACHE_OK) return st;
   if (splits > 1) {
     const int64_t most = static_cast<int64_t>(S) * r * (K > N ? K : N);
     ad_join_kernel<E><<<dim3(static_cast<unsigned>(ceil_div(most, 256)), 2), 256, 0, s>>>(ga, gb, r, S, splits, a.ad.scale, ws.g);
@@ -1280,7 +1292,7 @@ lipcache_status ad_check(const lipcache_adapters* ad, int64_t T, int32_t K, int3
   if (ad->R > 0 && (!ad->offsets || !ad->adapter || ad_unaligned(ad->offsets, LIPCACHE_F32) ||
                     ad_unaligned(ad->adapter, LIPCACHE_F32)))
     return LIPCACHE_EINVAL;
-  if (ad->r > kAdMaxRank || K > kAdMaxWidth || N > kAdMaxWidth || T > 0x7fffffff || ad->S > kAdMaxPairs)
+  if (ad->r > kAdMaxRank || K > kAdMaxWidth || N > kAdMaxWidth || T > 0x7fffffff || ad->S > kAdMaxPairs || ad->R > kAdMaxRequests)
     return LIPCACHE_EUNSUPPORTED;
   return LIPCACHE_OK;
 }

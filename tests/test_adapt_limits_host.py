@@ -27,3 +27,13 @@ def test_operands_of_a_step():
     need = lib.lipcache_muon_step_workspace_bytes(2, 96, 128, L.BF16)
     for flags in (1, 1 | L.MUON_SHORT_OPERANDS):
         assert need > 0 and _step(batch=2, nesterov=flags, wsb=need - 1) == L.EWORKSPACE
+
+
+def test_requests_have_a_limit():
+    lib = L.load()
+    for requests, expect in ((1 << 30, L.EWORKSPACE), ((1 << 30) + 1, L.EUNSUPPORTED), ((1 << 31) - 1, L.EUNSUPPORTED)):
+        ad = L.LipcacheAdapters(FAKE.value, FAKE.value, FAKE.value, FAKE.value, FAKE.value, 3, 8, requests)
+        assert lib.lipcache_adapter_forward(FAKE, 64, 10, FAKE, 64, None, 64, 48, ctypes.byref(ad), L.BF16, FAKE, 48, None,
+                                            None, 0, None) == expect
+        assert lib.lipcache_adapter_backward(FAKE, 48, FAKE, 64, 10, FAKE, 64, 64, 48, ctypes.byref(ad), L.BF16, None, FAKE, 64,
+                                             FAKE, FAKE, None, 0, None) == expect

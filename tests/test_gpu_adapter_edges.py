@@ -139,3 +139,55 @@ def test_keep_with_an_output_of_the_callers(T):
     out = api.AdapterOutput(torch.empty_like(ref.y), torch.empty_like(ref.v))
     v = out.v
     assert api.adapter_forward(*args, out=out).v is v and torch.equal(v, ref.v)
+
+
+# Sizes whose kernels have more workgroups than a launch takes (2^32 threads).
+def test_copies_of_more_workgroups_than_a_launch_takes():
+    T, K = (1 << 28) + 100, 33
+    say("copies", T, K)
+    x = torch.empty(T, K, dtype=torch.bfloat16, device=DEV).random_(-4, 5)
+    W = torch.ones(1, K, dtype=torch.bfloat16, device=DEV)
+    none = torch.empty(0, 1, K, dtype=torch.bfloat16, device=DEV)
+    y = api.adapter_forward(x, W, None, none, torch.empty(0, 1, 1, dtype=torch.bfloat16, device=DEV), torch.empty(0, device=DEV),
+                            torch.tensor([0, T], dtype=torch.int32, device=DEV), torch.tensor([-1], dtype=torch.int32, device=DEV)).y
+    for t in range(0, T, 1 << 25):
+        assert torch.equal(y[t:t + (1 << 25), 0], x[t:t + (1 << 25)].float().sum(1).bfloat16()), t
+
+
+def test_rows_of_more_workgroups_than_a_launch_takes():
+    T, K, N = (1 << 29) + 64, 8, 8
+    say("rows", T)
+    g = torch.Generator().manual_seed(1)
+    at = torch.cat([torch.randint(0, T, (2000,), generator=g), torch.tensor([0, T - 1])]).unique()
+    n = at.numel()
+    sx, sdy, sv, B = ints(g, -3, 3, n, K), ints(g, -3, 3, n, N), ints(g, -9, 9, n, 1), ints(g, -3, 3, 1, N, 1)
+    x, dy = (torch.zeros(T, 8, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    v = torch.zeros(T, 1, device=DEV)
+    for full, some in ((x, sx), (dy, sdy), (v, sv)):
+        full[at.to(DEV)] = some.to(full.dtype).to(DEV)
+    out = api.adapter_backward(dy, x, torch.zeros(N, K, dtype=torch.bfloat16, device=DEV),
+                               torch.zeros(1, 1, K, dtype=torch.bfloat16, device=DEV), B.bfloat16().to(DEV), torch.ones(1, device=DEV),
+                               torch.tensor([0, 5, T], dtype=torch.int32, device=DEV),
+                               torch.tensor([0, 0], dtype=torch.int32, device=DEV), v=v, want_dx=False)
+    u = sdy @ B[0]
+    assert torch.equal(out.dA[0].cpu(), (u.t() @ sx).bfloat16())
+    assert torch.equal(out.dB[0].cpu(), (sdy.t() @ sv).bfloat16())
+
+
+def test_pairs_of_more_workgroups_than_a_launch_takes():
+    T, K, N, S = 6, 1 << 17, 1 << 17, 8192
+    say("pairs", S, K, N)
+    g = torch.Generator().manual_seed(2)
+    x, dy, v = ints(g, -3, 3, T, K), ints(g, -1, 1, T, N), ints(g, -9, 9, T, 1)
+    B = torch.empty(S, N, 1, dtype=torch.bfloat16, device=DEV).random_(-1, 2)
+    adapter = torch.tensor([5, S - 1, 0, -1, 4097, 5])
+    out = api.adapter_backward(dy.bfloat16().to(DEV), x.bfloat16().to(DEV), torch.zeros(N, K, dtype=torch.bfloat16, device=DEV),
+                               torch.empty(S, 1, K, dtype=torch.bfloat16, device=DEV), B, torch.ones(S, device=DEV),
+                               torch.arange(T + 1, dtype=torch.int32, device=DEV), adapter.int().to(DEV), v=v.to(DEV), want_dx=False)
+    used = sorted(set(adapter.tolist()) - {-1})
+    for grad in (out.dA, out.dB):
+        assert set((grad != 0).flatten(1).any(1).nonzero().flatten().tolist()) <= set(used)
+    for a in used:
+        t = adapter == a
+        assert torch.equal(out.dA[a].cpu(), ((dy[t] @ B[a].float().cpu()).t() @ x[t]).bfloat16())
+        assert torch.equal(out.dB[a].cpu(), (dy[t].t() @ v[t]).bfloat16())
