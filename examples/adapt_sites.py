@@ -8,7 +8,7 @@ each.  Every site names the classes its own way, here by a swap of some labels.
           ``muon_step`` moves all factors along their orthogonalised momentum
   serve   single queries of different sites in one ``adapter_forward``
   cache   a site's own head W + scale B A certifies and fills a cache of its own;
-          a step on W itself moves sigma_max(W) by a bounded amount
+          a step on W itself moves sigma_max(W) by a bounded amount (float32 here: up to W's rounding)
 
     python examples/adapt_sites.py [--sites 16] [--steps 60]
 """
@@ -96,7 +96,7 @@ def run(sites: int = 16, d: int = 256, C: int = 200, r: int = 8, rows: int = 64,
     answers = cache.lookup(z)
     agree, hits = (answers.label == cert.label) & (answers.label >= 0), answers.label >= 0
 
-    # a step on the shared head: its spectral norm moves by at most MOST lr scale and the decay
+    # a step on the shared head: its spectral norm moves by at most MOST lr scale (no decay here) and W's rounding
     before = api.spectral_norm(W).sigma
     x, y = batch()
     p = torch.softmax(api.adapter_forward(x, W, bias, A, B, scale, offsets, adapter).y, 1)

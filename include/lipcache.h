@@ -450,9 +450,14 @@ lipcache_status lipcache_lookup_filter_dump(const lipcache_cache* c, const float
  * sites share.  Their matrices take float32, bfloat16 or float16 (`dtype`),
  * any sizes >= 1, and rows at a stride where an `ld*` argument is given (in
  * elements, at least the row's width).  Widths reach 2^20, rows 2^31 - 1,
- * pairs 8,192, requests 2^30 and stacks 65,535 (beyond: EUNSUPPORTED).  16-bit rows that start on 16-byte
- * boundaries are read in place; others are first copied into the workspace.
- * A workspace may be reused by the next call on the same stream.
+ * pairs 8,192, requests 2^30 and stacks 65,535 (beyond: EUNSUPPORTED).  Rows
+ * of whole 16-byte vectors, on 16-byte boundaries and at most 4 MiB apart, are
+ * read in place; others are first copied into the workspace.  A workspace may
+ * be reused by the next call on the same stream.
+ *
+ * What grows with the pairs beside the rows' own work: batches whose rows are
+ * sorted by pair read the offsets and indices of all R requests S + 1 times, and
+ * the backward pass transposes all S pairs, also those that no request names.
  */
 
 /*
@@ -577,8 +582,13 @@ typedef struct lipcache_muon {
  *   W <- (1 - lr weight_decay) W - lr scale O.
  * O is as lipcache_orthogonalise gives it, before its rounding to 16 bits.
  * Every singular value of O is at most the last step's bound (1.21 for the
- * coefficients above), so sigma_max(W) moves by at most 1.21 lr scale and
- * the decay: what the certified radii are divided by stays known.
+ * coefficients above), so a step moves sigma_max(W), which the certified radii
+ * are divided by, by at most
+ *   1.21 |lr scale| + |lr weight_decay| sigma_max(W) + u ||W||_F,
+ * the last term the rounding of the new W, with u = 2^-24 (float32), 2^-8 (bfloat16)
+ * or 2^-11 (float16).  For 16-bit W that term passes the others where steps are
+ * small, and it adds up: take sigma_max anew before certifying with such a W.
+ * (Short operands: 4e-3 |lr scale| ||O||_F more.)
  *
  *  W, G [batch][m][n] contiguous, dtype;  M [batch][m][n] float
  *  opt  (host);  sizes as in lipcache_orthogonalise

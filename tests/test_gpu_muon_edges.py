@@ -160,3 +160,20 @@ def test_matrices_near_the_ends_of_the_range(shape, dtype, size):
     api.muon_step(W, torch.zeros_like(H), M, lr=1.0, momentum=2.0, nesterov=False, scale=1.0, eps=0.0)
     ref = R.newton_schulz(n64(M), 5, NS5, 0.0)
     assert far(W, -ref) <= R.NS_TOL[dtype], far(W, -ref)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("lr,decay", [(0.05, 0.0), (0.05, 2.0), (1e-4, 0.5)])
+def test_how_far_a_step_moves_the_spectral_norm(dtype, lr, decay):
+    """By 1.21 lr scale, the decay and the rounding of W, step after step."""
+    W = matrices(60, 1, 200, 256, dtype, size=256 ** -0.5)[0].contiguous()
+    M = torch.zeros(W.shape, device=DEV)
+    sigma = api.spectral_norm(W.float()).sigma
+    for step in range(6):
+        G = matrices(61 + step, 1, 200, 256, dtype, "strong")[0].contiguous()
+        api.muon_step(W, G, M, lr=lr, weight_decay=decay, short_operands=dtype != "f32" and step % 2 == 1)
+        new = api.spectral_norm(W.float()).sigma
+        short = 4e-3 * 1.21 * 200 ** 0.5 if dtype != "f32" and step % 2 == 1 else 0.0
+        most = (1.21 + short) * lr + lr * decay * sigma + R.U[dtype] * float(W.double().norm())
+        assert abs(new - sigma) <= most, (step, new, sigma, most)
+        sigma = new
