@@ -340,7 +340,7 @@ struct AdCopyList {
 // workgroups past the table write zeros to the rows without a pair.  peak[row]
 // (or NULL): the largest finite |out| of a row with one.  Bound by reading x
 // once, and F_a once a tile: 8192 rows of 4096 bf16, rank 32, 24 us (2.8 TB/s
-// of x); short batches by three dependent rounds of loads, 7 us.
+// of x); short batches by three dependent rounds of loads, 7 us (float16, with the rows' largest values, 12).
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void ad_thin_kernel(const typename S::E* __restrict__ x, int64_t ldx, int width,
                                                               const typename S::E* __restrict__ F, int64_t ldf, int r,
@@ -511,7 +511,7 @@ __device__ __forceinline__ void add_low_rank(const AdLow& low, const AdTileRows<
 }
 
 // out[row] = P[row] Q^T + bias + the low-rank part, for the sorted rows of this tile.  Bound by the matrix cores: 8192
-// x 4096 -> 8192 bf16 with rank 64 590 us (0.95 PFLOP/s), 4096 -> 4096 backward 270 us (1.0).
+// x 4096 -> 8192 bf16 with rank 64 590 to 615 us (0.93 PFLOP/s), 4096 -> 4096 backward 280 us (0.98).
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void ad_main_kernel(const typename S::E* __restrict__ P, int64_t ldp,
                                                               const typename S::E* __restrict__ Q, int64_t ldq, int T,
@@ -823,8 +823,8 @@ __global__ __launch_bounds__(256) void ad_factor_kernel(const float* __restrict_
 // rows of z come gathered into LDS through a ring of buffers, two tiles a step,
 // and are read across (the contraction runs over the rows); their row numbers
 // come by scalar loads, which vmcnt does not count, so the ring's waits are
-// exact.  Bound by reading x and dy once: 134 MB of bf16 in 30 us (4.4 TB/s);
-// with the row numbers loaded where they are used it took 42.
+// exact.  Bound by reading x and dy once: 134 MB of bf16 in 35 us (3.8 TB/s; 30
+// when the factors were two numbers, 42 with the row numbers loaded where they are used).
 template <class E>
 struct AdGradSide {
   const E* z;
@@ -1153,8 +1153,8 @@ lipcache_status ad_forward(const AdArgs& a, const float* bias, void* y, int64_t 
 }
 
 // Shares of a pair's rows, so that few pairs still fill the chip: about 1024 workgroups, at least 128 rows each.
-// 8192 rows of four pairs, 4096 wide: 70 us with 256 workgroups, 42 + 8 (the join) with 512, 30 + 9 with 1024; 4096
-// rows of 16 pairs, 256 wide: 19 us with 64, 12 + 4 with 128.
+// 8192 rows of four pairs, 4096 wide, bfloat16 as two numbers: 70 us with 256 workgroups, 42 + 8 (the join) with 512, 30 + 9
+// with 1024; 4096 rows of 16 pairs, 256 wide: 19 us with 64, 12 + 4 with 128.
 inline int ad_splits(int64_t T, int K, int N, int S) {
   const int64_t blocks = (ceil_div(K, 128) + ceil_div(N, 128)) * (S > 0 ? S : 1);
   int64_t n = 1024 / blocks;

@@ -210,8 +210,8 @@ __global__ __launch_bounds__(256) void ns_plain_kernel(const T* G, float* __rest
 }
 
 // A symmetric product: out = f_sum F F^T + f_in in  (F p8 x k8 "row", or k8 x p8 "col" with rows of `width`), the
-// lower tiles computed and mirrored.  4096 wide, 11 bits: 85 us (0.82 PFLOP/s of the triangle); 200 wide, 22 bits: 5.7 us,
-// most of it the launch and one round of loads.
+// lower tiles computed and mirrored.  4096 wide: 215 us (0.96 PFLOP/s: three products of the triangle), 11 bits 80 us
+// (0.86); 200 wide: 5.9 us, most of it the launch and one round of loads.
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void ns_square_kernel(const _Float16* __restrict__ F, int p8, int k8,
                                                                 int width, const _Float16* __restrict__ in,
@@ -270,8 +270,8 @@ struct NsOut {
   float keep, gain;
 };
 
-// X' = a X + B X (wide: P = B, Q = X "col") or a X + X B (tall: P = X, Q = B).  4096 x 4096, 11 bits: 152 us (0.90
-// PFLOP/s); three of 1000 x 777, 22 bits: 22 us.
+// X' = a X + B X (wide: P = B, Q = X "col") or a X + X B (tall: P = X, Q = B).  4096 x 4096: 362 us (1.14
+// PFLOP/s: three products), 11 bits 147 us (0.94); three of 1000 x 777: 22 us.
 template <class S, bool kWide, bool kLast, typename T, bool kStep>
 __global__ __launch_bounds__(S::kThreads) void ns_apply_kernel(const _Float16* __restrict__ X,
                                                                const _Float16* __restrict__ B, int m8, int n8,
@@ -346,8 +346,8 @@ __global__ __launch_bounds__(S::kThreads) void ns_apply_kernel(const _Float16* _
 // next round starts from its Gram matrix, whose eigenvalues are squares again.
 //
 // Bound by reading and writing the long matrices, and by the chain of
-// small products between: 64 of 16 x 4096 (bf16, with the momentum) 12 + 8 + 12 us
-// for 84 MB.
+// small products between: 64 of 16 x 4096 (bf16, with the momentum) 11 + 8 + 12 us
+// for 84 MB; without it 26 us, 7 steps 27, 8 steps (two rounds) 56.
 constexpr int kShortMost = 64;
 constexpr int kShortBlock = 256;  // of the long side, in LDS at a time
 
@@ -739,7 +739,8 @@ inline int64_t tiles_of(int rows, int side) { return (rows + side - 1) / side; }
 //   192, 256  one workgroup a CU, where their tiles fill at least 4/5 of the rounds of 256 CUs
 // One step of a square matrix in us (P, P^2, X'; 22-bit operands): 1536 wide 26 + 27 + 39 with 64, 32 + 35 + 35
 // with 128d, 40 + 43 + 43 with 128; 2048 wide 48 + 49 + 67, 46 + 47 + 53, 51 + 54 + 61; four of 2048: 140 + 141 + 243,
-// 135 + 139 + 200, 131 + 135 + 189.  4096 wide (11 bits): P 85 with 192 against 100 with 128, X' 152 with 256 against 165.
+// 135 + 139 + 200, 131 + 135 + 189.  4096 wide: P 215 with 192 against 252 with 128; 11 bits: 85 against 100, X' 152 with 256
+// against 165.
 enum NsTile { kNs64, kNs128Deep, kNs128, kNs192, kNs256 };
 
 inline bool fills_chip(int64_t tiles) { return 5 * tiles >= 4 * 256 * ((tiles + 255) / 256); }
