@@ -780,7 +780,8 @@ struct NsPlan {
     if constexpr (!kCol) {
       const int64_t ld = static_cast<int64_t>(width) * static_cast<int64_t>(sizeof(E));
       if (!rows_fit(tile_side(tile), ld)) tile = kNs64;
-      if (!rows_fit(64, ld)) return square_with<TileShape<E, 32, 32, 1, 1, 4, 4, 2, false, false>>(F, k8, width, in, f_sum, f_in, out);
+      if constexpr (__is_same(E, Split))  // 64 rows of 11-bit operands always fit
+        if (!rows_fit(64, ld)) return square_with<TileShape<E, 32, 32, 1, 1, 4, 4, 2, false, false>>(F, k8, width, in, f_sum, f_in, out);
     }
     switch (tile) {
       case kNs64: return square_with<TileShape<E, 64, 64, 2, 2, 1, 3, 1, kCol, kCol>>(F, k8, width, in, f_sum, f_in, out);
