@@ -600,6 +600,101 @@ lipcache_status lipcache_muon_step(void* W, const void* G, float* M, int64_t bat
                                    void* ws, size_t ws_bytes, lipcache_stream_t stream);
 size_t lipcache_muon_step_workspace_bytes(int64_t batch, int32_t m, int32_t n, int32_t dtype);
 
+/* Limits of the calls below. */
+#define LIPCACHE_MOST_TOP 64        /* alternatives of a row that lipcache_logprobs lists       */
+#define LIPCACHE_MOST_ENTRIES 1024  /* entries of a row that a gradient or a teacher names      */
+
+/*
+ * Log probabilities of rows of logits.  With m_t = max_j x_tj and
+ * a_tj = (x_tj - m_t) / temperature, for every row
+ *   lse = m / temperature + log sum_j exp a_j          log p_j = a_j - log sum_i exp a_i
+ *   logp = log p_y of the row's label y, 0 where it has none
+ *   entropy = - sum_j p_j log p_j
+ *   top: the k largest logits in falling order, equal ones by rising index
+ * Differences to the largest logit are formed before the division, so logits of
+ * the type's lowest value are logits like others.  A logit of -inf has p = 0, adds
+ * nothing and is no alternative; a row of nothing else has lse = -inf,
+ * logp = -inf (with a label), entropy 0.  A row that holds a NaN or +inf has NaN
+ * for lse, entropy, logp (with a label) and log probabilities of alternatives; a NaN is no
+ * alternative.  Sums are held in float32.
+ *
+ *  x     [T][C] (ldx >= C elements between rows), dtype; 1 <= C <= 2^20, T < 2^31
+ *  temperature  2^-20 <= temperature <= 2^20
+ *  label [T], or NULL: none; a label outside [0, C) is none
+ *  logp, lse, entropy [T] out, each may be NULL
+ *  top_index, top_logp [T][k] out, 0 <= k <= LIPCACHE_MOST_TOP: index and log
+ *        probability of each alternative; -1 and -inf where a row has fewer
+ * T = 0 is valid and does nothing.  Outputs overlap neither inputs nor each other. (async)
+ */
+lipcache_status lipcache_logprobs(const void* x, int64_t ldx, int64_t T, int32_t C, int32_t dtype,
+                                  float temperature, const int32_t* label, int32_t k, float* logp,
+                                  float* lse, float* entropy, int32_t* top_index, float* top_logp,
+                                  lipcache_stream_t stream);
+
+/*
+ * The gradient of the same with regard to the logits:
+ *   temperature dx_j = g_logp [j = y] + sum_i g_top_i [j = top_i]
+ *                      - p_j (g_logp + sum_i g_top_i - g_lse)
+ *                      - g_entropy p_j (log p_j + entropy).
+ * g_logp counts in rows with a label, g_top where its index is in [0, C) (the
+ * indices are the caller's: the same one twice adds up, in the row's order).  A
+ * row whose gradients are all zero gets zeros, whatever it holds; so does a row of -inf.
+ *
+ *  label [T] or NULL (then g_logp is NULL too);  g_logp, g_lse, g_entropy [T], each may be NULL
+ *  top_index, g_top [T][k], 0 <= k <= LIPCACHE_MOST_ENTRIES
+ *  dx    [T][C] (lddx) out, dtype; may be x itself (lddx = ldx), overlaps no input else
+ * The others as above. (async)
+ */
+lipcache_status lipcache_logprobs_backward(const void* x, int64_t ldx, int64_t T, int32_t C, int32_t dtype,
+                                           float temperature, const int32_t* label, const float* g_logp,
+                                           const float* g_lse, const float* g_entropy, int32_t k,
+                                           const int32_t* top_index, const float* g_top, void* dx,
+                                           int64_t lddx, lipcache_stream_t stream);
+
+/*
+ * Learning from labels and from a teacher's top logits.  With p^u the softmax of
+ * the row's logits at temperature u, q the softmax of the row's teacher entries
+ * at `temperature` (over the entries that are there alone):
+ *   ce = - log p^1_y,   kl = sum_i q_i (log q_i - log p^temperature_{index_i}),
+ *   dx = weight (hard dce/dx + soft dkl/dx)
+ *      = weight (hard (p^1 - [y]) + soft / temperature (p^temperature - sum_i q_i [index_i])).
+ * (For a mean over T rows of (1 - a) ce + a u^2 kl take hard = 1 - a, soft = a u^2, weight = 1/T.)
+ * ce is 0 in rows without a label, kl in rows without an entry; such a row's
+ * part of dx is zero.  A class named twice counts twice.  A teacher's logit of
+ * -inf has q = 0; a class with q > 0 whose own logit is -inf gives kl = inf.
+ * Rows of dx whose parts are all zero, by weight, hard and soft too, are
+ * zeros whatever x holds, and so are those of a row of -inf (ce = kl = inf there).
+ *
+ *  x       [T][C] (ldx), temperature, T and C as in lipcache_logprobs
+ *  teacher [T][k] float, index [T][k], 0 <= k <= LIPCACHE_MOST_ENTRIES, any order; an
+ *          index outside [0, C) is no entry
+ *  label   [T] or NULL;  weight [T] or NULL (1);  hard, soft finite
+ *  ce, kl  [T] out, each may be NULL
+ *  dx      [T][C] (lddx) out, dtype, or NULL; may be x itself (lddx = ldx)
+ * T = 0 is valid and does nothing.  Outputs overlap no input else. (async)
+ */
+lipcache_status lipcache_distill(const void* x, int64_t ldx, int64_t T, int32_t C, int32_t dtype,
+                                 float temperature, float hard, float soft, int32_t k,
+                                 const float* teacher, const int32_t* index, const int32_t* label,
+                                 const float* weight, float* ce, float* kl, void* dx, int64_t lddx,
+                                 lipcache_stream_t stream);
+
+/*
+ * lipcache_logprobs of the logits W x + bias, which are not written: features
+ * and a head, as lipcache_certify takes them.  Products on the matrix cores, sums
+ * in float32, logits not rounded in between.  A bias of -inf masks its class.
+ *
+ *  x [T][K] (ldx), W [C][K] (ldw), dtype; bias [C] float or NULL;  K, C <= 2^20
+ *  logp, lse, entropy [T] out, each may be NULL
+ *  ws  lipcache_head_logprobs_workspace_bytes(T, K, C, dtype) bytes
+ * The others as in lipcache_logprobs. (async)
+ */
+lipcache_status lipcache_head_logprobs(const void* x, int64_t ldx, int64_t T, const void* W, int64_t ldw,
+                                       const float* bias, int32_t K, int32_t C, int32_t dtype,
+                                       float temperature, const int32_t* label, float* logp, float* lse,
+                                       float* entropy, void* ws, size_t ws_bytes, lipcache_stream_t stream);
+size_t lipcache_head_logprobs_workspace_bytes(int64_t T, int32_t K, int32_t C, int32_t dtype);
+
 /* Static description of a status code. */
 const char* lipcache_status_string(lipcache_status status);
 

@@ -7,6 +7,7 @@ the C ABI names (``lipcache_spectral_norm`` -> ``spectral_norm`` ...).
 from __future__ import annotations
 
 import ctypes
+import functools
 from dataclasses import dataclass
 
 import torch
@@ -604,3 +605,179 @@ def muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, lr: float, mome
     st = lib.lipcache_muon_step(W.data_ptr(), G.data_ptr(), M.data_ptr(), b, m, n, code, ctypes.byref(opt),
                                 ws.data_ptr(), ws.numel(), _stream_of(W.device))
     L.check("lipcache_muon_step", st)
+
+
+# ------------------------------------------- scoring answers, learning from a teacher
+@dataclass
+class LogProbs:
+    logp: torch.Tensor                # float32 [T]: log probability of the row's label, 0 where it has none
+    lse: torch.Tensor                 # float32 [T]: log of the sum of exponentials
+    entropy: torch.Tensor             # float32 [T]
+    top_index: torch.Tensor | None    # int32 [T, top]: classes by falling logit, -1 where a row has fewer
+    top_logp: torch.Tensor | None     # float32 [T, top]: their log probabilities
+
+
+def _on_device(call):
+    """The call with its first tensor's device current: a stream's handle alone does not say which device's it is."""
+    @functools.wraps(call)
+    def on_device(first, *args, **kw):
+        if not isinstance(first, torch.Tensor) or not first.is_cuda or first.device.index == torch.cuda.current_device():
+            return call(first, *args, **kw)
+        with torch.cuda.device(first.device):
+            return call(first, *args, **kw)
+    return on_device
+
+
+def _rows_of(t: torch.Tensor, name: str) -> tuple[int, int, int]:
+    """[T, C] rows: T, C and the distance between rows."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be [T, C]")
+    T, C = t.shape
+    return T, C, _need_rows(t, name, t.dtype, t.device, T, C)
+
+
+def _of_rows(t: torch.Tensor | None, name: str, dtype: torch.dtype, device: torch.device, shape: tuple):
+    """The address of a [T] or [T, k] tensor, None where it is None."""
+    if t is None:
+        return None
+    _need_shape(t, name, dtype, device, shape)
+    return t.data_ptr()
+
+
+def _entries(index: torch.Tensor | None, value: torch.Tensor | None, names: tuple[str, str], device: torch.device, T: int):
+    """k and the addresses of [T, k] classes and their values."""
+    if (index is None) != (value is None):
+        raise ValueError(f"{names[0]} and {names[1]} go together")
+    if index is None:
+        return 0, None, None
+    if index.dim() != 2:
+        raise ValueError(f"{names[0]} must be [T, k]")
+    k = index.shape[1]
+    return (k, _of_rows(index, names[0], torch.int32, device, (T, k)),
+            _of_rows(value, names[1], torch.float32, device, (T, k)))
+
+
+@_on_device
+def logprobs(logits: torch.Tensor, labels: torch.Tensor | None = None, top: int = 0, temperature: float = 1.0,
+             out: LogProbs | None = None) -> LogProbs:
+    """lipcache_logprobs: log probabilities of labels, entropies and the ``top`` most likely classes of rows (async).
+
+    logits [T, C] float32, bfloat16 or float16 (rows may lie apart), labels int32 [T]
+    (outside [0, C): none) or None.  ``out`` must not overlap what is read."""
+    code = _dtype(logits, "logits")
+    T, C, ld = _rows_of(logits, "logits")
+    dev, k = logits.device, int(top)
+    if not 0 <= k <= L.MOST_TOP:
+        raise ValueError(f"top must be 0 to {L.MOST_TOP}")
+    label = _of_rows(labels, "labels", torch.int32, dev, (T,))
+    if out is None:
+        each = torch.empty((3, T), dtype=torch.float32, device=dev)
+        out = LogProbs(each[0], each[1], each[2], torch.empty((T, k), dtype=torch.int32, device=dev) if k else None,
+                       torch.empty((T, k), dtype=torch.float32, device=dev) if k else None)
+    elif k and (out.top_index is None or out.top_logp is None):
+        raise ValueError("out lacks top_index or top_logp")
+    f32 = torch.float32
+    lib = L.load()
+    st = lib.lipcache_logprobs(logits.data_ptr(), ld, T, C, code, float(temperature), label, k,
+                               _of_rows(out.logp, "out.logp", f32, dev, (T,)), _of_rows(out.lse, "out.lse", f32, dev, (T,)),
+                               _of_rows(out.entropy, "out.entropy", f32, dev, (T,)),
+                               _of_rows(out.top_index, "out.top_index", torch.int32, dev, (T, k)) if k else None,
+                               _of_rows(out.top_logp, "out.top_logp", f32, dev, (T, k)) if k else None, _stream_of(dev))
+    L.check("lipcache_logprobs", st)
+    return out
+
+
+@_on_device
+def logprobs_backward(logits: torch.Tensor, labels: torch.Tensor | None = None, g_logp: torch.Tensor | None = None,
+                      g_lse: torch.Tensor | None = None, g_entropy: torch.Tensor | None = None,
+                      top_index: torch.Tensor | None = None, g_top: torch.Tensor | None = None,
+                      temperature: float = 1.0, out: torch.Tensor | None = None) -> torch.Tensor:
+    """lipcache_logprobs_backward: the gradient of ``logprobs`` with regard to the logits [T, C], their type (async).
+
+    g_logp, g_lse, g_entropy float32 [T] and g_top float32 [T, k] are the gradients of
+    what ``logprobs`` gave (None: zero), top_index int32 [T, k] its classes, or any others.  ``out`` may be logits."""
+    code = _dtype(logits, "logits")
+    T, C, ld = _rows_of(logits, "logits")
+    dev, f32 = logits.device, torch.float32
+    label = _of_rows(labels, "labels", torch.int32, dev, (T,))
+    if g_logp is not None and labels is None:
+        raise ValueError("g_logp needs labels")
+    k, index, value = _entries(top_index, g_top, ("top_index", "g_top"), dev, T)
+    if k > L.MOST_ENTRIES:
+        raise ValueError(f"g_top must have at most {L.MOST_ENTRIES} columns")
+    if out is None:
+        out, ldd = logits.new_empty((T, C)), C
+    else:
+        ldd = _need_rows(out, "out", logits.dtype, dev, T, C)
+    lib = L.load()
+    st = lib.lipcache_logprobs_backward(logits.data_ptr(), ld, T, C, code, float(temperature), label,
+                                        _of_rows(g_logp, "g_logp", f32, dev, (T,)), _of_rows(g_lse, "g_lse", f32, dev, (T,)),
+                                        _of_rows(g_entropy, "g_entropy", f32, dev, (T,)), k, index, value, out.data_ptr(),
+                                        ldd, _stream_of(dev))
+    L.check("lipcache_logprobs_backward", st)
+    return out
+
+
+@dataclass
+class Distilled:
+    ce: torch.Tensor            # float32 [T]: cross entropy with the label, 0 where there is none
+    kl: torch.Tensor            # float32 [T]: divergence from the teacher's entries, 0 where there are none
+    grad: torch.Tensor | None   # [T, C], the logits' type: gradient of sum weight (hard ce + soft kl)
+
+
+@_on_device
+def distill(logits: torch.Tensor, teacher: torch.Tensor | None, index: torch.Tensor | None,
+            labels: torch.Tensor | None = None, weight: torch.Tensor | None = None, hard: float = 0.0, soft: float = 1.0,
+            temperature: float = 1.0, want_grad: bool = True, out: torch.Tensor | None = None) -> Distilled:
+    """lipcache_distill: losses against labels and a teacher's top logits, and their gradient, in one call (async).
+
+    logits [T, C] (rows may lie apart), teacher float32 [T, k] at the classes index
+    int32 [T, k] (outside [0, C): no entry), labels int32 [T] or None, weight float32 [T] or
+    None (1).  ``out``: where the gradient goes; may be logits."""
+    code = _dtype(logits, "logits")
+    T, C, ld = _rows_of(logits, "logits")
+    dev, f32 = logits.device, torch.float32
+    k, at, value = _entries(index, teacher, ("index", "teacher"), dev, T)
+    if k > L.MOST_ENTRIES:
+        raise ValueError(f"teacher must have at most {L.MOST_ENTRIES} columns")
+    label = _of_rows(labels, "labels", torch.int32, dev, (T,))
+    each = torch.empty((2, T), dtype=f32, device=dev)
+    ldd = C
+    if out is not None:
+        if not want_grad:
+            raise ValueError("out is the gradient's: it goes with want_grad")
+        ldd = _need_rows(out, "out", logits.dtype, dev, T, C)
+    elif want_grad:
+        out = logits.new_empty((T, C))
+    lib = L.load()
+    st = lib.lipcache_distill(logits.data_ptr(), ld, T, C, code, float(temperature), float(hard), float(soft), k, value, at,
+                              label, _of_rows(weight, "weight", f32, dev, (T,)), each[0].data_ptr(), each[1].data_ptr(),
+                              None if out is None else out.data_ptr(), ldd, _stream_of(dev))
+    L.check("lipcache_distill", st)
+    return Distilled(each[0], each[1], out)
+
+
+@_on_device
+def head_logprobs(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None, labels: torch.Tensor | None = None,
+                  temperature: float = 1.0) -> LogProbs:
+    """lipcache_head_logprobs: ``logprobs`` of W x + bias without the logits in memory (async).
+
+    x [T, K] and W [C, K] of one type (float32, bfloat16 or float16; rows may lie
+    apart), bias float32 [C] or None, labels int32 [T] or None."""
+    code = _dtype(x, "x")
+    dev, dt = x.device, x.dtype
+    if x.dim() != 2 or W.dim() != 2:
+        raise ValueError("x must be [T, K] and W [C, K]")
+    T, K = x.shape
+    C = W.shape[0]
+    ldx = _need_rows(x, "x", dt, dev, T, K)
+    ldw = _need_rows(W, "W", dt, dev, C, K)
+    each = torch.empty((3, T), dtype=torch.float32, device=dev)
+    lib = L.load()
+    ws = workspace(lib.lipcache_head_logprobs_workspace_bytes(T, K, C, code), dev)
+    st = lib.lipcache_head_logprobs(x.data_ptr(), ldx, T, W.data_ptr(), ldw,
+                                    _of_rows(bias, "bias", torch.float32, dev, (C,)), K, C, code, float(temperature),
+                                    _of_rows(labels, "labels", torch.int32, dev, (T,)), each[0].data_ptr(),
+                                    each[1].data_ptr(), each[2].data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(dev))
+    L.check("lipcache_head_logprobs", st)
+    return LogProbs(each[0], each[1], each[2], None, None)

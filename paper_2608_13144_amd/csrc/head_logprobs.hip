@@ -1,0 +1,263 @@
+// Log probabilities straight from features and a head: the product W x + bias
+// goes from the matrix cores' sums into each class tile's largest value and sums
+// of exponentials, and no logit is written (see lipcache.h).
+//
+// The classes lie along the accumulators' rows, the features' rows along their
+// columns: a lane holds 16 classes of one row in each 32 x 32 tile, so the sums over classes are sums over its registers, and only
+// the two halves of a wave meet at the end.  Every wave of a tile leaves
+// (largest value, sum, sum of the exponents weighted) of its classes; a second
+// launch joins them in order.
+#include "lc_common.hpp"
+#include "lc_mfma.hpp"
+
+namespace lc {
+
+constexpr int64_t kHlMostClasses = 1 << 20;
+constexpr int64_t kHlMostWidth = 1 << 20;
+constexpr float kHlLn2 = 0.6931471805599453f;
+constexpr float kHlLog2e = 1.4426950408889634f;
+constexpr float kHlInf = __builtin_huge_valf();
+constexpr float kHlLeast = -1000.0f;  // exponents below add nothing: 2^-1000 is zero, and -inf times zero is not
+
+inline int64_t hl_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Rows of 16-byte vectors, zeros past the width: what the tiles are copied from where a matrix's own rows are not aligned.
+template <class E>
+__global__ __launch_bounds__(256) void hl_copy_kernel(const E* __restrict__ from, int64_t ld, int64_t rows, int width,
+                                                      E* __restrict__ to, int64_t to_ld) {
+  const int64_t size = rows * to_ld, step = static_cast<int64_t>(gridDim.x) * 256;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < size; i += step) {
+    const int64_t row = i / to_ld;
+    const int col = static_cast<int>(i - row * to_ld);
+    to[i] = col < width ? from[row * ld + col] : static_cast<E>(0.0f);
+  }
+}
+
+// (largest value, sum of 2^(scale (x - m)), sum of those times their exponents) of some classes.
+struct HlPart {
+  float m, s, mean;
+};
+__device__ __forceinline__ HlPart hl_join(const HlPart& a, const HlPart& b, float scale) {
+  const float m = fmaxf(a.m, b.m);
+  if (m == -kHlInf) return {m, a.s + b.s, a.mean + b.mean};  // no class yet (sums are zero, or NaN)
+  const float da = (a.m - m) * scale, db = (b.m - m) * scale;
+  const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+  return {m, fmaf(a.s, fa, b.s * fb),
+          fa * fmaf(fmaxf(da, kHlLeast), a.s, a.mean) + fb * fmaf(fmaxf(db, kHlLeast), b.s, b.mean)};
+}
+
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void hl_tile_kernel(const typename S::E* __restrict__ W, int64_t ldw, int C,
+                                                              const typename S::E* __restrict__ x, int64_t ldx, int T,
+                                                              int K, const float* __restrict__ bias, float scale,
+                                                              const int32_t* __restrict__ label, int parts,
+                                                              float4* __restrict__ part, float* __restrict__ at) {
+  typedef typename S::E E;
+  __shared__ __align__(16) char lds[S::kLds];
+  int bi, bj;
+  tile_of(static_cast<int>((C + S::BM - 1) / S::BM), static_cast<int>((T + S::BN - 1) / S::BN), bi, bj);
+  const int i0 = bi * S::BM, j0 = bj * S::BN;
+  Side p{}, q{};
+  p.p = W + i0 * ldw;
+  p.ld = ldw * sizeof(E);
+  p.rows = C - i0 < S::BM ? C - i0 : S::BM;
+  q.p = x + j0 * ldx;
+  q.ld = ldx * sizeof(E);
+  q.rows = T - j0 < S::BN ? T - j0 : S::BN;
+  f32x16 acc[S::TM][S::TN] = {};
+  tile_products<S>(p, q, K, lds, acc);
+  const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+  if (S::WK > 1 && wave >= S::WM * S::WN) return;
+  const int wm = wave / S::WN, wn = wave % S::WN, first = 4 * (lane >> 5);
+#pragma unroll
+  for (int a = 0; a < S::TM; ++a) {
+    const int base = i0 + (wm * S::TM + a) * 32 + first;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int c = base + acc_row(v);
+      const float add = c < C ? bias ? bias[c] : 0.0f : -kHlInf;
+#pragma unroll
+      for (int b = 0; b < S::TN; ++b) acc[a][b][v] = c < C ? acc[a][b][v] + add : -kHlInf;
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < S::TN; ++b) {
+    const int j = (wn * S::TN + b) * 32 + (lane & 31), t = j0 + j;
+    const int y = label && t < T ? label[t] - (i0 + wm * S::TM * 32) : -1;
+    float m = -kHlInf;
+#pragma unroll
+    for (int a = 0; a < S::TM; ++a)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) m = fmaxf(m, acc[a][b][v]);
+    const float from = m == -kHlInf ? 0.0f : m;
+    HlPart sum{m, 0.0f, 0.0f};
+#pragma unroll
+    for (int a = 0; a < S::TM; ++a)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const float e = (acc[a][b][v] - from) * scale, w = __builtin_amdgcn_exp2f(e);
+        sum.s += w;
+        sum.mean = fmaf(fmaxf(e, kHlLeast), w, sum.mean);
+        if (y == a * 32 + first + acc_row(v) && label[t] < C) at[t] = acc[a][b][v];
+      }
+    const HlPart other{__shfl_xor(sum.m, 32, kWave), __shfl_xor(sum.s, 32, kWave), __shfl_xor(sum.mean, 32, kWave)};
+    sum = lane < 32 ? hl_join(sum, other, scale) : sum;
+    if (lane < 32 && t < T) part[static_cast<int64_t>(t) * parts + bi * S::WM + wm] = {sum.m, sum.s, sum.mean, 0.0f};
+  }
+}
+
+// One wave a row.
+__global__ __launch_bounds__(256) void hl_join_kernel(int T, int C, int parts, const float4* __restrict__ part,
+                                                      const float* __restrict__ at, const int32_t* __restrict__ label,
+                                                      float scale, float temperature, float* __restrict__ logp,
+                                                      float* __restrict__ lse, float* __restrict__ entropy) {
+  const int t = static_cast<int>(blockIdx.x) * 4 + static_cast<int>(threadIdx.x) / kWave, lane = lane_id();
+  if (t >= T) return;
+  HlPart sum{-kHlInf, 0.0f, 0.0f};
+  for (int i = lane; i < parts; i += kWave) {
+    const float4 p = part[static_cast<int64_t>(t) * parts + i];
+    sum = hl_join(sum, {p.x, p.y, p.z}, scale);
+  }
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1)
+    sum = hl_join(sum, {__shfl_xor(sum.m, o, kWave), __shfl_xor(sum.s, o, kWave), __shfl_xor(sum.mean, o, kWave)}, scale);
+  if (lane != 0) return;
+  const float m = sum.m == -kHlInf ? 0.0f : sum.m, log_s = __builtin_amdgcn_logf(sum.s);
+  if (logp) {
+    const int y = label ? label[t] : -1;
+    logp[t] = y < 0 || y >= C ? 0.0f : sum.s == 0.0f ? -kHlInf : (at[t] - m) / temperature - log_s * kHlLn2;
+  }
+  if (lse) lse[t] = m / temperature + log_s * kHlLn2;
+  if (entropy) entropy[t] = sum.s == 0.0f ? 0.0f : (log_s - sum.mean / sum.s) * kHlLn2;
+}
+
+// ----------------------------------------------------------------- host side
+template <class E>
+inline constexpr int kHlVector = 16 / static_cast<int>(sizeof(E));
+
+struct HlSpace {
+  char* at;
+  size_t used = 0;
+  template <class T>
+  T* take(int64_t n) {
+    T* p = reinterpret_cast<T*>(at + used);
+    used = align_up(used + static_cast<size_t>(n) * sizeof(T), 256);
+    return p;
+  }
+};
+
+
+inline int64_t hl_parts(int C) { return hl_ceil(C, 256) * 8; }  // at most, of any tile shape
+// Rows of a pass: their parts stay below 256 MiB.
+inline int64_t hl_rows(int64_t T, int C) {
+  const int64_t rows = (1ll << 28) / (hl_parts(C) * 16) / 256 * 256, most = rows < 256 ? 256 : rows;
+  return T < most ? T : most;
+}
+
+template <class E>
+struct HlBuffers {
+  float4* part;
+  float* at;
+  E *x, *W;
+  HlBuffers(HlSpace& ws, int64_t T, int K, int C) {
+    const int64_t rows = hl_rows(T, C), K8 = hl_ceil(K, kHlVector<E>) * kHlVector<E>;
+    part = ws.take<float4>(rows * hl_parts(C));
+    at = ws.take<float>(rows);
+    x = ws.take<E>(T * K8);
+    W = ws.take<E>(C * K8);
+  }
+};
+
+template <class E>
+lipcache_status hl_aligned(const E*& p, int64_t& ld, int64_t rows, int K, E* room, hipStream_t s) {
+  if ((reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % kHlVector<E> == 0 && K % kHlVector<E> == 0 &&
+      ld * static_cast<int64_t>(sizeof(E)) <= (4 << 20))
+    return LIPCACHE_OK;
+  const int64_t to = hl_ceil(K, kHlVector<E>) * kHlVector<E>, blocks = hl_ceil(rows * to, 1024);
+  hl_copy_kernel<E><<<static_cast<unsigned>(blocks < 8192 ? blocks : 8192), 256, 0, s>>>(p, ld, rows, K, room, to);
+  LC_LAUNCHED();
+  p = room;
+  ld = to;
+  return LIPCACHE_OK;
+}
+
+struct HlOut {
+  const int32_t* label;
+  float *logp, *lse, *entropy;
+};
+
+template <class E>
+lipcache_status hl_run(const E* x, int64_t ldx, int64_t T, const E* W, int64_t ldw, const float* bias, int K, int C,
+                       float temperature, const HlOut& out, void* ws_, hipStream_t s) {
+  HlSpace space{static_cast<char*>(ws_)};
+  const HlBuffers<E> ws(space, T, K, C);
+  lipcache_status st;
+  if ((st = hl_aligned(x, ldx, T, K, ws.x, s)) != LIPCACHE_OK) return st;
+  if ((st = hl_aligned(W, ldw, C, K, ws.W, s)) != LIPCACHE_OK) return st;
+  const float scale = kHlLog2e / temperature;
+  const int64_t pass = hl_rows(T, C);
+  for (int64_t t = 0; t < T; t += pass) {
+    const int n = static_cast<int>(T - t < pass ? T - t : pass);
+    const int32_t* label = out.label ? out.label + t : nullptr;
+    int parts = 0;
+    auto run = [&](auto shape) {
+      typedef decltype(shape) S;
+      parts = static_cast<int>(hl_ceil(C, S::BM)) * S::WM;
+      const int64_t tiles = hl_ceil(C, S::BM) * hl_ceil(n, S::BN);
+      hl_tile_kernel<S><<<static_cast<unsigned>(tiles), S::kThreads, 0, s>>>(W, ldw, C, x + t * ldx, ldx, n, K, bias, scale,
+                                                                           label, parts, ws.part, ws.at);
+      return hipGetLastError() == hipSuccess ? LIPCACHE_OK : LIPCACHE_EHIP;
+    };
+    if (n <= 32) st = run(TileShape<E, 128, 32, 4, 1, 1, 4, 1, false, false>{});
+    else if (sizeof(E) == 4 || hl_ceil(C, 256) * hl_ceil(n, 256) < 200) st = run(TileShape<E, 128, 128, 2, 2, 1, 2, 1, false, false>{});
+    else st = run(TileShape<E, 256, 256, 2, 4, 1, 2, 1, false, false>{});
+    if (st != LIPCACHE_OK) return st;
+    hl_join_kernel<<<static_cast<unsigned>(hl_ceil(n, 4)), 256, 0, s>>>(
+        n, C, parts, ws.part, ws.at, label, scale, temperature, out.logp ? out.logp + t : nullptr,
+        out.lse ? out.lse + t : nullptr, out.entropy ? out.entropy + t : nullptr);
+    LC_LAUNCHED();
+  }
+  return LIPCACHE_OK;
+}
+
+bool hl_sizes_bad(int64_t T, int32_t K, int32_t C, int32_t dtype) {
+  return T < 0 || K < 1 || C < 1 || dtype < LIPCACHE_F32 || dtype > LIPCACHE_F16;
+}
+bool hl_unaligned(const void* p, uintptr_t size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) != 0; }
+
+}  // namespace lc
+
+using namespace lc;
+
+extern "C" size_t lipcache_head_logprobs_workspace_bytes(int64_t T, int32_t K, int32_t C, int32_t dtype) {
+  if (hl_sizes_bad(T, K, C, dtype)) return 0;
+  HlSpace space{nullptr};
+  if (dtype == LIPCACHE_F32) HlBuffers<float>(space, T, K, C);
+  else HlBuffers<__bf16>(space, T, K, C);
+  return space.used;
+}
+
+extern "C" lipcache_status lipcache_head_logprobs(const void* x, int64_t ldx, int64_t T, const void* W, int64_t ldw,
+                                                  const float* bias, int32_t K, int32_t C, int32_t dtype,
+                                                  float temperature, const int32_t* label, float* logp, float* lse,
+                                                  float* entropy, void* ws, size_t ws_bytes, lipcache_stream_t stream) {
+  if (hl_sizes_bad(T, K, C, dtype) || ldx < K || ldw < K) return LIPCACHE_EINVAL;
+  if (!(temperature >= 0x1p-20f && temperature <= 0x1p20f)) return LIPCACHE_EINVAL;
+  if (!W || (T > 0 && !x)) return LIPCACHE_EINVAL;
+  const uintptr_t size = dtype == LIPCACHE_F32 ? 4 : 2;
+  if (hl_unaligned(x, size) || hl_unaligned(W, size) || hl_unaligned(bias, 4) || hl_unaligned(label, 4) ||
+      hl_unaligned(logp, 4) || hl_unaligned(lse, 4) || hl_unaligned(entropy, 4))
+    return LIPCACHE_EINVAL;
+  if (C > kHlMostClasses || K > kHlMostWidth || T > 0x7fffffff) return LIPCACHE_EUNSUPPORTED;
+  if (!ws || !aligned256(ws) || ws_bytes < lipcache_head_logprobs_workspace_bytes(T, K, C, dtype)) return LIPCACHE_EWORKSPACE;
+  const HlOut out{label, logp, lse, entropy};
+  auto run = [&](auto type) {
+    typedef decltype(type) E;
+    return hl_run<E>(static_cast<const E*>(x), ldx, T, static_cast<const E*>(W), ldw, bias, K, C, temperature, out, ws, stream);
+  };
+  switch (dtype) {
+    case LIPCACHE_F32: return run(float{});
+    case LIPCACHE_BF16: return run(__bf16{});
+    default: return run(_Float16{});
+  }
+}
