@@ -1,0 +1,227 @@
+// Distillation: losses of rows of logits against labels and a teacher's top
+// logits, and their gradient (see lipcache.h for the formulas).
+#include "lc_rows.hpp"
+
+namespace lc {
+
+struct LpDistill {
+  float temperature, hard, soft;
+  float scale, second;  // log2(e) over the temperature of the first sum, of the second
+  int hot, cold;        // which sum is the teacher's, the label's: 0 the first, 1 the second
+  const int32_t* label;
+  const float* weight;
+  int k;
+  const float* teacher;
+  const int32_t* index;
+  float *ce, *kl;
+  int bits;  // of the entries' index
+};
+
+struct LpShares {
+  float hard, soft;  // of the row, with its weight; zero where it has no label, no entry
+};
+
+// The label is the last of a row's k + 1 entries.
+template <class E, class S, bool kWhole, bool kTwo>
+__global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits, int64_t ldx, int64_t T, int C,
+                                                                 LpDistill a, E* grad, int64_t ldd) {
+  typedef RowData<E, S> Data;
+  constexpr RowWants kWants = kTwo ? RowWants::kTwo : RowWants::kSum;
+  constexpr int kSegment = S::G * S::N, kLanes = S::kLanes;
+  __shared__ RowSums room[2][S::kWaves];
+  __shared__ LpShares shares[2][S::kRows];
+  extern __shared__ __align__(16) char lds[];
+  const RowPlace<S> at;
+  const int n = a.k + 1, lane = at.g;  // (of the row's first wave, where lane matters)
+  const bool keeps = at.g < kLanes;
+  RowEntries entries(lds + at.row * entry_bytes(n, a.bits), n, a.bits);
+  const RowScale scale{a.scale, a.second};
+  const float hot_scale = kRowLog2e / a.temperature;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * S::kRows;
+  const int full = C / Data::V;
+  auto row_of = [&](int64_t t) { return logits + (t < T ? t : T - 1) * ldx; };
+  struct Entry {
+    int at;
+    float value;
+  };
+  auto entry_of = [&](int64_t t, int i) {
+    Entry e{-1, 0.0f};
+    if (t >= T || i >= n) return e;
+    if (i < a.k) {
+      e = {a.index[t * a.k + i], a.teacher[t * a.k + i]};
+    } else if (a.label) {
+      e.at = a.label[t];
+    }
+    return e;
+  };
+  auto checked = [&](Entry e) {
+    if (e.at >= C) e.at = -1;
+    return e;
+  };
+  auto logit_of = [&](int64_t t, int c) { return c >= 0 ? static_cast<float>(row_of(t)[c]) : 0.0f; };
+  Data data;
+  int64_t t = static_cast<int64_t>(blockIdx.x) * S::kRows + at.row;
+  Entry mine{-1, 0.0f};
+  float logit = 0.0f;
+  if (keeps) {
+    mine = checked(entry_of(t, lane));
+    logit = logit_of(t, mine.at);
+  }
+  data.load(row_of(t), 0, C, at.g);
+  for (int turn = 0; t - at.row < T; t += step, turn ^= 1) {
+    const E* x = row_of(t);
+    Entry next_entry{-1, 0.0f};
+    float w = 1.0f;
+    if (keeps) {
+      next_entry = entry_of(t + step, lane);
+      if (a.weight && t < T) w = a.weight[t];
+    }
+    RowSums r;
+    data.template add<kWants, true>(r, scale);
+    if constexpr (!kWhole) {
+      for (int first = kSegment; first < full; first += kSegment) {
+#pragma unroll
+        for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, full, at.g);
+        data.template add<kWants, false>(r, scale);
+      }
+    }
+    next_entry = checked(next_entry);
+    float top = -kRowInf, sum = 0.0f, some = 0.0f;
+    if (keeps) {
+      for (int i = lane; i < n; i += kLanes) {
+        if (i != lane) {
+          mine = checked(entry_of(t, i));
+          logit = logit_of(t, mine.at);
+        }
+        entries.at[i] = mine.at;
+        entries.value[i] = mine.value;
+        entries.logit[i] = logit;
+        if (i < a.k && mine.at >= 0) {
+          top = fmaxf(top, mine.value);
+          some = mine.value == -kRowInf ? some : 1.0f;  // (a NaN is an entry)
+        }
+      }
+      wave_sync();
+      top = row_from(lanes_max<kLanes>(top));
+      some = lanes_max<kLanes>(some);
+      for (int i = lane; i < a.k; i += kLanes)
+        if (entries.at[i] >= 0) sum += row_exp2((entries.value[i] - top) * hot_scale);
+      sum = lanes_sum<kLanes>(sum);
+      if (lane == 0)
+        shares[turn][at.row] = {entries.at[a.k] >= 0 ? w * a.hard : 0.0f, some != 0.0f ? w * a.soft / a.temperature : 0.0f};
+      wave_sync();
+    }
+    row_join<S, kWants>(r, scale, room[turn]);
+    const LpShares share = shares[turn][at.row];
+    const float from = row_from(r.m), hot_s = kTwo && a.hot ? r.more : r.s, cold_s = kTwo && a.cold ? r.more : r.s;
+    const bool any = (share.hard != 0.0f || share.soft != 0.0f) && r.s != 0.0f;
+    // what an element adds: one exponential with both parts' factor, or one for each
+    const float one = kTwo ? (a.hot ? share.hard : share.soft) / r.s : (share.hard + share.soft) / r.s,
+                two = kTwo ? (a.hot ? share.soft : share.hard) / r.more : 0.0f;
+    auto smooth = [&](float v) {
+      const float d = v - from;
+      float g = row_exp2(d * scale.scale) * one;
+      if constexpr (kTwo) g = fmaf(row_exp2(d * scale.second), two, g);
+      return g;
+    };
+    if (keeps) {
+      float kl = 0.0f;
+      for (int i = lane; i < a.k; i += kLanes) {
+        if (entries.at[i] < 0) continue;
+        const float b = entries.value[i] - top, q = some != 0.0f ? row_exp2(b * hot_scale) / sum : 0.0f;
+        if (!(q == 0.0f)) kl += q * ((b - (entries.logit[i] - from)) * hot_scale);
+        const float part = share.soft * q;
+        entries.value[i] = part;
+        if (part == 0.0f) entries.at[i] = -1;
+      }
+      kl = lanes_sum<kLanes>(kl);
+      if (lane == 0) {
+        const int y = entries.at[a.k];
+        if (t < T && a.ce)
+          a.ce[t] = y < 0 ? 0.0f : r.s == 0.0f ? kRowInf : row_log2(cold_s) * kRowLn2 - (entries.logit[a.k] - from);
+        if (t < T && a.kl) a.kl[t] = some == 0.0f ? 0.0f : r.s == 0.0f ? kRowInf : (kl + row_log2(hot_s) - row_log2(sum)) * kRowLn2;
+        entries.value[a.k] = share.hard;
+        if (share.hard == 0.0f) entries.at[a.k] = -1;
+      }
+      wave_sync();
+    }
+    const E* following = row_of(t + step);
+    if (keeps) {
+      mine = next_entry;
+      logit = logit_of(t + step, mine.at);
+    }
+    if (!grad) {
+      data.load(following, 0, C, at.g);
+      RowPlace<S>::sync();
+      continue;
+    }
+    E* dx = grad + (t < T ? t : T - 1) * ldd;
+    auto dx_of = [&](float v) { return any ? smooth(v) : 0.0f; };
+    if (kWhole) {
+#pragma unroll
+      for (int i = 0; i < S::N; ++i) {
+        if (t < T) data.store_chunk(i, dx, 0, full, at.g, dx_of);
+        data.load_chunk(i, following, 0, full, at.g);
+      }
+    } else {
+      for (int first = 0; first < full; first += kSegment) {
+#pragma unroll
+        for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, full, at.g);
+#pragma unroll
+        for (int i = 0; i < S::N; ++i)
+          if (t < T) data.store_chunk(i, dx, first, full, at.g, dx_of);
+      }
+#pragma unroll
+      for (int i = 0; i < S::N; ++i) data.load_chunk(i, following, 0, full, at.g);
+    }
+    if (t < T) data.store_tail(dx, C, at.g, dx_of);
+    data.load_tail(following, C, at.g);
+    RowPlace<S>::sync();  // the row is written before its entries are
+    if (keeps && any && t < T) {
+      entries.index<kLanes>(lane, n);
+      for (int i = lane; i < n; i += kLanes) {
+        float q;
+        if (entries.first(i, n, q)) dx[entries.at[i]] = static_cast<E>(smooth(entries.logit[i]) - q);
+      }
+    }
+  }
+}
+
+}  // namespace lc
+
+using namespace lc;
+
+extern "C" lipcache_status lipcache_distill(const void* x, int64_t ldx, int64_t T, int32_t C, int32_t dtype,
+                                            float temperature, float hard, float soft, int32_t k,
+                                            const float* teacher, const int32_t* index, const int32_t* label,
+                                            const float* weight, float* ce, float* kl, void* dx, int64_t lddx,
+                                            lipcache_stream_t stream) {
+  if (lipcache_status st = row_check(x, ldx, T, C, dtype, temperature); st != LIPCACHE_OK) return st;
+  if (k < 0 || (dx && lddx < C) || (T > 0 && k > 0 && (!teacher || !index))) return LIPCACHE_EINVAL;
+  if (!(__builtin_fabsf(hard) < kRowInf) || !(__builtin_fabsf(soft) < kRowInf)) return LIPCACHE_EINVAL;
+  if (row_unaligned(dx, dtype) || row_unaligned4(teacher) || row_unaligned4(index) || row_unaligned4(label) ||
+      row_unaligned4(weight) || row_unaligned4(ce) || row_unaligned4(kl))
+    return LIPCACHE_EINVAL;
+  if (k > LIPCACHE_MOST_ENTRIES) return LIPCACHE_EUNSUPPORTED;
+  if (T == 0) return LIPCACHE_OK;
+  const int bits = entry_bits(C);
+  // which sums there are: the label's at temperature 1, the teacher's at its own, one where they are the same
+  const bool cold = label && (hard != 0.0f || ce), hot = k > 0 && (soft != 0.0f || kl);
+  const bool two = cold && hot && temperature != 1.0f;
+  const float at_one = kRowLog2e, at_own = kRowLog2e / temperature;
+  const LpDistill a{temperature, hard, soft, hot ? at_own : at_one, at_one, 0, two ? 1 : 0, label, weight, k,
+                    teacher, index, ce, kl, bits};
+  return row_typed(dtype, [&](auto type) {
+    typedef decltype(type) E;
+    return row_shaped_entries<E>(C, k + 1, [&](auto shape, auto whole) {
+      typedef decltype(shape) S;
+      auto run = [&](auto both) {
+        lp_distill_kernel<E, S, decltype(whole)::value, decltype(both)::value>
+            <<<row_blocks<S>(T), S::kThreads, S::kRows * entry_bytes(k + 1, bits), stream>>>(
+                static_cast<const E*>(x), ldx, T, C, a, static_cast<E*>(dx), lddx);
+        return hipGetLastError() == hipSuccess ? LIPCACHE_OK : LIPCACHE_EHIP;
+      };
+      return two ? run(std::true_type{}) : run(std::false_type{});
+    });
+  });
+}

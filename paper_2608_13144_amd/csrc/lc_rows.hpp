@@ -1,0 +1,397 @@
+// Rows of logits in registers: what the scoring and distillation kernels share.
+//
+// G threads take a row (several rows a wave, one a wave, or one a workgroup) and
+// hold it as N chunks of 16 bytes each, chunk c in thread c % G, beside up to seven
+// single elements past the last whole chunk, one in each of the first threads.  Chunks are read and
+// written as vectors whatever the row's alignment (the hardware takes them from any element's address).
+// What lies past the row is -inf, which adds nothing to any sum.
+//
+// A row is read from memory once.  A thread's sums follow its own largest value, block after block as the
+// chunks arrive, and are scaled to the row's when the threads' are joined.  A
+// workgroup goes on to another row where there are more rows than workgroups, and
+// asks for each chunk of it as soon as the old one is not needed any more, so that memory has
+// work while a row is finished.
+#pragma once
+
+#include <type_traits>
+
+#include "lc_common.hpp"
+
+namespace lc {
+
+constexpr int kRowMostClasses = 1 << 20;
+constexpr float kRowInf = __builtin_huge_valf();
+constexpr float kRowLn2 = 0.6931471805599453f;
+constexpr float kRowLog2e = 1.4426950408889634f;
+constexpr float kRowLeast = -1000.0f;  // exponents below add nothing: 2^-1000 is zero, and -inf times zero is not
+
+__device__ __forceinline__ float row_exp2(float v) { return __builtin_amdgcn_exp2f(v); }
+__device__ __forceinline__ float row_log2(float v) { return __builtin_amdgcn_logf(v); }
+
+// ------------------------------------------------------------ element types
+template <class E>
+struct RowType;
+template <>
+struct RowType<float> {
+  static constexpr int V = 4;
+  static constexpr uint32_t kFill = 0xff800000u;
+  typedef u32x4 __attribute__((aligned(4))) vec;
+  static __device__ __forceinline__ float get(const u32x4& r, int e) { return __builtin_bit_cast(f32x4, r)[e]; }
+  static __device__ __forceinline__ u32x4 pack(const float* v) {
+    return __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
+  }
+};
+template <>
+struct RowType<__bf16> {
+  static constexpr int V = 8;
+  static constexpr uint32_t kFill = 0xff80ff80u;
+  typedef u32x4 __attribute__((aligned(2))) vec;
+  static __device__ __forceinline__ float get(const u32x4& r, int e) {
+    const uint32_t both = r[e >> 1];
+    return __builtin_bit_cast(float, e & 1 ? both & 0xffff0000u : both << 16);
+  }
+  static __device__ __forceinline__ u32x4 pack(const float* v) { return pack_bf16x8(v); }
+};
+template <>
+struct RowType<_Float16> {
+  static constexpr int V = 8;
+  static constexpr uint32_t kFill = 0xfc00fc00u;
+  typedef u32x4 __attribute__((aligned(2))) vec;
+  static __device__ __forceinline__ float get(const u32x4& r, int e) {
+    return static_cast<float>(__builtin_bit_cast(f16x8, r)[e]);
+  }
+  static __device__ __forceinline__ u32x4 pack(const float* v) {
+    f16x8 h;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = static_cast<_Float16>(v[e]);
+    return __builtin_bit_cast(u32x4, h);
+  }
+};
+
+// ------------------------------------------------------ lanes of one wave
+template <int CTRL>
+__device__ __forceinline__ float dpp_f32(float v) {
+  const int b = __builtin_bit_cast(int, v);
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(b, b, CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ float lane_f32(float v, int lane) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+}
+
+constexpr int kDppHalfMirror = 0x141;  // lane i of each 8 <- lane 7 - i
+constexpr int kDppMirror = 0x140;      // lane i of each 16 <- lane 15 - i
+
+// The join of a value over groups of L lanes (16: a row of the wave; 64: the wave).  Every step joins two halves that
+// are alike throughout, so all lanes get the same bits (a product must not be fused into the first sum: it would be
+// exact on one side of it and rounded on the other).
+template <int L, class F>
+__device__ __forceinline__ float lanes_join(float v, F join) {
+  asm("" : "+v"(v));
+  v = join(v, dpp_f32<kDppQuadXor1>(v));
+  v = join(v, dpp_f32<kDppQuadXor2>(v));
+  v = join(v, dpp_f32<kDppHalfMirror>(v));
+  v = join(v, dpp_f32<kDppMirror>(v));
+  if constexpr (L == 64) v = join(join(lane_f32(v, 0), lane_f32(v, 16)), join(lane_f32(v, 32), lane_f32(v, 48)));
+  return v;
+}
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+  return lanes_join<L>(v, [](float a, float b) { return a + b; });
+}
+template <int L>
+__device__ __forceinline__ float lanes_max(float v) {
+  return lanes_join<L>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// LDS written by lanes of a wave, read by others of it.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// ------------------------------------------------------------- a row's sums
+// kMean: s and the sum of the exponents (to base 2) weighted by what they add to
+// s; kTwo: s and the sum at a second temperature.
+enum class RowWants { kSum, kMean, kTwo };
+
+// About the value m: s = sum 2^(scale (x - m)), more as RowWants says.
+struct RowSums {
+  float m, s, more;
+};
+struct RowScale {
+  float scale, second;  // log2(e) / temperature
+};
+
+// The same about another value, m or larger; from is finite unless m is +inf.
+template <RowWants W>
+__device__ __forceinline__ void row_move(RowSums& r, float from, const RowScale& k) {
+  const float d = (r.m - from) * k.scale, f = row_exp2(d);
+  if constexpr (W == RowWants::kMean) r.more = f * fmaf(fmaxf(d, kRowLeast), r.s, r.more);
+  if constexpr (W == RowWants::kTwo) r.more *= row_exp2((r.m - from) * k.second);
+  r.s *= f;
+}
+__device__ __forceinline__ float row_from(float m) { return m == -kRowInf ? 0.0f : m; }
+
+template <int G_, int N_>
+struct RowShape {
+  static constexpr int G = G_, N = N_;
+  static constexpr int kThreads = G > 256 ? G : 256;
+  static constexpr int kRows = kThreads / G;             // of a workgroup
+  static constexpr int kLanes = G < 64 ? G : 64;         // of a row in one wave
+  static constexpr int kWaves = G <= 64 ? 1 : G / 64;    // of a row
+};
+
+// Where a thread stands in its row.
+template <class S>
+struct RowPlace {
+  int g, row;  // thread of the row, row of the workgroup
+  __device__ __forceinline__ RowPlace()
+      : g(static_cast<int>(threadIdx.x) % S::G), row(static_cast<int>(threadIdx.x) / S::G) {
+    if constexpr (S::G >= 64) row = uniform(row);
+  }
+  // Between the threads of a row.
+  static __device__ __forceinline__ void sync() {
+    if constexpr (S::G <= 64) wave_sync();
+    else __syncthreads();
+  }
+};
+
+// A segment of a row in registers: N chunks a thread from element `begin` (a multiple of a chunk) on, and the elements
+// past the last whole chunk, which every segment holds.
+template <class E, class S>
+struct RowData {
+  typedef RowType<E> Type;
+  static constexpr int V = Type::V, N = S::N, G = S::G;
+  u32x4 raw[N];
+  float tail;
+
+  // Chunk i as bits again: without it the compiler keeps the numbers that one pass made of them for the next, in two
+  // to four times the registers.
+  __device__ __forceinline__ void pin(int i) { asm volatile("" : "+v"(raw[i])); }
+  static __device__ __forceinline__ u32x4 fill() { return u32x4{Type::kFill, Type::kFill, Type::kFill, Type::kFill}; }
+  // Chunk first + G i + g of the row at x: a row's address (one for all lanes, where a row has whole waves), and a
+  // lane's offset that is the same for all chunks.
+  static __device__ __forceinline__ const char* chunk_at(const E* x, int first, int i, int g) {
+    return reinterpret_cast<const char*>(x) + static_cast<int64_t>(first + G * i) * 16 + static_cast<uint32_t>(g * 16);
+  }
+  __device__ __forceinline__ void load_chunk(int i, const E* x, int first, int full, int g) {
+    raw[i] = fill();
+    if (g < full - (first + G * i)) raw[i] = *reinterpret_cast<const typename Type::vec*>(chunk_at(x, first, i, g));
+  }
+  __device__ __forceinline__ void load_tail(const E* x, int C, int g) {
+    const int full = C / V, j = full * V + g;
+    tail = g < V && j < C ? static_cast<float>(x[j]) : -kRowInf;
+  }
+  __device__ __forceinline__ void load(const E* x, int first, int C, int g) {
+    load_tail(x, C, g);
+#pragma unroll
+    for (int i = 0; i < N; ++i) load_chunk(i, x, first, C / V, g);
+  }
+  // f(value, index) for every element of the thread's chunks, rising index.
+  template <class F>
+  __device__ __forceinline__ void each(int first, int g, F f) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      pin(i);
+#pragma unroll
+      for (int e = 0; e < V; ++e) f(Type::get(raw[i], e), (first + G * i + g) * V + e);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // Writes f of every element of chunk i to the row at out, where it has the chunk.
+  template <class F>
+  __device__ __forceinline__ void store_chunk(int i, E* out, int first, int full, int g, F f) {
+    if (g >= full - (first + G * i)) return;
+    pin(i);
+    float v[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = f(Type::get(raw[i], e));
+    *reinterpret_cast<typename Type::vec*>(const_cast<char*>(chunk_at(out, first, i, g))) = Type::pack(v);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  template <class F>
+  __device__ __forceinline__ void store_tail(E* out, int C, int g, F f) const {
+    const int j = C / V * V + g;
+    if (g < V && j < C) out[j] = static_cast<E>(f(tail));
+  }
+
+  // Adds the chunks to a thread's sums, a block of up to 16 elements at a time.  FIRST: nothing is in them yet.
+  template <RowWants W, bool FIRST>
+  __device__ __forceinline__ void add(RowSums& r, const RowScale& k) {
+    constexpr int B = 16 / V < N ? 16 / V : N;  // chunks of a block
+#pragma unroll
+    for (int b = 0; b < N; b += B) {
+      float m = -kRowInf;
+#pragma unroll
+      for (int i = b; i < b + B; ++i) pin(i);
+#pragma unroll
+      for (int i = b; i < b + B; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) m = fmaxf(m, Type::get(raw[i], e));
+      if (FIRST && b == 0) {
+        m = fmaxf(m, tail);
+        r = {m, 0.0f, 0.0f};
+      } else {
+        m = fmaxf(m, r.m);
+        row_move<W>(r, row_from(m), k);
+        r.m = m;
+      }
+      const float from = row_from(m);
+      if (FIRST && b == 0) one<W>(tail, from, r, k);
+#pragma unroll
+      for (int i = b; i < b + B; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) one<W>(Type::get(raw[i], e), from, r, k);
+      __builtin_amdgcn_sched_barrier(0);  // a block's numbers are not formed while the one before holds its own
+    }
+  }
+  template <RowWants W>
+  static __device__ __forceinline__ void one(float x, float from, RowSums& r, const RowScale& k) {
+    const float d = x - from, a = d * k.scale, e = row_exp2(a);
+    r.s += e;
+    if constexpr (W == RowWants::kMean) r.more = fmaf(fmaxf(a, kRowLeast), e, r.more);
+    if constexpr (W == RowWants::kTwo) r.more += row_exp2(d * k.second);
+  }
+};
+
+// The sums of the row's threads, joined in one order: every thread gets them, about row_from(m).  Rows of more than a
+// wave leave the waves' sums in `room` (kWaves of them) and meet at one barrier: what the row's threads wrote to LDS before is there after it.  The room
+// may be written again after the next barrier.
+template <class S, RowWants W>
+__device__ __forceinline__ void row_join(RowSums& r, const RowScale& k, RowSums* room) {
+  const float m = lanes_max<S::kLanes>(r.m);
+  row_move<W>(r, row_from(m), k);
+  r.m = m;
+  r.s = lanes_sum<S::kLanes>(r.s);
+  if constexpr (W != RowWants::kSum) r.more = lanes_sum<S::kLanes>(r.more);
+  if constexpr (S::kWaves > 1) {
+    static_assert(S::kWaves <= 16, "joined by 16 lanes");
+    if (lane_id() == 0) room[threadIdx.x / kWave] = r;
+    __syncthreads();
+    const int w = lane_id() & 15;
+    r = w < S::kWaves ? room[w] : RowSums{-kRowInf, 0.0f, 0.0f};
+    const float all = lanes_max<16>(r.m);
+    row_move<W>(r, row_from(all), k);
+    r.m = all;
+    r.s = lanes_sum<16>(r.s);
+    if constexpr (W != RowWants::kSum) r.more = lanes_sum<16>(r.more);
+  }
+}
+
+// --------------------------------------------------- classes named in a row
+// Entries (class, value) of a row in LDS, at most `most` of them, kept by the
+// row's first wave (or its lanes).  Those of one class are added up, in their
+// order, by the first of them: a bit of `seen` for each class (or for several, where there are more
+// than 8192) finds out in one pass which entries may be alone.
+constexpr int kEntryBits = 8192;
+inline int entry_bits(int C) {
+  int bits = 256;
+  while (bits < C && bits < kEntryBits) bits *= 2;
+  return bits;
+}
+__host__ __device__ inline size_t entry_bytes(int most, int bits) { return (static_cast<size_t>(most) * 12 + bits / 4 + 15) / 16 * 16; }
+
+struct RowEntries {
+  int* at;        // [most] class, -1: none
+  float* value;   // [most]
+  float* logit;   // [most] the row's own at the class
+  uint32_t *seen, *twice;
+  int bits;
+  __device__ __forceinline__ RowEntries(char* lds, int most, int bits_)
+      : at(reinterpret_cast<int*>(lds + bits_ / 4)),
+        value(reinterpret_cast<float*>(lds + bits_ / 4) + most),
+        logit(reinterpret_cast<float*>(lds + bits_ / 4) + 2 * most),
+        seen(reinterpret_cast<uint32_t*>(lds)),
+        twice(reinterpret_cast<uint32_t*>(lds) + bits_ / 32),
+        bits(bits_) {}
+  // By the lanes that keep the entries.  After it, first() may be asked of any.
+  template <int LANES>
+  __device__ __forceinline__ void index(int lane, int count) {
+    for (int i = lane; i < bits / 16; i += LANES) seen[i] = 0;
+    wave_sync();
+    for (int i = lane; i < count; i += LANES) {
+      const int c = at[i];
+      if (c < 0) continue;
+      const uint32_t b = static_cast<uint32_t>(c) & (bits - 1), bit = 1u << (b & 31);
+      if (atomicOr(&seen[b >> 5], bit) & bit) atomicOr(&twice[b >> 5], bit);
+    }
+    wave_sync();
+  }
+  // Whether entry i is the first of its class; if so `sum` is the class's.
+  __device__ __forceinline__ bool first(int i, int count, float& sum) const {
+    const int c = at[i];
+    if (c < 0) return false;
+    sum = value[i];
+    const uint32_t b = static_cast<uint32_t>(c) & (bits - 1);
+    if (!(twice[b >> 5] >> (b & 31) & 1)) return true;
+    float all = 0.0f;
+    bool mine = true;
+    for (int j = 0; j < count; ++j)
+      if (at[j] == c) {
+        mine = mine && j >= i;
+        all += value[j];
+      }
+    sum = all;
+    return mine;
+  }
+};
+
+// ----------------------------------------------------------------- host side
+inline bool row_unaligned(const void* p, int32_t dtype) {
+  return (reinterpret_cast<uintptr_t>(p) & (dtype == LIPCACHE_F32 ? 3u : 1u)) != 0;
+}
+inline bool row_unaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+
+inline lipcache_status row_check(const void* x, int64_t ldx, int64_t T, int32_t C, int32_t dtype, float temperature) {
+  if (T < 0 || C < 1 || ldx < C || dtype < LIPCACHE_F32 || dtype > LIPCACHE_F16) return LIPCACHE_EINVAL;
+  if (!(temperature >= 0x1p-20f && temperature <= 0x1p20f)) return LIPCACHE_EINVAL;
+  if ((T > 0 && !x) || row_unaligned(x, dtype)) return LIPCACHE_EINVAL;
+  if (C > kRowMostClasses || T > 0x7fffffff) return LIPCACHE_EUNSUPPORTED;
+  return LIPCACHE_OK;
+}
+
+template <class F>
+lipcache_status row_typed(int32_t dtype, F f) {
+  switch (dtype) {
+    case LIPCACHE_F32: return f(float{});
+    case LIPCACHE_BF16: return f(__bf16{});
+    default: return f(_Float16{});
+  }
+}
+
+// Calls f(shape) with the smallest shape that holds a row of C, or the largest and false: the row goes in segments.
+template <class E, class F>
+lipcache_status row_shaped(int C, F f) {
+  const int chunks = C / RowType<E>::V;
+  auto holds = [&](auto shape) { return chunks <= decltype(shape)::G * decltype(shape)::N; };
+  if (holds(RowShape<16, 1>{})) return f(RowShape<16, 1>{}, std::true_type{});
+  if (holds(RowShape<16, 4>{})) return f(RowShape<16, 4>{}, std::true_type{});
+  if (holds(RowShape<64, 4>{})) return f(RowShape<64, 4>{}, std::true_type{});
+  if (holds(RowShape<256, 4>{})) return f(RowShape<256, 4>{}, std::true_type{});
+  if (holds(RowShape<256, 8>{})) return f(RowShape<256, 8>{}, std::true_type{});
+  if (holds(RowShape<512, 8>{})) return f(RowShape<512, 8>{}, std::true_type{});
+  if (holds(RowShape<1024, 8>{})) return f(RowShape<1024, 8>{}, std::true_type{});
+  if (holds(RowShape<1024, 16>{})) return f(RowShape<1024, 16>{}, std::true_type{});
+  return f(RowShape<1024, 8>{}, std::false_type{});
+}
+
+// The same for kernels that keep n entries of each row in LDS: a wave or more for a row where they are many.
+template <class E, class F>
+lipcache_status row_shaped_entries(int C, int n, F f) {
+  return row_shaped<E>(C, [&](auto shape, auto whole) {
+    if constexpr (decltype(shape)::G < 64) {
+      if (n > 32) return f(RowShape<64, 4>{}, std::true_type{});
+    }
+    return f(shape, whole);
+  });
+}
+
+// Workgroups: the rows, or as many as the chip holds at a time (256 CUs of 2048 threads).
+template <class S>
+unsigned row_blocks(int64_t T) {
+  const int64_t need = (T + S::kRows - 1) / S::kRows, most = 256 * (2048 / S::kThreads);
+  return static_cast<unsigned>(need < most ? need : most);
+}
+
+}  // namespace lc

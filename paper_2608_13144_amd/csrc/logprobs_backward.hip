@@ -1,0 +1,187 @@
+// The gradient of log probabilities, sums, entropies and alternatives with
+// regard to the logits (see lipcache.h for the formulas).
+#include "lc_rows.hpp"
+
+namespace lc {
+
+struct LpBackward {
+  float temperature;
+  const int32_t* label;
+  const float *g_logp, *g_lse, *g_entropy;
+  int k;
+  const int32_t* top_index;
+  const float* g_top;
+  int bits;  // of the entries' index
+};
+
+// What a row's elements share: dx = 2^a (flat + slope a), a the exponent to base 2.
+struct LpSlope {
+  float mass;  // gl - sum of the entries' gradients
+  float ge;
+  int some;    // any gradient that is not zero
+};
+
+// The label is the last of a row's k + 1 entries.
+template <class E, class S, bool kWhole, bool kEntropy>
+__global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logits, int64_t ldx, int64_t T, int C,
+                                                                  LpBackward a, E* grad, int64_t ldd) {
+  typedef RowData<E, S> Data;
+  constexpr RowWants kWants = kEntropy ? RowWants::kMean : RowWants::kSum;
+  constexpr int kSegment = S::G * S::N, kLanes = S::kLanes;
+  __shared__ RowSums room[S::kWaves];
+  __shared__ LpSlope slope[S::kRows];
+  extern __shared__ __align__(16) char lds[];
+  const RowPlace<S> at;
+  const int n = a.k + 1, lane = at.g;  // (of the row's first wave, where lane matters)
+  const bool keeps = at.g < kLanes;
+  RowEntries entries(lds + at.row * entry_bytes(n, a.bits), n, a.bits);
+  const RowScale scale{kRowLog2e / a.temperature, 0.0f};
+  const float inv_t = 1.0f / a.temperature;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * S::kRows;
+  const int full = C / Data::V;
+  auto row_of = [&](int64_t t) { return logits + (t < T ? t : T - 1) * ldx; };
+  struct Entry {
+    int at;
+    float value;
+  };
+  auto entry_of = [&](int64_t t, int i) {
+    Entry e{-1, 0.0f};
+    if (t >= T || i >= n) return e;
+    if (i < a.k) {
+      e = {a.top_index[t * a.k + i], a.g_top[t * a.k + i]};
+    } else if (a.g_logp) {
+      e = {a.label[t], a.g_logp[t]};
+    }
+    return e;
+  };
+  auto checked = [&](Entry e) {
+    if (e.at < 0 || e.at >= C || e.value == 0.0f) e = {-1, 0.0f};
+    return e;
+  };
+  auto logit_of = [&](int64_t t, int c) { return c >= 0 ? static_cast<float>(row_of(t)[c]) : 0.0f; };
+  Data data;
+  int64_t t = static_cast<int64_t>(blockIdx.x) * S::kRows + at.row;
+  Entry mine{-1, 0.0f};
+  float logit = 0.0f;
+  if (keeps) {
+    mine = checked(entry_of(t, lane));
+    logit = logit_of(t, mine.at);
+  }
+  data.load(row_of(t), 0, C, at.g);
+  for (; t - at.row < T; t += step) {
+    const E* x = row_of(t);
+    E* dx = grad + (t < T ? t : T - 1) * ldd;
+    Entry next_entry{-1, 0.0f};
+    float gl = 0.0f, ge = 0.0f;
+    if (keeps) {
+      next_entry = entry_of(t + step, lane);
+      if (a.g_lse && t < T) gl = a.g_lse[t];
+      if (kEntropy && t < T) ge = a.g_entropy[t];
+    }
+    RowSums r;
+    data.template add<kWants, true>(r, scale);
+    if constexpr (!kWhole) {
+      for (int first = kSegment; first < full; first += kSegment) {
+#pragma unroll
+        for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, full, at.g);
+        data.template add<kWants, false>(r, scale);
+      }
+    }
+    next_entry = checked(next_entry);
+    if (keeps) {
+      float mass = 0.0f, any = gl != 0.0f || ge != 0.0f ? 1.0f : 0.0f;
+      for (int i = lane; i < n; i += kLanes) {
+        if (i != lane) {
+          mine = checked(entry_of(t, i));
+          logit = logit_of(t, mine.at);
+        }
+        entries.at[i] = mine.at;
+        entries.value[i] = mine.value;
+        entries.logit[i] = logit;
+        mass += mine.value;
+        any = mine.value != 0.0f ? 1.0f : any;
+      }
+      mass = lanes_sum<kLanes>(mass);
+      any = lanes_max<kLanes>(any);
+      if (lane == 0) slope[at.row] = {gl - mass, ge, any != 0.0f ? 1 : 0};
+      wave_sync();
+    }
+    row_join<S, kWants>(r, scale, room);
+    const LpSlope k = slope[at.row];
+    const bool some = k.some != 0 && r.s != 0.0f;  // (true for NaN)
+    const float from = row_from(r.m), inv = inv_t / r.s, steep = kEntropy ? -k.ge * kRowLn2 * inv : 0.0f,
+                flat = k.mass * inv - steep * (r.more / r.s);
+    auto smooth = [&](float v) {
+      const float e = (v - from) * scale.scale;
+      if constexpr (kEntropy) return row_exp2(e) * fmaf(steep, fmaxf(e, kRowLeast), flat);
+      else return row_exp2(e) * flat;
+    };
+    auto dx_of = [&](float v) { return some ? smooth(v) : 0.0f; };
+    const E* following = row_of(t + step);
+    if (keeps) {
+      mine = next_entry;
+      logit = logit_of(t + step, mine.at);
+    }
+    if (kWhole) {
+#pragma unroll
+      for (int i = 0; i < S::N; ++i) {
+        if (t < T) data.store_chunk(i, dx, 0, full, at.g, dx_of);
+        data.load_chunk(i, following, 0, full, at.g);
+      }
+    } else {
+      for (int first = 0; first < full; first += kSegment) {
+#pragma unroll
+        for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, full, at.g);
+#pragma unroll
+        for (int i = 0; i < S::N; ++i)
+          if (t < T) data.store_chunk(i, dx, first, full, at.g, dx_of);
+      }
+#pragma unroll
+      for (int i = 0; i < S::N; ++i) data.load_chunk(i, following, 0, full, at.g);
+    }
+    if (t < T) data.store_tail(dx, C, at.g, dx_of);
+    data.load_tail(following, C, at.g);
+    RowPlace<S>::sync();  // the row is written before its entries are
+    if (keeps && some && t < T) {
+      entries.index<kLanes>(lane, n);
+      for (int i = lane; i < n; i += kLanes) {
+        float g;
+        if (entries.first(i, n, g)) dx[entries.at[i]] = static_cast<E>(fmaf(g, inv_t, smooth(entries.logit[i])));
+      }
+    }
+  }
+}
+
+}  // namespace lc
+
+using namespace lc;
+
+extern "C" lipcache_status lipcache_logprobs_backward(const void* x, int64_t ldx, int64_t T, int32_t C, int32_t dtype,
+                                                      float temperature, const int32_t* label, const float* g_logp,
+                                                      const float* g_lse, const float* g_entropy, int32_t k,
+                                                      const int32_t* top_index, const float* g_top, void* dx,
+                                                      int64_t lddx, lipcache_stream_t stream) {
+  if (lipcache_status st = row_check(x, ldx, T, C, dtype, temperature); st != LIPCACHE_OK) return st;
+  if (k < 0 || lddx < C || (T > 0 && !dx) || (T > 0 && k > 0 && (!top_index || !g_top)) || (g_logp && !label))
+    return LIPCACHE_EINVAL;
+  if (row_unaligned(dx, dtype) || row_unaligned4(label) || row_unaligned4(g_logp) || row_unaligned4(g_lse) ||
+      row_unaligned4(g_entropy) || row_unaligned4(top_index) || row_unaligned4(g_top))
+    return LIPCACHE_EINVAL;
+  if (k > LIPCACHE_MOST_ENTRIES) return LIPCACHE_EUNSUPPORTED;
+  if (T == 0) return LIPCACHE_OK;
+  const int bits = entry_bits(C);
+  const LpBackward a{temperature, label, g_logp, g_lse, g_entropy, k, top_index, g_top, bits};
+  return row_typed(dtype, [&](auto type) {
+    typedef decltype(type) E;
+    return row_shaped_entries<E>(C, k + 1, [&](auto shape, auto whole) {
+      typedef decltype(shape) S;
+      auto run = [&](auto entropy) {
+        lp_backward_kernel<E, S, decltype(whole)::value, decltype(entropy)::value>
+            <<<row_blocks<S>(T), S::kThreads, S::kRows * entry_bytes(k + 1, bits), stream>>>(
+                static_cast<const E*>(x), ldx, T, C, a, static_cast<E*>(dx), lddx);
+        return hipGetLastError() == hipSuccess ? LIPCACHE_OK : LIPCACHE_EHIP;
+      };
+      return g_entropy ? run(std::true_type{}) : run(std::false_type{});
+    });
+  });
+}
