@@ -6,8 +6,7 @@ namespace lc {
 
 struct LpDistill {
   float temperature, hard, soft;
-  float scale, second;  // log2(e) over the temperature of the first sum, of the second
-  int hot, cold;        // which sum is the teacher's, the label's: 0 the first, 1 the second
+  float scale, second;  // log2(e) over the temperature of the first sum (the teacher's, where there are two), of the second
   const int32_t* label;
   const float* weight;
   int k;
@@ -21,7 +20,6 @@ struct LpShares {
   float hard, soft;  // of the row, with its weight; zero where it has no label, no entry
 };
 
-// The label is the last of a row's k + 1 entries.
 template <class E, class S, bool kWhole, bool kTwo>
 __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits, int64_t ldx, int64_t T, int C,
                                                                  LpDistill a, E* grad, int64_t ldd) {
@@ -32,48 +30,43 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
   __shared__ LpShares shares[2][S::kRows];
   extern __shared__ __align__(16) char lds[];
   const RowPlace<S> at;
-  const int n = a.k + 1, lane = at.g;  // (of the row's first wave, where lane matters)
+  const int lane = at.g;  // (of the row's first wave, where it matters)
   const bool keeps = at.g < kLanes;
-  RowEntries entries(lds + at.row * entry_bytes(n, a.bits), n, a.bits);
+  RowEntries<kLanes> entries(lds + at.row * entry_bytes(a.k, a.bits), a.k, a.bits);
   const RowScale scale{a.scale, a.second};
   const float hot_scale = kRowLog2e / a.temperature;
   const int64_t step = static_cast<int64_t>(gridDim.x) * S::kRows;
   const int full = C / Data::V;
   auto row_of = [&](int64_t t) { return logits + (t < T ? t : T - 1) * ldx; };
-  struct Entry {
-    int at;
-    float value;
-  };
   auto entry_of = [&](int64_t t, int i) {
-    Entry e{-1, 0.0f};
-    if (t >= T || i >= n) return e;
-    if (i < a.k) {
-      e = {a.index[t * a.k + i], a.teacher[t * a.k + i]};
-    } else if (a.label) {
-      e.at = a.label[t];
-    }
+    RowEntry e{-1, 0.0f};
+    if (t < T && i < a.k) e = {a.index[t * a.k + i], a.teacher[t * a.k + i]};
     return e;
   };
-  auto checked = [&](Entry e) {
-    if (e.at >= C) e.at = -1;
-    return e;
-  };
+  auto label_of = [&](int64_t t) { return t < T && a.label ? a.label[t] : -1; };
+  auto inside = [&](int c) { return c < C ? c : -1; };
   auto logit_of = [&](int64_t t, int c) { return c >= 0 ? static_cast<float>(row_of(t)[c]) : 0.0f; };
   Data data;
   int64_t t = static_cast<int64_t>(blockIdx.x) * S::kRows + at.row;
-  Entry mine{-1, 0.0f};
-  float logit = 0.0f;
+  RowEntry mine{-1, 0.0f};
+  int y = -1;
+  float logit = 0.0f, y_logit = 0.0f;
   if (keeps) {
-    mine = checked(entry_of(t, lane));
+    mine = entry_of(t, lane);
+    mine.at = inside(mine.at);
+    y = inside(label_of(t));
     logit = logit_of(t, mine.at);
+    y_logit = logit_of(t, y);
   }
   data.load(row_of(t), 0, C, at.g);
   for (int turn = 0; t - at.row < T; t += step, turn ^= 1) {
     const E* x = row_of(t);
-    Entry next_entry{-1, 0.0f};
+    RowEntry next_entry{-1, 0.0f};
+    int next_y = -1;
     float w = 1.0f;
     if (keeps) {
       next_entry = entry_of(t + step, lane);
+      next_y = label_of(t + step);
       if (a.weight && t < T) w = a.weight[t];
     }
     RowSums r;
@@ -85,45 +78,44 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
         data.template add<kWants, false>(r, scale);
       }
     }
-    next_entry = checked(next_entry);
+    next_entry.at = inside(next_entry.at);
+    next_y = inside(next_y);
     float top = -kRowInf, sum = 0.0f, some = 0.0f;
     if (keeps) {
-      for (int i = lane; i < n; i += kLanes) {
-        if (i != lane) {
-          mine = checked(entry_of(t, i));
-          logit = logit_of(t, mine.at);
+      auto loaded = [&](int i) {
+        RowEntry e = entry_of(t, i);
+        e.at = inside(e.at);
+        return e;
+      };
+      entries.keep(lane, mine, logit, loaded, [&](int c) { return logit_of(t, c); });
+      for (int i = lane; i < a.k; i += kLanes)
+        if (entries.at[i] >= 0) {
+          const float v = entries.value[i];
+          top = fmaxf(top, v);
+          some = v == -kRowInf ? some : 1.0f;  // (a NaN is an entry)
         }
-        entries.at[i] = mine.at;
-        entries.value[i] = mine.value;
-        entries.logit[i] = logit;
-        if (i < a.k && mine.at >= 0) {
-          top = fmaxf(top, mine.value);
-          some = mine.value == -kRowInf ? some : 1.0f;  // (a NaN is an entry)
-        }
-      }
-      wave_sync();
       top = row_from(lanes_max<kLanes>(top));
       some = lanes_max<kLanes>(some);
       for (int i = lane; i < a.k; i += kLanes)
         if (entries.at[i] >= 0) sum += row_exp2((entries.value[i] - top) * hot_scale);
       sum = lanes_sum<kLanes>(sum);
-      if (lane == 0)
-        shares[turn][at.row] = {entries.at[a.k] >= 0 ? w * a.hard : 0.0f, some != 0.0f ? w * a.soft / a.temperature : 0.0f};
+      if (lane == 0) shares[turn][at.row] = {y >= 0 ? w * a.hard : 0.0f, some != 0.0f ? w * a.soft / a.temperature : 0.0f};
       wave_sync();
     }
     row_join<S, kWants>(r, scale, room[turn]);
     const LpShares share = shares[turn][at.row];
-    const float from = row_from(r.m), hot_s = kTwo && a.hot ? r.more : r.s, cold_s = kTwo && a.cold ? r.more : r.s;
+    const float from = row_from(r.m);
     const bool any = (share.hard != 0.0f || share.soft != 0.0f) && r.s != 0.0f;
     // what an element adds: one exponential with both parts' factor, or one for each
-    const float one = kTwo ? (a.hot ? share.hard : share.soft) / r.s : (share.hard + share.soft) / r.s,
-                two = kTwo ? (a.hot ? share.soft : share.hard) / r.more : 0.0f;
+    const float one = (kTwo ? share.soft : share.hard + share.soft) / r.s, two = kTwo ? share.hard / r.more : 0.0f;
     auto smooth = [&](float v) {
       const float d = v - from;
       float g = row_exp2(d * scale.scale) * one;
       if constexpr (kTwo) g = fmaf(row_exp2(d * scale.second), two, g);
       return g;
     };
+    const int now_y = y;
+    const float now_logit = y_logit;
     if (keeps) {
       float kl = 0.0f;
       for (int i = lane; i < a.k; i += kLanes) {
@@ -135,24 +127,20 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
         if (part == 0.0f) entries.at[i] = -1;
       }
       kl = lanes_sum<kLanes>(kl);
-      if (lane == 0) {
-        const int y = entries.at[a.k];
-        if (t < T && a.ce)
-          a.ce[t] = y < 0 ? 0.0f : r.s == 0.0f ? kRowInf : row_log2(cold_s) * kRowLn2 - (entries.logit[a.k] - from);
-        if (t < T && a.kl) a.kl[t] = some == 0.0f ? 0.0f : r.s == 0.0f ? kRowInf : (kl + row_log2(hot_s) - row_log2(sum)) * kRowLn2;
-        entries.value[a.k] = share.hard;
-        if (share.hard == 0.0f) entries.at[a.k] = -1;
+      if (lane == 0 && t < T) {
+        if (a.ce)
+          a.ce[t] = y < 0 ? 0.0f : r.s == 0.0f ? kRowInf : row_log2(kTwo ? r.more : r.s) * kRowLn2 - (y_logit - from);
+        if (a.kl) a.kl[t] = some == 0.0f ? 0.0f : r.s == 0.0f ? kRowInf : (kl + row_log2(r.s) - row_log2(sum)) * kRowLn2;
       }
       wave_sync();
+      mine = next_entry;
+      y = next_y;
+      logit = logit_of(t + step, mine.at);
+      y_logit = logit_of(t + step, y);
     }
     const E* following = row_of(t + step);
-    if (keeps) {
-      mine = next_entry;
-      logit = logit_of(t + step, mine.at);
-    }
     if (!grad) {
       data.load(following, 0, C, at.g);
-      RowPlace<S>::sync();
       continue;
     }
     E* dx = grad + (t < T ? t : T - 1) * ldd;
@@ -178,11 +166,13 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
     data.load_tail(following, C, at.g);
     RowPlace<S>::sync();  // the row is written before its entries are
     if (keeps && any && t < T) {
-      entries.index<kLanes>(lane, n);
-      for (int i = lane; i < n; i += kLanes) {
+      const bool named = now_y >= 0 && share.hard != 0.0f, met = named && entries.add(lane, now_y, share.hard);
+      entries.index(lane);
+      for (int i = lane; i < a.k; i += kLanes) {
         float q;
-        if (entries.first(i, n, q)) dx[entries.at[i]] = static_cast<E>(smooth(entries.logit[i]) - q);
+        if (entries.first(i, q)) dx[entries.at[i]] = static_cast<E>(smooth(entries.logit[i]) - q);
       }
+      if (lane == 0 && named && !met) dx[now_y] = static_cast<E>(smooth(now_logit) - share.hard);
     }
   }
 }
@@ -209,15 +199,15 @@ extern "C" lipcache_status lipcache_distill(const void* x, int64_t ldx, int64_t 
   const bool cold = label && (hard != 0.0f || ce), hot = k > 0 && (soft != 0.0f || kl);
   const bool two = cold && hot && temperature != 1.0f;
   const float at_one = kRowLog2e, at_own = kRowLog2e / temperature;
-  const LpDistill a{temperature, hard, soft, hot ? at_own : at_one, at_one, 0, two ? 1 : 0, label, weight, k,
+  const LpDistill a{temperature, hard, soft, hot ? at_own : at_one, at_one, label, weight, k,
                     teacher, index, ce, kl, bits};
   return row_typed(dtype, [&](auto type) {
     typedef decltype(type) E;
-    return row_shaped_entries<E>(C, k + 1, [&](auto shape, auto whole) {
+    return row_shaped_entries<E>(C, k, [&](auto shape, auto whole) {
       typedef decltype(shape) S;
       auto run = [&](auto both) {
         lp_distill_kernel<E, S, decltype(whole)::value, decltype(both)::value>
-            <<<row_blocks<S>(T), S::kThreads, S::kRows * entry_bytes(k + 1, bits), stream>>>(
+            <<<row_blocks<S>(T), S::kThreads, S::kRows * entry_bytes(k, bits), stream>>>(
                 static_cast<const E*>(x), ldx, T, C, a, static_cast<E*>(dx), lddx);
         return hipGetLastError() == hipSuccess ? LIPCACHE_OK : LIPCACHE_EHIP;
       };

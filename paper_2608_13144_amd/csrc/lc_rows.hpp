@@ -199,6 +199,30 @@ struct RowData {
       __builtin_amdgcn_sched_barrier(0);
     }
   }
+  // f(index) for every element of the thread's chunks that is `least` or more and not -inf.  Found in one pass over the
+  // registers, two instructions an element.
+  template <class F>
+  __device__ __forceinline__ void reaching(float least, int first, int g, F f) {
+    constexpr int kMasks = (N * V + 31) / 32, kEach = 32 / V < N ? 32 / V : N;  // chunks of a mask
+#pragma unroll
+    for (int h = 0; h < kMasks; ++h) {
+      uint32_t mask = 0;
+#pragma unroll
+      for (int i = h * kEach; i < (h + 1) * kEach; ++i) {
+        pin(i);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float v = Type::get(raw[i], e);
+          mask = 2 * mask + (v >= least && v > -kRowInf ? 1u : 0u);
+        }
+      }
+      while (mask) {
+        const int at = __builtin_clz(mask) - (32 - kEach * V);  // element of the mask's, in order
+        mask &= ~(0x80000000u >> __builtin_clz(mask));
+        f((first + G * (h * kEach + at / V) + g) * V + at % V);
+      }
+    }
+  }
   // Writes f of every element of chunk i to the row at out, where it has the chunk.
   template <class F>
   __device__ __forceinline__ void store_chunk(int i, E* out, int first, int full, int g, F f) {
@@ -290,27 +314,74 @@ inline int entry_bits(int C) {
   while (bits < C && bits < kEntryBits) bits *= 2;
   return bits;
 }
-__host__ __device__ inline size_t entry_bytes(int most, int bits) { return (static_cast<size_t>(most) * 12 + bits / 4 + 15) / 16 * 16; }
+__host__ __device__ inline size_t entry_bytes(int most, int bits) {
+  return most == 0 ? 0 : (static_cast<size_t>(most) * 12 + bits / 4 + 15) / 16 * 16;
+}
 
+struct RowEntry {
+  int at;       // class, -1: none
+  float value;
+};
+
+template <int LANES>
 struct RowEntries {
-  int* at;        // [most] class, -1: none
-  float* value;   // [most]
-  float* logit;   // [most] the row's own at the class
+  int* at;        // [n] class, -1: none
+  float* value;   // [n]
+  float* logit;   // [n] the row's own at the class
   uint32_t *seen, *twice;
-  int bits;
-  __device__ __forceinline__ RowEntries(char* lds, int most, int bits_)
+  int n, bits;
+  __device__ __forceinline__ RowEntries(char* lds, int n_, int bits_)
       : at(reinterpret_cast<int*>(lds + bits_ / 4)),
-        value(reinterpret_cast<float*>(lds + bits_ / 4) + most),
-        logit(reinterpret_cast<float*>(lds + bits_ / 4) + 2 * most),
+        value(reinterpret_cast<float*>(lds + bits_ / 4) + n_),
+        logit(reinterpret_cast<float*>(lds + bits_ / 4) + 2 * n_),
         seen(reinterpret_cast<uint32_t*>(lds)),
         twice(reinterpret_cast<uint32_t*>(lds) + bits_ / 32),
+        n(n_),
         bits(bits_) {}
-  // By the lanes that keep the entries.  After it, first() may be asked of any.
-  template <int LANES>
-  __device__ __forceinline__ void index(int lane, int count) {
+  // By the lanes that keep the entries: entry `lane` is `mine` with its logit; entry_of and logit_of load the others, four at a
+  // time so that their loads wait together.
+  template <class Entry, class Logit>
+  __device__ __forceinline__ void keep(int lane, RowEntry mine, float mine_logit, Entry entry_of, Logit logit_of) {
+    if (lane < n) {
+      at[lane] = mine.at;
+      value[lane] = mine.value;
+      logit[lane] = mine_logit;
+    }
+    for (int i = lane + LANES; i < n; i += 4 * LANES) {
+      RowEntry e[4];
+      float l[4];
+#pragma unroll
+      for (int p = 0; p < 4; ++p) e[p] = entry_of(i + p * LANES);
+#pragma unroll
+      for (int p = 0; p < 4; ++p) l[p] = logit_of(e[p].at);
+#pragma unroll
+      for (int p = 0; p < 4; ++p)
+        if (i + p * LANES < n) {
+          at[i + p * LANES] = e[p].at;
+          value[i + p * LANES] = e[p].value;
+          logit[i + p * LANES] = l[p];
+        }
+    }
+    wave_sync();
+  }
+  // Adds v to the first entry of class c; false where there is none.
+  __device__ __forceinline__ bool add(int lane, int c, float v) {
+    const int group = LANES == 64 ? 0 : lane_id() / LANES * LANES;  // first lane of the row
+    for (int i = lane; i - lane < n; i += LANES) {
+      const uint64_t all = __ballot(i < n && at[i] == c) >> group;
+      const uint64_t hit = LANES == 64 ? all : all & ((1ull << (LANES & 63)) - 1);
+      if (hit) {
+        if (lane == __builtin_ctzll(hit)) value[i] += v;
+        return true;
+      }
+    }
+    return false;
+  }
+  // Which classes may be named twice.
+  __device__ __forceinline__ void index(int lane) {
     for (int i = lane; i < bits / 16; i += LANES) seen[i] = 0;
     wave_sync();
-    for (int i = lane; i < count; i += LANES) {
+    for (int i = lane; i < n; i += LANES) {
       const int c = at[i];
       if (c < 0) continue;
       const uint32_t b = static_cast<uint32_t>(c) & (bits - 1), bit = 1u << (b & 31);
@@ -318,8 +389,8 @@ struct RowEntries {
     }
     wave_sync();
   }
-  // Whether entry i is the first of its class; if so `sum` is the class's.
-  __device__ __forceinline__ bool first(int i, int count, float& sum) const {
+  // After index(): whether entry i is the first of its class; if so `sum` is the class's.
+  __device__ __forceinline__ bool first(int i, float& sum) const {
     const int c = at[i];
     if (c < 0) return false;
     sum = value[i];
@@ -327,11 +398,13 @@ struct RowEntries {
     if (!(twice[b >> 5] >> (b & 31) & 1)) return true;
     float all = 0.0f;
     bool mine = true;
-    for (int j = 0; j < count; ++j)
-      if (at[j] == c) {
-        mine = mine && j >= i;
-        all += value[j];
-      }
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) {
+      const bool same = at[j] == c;
+      const float v = value[j];
+      mine = mine && !(same && j < i);
+      all = same ? all + v : all;
+    }
     sum = all;
     return mine;
   }
@@ -381,7 +454,7 @@ template <class E, class F>
 lipcache_status row_shaped_entries(int C, int n, F f) {
   return row_shaped<E>(C, [&](auto shape, auto whole) {
     if constexpr (decltype(shape)::G < 64) {
-      if (n > 32) return f(RowShape<64, 4>{}, std::true_type{});
+      if (n > 16) return f(RowShape<64, 4>{}, std::true_type{});
     }
     return f(shape, whole);
   });

@@ -5,7 +5,11 @@
 namespace lc {
 
 constexpr int kTopMost = LIPCACHE_MOST_TOP;
-constexpr int kTopList = 512;  // candidates that a row's list holds (rows of a wave and more)
+// Candidates that a row's list holds, and the groups of threads whose largest values give the threshold.
+template <class S>
+inline constexpr int kTopList = S::G >= 64 ? 512 : 32;
+template <class S>
+inline constexpr int kTopGroups = S::G >= 64 ? 64 : 16;
 
 struct LpScore {
   float temperature;
@@ -23,10 +27,10 @@ struct TopCandidate {
 
 template <class S>
 struct TopSpace {
-  float maxima[S::kRows][S::G >= 64 ? 64 : 1];
+  float maxima[S::kRows][kTopGroups<S>];
   float least[S::kRows];
   int count[S::kRows];
-  TopCandidate list[S::kRows][S::G >= 64 ? kTopList : 1];
+  TopCandidate list[S::kRows][kTopList<S>];
 };
 template <class S>
 struct TopRoom {
@@ -72,20 +76,21 @@ __device__ __forceinline__ void top_rounds(int k, TopRoom<S>& room, Each each, P
   }
 }
 
-// A row's k largest by a threshold: the largest value that k of 64 groups of threads reach.  What reaches it
-// is a list of little more than k, each of which finds its place by counting.  Rows whose list would be
-// longer (many equal values) go round by round.
-template <class S, class Each, class Put>
+// A row's k largest by a threshold: the largest value that k of the groups of threads reach.  What reaches it
+// is a list of little more than k, each of which finds its place by counting: reaching(least, f) calls f(index) for
+// the thread's elements that do, logit_of(index) gives the value.  Rows whose list would be longer (many equal
+// values, or all large ones in few threads) go round by round.
+template <class S, class Each, class Reaching, class Logit, class Put>
 __device__ __forceinline__ void top_listed(int k, float own, const RowPlace<S>& at, TopSpace<S>& top, TopRoom<S>& room,
-                                           Each each, Put put) {
-  const int lane = lane_id();
+                                           Each each, Reaching reaching, Logit logit_of, Put put) {
+  constexpr int kGroups = kTopGroups<S>;
   if (S::kWaves == 1 || threadIdx.x < kWave) {
-    const float v = top.maxima[at.row][lane];
+    const float v = top.maxima[at.row][at.g % kGroups];
     int n = 0;
 #pragma unroll
-    for (int j = 0; j < 64; ++j) n += lane_f32(v, j) >= v ? 1 : 0;
-    const float least = lanes_max<64>(n >= k ? v : -kRowInf);
-    if (lane == 0) {
+    for (int j = 0; j < kGroups; ++j) n += (kGroups == 64 ? lane_f32(v, j) : top.maxima[at.row][j]) >= v ? 1 : 0;
+    const float least = lanes_max<kGroups>(n >= k ? v : -kRowInf);
+    if (at.g == 0) {
       top.least[at.row] = least;
       top.count[at.row] = 0;
     }
@@ -93,15 +98,13 @@ __device__ __forceinline__ void top_listed(int k, float own, const RowPlace<S>& 
   RowPlace<S>::sync();
   const float least = top.least[at.row];
   if (own >= least && own > -kRowInf)
-    each([&](float v, int j) {
-      if (v >= least && v > -kRowInf) {
-        const int n = atomicAdd(&top.count[at.row], 1);
-        if (n < kTopList) top.list[at.row][n] = {v, j};
-      }
+    reaching(least, [&](int j) {
+      const int n = atomicAdd(&top.count[at.row], 1);
+      if (n < kTopList<S>) top.list[at.row][n] = {logit_of(j), j};
     });
   RowPlace<S>::sync();
   const int n = top.count[at.row];
-  if (n > kTopList) {
+  if (n > kTopList<S>) {
     top_rounds<S>(k, room, each, [&](int i, float v, int j) {
       if (at.g == 0) put(i, v, j);
     });
@@ -111,6 +114,7 @@ __device__ __forceinline__ void top_listed(int k, float own, const RowPlace<S>& 
     if (c < n) {
       const TopCandidate mine = top.list[at.row][c];
       int place = 0;
+#pragma unroll 4
       for (int i = 0; i < n; ++i) {
         const TopCandidate other = top.list[at.row][i];
         place += top_before(other.v, other.j, mine.v, mine.j) ? 1 : 0;
@@ -158,18 +162,18 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
     const float own = r.m;
     next_y = checked(next_y);
     const float next_logit = logit_of(t + step, next_y);
-    if (S::G >= 64 && a.k > 0) {
+    if (a.k > 0) {
       float m = own;
       if constexpr (S::G >= 128) m = fmaxf(m, dpp_f32<kDppQuadXor1>(m));
       if constexpr (S::G >= 256) m = fmaxf(m, dpp_f32<kDppQuadXor2>(m));
       if constexpr (S::G >= 512) m = fmaxf(m, dpp_f32<kDppHalfMirror>(m));
       if constexpr (S::G >= 1024) m = fmaxf(m, dpp_f32<kDppMirror>(m));
-      constexpr int kEach = S::G / 64;
+      constexpr int kEach = S::G / kTopGroups<S>;
       if (at.g % kEach == 0) top.maxima[at.row][at.g / kEach] = m;
     }
     auto next = [&] { data.load(row_of(t + step), 0, C, at.g); };
     if (kWhole && a.k == 0) next();
-    if constexpr (S::G == 64) wave_sync();  // the join of longer rows has a barrier
+    if constexpr (S::G <= 64) wave_sync();  // the join of longer rows has a barrier
     row_join<S, RowWants::kMean>(r, scale, room[turn]);
     const float from = row_from(r.m), log_s = row_log2(r.s);
     auto logp = [&](float v) { return r.s == 0.0f ? -kRowInf : (v - from) / a.temperature - log_s * kRowLn2; };
@@ -184,20 +188,30 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
         a.top_index[t * a.k + i] = v == -kRowInf ? -1 : j;
         a.top_logp[t * a.k + i] = v == -kRowInf ? -kRowInf : logp(v);
       };
+      // the rare ways through the row read it again
       auto each = [&](auto f) {
+#pragma unroll 1
+        for (int c = at.g; c < full; c += S::G) {
+          const u32x4 raw = *reinterpret_cast<const typename Data::Type::vec*>(x + static_cast<int64_t>(c) * Data::V);
+#pragma unroll
+          for (int e = 0; e < Data::V; ++e) f(Data::Type::get(raw, e), c * Data::V + e);
+        }
+        f(data.tail, full * Data::V + at.g);
+      };
+      auto reaching = [&](float least, auto f) {
         if constexpr (kWhole) {
-          data.each(0, at.g, f);
+          data.reaching(least, 0, at.g, f);
         } else {
           for (int first = 0; first < full; first += kSegment) {
 #pragma unroll
             for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, full, at.g);
-            data.each(first, at.g, f);
+            data.reaching(least, first, at.g, f);
           }
         }
-        f(data.tail, full * Data::V + at.g);
+        if (data.tail >= least && data.tail > -kRowInf) f(full * Data::V + at.g);
       };
-      if constexpr (S::G >= 64) {
-        top_listed<S>(a.k, own, at, top, top_room, each, put);
+      if (a.k <= kTopGroups<S>) {
+        top_listed<S>(a.k, own, at, top, top_room, each, reaching, [&](int j) { return static_cast<float>(x[j]); }, put);
       } else {
         top_rounds<S>(a.k, top_room, each, [&](int i, float v, int j) {
           if (at.g == 0) put(i, v, j);

@@ -21,7 +21,6 @@ struct LpSlope {
   int some;    // any gradient that is not zero
 };
 
-// The label is the last of a row's k + 1 entries.
 template <class E, class S, bool kWhole, bool kEntropy>
 __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logits, int64_t ldx, int64_t T, int C,
                                                                   LpBackward a, E* grad, int64_t ldd) {
@@ -32,49 +31,48 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
   __shared__ LpSlope slope[S::kRows];
   extern __shared__ __align__(16) char lds[];
   const RowPlace<S> at;
-  const int n = a.k + 1, lane = at.g;  // (of the row's first wave, where lane matters)
+  const int lane = at.g;  // (of the row's first wave, where it matters)
   const bool keeps = at.g < kLanes;
-  RowEntries entries(lds + at.row * entry_bytes(n, a.bits), n, a.bits);
+  RowEntries<kLanes> entries(lds + at.row * entry_bytes(a.k, a.bits), a.k, a.bits);
   const RowScale scale{kRowLog2e / a.temperature, 0.0f};
   const float inv_t = 1.0f / a.temperature;
   const int64_t step = static_cast<int64_t>(gridDim.x) * S::kRows;
   const int full = C / Data::V;
   auto row_of = [&](int64_t t) { return logits + (t < T ? t : T - 1) * ldx; };
-  struct Entry {
-    int at;
-    float value;
-  };
   auto entry_of = [&](int64_t t, int i) {
-    Entry e{-1, 0.0f};
-    if (t >= T || i >= n) return e;
-    if (i < a.k) {
-      e = {a.top_index[t * a.k + i], a.g_top[t * a.k + i]};
-    } else if (a.g_logp) {
-      e = {a.label[t], a.g_logp[t]};
-    }
+    RowEntry e{-1, 0.0f};
+    if (t < T && i < a.k) e = {a.top_index[t * a.k + i], a.g_top[t * a.k + i]};
     return e;
   };
-  auto checked = [&](Entry e) {
+  auto label_of = [&](int64_t t) {
+    RowEntry e{-1, 0.0f};
+    if (t < T && a.g_logp) e = {a.label[t], a.g_logp[t]};
+    return e;
+  };
+  auto checked = [&](RowEntry e) {
     if (e.at < 0 || e.at >= C || e.value == 0.0f) e = {-1, 0.0f};
     return e;
   };
   auto logit_of = [&](int64_t t, int c) { return c >= 0 ? static_cast<float>(row_of(t)[c]) : 0.0f; };
   Data data;
   int64_t t = static_cast<int64_t>(blockIdx.x) * S::kRows + at.row;
-  Entry mine{-1, 0.0f};
-  float logit = 0.0f;
+  RowEntry mine{-1, 0.0f}, label{-1, 0.0f};
+  float logit = 0.0f, label_logit = 0.0f;
   if (keeps) {
     mine = checked(entry_of(t, lane));
+    label = checked(label_of(t));
     logit = logit_of(t, mine.at);
+    label_logit = logit_of(t, label.at);
   }
   data.load(row_of(t), 0, C, at.g);
   for (; t - at.row < T; t += step) {
     const E* x = row_of(t);
     E* dx = grad + (t < T ? t : T - 1) * ldd;
-    Entry next_entry{-1, 0.0f};
+    RowEntry next_entry{-1, 0.0f}, next_label{-1, 0.0f};
     float gl = 0.0f, ge = 0.0f;
     if (keeps) {
       next_entry = entry_of(t + step, lane);
+      next_label = label_of(t + step);
       if (a.g_lse && t < T) gl = a.g_lse[t];
       if (kEntropy && t < T) ge = a.g_entropy[t];
     }
@@ -88,20 +86,16 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
       }
     }
     next_entry = checked(next_entry);
+    next_label = checked(next_label);
     if (keeps) {
-      float mass = 0.0f, any = gl != 0.0f || ge != 0.0f ? 1.0f : 0.0f;
-      for (int i = lane; i < n; i += kLanes) {
-        if (i != lane) {
-          mine = checked(entry_of(t, i));
-          logit = logit_of(t, mine.at);
-        }
-        entries.at[i] = mine.at;
-        entries.value[i] = mine.value;
-        entries.logit[i] = logit;
-        mass += mine.value;
-        any = mine.value != 0.0f ? 1.0f : any;
+      entries.keep(lane, mine, logit, [&](int i) { return checked(entry_of(t, i)); }, [&](int c) { return logit_of(t, c); });
+      float mass = 0.0f, any = gl != 0.0f || ge != 0.0f || label.value != 0.0f ? 1.0f : 0.0f;
+      for (int i = lane; i < a.k; i += kLanes) {
+        const float v = entries.value[i];
+        mass += v;
+        any = v != 0.0f ? 1.0f : any;
       }
-      mass = lanes_sum<kLanes>(mass);
+      mass = lanes_sum<kLanes>(mass) + label.value;
       any = lanes_max<kLanes>(any);
       if (lane == 0) slope[at.row] = {gl - mass, ge, any != 0.0f ? 1 : 0};
       wave_sync();
@@ -118,9 +112,13 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
     };
     auto dx_of = [&](float v) { return some ? smooth(v) : 0.0f; };
     const E* following = row_of(t + step);
+    const RowEntry now = label;
+    const float now_logit = label_logit;
     if (keeps) {
       mine = next_entry;
+      label = next_label;
       logit = logit_of(t + step, mine.at);
+      label_logit = logit_of(t + step, label.at);
     }
     if (kWhole) {
 #pragma unroll
@@ -143,11 +141,13 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
     data.load_tail(following, C, at.g);
     RowPlace<S>::sync();  // the row is written before its entries are
     if (keeps && some && t < T) {
-      entries.index<kLanes>(lane, n);
-      for (int i = lane; i < n; i += kLanes) {
+      const bool met = now.at >= 0 && entries.add(lane, now.at, now.value);
+      entries.index(lane);
+      for (int i = lane; i < a.k; i += kLanes) {
         float g;
-        if (entries.first(i, n, g)) dx[entries.at[i]] = static_cast<E>(fmaf(g, inv_t, smooth(entries.logit[i])));
+        if (entries.first(i, g)) dx[entries.at[i]] = static_cast<E>(fmaf(g, inv_t, smooth(entries.logit[i])));
       }
+      if (lane == 0 && now.at >= 0 && !met) dx[now.at] = static_cast<E>(fmaf(now.value, inv_t, smooth(now_logit)));
     }
   }
 }
@@ -173,11 +173,11 @@ extern "C" lipcache_status lipcache_logprobs_backward(const void* x, int64_t ldx
   const LpBackward a{temperature, label, g_logp, g_lse, g_entropy, k, top_index, g_top, bits};
   return row_typed(dtype, [&](auto type) {
     typedef decltype(type) E;
-    return row_shaped_entries<E>(C, k + 1, [&](auto shape, auto whole) {
+    return row_shaped_entries<E>(C, k, [&](auto shape, auto whole) {
       typedef decltype(shape) S;
       auto run = [&](auto entropy) {
         lp_backward_kernel<E, S, decltype(whole)::value, decltype(entropy)::value>
-            <<<row_blocks<S>(T), S::kThreads, S::kRows * entry_bytes(k + 1, bits), stream>>>(
+            <<<row_blocks<S>(T), S::kThreads, S::kRows * entry_bytes(k, bits), stream>>>(
                 static_cast<const E*>(x), ldx, T, C, a, static_cast<E*>(dx), lddx);
         return hipGetLastError() == hipSuccess ? LIPCACHE_OK : LIPCACHE_EHIP;
       };
