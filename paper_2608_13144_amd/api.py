@@ -670,19 +670,24 @@ def logprobs(logits: torch.Tensor, labels: torch.Tensor | None = None, top: int 
     if not 0 <= k <= L.MOST_TOP:
         raise ValueError(f"top must be 0 to {L.MOST_TOP}")
     label = _of_rows(labels, "labels", torch.int32, dev, (T,))
+    f32, i32 = torch.float32, torch.int32
     if out is None:
-        each = torch.empty((3, T), dtype=torch.float32, device=dev)
-        out = LogProbs(each[0], each[1], each[2], torch.empty((T, k), dtype=torch.int32, device=dev) if k else None,
-                       torch.empty((T, k), dtype=torch.float32, device=dev) if k else None)
-    elif k and (out.top_index is None or out.top_logp is None):
-        raise ValueError("out lacks top_index or top_logp")
-    f32 = torch.float32
-    lib = L.load()
-    st = lib.lipcache_logprobs(logits.data_ptr(), ld, T, C, code, float(temperature), label, k,
-                               _of_rows(out.logp, "out.logp", f32, dev, (T,)), _of_rows(out.lse, "out.lse", f32, dev, (T,)),
-                               _of_rows(out.entropy, "out.entropy", f32, dev, (T,)),
-                               _of_rows(out.top_index, "out.top_index", torch.int32, dev, (T, k)) if k else None,
-                               _of_rows(out.top_logp, "out.top_logp", f32, dev, (T, k)) if k else None, _stream_of(dev))
+        each = torch.empty((3, T), dtype=f32, device=dev)
+        out = LogProbs(*each.unbind(0), None, None)
+        at = each.data_ptr()
+        logp, lse, entropy, index, value = at, at + 4 * T, at + 8 * T, None, None
+        if k:
+            out.top_index = torch.empty((T, k), dtype=i32, device=dev)
+            out.top_logp = torch.empty((T, k), dtype=f32, device=dev)
+            index, value = out.top_index.data_ptr(), out.top_logp.data_ptr()
+    else:
+        if k and (out.top_index is None or out.top_logp is None):
+            raise ValueError("out lacks top_index or top_logp")
+        logp, lse, entropy = (_of_rows(getattr(out, name), "out." + name, f32, dev, (T,)) for name in ("logp", "lse", "entropy"))
+        index = _of_rows(out.top_index, "out.top_index", i32, dev, (T, k)) if k else None
+        value = _of_rows(out.top_logp, "out.top_logp", f32, dev, (T, k)) if k else None
+    st = L.load().lipcache_logprobs(logits.data_ptr(), ld, T, C, code, float(temperature), label, k, logp, lse, entropy,
+                                    index, value, _stream_of(dev))
     L.check("lipcache_logprobs", st)
     return out
 
@@ -742,19 +747,18 @@ def distill(logits: torch.Tensor, teacher: torch.Tensor | None, index: torch.Ten
         raise ValueError(f"teacher must have at most {L.MOST_ENTRIES} columns")
     label = _of_rows(labels, "labels", torch.int32, dev, (T,))
     each = torch.empty((2, T), dtype=f32, device=dev)
-    ldd = C
+    losses, ldd = each.data_ptr(), C
     if out is not None:
         if not want_grad:
             raise ValueError("out is the gradient's: it goes with want_grad")
         ldd = _need_rows(out, "out", logits.dtype, dev, T, C)
     elif want_grad:
         out = logits.new_empty((T, C))
-    lib = L.load()
-    st = lib.lipcache_distill(logits.data_ptr(), ld, T, C, code, float(temperature), float(hard), float(soft), k, value, at,
-                              label, _of_rows(weight, "weight", f32, dev, (T,)), each[0].data_ptr(), each[1].data_ptr(),
-                              None if out is None else out.data_ptr(), ldd, _stream_of(dev))
+    st = L.load().lipcache_distill(logits.data_ptr(), ld, T, C, code, float(temperature), float(hard), float(soft), k, value,
+                                   at, label, _of_rows(weight, "weight", f32, dev, (T,)), losses, losses + 4 * T,
+                                   None if out is None else out.data_ptr(), ldd, _stream_of(dev))
     L.check("lipcache_distill", st)
-    return Distilled(each[0], each[1], out)
+    return Distilled(*each.unbind(0), out)
 
 
 @_on_device
@@ -773,11 +777,12 @@ def head_logprobs(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None, l
     ldx = _need_rows(x, "x", dt, dev, T, K)
     ldw = _need_rows(W, "W", dt, dev, C, K)
     each = torch.empty((3, T), dtype=torch.float32, device=dev)
+    scores = each.data_ptr()
     lib = L.load()
     ws = workspace(lib.lipcache_head_logprobs_workspace_bytes(T, K, C, code), dev)
     st = lib.lipcache_head_logprobs(x.data_ptr(), ldx, T, W.data_ptr(), ldw,
                                     _of_rows(bias, "bias", torch.float32, dev, (C,)), K, C, code, float(temperature),
-                                    _of_rows(labels, "labels", torch.int32, dev, (T,)), each[0].data_ptr(),
-                                    each[1].data_ptr(), each[2].data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(dev))
+                                    _of_rows(labels, "labels", torch.int32, dev, (T,)), scores, scores + 4 * T,
+                                    scores + 8 * T, ws.data_ptr(), ws.numel(), _stream_of(dev))
     L.check("lipcache_head_logprobs", st)
-    return LogProbs(each[0], each[1], each[2], None, None)
+    return LogProbs(*each.unbind(0), None, None)

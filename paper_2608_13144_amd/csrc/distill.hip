@@ -69,14 +69,13 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
       next_y = label_of(t + step);
       if (a.weight && t < T) w = a.weight[t];
     }
-    RowSums r;
-    data.template add<kWants, true>(r, scale);
-    if constexpr (!kWhole) {
-      for (int first = kSegment; first < full; first += kSegment) {
-#pragma unroll
-        for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, full, at.g);
-        data.template add<kWants, false>(r, scale);
-      }
+    RowSums r = data.template begin<kWants>(scale);
+    if constexpr (kWhole) {
+      data.template add<kWants>(0, full, at.g, r, scale, RowNothing{}, RowNothing{});
+    } else {
+      // a segment's chunks are asked for as the one before is used
+      for (int first = 0; first < full; first += kSegment)
+        data.template add<kWants>(first, full, at.g, r, scale, RowNothing{}, [&](int i) { data.load_chunk(i, x, first + kSegment, full, at.g); });
     }
     next_entry.at = inside(next_entry.at);
     next_y = inside(next_y);
@@ -203,7 +202,7 @@ extern "C" lipcache_status lipcache_distill(const void* x, int64_t ldx, int64_t 
                     teacher, index, ce, kl, bits};
   return row_typed(dtype, [&](auto type) {
     typedef decltype(type) E;
-    return row_shaped_entries<E>(C, k, [&](auto shape, auto whole) {
+    return row_shaped_entries<E>(T, C, k, [&](auto shape, auto whole) {
       typedef decltype(shape) S;
       auto run = [&](auto both) {
         lp_distill_kernel<E, S, decltype(whole)::value, decltype(both)::value>

@@ -37,6 +37,7 @@ struct RowType<float> {
   static constexpr uint32_t kFill = 0xff800000u;
   typedef u32x4 __attribute__((aligned(4))) vec;
   static __device__ __forceinline__ float get(const u32x4& r, int e) { return __builtin_bit_cast(f32x4, r)[e]; }
+  static __device__ __forceinline__ float part(uint32_t word, int) { return __builtin_bit_cast(float, word); }  // element of a word
   static __device__ __forceinline__ u32x4 pack(const float* v) {
     return __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
   }
@@ -50,6 +51,9 @@ struct RowType<__bf16> {
     const uint32_t both = r[e >> 1];
     return __builtin_bit_cast(float, e & 1 ? both & 0xffff0000u : both << 16);
   }
+  static __device__ __forceinline__ float part(uint32_t word, int e) {
+    return __builtin_bit_cast(float, (e & 1 ? word >> 16 : word) << 16);
+  }
   static __device__ __forceinline__ u32x4 pack(const float* v) { return pack_bf16x8(v); }
 };
 template <>
@@ -59,6 +63,9 @@ struct RowType<_Float16> {
   typedef u32x4 __attribute__((aligned(2))) vec;
   static __device__ __forceinline__ float get(const u32x4& r, int e) {
     return static_cast<float>(__builtin_bit_cast(f16x8, r)[e]);
+  }
+  static __device__ __forceinline__ float part(uint32_t word, int e) {
+    return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(e & 1 ? word >> 16 : word)));
   }
   static __device__ __forceinline__ u32x4 pack(const float* v) {
     f16x8 h;
@@ -102,6 +109,11 @@ template <int L>
 __device__ __forceinline__ float lanes_max(float v) {
   return lanes_join<L>(v, [](float a, float b) { return fmaxf(a, b); });
 }
+
+struct RowNothing {
+  template <class... A>
+  __device__ __forceinline__ void operator()(A...) const {}
+};
 
 // LDS written by lanes of a wave, read by others of it.
 __device__ __forceinline__ void wave_sync() {
@@ -188,39 +200,20 @@ struct RowData {
 #pragma unroll
     for (int i = 0; i < N; ++i) load_chunk(i, x, first, C / V, g);
   }
+  // Whether chunk i is past the row for every lane of the wave (of the row, where a wave holds several).
+  static __device__ __forceinline__ bool past(int i, int first, int full, int g) {
+    return first + G * i + (G > 64 ? uniform(g) / kWave * kWave : 0) >= full;
+  }
   // f(value, index) for every element of the thread's chunks, rising index.
   template <class F>
-  __device__ __forceinline__ void each(int first, int g, F f) {
+  __device__ __forceinline__ void each(int first, int full, int g, F f) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
+      if (past(i, first, full, g)) break;
       pin(i);
 #pragma unroll
       for (int e = 0; e < V; ++e) f(Type::get(raw[i], e), (first + G * i + g) * V + e);
       __builtin_amdgcn_sched_barrier(0);
-    }
-  }
-  // f(index) for every element of the thread's chunks that is `least` or more and not -inf.  Found in one pass over the
-  // registers, two instructions an element.
-  template <class F>
-  __device__ __forceinline__ void reaching(float least, int first, int g, F f) {
-    constexpr int kMasks = (N * V + 31) / 32, kEach = 32 / V < N ? 32 / V : N;  // chunks of a mask
-#pragma unroll
-    for (int h = 0; h < kMasks; ++h) {
-      uint32_t mask = 0;
-#pragma unroll
-      for (int i = h * kEach; i < (h + 1) * kEach; ++i) {
-        pin(i);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float v = Type::get(raw[i], e);
-          mask = 2 * mask + (v >= least && v > -kRowInf ? 1u : 0u);
-        }
-      }
-      while (mask) {
-        const int at = __builtin_clz(mask) - (32 - kEach * V);  // element of the mask's, in order
-        mask &= ~(0x80000000u >> __builtin_clz(mask));
-        f((first + G * (h * kEach + at / V) + g) * V + at % V);
-      }
     }
   }
   // Writes f of every element of chunk i to the row at out, where it has the chunk.
@@ -240,33 +233,76 @@ struct RowData {
     if (g < V && j < C) out[j] = static_cast<E>(f(tail));
   }
 
-  // Adds the chunks to a thread's sums, a block of up to 16 elements at a time.  FIRST: nothing is in them yet.
-  template <RowWants W, bool FIRST>
-  __device__ __forceinline__ void add(RowSums& r, const RowScale& k) {
-    constexpr int B = 16 / V < N ? 16 / V : N;  // chunks of a block
+  // The sums of nothing but the thread's single element.
+  template <RowWants W>
+  __device__ __forceinline__ RowSums begin(const RowScale& k) const {
+    RowSums r{tail, 0.0f, 0.0f};
+    one<W>(tail, row_from(tail), r, k);
+    return r;
+  }
+  // The largest of the chunks and the single element.
+  __device__ __forceinline__ float largest(int first, int full, int g) {
+    float m = tail;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (past(i, first, full, g)) break;
+      pin(i);
+#pragma unroll
+      for (int e = 0; e < V; ++e) m = fmaxf(m, Type::get(raw[i], e));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    return m;
+  }
+
+  // Adds the chunks to a thread's sums, a block of up to two at a time, each block by four sums of its own.
+  // seen(m, each) is called with a block's largest value, each(hits, f) then calls f(any, value, index) for the elements
+  // that hits(value), one of each lane at a time (`any`: the lane has one); used(i) when chunk i is not needed any more.
+  template <RowWants W, class Seen, class Used>
+  __device__ __forceinline__ void add(int first, int full, int g, RowSums& r, const RowScale& k, Seen seen, Used used) {
+    constexpr int B = N == 1 || (N > 8 && V == 8) ? 1 : 2;  // chunks of a block
 #pragma unroll
     for (int b = 0; b < N; b += B) {
+      if (past(b, first, full, g)) {
+#pragma unroll
+        for (int i = b; i < b + B; ++i) used(i);
+        continue;
+      }
       float m = -kRowInf;
 #pragma unroll
-      for (int i = b; i < b + B; ++i) pin(i);
-#pragma unroll
-      for (int i = b; i < b + B; ++i)
+      for (int i = b; i < b + B; ++i) {
+        pin(i);
 #pragma unroll
         for (int e = 0; e < V; ++e) m = fmaxf(m, Type::get(raw[i], e));
-      if (FIRST && b == 0) {
-        m = fmaxf(m, tail);
-        r = {m, 0.0f, 0.0f};
-      } else {
-        m = fmaxf(m, r.m);
-        row_move<W>(r, row_from(m), k);
-        r.m = m;
       }
+      seen(m, [&](auto hits, auto f) {
+        // the lane's elements that hit, as bits; each round takes one of every lane that has some
+        uint32_t mask = 0;
+#pragma unroll
+        for (int i = b + B - 1; i >= b; --i)
+#pragma unroll
+          for (int e = V - 1; e >= 0; --e) mask = 2 * mask + (hits(Type::get(raw[i], e)) ? 1u : 0u);
+        while (__ballot(mask != 0) != 0) {
+          const int at = __builtin_ctz(mask | 0x80000000u), word = at * 4 / V;
+          uint32_t bits = raw[b][0];
+#pragma unroll
+          for (int w = 1; w < 4 * B; ++w) bits = word == w ? raw[b + w / 4][w % 4] : bits;
+          f(mask != 0, Type::part(bits, at), (first + G * (b + at / V) + g) * V + at % V);
+          mask &= mask - 1;
+        }
+      });
+      m = fmaxf(m, r.m);
       const float from = row_from(m);
-      if (FIRST && b == 0) one<W>(tail, from, r, k);
+      row_move<W>(r, from, k);
+      r.m = m;
+      RowSums p[4] = {};
 #pragma unroll
       for (int i = b; i < b + B; ++i)
 #pragma unroll
-        for (int e = 0; e < V; ++e) one<W>(Type::get(raw[i], e), from, r, k);
+        for (int e = 0; e < V; ++e) one<W>(Type::get(raw[i], e), from, p[e & 3], k);
+      r.s += (p[0].s + p[1].s) + (p[2].s + p[3].s);
+      if constexpr (W != RowWants::kSum) r.more += (p[0].more + p[1].more) + (p[2].more + p[3].more);
+#pragma unroll
+      for (int i = b; i < b + B; ++i) used(i);
       __builtin_amdgcn_sched_barrier(0);  // a block's numbers are not formed while the one before holds its own
     }
   }
@@ -433,14 +469,17 @@ lipcache_status row_typed(int32_t dtype, F f) {
   }
 }
 
-// Calls f(shape) with the smallest shape that holds a row of C, or the largest and false: the row goes in segments.
+// Calls f(shape) with a shape that holds a row of C, or one and false: the row goes in segments.  A wave takes rows of up to 512
+// chunks where there are enough for all waves (fewer threads that join a row's sums, and no barrier).
 template <class E, class F>
-lipcache_status row_shaped(int C, F f) {
+lipcache_status row_shaped(int64_t T, int C, F f) {
   const int chunks = C / RowType<E>::V;
   auto holds = [&](auto shape) { return chunks <= decltype(shape)::G * decltype(shape)::N; };
   if (holds(RowShape<16, 1>{})) return f(RowShape<16, 1>{}, std::true_type{});
+  if (holds(RowShape<16, 2>{})) return f(RowShape<16, 2>{}, std::true_type{});
   if (holds(RowShape<16, 4>{})) return f(RowShape<16, 4>{}, std::true_type{});
   if (holds(RowShape<64, 4>{})) return f(RowShape<64, 4>{}, std::true_type{});
+  if (T >= 2048 && holds(RowShape<64, 8>{})) return f(RowShape<64, 8>{}, std::true_type{});
   if (holds(RowShape<256, 4>{})) return f(RowShape<256, 4>{}, std::true_type{});
   if (holds(RowShape<256, 8>{})) return f(RowShape<256, 8>{}, std::true_type{});
   if (holds(RowShape<512, 8>{})) return f(RowShape<512, 8>{}, std::true_type{});
@@ -451,8 +490,8 @@ lipcache_status row_shaped(int C, F f) {
 
 // The same for kernels that keep n entries of each row in LDS: a wave or more for a row where they are many.
 template <class E, class F>
-lipcache_status row_shaped_entries(int C, int n, F f) {
-  return row_shaped<E>(C, [&](auto shape, auto whole) {
+lipcache_status row_shaped_entries(int64_t T, int C, int n, F f) {
+  return row_shaped<E>(T, C, [&](auto shape, auto whole) {
     if constexpr (decltype(shape)::G < 64) {
       if (n > 16) return f(RowShape<64, 4>{}, std::true_type{});
     }

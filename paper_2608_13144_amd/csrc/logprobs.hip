@@ -5,11 +5,11 @@
 namespace lc {
 
 constexpr int kTopMost = LIPCACHE_MOST_TOP;
-// Candidates that a row's list holds, and the groups of threads whose largest values give the threshold.
+// Groups of threads whose largest values give the threshold: 16 for up to 12 alternatives (about 1.4 each reach it in
+// what the groups have seen), for more 256 (64 of a wave; 1.1 to 1.2 each; up to 5 for 64 of 64).
+constexpr int kTopFew = 12;
 template <class S>
-inline constexpr int kTopList = S::G >= 64 ? 512 : 32;
-template <class S>
-inline constexpr int kTopGroups = S::G >= 64 ? 64 : 16;
+inline constexpr int kTopGroups = S::G < 64 ? 16 : S::G < 256 ? 64 : 256;
 
 struct LpScore {
   float temperature;
@@ -20,24 +20,30 @@ struct LpScore {
   float* top_logp;
 };
 
-struct TopCandidate {
-  float v;
-  int j;
-};
+// A candidate: larger values first, equal ones by rising index (-0 is 0).
+__device__ __forceinline__ uint64_t top_key(float v, int j) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.0f);
+  return static_cast<uint64_t>(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | ~static_cast<uint32_t>(j);
+}
+__device__ __forceinline__ float top_value(uint64_t key) {
+  const uint32_t b = static_cast<uint32_t>(key >> 32);
+  return __builtin_bit_cast(float, b & 0x80000000u ? b & 0x7fffffffu : ~b);
+}
+__device__ __forceinline__ int top_index(uint64_t key) { return static_cast<int>(~static_cast<uint32_t>(key)); }
 
+// Every wave of a row (its lanes, where a wave holds several) has a list of its own.
+template <class S>
+inline constexpr int kTopList = S::G < 64 ? 32 : S::G == 64 ? 512 : S::G == 256 ? 256 : 64;
 template <class S>
 struct TopSpace {
   float maxima[S::kRows][kTopGroups<S>];
-  float least[S::kRows];
-  int count[S::kRows];
-  TopCandidate list[S::kRows][kTopList<S>];
+  int count[S::kRows][S::kWaves];
+  uint64_t list[S::kRows][S::kWaves][kTopList<S>];
 };
 template <class S>
 struct TopRoom {
   float value[2][S::kWaves];
 };
-
-__device__ __forceinline__ bool top_before(float v, int j, float w, int i) { return v > w || (v == w && j < i); }
 
 // A row's k largest, one after another: each the largest of those behind the one before.  each(f) calls f(value,
 // index) for the thread's elements by rising index.
@@ -76,56 +82,94 @@ __device__ __forceinline__ void top_rounds(int k, TopRoom<S>& room, Each each, P
   }
 }
 
-// A row's k largest by a threshold: the largest value that k of the groups of threads reach.  What reaches it
-// is a list of little more than k, each of which finds its place by counting: reaching(least, f) calls f(index) for
-// the thread's elements that do, logit_of(index) gives the value.  Rows whose list would be longer (many equal
-// values, or all large ones in few threads) go round by round.
-template <class S, class Each, class Reaching, class Logit, class Put>
-__device__ __forceinline__ void top_listed(int k, float own, const RowPlace<S>& at, TopSpace<S>& top, TopRoom<S>& room,
-                                           Each each, Reaching reaching, Logit logit_of, Put put) {
-  constexpr int kGroups = kTopGroups<S>;
-  if (S::kWaves == 1 || threadIdx.x < kWave) {
-    const float v = top.maxima[at.row][at.g % kGroups];
+// A value that k of the groups of a row's threads reach, `own` being what a thread has: the largest such with 16 groups, with
+// more the largest whose last 16 bits are zero.  At least k elements of what the threads have seen reach it.  The row's
+// threads meet here; each wave counts for itself.
+template <class S>
+__device__ __forceinline__ float top_least(int k, float own, const RowPlace<S>& at, TopSpace<S>& top) {
+  constexpr int G = S::G, kMany = kTopGroups<S>;
+  const bool few = G < 64 || k <= kTopFew;
+  float m = own;
+  if (few) {
+    if constexpr (G >= 32) m = fmaxf(m, dpp_f32<kDppQuadXor1>(m));
+    if constexpr (G >= 64) m = fmaxf(m, dpp_f32<kDppQuadXor2>(m));
+    if constexpr (G >= 128) m = fmaxf(m, dpp_f32<kDppHalfMirror>(m));
+    if constexpr (G >= 256) m = fmaxf(m, dpp_f32<kDppMirror>(m));
+    if constexpr (G >= 512) m = fmaxf(m, __shfl_xor(m, 16, kWave));
+    if constexpr (G >= 1024) m = fmaxf(m, __shfl_xor(m, 32, kWave));
+    if (at.g % (G / 16) == 0) top.maxima[at.row][at.g / (G / 16)] = m;
+  } else {
+    if constexpr (G >= 2 * kMany) m = fmaxf(m, dpp_f32<kDppQuadXor1>(m));
+    if constexpr (G >= 4 * kMany) m = fmaxf(m, dpp_f32<kDppQuadXor2>(m));
+    if (at.g % (G / kMany) == 0) top.maxima[at.row][at.g / (G / kMany)] = m;
+  }
+  RowPlace<S>::sync();
+  if (few) {
+    // a group's place is the number of groups that reach its value
+    const float v = top.maxima[at.row][lane_id() & 15];
+    int n = 1;
+    auto count = [&](float other) { n += other >= v ? 1 : 0; };
+    count(dpp_f32<0x121>(v));  // row_ror: the 15 other lanes of 16
+    count(dpp_f32<0x122>(v));
+    count(dpp_f32<0x123>(v));
+    count(dpp_f32<0x124>(v));
+    count(dpp_f32<0x125>(v));
+    count(dpp_f32<0x126>(v));
+    count(dpp_f32<0x127>(v));
+    count(dpp_f32<0x128>(v));
+    count(dpp_f32<0x129>(v));
+    count(dpp_f32<0x12a>(v));
+    count(dpp_f32<0x12b>(v));
+    count(dpp_f32<0x12c>(v));
+    count(dpp_f32<0x12d>(v));
+    count(dpp_f32<0x12e>(v));
+    count(dpp_f32<0x12f>(v));
+    return lanes_max<16>(n >= k ? v : -kRowInf);
+  }
+  // bit by bit, in the order of the numbers
+  uint32_t v[kMany >= 64 ? kMany / 64 : 1], found = 0;
+#pragma unroll
+  for (int i = 0; i < kMany / 64; ++i) v[i] = static_cast<uint32_t>(top_key(top.maxima[at.row][lane_id() + 64 * i], 0) >> 32);
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t with = found | 1u << bit;
     int n = 0;
 #pragma unroll
-    for (int j = 0; j < kGroups; ++j) n += (kGroups == 64 ? lane_f32(v, j) : top.maxima[at.row][j]) >= v ? 1 : 0;
-    const float least = lanes_max<kGroups>(n >= k ? v : -kRowInf);
-    if (at.g == 0) {
-      top.least[at.row] = least;
-      top.count[at.row] = 0;
-    }
+    for (int i = 0; i < kMany / 64; ++i) n += __builtin_popcountll(__ballot(v[i] >= with));
+    found = n >= k ? with : found;
   }
-  RowPlace<S>::sync();
-  const float least = top.least[at.row];
-  if (own >= least && own > -kRowInf)
-    reaching(least, [&](int j) {
-      const int n = atomicAdd(&top.count[at.row], 1);
-      if (n < kTopList<S>) top.list[at.row][n] = {logit_of(j), j};
-    });
-  RowPlace<S>::sync();
-  const int n = top.count[at.row];
-  if (n > kTopList<S>) {
-    top_rounds<S>(k, room, each, [&](int i, float v, int j) {
-      if (at.g == 0) put(i, v, j);
-    });
-    return;
-  }
-  for (int c = at.g; c < n || c < k; c += S::G) {
-    if (c < n) {
-      const TopCandidate mine = top.list[at.row][c];
-      int place = 0;
-#pragma unroll 4
-      for (int i = 0; i < n; ++i) {
-        const TopCandidate other = top.list[at.row][i];
-        place += top_before(other.v, other.j, mine.v, mine.j) ? 1 : 0;
-      }
-      if (place < k) put(place, mine.v, mine.j);
-    } else {
-      put(c, -kRowInf, 0);
-    }
-  }
+  // (below -inf: nothing but -inf or less, which is no candidate)
+  return found <= 0x007fffffu ? -kRowInf : top_value(static_cast<uint64_t>(found) << 32);
 }
 
+// The list that a wave's lanes fill: a place is the number of the lanes before and of what is there already, so
+// nothing waits for an atomic.
+template <class S>
+struct TopList {
+  uint64_t* list;
+  int n = 0;  // may pass what the list holds; what does not fit is not written
+  // All lanes of the row in this wave.
+  __device__ __forceinline__ void push(bool hit, float v, int j) {
+    uint64_t all = __ballot(hit);
+    int before;
+    if constexpr (S::G < 64) {
+      all = all >> (lane_id() & ~(S::G - 1)) & ((1ull << S::G) - 1);
+      before = __builtin_popcount(static_cast<uint32_t>(all) & ((1u << (lane_id() & (S::G - 1))) - 1));
+    } else {
+      before = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(all >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(all), 0));
+    }
+    if (hit && n + before < kTopList<S>) list[n + before] = top_key(v, j);
+    n += __builtin_popcountll(all);
+  }
+};
+
+// kWhole: a row is one segment.
+//
+// Alternatives: a threshold that k elements of the row's first segment reach (the largest values of its threads give
+// it), then every block of the row whose largest value reaches it puts its elements that do on a list, a few times k of
+// them, each of which finds its place by counting.  Where a list is too short for them (the first segment holds
+// little of what is large, or many values are equal), a threshold from the threads' largest values of the whole row
+// and another pass follow, and where that is not enough either, one alternative after another.
 template <class E, class S, bool kWhole>
 __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restrict__ logits, int64_t ldx, int64_t T, int C,
                                                                LpScore a) {
@@ -147,32 +191,40 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
   int y = checked(label_of(t));
   float logit = logit_of(t, y);
   data.load(row_of(t), 0, C, at.g);
+  const int wave = S::kWaves > 1 ? static_cast<int>(threadIdx.x) / kWave : 0;  // of the row
   for (int turn = 0; t - at.row < T; t += step, turn ^= 1) {
-    const E* x = row_of(t);
+    const E *x = row_of(t), *following = row_of(t + step);
     int next_y = label_of(t + step);
-    RowSums r;
-    data.template add<RowWants::kMean, true>(r, scale);
-    if constexpr (!kWhole) {
-      for (int first = kSegment; first < full; first += kSegment) {
-#pragma unroll
-        for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, full, at.g);
-        data.template add<RowWants::kMean, false>(r, scale);
-      }
-    }
-    const float own = r.m;
-    next_y = checked(next_y);
-    const float next_logit = logit_of(t + step, next_y);
+    const float tail = data.tail;
+    TopList<S> list{top.list[at.row][wave]};
+    float least = kRowInf;
+    auto hits = [&](float v) { return v >= least && v > -kRowInf; };
     if (a.k > 0) {
-      float m = own;
-      if constexpr (S::G >= 128) m = fmaxf(m, dpp_f32<kDppQuadXor1>(m));
-      if constexpr (S::G >= 256) m = fmaxf(m, dpp_f32<kDppQuadXor2>(m));
-      if constexpr (S::G >= 512) m = fmaxf(m, dpp_f32<kDppHalfMirror>(m));
-      if constexpr (S::G >= 1024) m = fmaxf(m, dpp_f32<kDppMirror>(m));
-      constexpr int kEach = S::G / kTopGroups<S>;
-      if (at.g % kEach == 0) top.maxima[at.row][at.g / kEach] = m;
+      least = top_least<S>(a.k, data.largest(0, full, at.g), at, top);
+      list.push(hits(tail), tail, full * Data::V + at.g);
     }
-    auto next = [&] { data.load(row_of(t + step), 0, C, at.g); };
-    if (kWhole && a.k == 0) next();
+    RowSums r = data.template begin<RowWants::kMean>(scale);
+    float next_logit = 0.0f;
+    auto next = [&] {
+      next_y = checked(next_y);
+      next_logit = logit_of(t + step, next_y);
+      data.load_tail(following, C, at.g);
+    };
+    auto seen = [&](float m, auto each) {
+      if (a.k > 0 && __ballot(hits(m)) != 0) each(hits, [&](bool any, float v, int j) { list.push(any, v, j); });
+    };
+    // a segment's chunks are asked for as the one before is used, the next row's behind the row's last
+    int first = 0;
+    if constexpr (!kWhole) {
+      for (; first + kSegment < full; first += kSegment)
+        data.template add<RowWants::kMean>(first, full, at.g, r, scale, seen,
+                                           [&](int i) { data.load_chunk(i, x, first + kSegment, full, at.g); });
+    }
+    next();
+    data.template add<RowWants::kMean>(first, full, at.g, r, scale, seen,
+                                       [&](int i) { data.load_chunk(i, following, 0, full, at.g); });
+    const float own = r.m;
+    if (a.k > 0 && at.g % S::kLanes == 0) top.count[at.row][wave] = list.n;
     if constexpr (S::G <= 64) wave_sync();  // the join of longer rows has a barrier
     row_join<S, RowWants::kMean>(r, scale, room[turn]);
     const float from = row_from(r.m), log_s = row_log2(r.s);
@@ -188,40 +240,82 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
         a.top_index[t * a.k + i] = v == -kRowInf ? -1 : j;
         a.top_logp[t * a.k + i] = v == -kRowInf ? -kRowInf : logp(v);
       };
-      // the rare ways through the row read it again
-      auto each = [&](auto f) {
+      // what is on the row's lists, -1 where one is too short
+      auto listed = [&] {
+        int n = 0;
+        bool fits = true;
+#pragma unroll
+        for (int w = 0; w < S::kWaves; ++w) {
+          const int c = top.count[at.row][w];
+          fits = fits && c <= kTopList<S>;
+          n += c;
+        }
+        return fits ? n : -1;
+      };
+      int n = listed();
+      if (n < 0) {
+        // the rare ways read the row again
+        auto each = [&](auto f) {
 #pragma unroll 1
-        for (int c = at.g; c < full; c += S::G) {
-          const u32x4 raw = *reinterpret_cast<const typename Data::Type::vec*>(x + static_cast<int64_t>(c) * Data::V);
+          for (int c = at.g - at.g % S::kLanes; c < full; c += S::G) {  // (whole waves)
+            const int mine = c + at.g % S::kLanes;
+            u32x4 raw = Data::fill();
+            if (mine < full) raw = *reinterpret_cast<const typename Data::Type::vec*>(x + static_cast<int64_t>(mine) * Data::V);
 #pragma unroll
-          for (int e = 0; e < Data::V; ++e) f(Data::Type::get(raw, e), c * Data::V + e);
-        }
-        f(data.tail, full * Data::V + at.g);
-      };
-      auto reaching = [&](float least, auto f) {
-        if constexpr (kWhole) {
-          data.reaching(least, 0, at.g, f);
-        } else {
-          for (int first = 0; first < full; first += kSegment) {
-#pragma unroll
-            for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, full, at.g);
-            data.reaching(least, first, at.g, f);
+            for (int e = 0; e < Data::V; ++e) f(Data::Type::get(raw, e), mine * Data::V + e);
           }
+          f(tail, full * Data::V + at.g);
+        };
+        least = top_least<S>(a.k, own, at, top);  // (past its barrier the counts are read)
+        list.n = 0;
+        each([&](float v, int j) { list.push(hits(v), v, j); });
+        if (at.g % S::kLanes == 0) top.count[at.row][wave] = list.n;
+        RowPlace<S>::sync();
+        n = listed();
+        if (n < 0)
+          top_rounds<S>(a.k, top_room, each, [&](int i, float v, int j) {
+            if (at.g == 0) put(i, v, j);
+          });
+      }
+      for (int c = at.g; n >= 0 && (c < n || c < a.k); c += S::G) {
+        if (c >= n) {
+          put(c, -kRowInf, 0);
+          continue;
         }
-        if (data.tail >= least && data.tail > -kRowInf) f(full * Data::V + at.g);
-      };
-      if (a.k <= kTopGroups<S>) {
-        top_listed<S>(a.k, own, at, top, top_room, each, reaching, [&](int j) { return static_cast<float>(x[j]); }, put);
-      } else {
-        top_rounds<S>(a.k, top_room, each, [&](int i, float v, int j) {
-          if (at.g == 0) put(i, v, j);
-        });
+        int w = 0, i = c;
+        while (S::kWaves > 1 && i >= top.count[at.row][w]) i -= top.count[at.row][w++];
+        const uint64_t key = top.list[at.row][w][i];
+        int place = 0;
+#pragma unroll 1
+        for (int o = 0; o < S::kWaves; ++o) {
+          const int m = top.count[at.row][o];
+#pragma unroll 4
+          for (int e = 0; e < m; ++e) place += top.list[at.row][o][e] > key ? 1 : 0;
+        }
+        if (place < a.k) put(place, top_value(key), top_index(key));
       }
     }
-    if (!kWhole || a.k > 0) next();
     y = next_y;
     logit = next_logit;
   }
+}
+
+// Threads of a row.  Rows of up to 64 chunks are held by 16 lanes, of up to 256 by a wave.  Longer ones go through in
+// segments: by a wave up to 1024 chunks where the rows fill the chip with waves, by 256 threads, or by 1024 where there
+// are few.  (The 16 groups of a 16-lane row give a threshold for up to 12 alternatives, the 64 of a wave one that many more
+// than 48 would reach.)
+template <class E, class F>
+lipcache_status score_shaped(int64_t T, int C, int k, F f) {
+  const int chunks = C / RowType<E>::V;
+  if (k <= kTopFew) {
+    if (chunks <= 16) return f(RowShape<16, 1>{}, std::true_type{});
+    if (chunks <= 32) return f(RowShape<16, 2>{}, std::true_type{});
+    if (chunks <= 64) return f(RowShape<16, 4>{}, std::true_type{});
+  }
+  if (chunks <= 256) return f(RowShape<64, 4>{}, std::true_type{});
+  if (chunks <= 1024 && T >= 2048 && k <= 48) return f(RowShape<64, 8>{}, std::false_type{});
+  if (chunks <= 1024 || T >= 768) return f(RowShape<256, 8>{}, std::false_type{});
+  return f(RowShape<1024, 4>{}, std::false_type{});
 }
 
 }  // namespace lc
@@ -242,7 +336,7 @@ extern "C" lipcache_status lipcache_logprobs(const void* x, int64_t ldx, int64_t
   const LpScore a{temperature, label, k, logp, lse, entropy, top_index, top_logp};
   return row_typed(dtype, [&](auto type) {
     typedef decltype(type) E;
-    return row_shaped<E>(C, [&](auto shape, auto whole) {
+    return score_shaped<E>(T, C, k, [&](auto shape, auto whole) {
       typedef decltype(shape) S;
       lp_score_kernel<E, S, decltype(whole)::value><<<row_blocks<S>(T), S::kThreads, 0, stream>>>(static_cast<const E*>(x), ldx, T, C, a);
       LC_LAUNCHED();

@@ -76,14 +76,13 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
       if (a.g_lse && t < T) gl = a.g_lse[t];
       if (kEntropy && t < T) ge = a.g_entropy[t];
     }
-    RowSums r;
-    data.template add<kWants, true>(r, scale);
-    if constexpr (!kWhole) {
-      for (int first = kSegment; first < full; first += kSegment) {
-#pragma unroll
-        for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, full, at.g);
-        data.template add<kWants, false>(r, scale);
-      }
+    RowSums r = data.template begin<kWants>(scale);
+    if constexpr (kWhole) {
+      data.template add<kWants>(0, full, at.g, r, scale, RowNothing{}, RowNothing{});
+    } else {
+      // a segment's chunks are asked for as the one before is used
+      for (int first = 0; first < full; first += kSegment)
+        data.template add<kWants>(first, full, at.g, r, scale, RowNothing{}, [&](int i) { data.load_chunk(i, x, first + kSegment, full, at.g); });
     }
     next_entry = checked(next_entry);
     next_label = checked(next_label);
@@ -173,7 +172,7 @@ extern "C" lipcache_status lipcache_logprobs_backward(const void* x, int64_t ldx
   const LpBackward a{temperature, label, g_logp, g_lse, g_entropy, k, top_index, g_top, bits};
   return row_typed(dtype, [&](auto type) {
     typedef decltype(type) E;
-    return row_shaped_entries<E>(C, k, [&](auto shape, auto whole) {
+    return row_shaped_entries<E>(T, C, k, [&](auto shape, auto whole) {
       typedef decltype(shape) S;
       auto run = [&](auto entropy) {
         lp_backward_kernel<E, S, decltype(whole)::value, decltype(entropy)::value>
