@@ -7,6 +7,8 @@
 // the two halves of a wave meet at the end.  Every wave of a tile leaves
 // (largest value, sum, sum of the exponents weighted) of its classes; a second
 // launch joins them in order.
+#include <type_traits>
+
 #include "lc_common.hpp"
 #include "lc_mfma.hpp"
 
@@ -46,13 +48,34 @@ __device__ __forceinline__ HlPart hl_join(const HlPart& a, const HlPart& b, floa
           fa * fmaf(fmaxf(da, kHlLeast), a.s, a.mean) + fb * fmaf(fmaxf(db, kHlLeast), b.s, b.mean)};
 }
 
-template <class S>
-__global__ __launch_bounds__(S::kThreads) void hl_tile_kernel(const typename S::E* __restrict__ W, int64_t ldw, int C,
+// The same sums about m, which is no smaller.
+__device__ __forceinline__ void hl_move(HlPart& p, float m, float scale) {
+  const float d = (p.m - (m == -kHlInf ? 0.0f : m)) * scale, f = __builtin_amdgcn_exp2f(d);
+  p.mean = f * fmaf(fmaxf(d, kHlLeast), p.s, p.mean);
+  p.s *= f;
+  p.m = m;
+}
+
+struct HlOut {
+  const int32_t* label;
+  float *logp, *lse, *entropy;
+  float scale, temperature;  // log2(e) / temperature
+  __device__ __forceinline__ void write(int t, const HlPart& sum, bool labelled, float logit) const {
+    const float m = sum.m == -kHlInf ? 0.0f : sum.m, log_s = __builtin_amdgcn_logf(sum.s);
+    if (logp) logp[t] = !labelled ? 0.0f : sum.s == 0.0f ? -kHlInf : (logit - m) / temperature - log_s * kHlLn2;
+    if (lse) lse[t] = m / temperature + log_s * kHlLn2;
+    if (entropy) entropy[t] = sum.s == 0.0f ? 0.0f : (log_s - sum.mean / sum.s) * kHlLn2;
+  }
+};
+
+// kAll: the tile holds all classes and each wave those of its rows, which it finishes itself.
+template <class S, bool kAll>
+__global__ __launch_bounds__(S::kThreads, 2) void hl_tile_kernel(const typename S::E* __restrict__ W, int64_t ldw, int C,
                                                               const typename S::E* __restrict__ x, int64_t ldx, int T,
-                                                              int K, const float* __restrict__ bias, float scale,
-                                                              const int32_t* __restrict__ label, int parts,
+                                                              int K, const float* __restrict__ bias, HlOut out, int parts,
                                                               float4* __restrict__ part, float* __restrict__ at) {
   typedef typename S::E E;
+  static_assert(!kAll || S::WM == 1, "one wave for all classes of a row");
   __shared__ __align__(16) char lds[S::kLds];
   int bi, bj;
   tile_of(static_cast<int>((C + S::BM - 1) / S::BM), static_cast<int>((T + S::BN - 1) / S::BN), bi, bj);
@@ -68,67 +91,99 @@ __global__ __launch_bounds__(S::kThreads) void hl_tile_kernel(const typename S::
   tile_products<S>(p, q, K, lds, acc);
   const int lane = lane_id(), wave = uniform(static_cast<int>(threadIdx.x) / kWave);
   if (S::WK > 1 && wave >= S::WM * S::WN) return;
-  const int wm = wave / S::WN, wn = wave % S::WN, first = 4 * (lane >> 5);
+  const int wm = wave / S::WN, wn = wave % S::WN, half = 4 * (lane >> 5);
+  HlPart sum[S::TN];
+  int y[S::TN];  // the label as a row of the wave's, counted from the lane's first
+  float logit[S::TN];
+  bool labelled[S::TN];
+#pragma unroll
+  for (int b = 0; b < S::TN; ++b) {
+    const int t = j0 + (wn * S::TN + b) * 32 + (lane & 31);
+    const int label = out.label && t < T ? out.label[t] : -1;
+    labelled[b] = label >= 0 && label < C;
+    y[b] = labelled[b] ? label - (i0 + wm * S::TM * 32 + half) : -1;
+    logit[b] = 0.0f;
+    sum[b] = {-kHlInf, 0.0f, 0.0f};
+  }
 #pragma unroll
   for (int a = 0; a < S::TM; ++a) {
-    const int base = i0 + (wm * S::TM + a) * 32 + first;
+    const int base = i0 + (wm * S::TM + a) * 32 + half;
+    float add[16];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int c = base + acc_row(v);
-      const float add = c < C ? bias ? bias[c] : 0.0f : -kHlInf;
+    for (int v = 0; v < 16; ++v) add[v] = bias && base + acc_row(v) < C ? bias[base + acc_row(v)] : 0.0f;
 #pragma unroll
-      for (int b = 0; b < S::TN; ++b) acc[a][b][v] = c < C ? acc[a][b][v] + add : -kHlInf;
+    for (int b = 0; b < S::TN; ++b) {
+      float x16[16], m = -kHlInf;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        x16[v] = base + acc_row(v) < C ? acc[a][b][v] + add[v] : -kHlInf;
+        m = fmaxf(m, x16[v]);
+      }
+      hl_move(sum[b], fmaxf(m, sum[b].m), out.scale);
+      const float from = sum[b].m == -kHlInf ? 0.0f : sum[b].m;
+      float s = 0.0f, mean = 0.0f;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const float e = (x16[v] - from) * out.scale, w = __builtin_amdgcn_exp2f(e);
+        s += w;
+        mean = fmaf(fmaxf(e, kHlLeast), w, mean);
+      }
+      sum[b].s += s;
+      sum[b].mean += mean;
+      const int row = y[b] - a * 32;
+      if (__ballot(row >= 0 && row < 32) != 0) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) logit[b] = row == acc_row(v) ? x16[v] : logit[b];
+      }
+      __builtin_amdgcn_sched_barrier(0);  // one tile's numbers at a time beside the accumulators
     }
   }
 #pragma unroll
   for (int b = 0; b < S::TN; ++b) {
-    const int j = (wn * S::TN + b) * 32 + (lane & 31), t = j0 + j;
-    const int y = label && t < T ? label[t] - (i0 + wm * S::TM * 32) : -1;
-    float m = -kHlInf;
-#pragma unroll
-    for (int a = 0; a < S::TM; ++a)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) m = fmaxf(m, acc[a][b][v]);
-    const float from = m == -kHlInf ? 0.0f : m;
-    HlPart sum{m, 0.0f, 0.0f};
-#pragma unroll
-    for (int a = 0; a < S::TM; ++a)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const float e = (acc[a][b][v] - from) * scale, w = __builtin_amdgcn_exp2f(e);
-        sum.s += w;
-        sum.mean = fmaf(fmaxf(e, kHlLeast), w, sum.mean);
-        if (y == a * 32 + first + acc_row(v) && label[t] < C) at[t] = acc[a][b][v];
-      }
-    const HlPart other{__shfl_xor(sum.m, 32, kWave), __shfl_xor(sum.s, 32, kWave), __shfl_xor(sum.mean, 32, kWave)};
-    sum = lane < 32 ? hl_join(sum, other, scale) : sum;
-    if (lane < 32 && t < T) part[static_cast<int64_t>(t) * parts + bi * S::WM + wm] = {sum.m, sum.s, sum.mean, 0.0f};
+    const int t = j0 + (wn * S::TN + b) * 32 + (lane & 31);
+    const HlPart other{__shfl_xor(sum[b].m, 32, kWave), __shfl_xor(sum[b].s, 32, kWave), __shfl_xor(sum[b].mean, 32, kWave)};
+    const HlPart both = hl_join(sum[b], other, out.scale);
+    const bool mine = y[b] >= 0 && y[b] < S::TM * 32 && (y[b] & 4) == 0;
+    if constexpr (kAll) {
+      const float across = __shfl_xor(logit[b], 32, kWave);
+      const int there = __shfl_xor(mine ? 1 : 0, 32, kWave);
+      if (lane < 32 && t < T) out.write(t, both, labelled[b], there ? across : logit[b]);
+    } else {
+      if (mine) at[t] = logit[b];
+      if (lane < 32 && t < T) part[static_cast<int64_t>(t) * parts + bi * S::WM + wm] = {both.m, both.s, both.mean, 0.0f};
+    }
   }
 }
 
-// One wave a row.
+// WAVES of a workgroup join a row's parts; a workgroup has 4.
+template <int WAVES>
 __global__ __launch_bounds__(256) void hl_join_kernel(int T, int C, int parts, const float4* __restrict__ part,
-                                                      const float* __restrict__ at, const int32_t* __restrict__ label,
-                                                      float scale, float temperature, float* __restrict__ logp,
-                                                      float* __restrict__ lse, float* __restrict__ entropy) {
-  const int t = static_cast<int>(blockIdx.x) * 4 + static_cast<int>(threadIdx.x) / kWave, lane = lane_id();
-  if (t >= T) return;
+                                                      const float* __restrict__ at, HlOut out) {
+  __shared__ HlPart room[4];
+  const int wave = static_cast<int>(threadIdx.x) / kWave, lane = lane_id();
+  const int t = static_cast<int>(blockIdx.x) * (4 / WAVES) + (WAVES == 1 ? wave : 0);
   HlPart sum{-kHlInf, 0.0f, 0.0f};
-  for (int i = lane; i < parts; i += kWave) {
-    const float4 p = part[static_cast<int64_t>(t) * parts + i];
-    sum = hl_join(sum, {p.x, p.y, p.z}, scale);
+  if (t < T) {
+#pragma unroll 4
+    for (int i = lane + (WAVES == 1 ? 0 : wave * kWave); i < parts; i += WAVES * kWave) {
+      const float4 p = part[static_cast<int64_t>(t) * parts + i];
+      sum = hl_join(sum, {p.x, p.y, p.z}, out.scale);
+    }
   }
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1)
-    sum = hl_join(sum, {__shfl_xor(sum.m, o, kWave), __shfl_xor(sum.s, o, kWave), __shfl_xor(sum.mean, o, kWave)}, scale);
-  if (lane != 0) return;
-  const float m = sum.m == -kHlInf ? 0.0f : sum.m, log_s = __builtin_amdgcn_logf(sum.s);
-  if (logp) {
-    const int y = label ? label[t] : -1;
-    logp[t] = y < 0 || y >= C ? 0.0f : sum.s == 0.0f ? -kHlInf : (at[t] - m) / temperature - log_s * kHlLn2;
+    sum = hl_join(sum, {__shfl_xor(sum.m, o, kWave), __shfl_xor(sum.s, o, kWave), __shfl_xor(sum.mean, o, kWave)}, out.scale);
+  if constexpr (WAVES > 1) {
+    if (lane == 0) room[wave] = sum;
+    __syncthreads();
+    sum = room[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) sum = hl_join(sum, room[w], out.scale);
   }
-  if (lse) lse[t] = m / temperature + log_s * kHlLn2;
-  if (entropy) entropy[t] = sum.s == 0.0f ? 0.0f : (log_s - sum.mean / sum.s) * kHlLn2;
+  if (lane != 0 || (WAVES > 1 && wave != 0) || t >= T) return;
+  const int y = out.label ? out.label[t] : -1;
+  const bool labelled = y >= 0 && y < C;
+  out.write(t, sum, labelled, labelled ? at[t] : 0.0f);
 }
 
 // ----------------------------------------------------------------- host side
@@ -181,40 +236,93 @@ lipcache_status hl_aligned(const E*& p, int64_t& ld, int64_t rows, int K, E* roo
   return LIPCACHE_OK;
 }
 
-struct HlOut {
-  const int32_t* label;
-  float *logp, *lse, *entropy;
-};
+// Heads of up to 256 classes and many rows: one tile has all classes, and a row is finished where its sums are.  float32 products
+// are what bounds such a call, so their tiles come in steps of 32 classes; 16-bit ones wait for the features.  Fewer rows
+// leave CUs idle that way (64 rows of 256 -> 200 float32: 20 us against 12 of the tiles below and the join).
+inline bool hl_whole(int64_t T, int C) { return C <= 256 && T > 64 * 128; }
+
+template <class E>
+lipcache_status hl_all(const E* x, int64_t ldx, int64_t T, const E* W, int64_t ldw, const float* bias, int K, int C,
+                       const HlOut& out, hipStream_t s) {
+  auto run = [&](auto shape) {
+    typedef decltype(shape) S;
+    hl_tile_kernel<S, true><<<static_cast<unsigned>(hl_ceil(T, S::BN)), S::kThreads, 0, s>>>(
+        W, ldw, C, x, ldx, static_cast<int>(T), K, bias, out, 0, nullptr, nullptr);
+    return hipGetLastError() == hipSuccess ? LIPCACHE_OK : LIPCACHE_EHIP;
+  };
+  // 128 rows a workgroup where that fills the CUs, else 64, whose waves share the contraction two by two.  32768 x 256 ->
+  // 200 float32: 38 us of 128 rows, 44 of 64 (the shares are joined in LDS), 78 of 32.
+  auto sized = [&](auto tm) {
+    constexpr int BM = 32 * decltype(tm)::value;
+    if (T > 128 * 192) return run(TileShape<E, BM, 128, 1, 4, 1, 3, 1, false, false>{});
+    return run(TileShape<E, BM, 64, 1, 2, 2, 2, 1, false, false>{});
+  };
+  const int tiles = static_cast<int>(hl_ceil(C, 32));
+  if constexpr (sizeof(E) == 4) {
+    switch (tiles) {
+      case 1: return sized(std::integral_constant<int, 1>{});
+      case 2: return sized(std::integral_constant<int, 2>{});
+      case 3: return sized(std::integral_constant<int, 3>{});
+      case 4: return sized(std::integral_constant<int, 4>{});
+      case 5: return sized(std::integral_constant<int, 5>{});
+      case 6: return sized(std::integral_constant<int, 6>{});
+      case 7: return sized(std::integral_constant<int, 7>{});
+      default: return sized(std::integral_constant<int, 8>{});
+    }
+  } else {
+    if (tiles <= 1) return sized(std::integral_constant<int, 1>{});
+    if (tiles <= 4) return sized(std::integral_constant<int, 4>{});
+    return sized(std::integral_constant<int, 8>{});
+  }
+}
 
 template <class E>
 lipcache_status hl_run(const E* x, int64_t ldx, int64_t T, const E* W, int64_t ldw, const float* bias, int K, int C,
-                       float temperature, const HlOut& out, void* ws_, hipStream_t s) {
+                       HlOut out, void* ws_, hipStream_t s) {
   HlSpace space{static_cast<char*>(ws_)};
   const HlBuffers<E> ws(space, T, K, C);
   lipcache_status st;
   if ((st = hl_aligned(x, ldx, T, K, ws.x, s)) != LIPCACHE_OK) return st;
   if ((st = hl_aligned(W, ldw, C, K, ws.W, s)) != LIPCACHE_OK) return st;
-  const float scale = kHlLog2e / temperature;
   const int64_t pass = hl_rows(T, C);
   for (int64_t t = 0; t < T; t += pass) {
     const int n = static_cast<int>(T - t < pass ? T - t : pass);
-    const int32_t* label = out.label ? out.label + t : nullptr;
+    HlOut o = out;
+    if (out.label) o.label = out.label + t;
+    if (out.logp) o.logp = out.logp + t;
+    if (out.lse) o.lse = out.lse + t;
+    if (out.entropy) o.entropy = out.entropy + t;
+    if (hl_whole(n, C)) {
+      if ((st = hl_all<E>(x + t * ldx, ldx, n, W, ldw, bias, K, C, o, s)) != LIPCACHE_OK) return st;
+      continue;
+    }
     int parts = 0;
     auto run = [&](auto shape) {
       typedef decltype(shape) S;
       parts = static_cast<int>(hl_ceil(C, S::BM)) * S::WM;
       const int64_t tiles = hl_ceil(C, S::BM) * hl_ceil(n, S::BN);
-      hl_tile_kernel<S><<<static_cast<unsigned>(tiles), S::kThreads, 0, s>>>(W, ldw, C, x + t * ldx, ldx, n, K, bias, scale,
-                                                                           label, parts, ws.part, ws.at);
+      hl_tile_kernel<S, false><<<static_cast<unsigned>(tiles), S::kThreads, 0, s>>>(W, ldw, C, x + t * ldx, ldx, n, K, bias, o,
+                                                                                  parts, ws.part, ws.at);
       return hipGetLastError() == hipSuccess ? LIPCACHE_OK : LIPCACHE_EHIP;
     };
-    if (n <= 32) st = run(TileShape<E, 128, 32, 4, 1, 1, 4, 1, false, false>{});
-    else if (sizeof(E) == 4 || hl_ceil(C, 256) * hl_ceil(n, 256) < 200) st = run(TileShape<E, 128, 128, 2, 2, 1, 2, 1, false, false>{});
-    else st = run(TileShape<E, 256, 256, 2, 4, 1, 2, 1, false, false>{});
+    const int64_t t128 = hl_ceil(C, 128) * hl_ceil(n, 128), t256 = hl_ceil(C, 256) * hl_ceil(n, 256);
+    if (n <= 32) {
+      // bound by reading W: tiles of 32 classes until they fill the CUs
+      st = hl_ceil(C, 128) >= 256 ? run(TileShape<E, 128, 32, 4, 1, 1, 4, 1, false, false>{})
+                                  : run(TileShape<E, 32, 32, 1, 1, 4, 4, 1, false, false>{});
+    } else if (t128 < 128) {
+      st = run(TileShape<E, 64, 64, 2, 2, 1, 3, 1, false, false>{});
+    } else if (sizeof(E) == 2 && 5 * t256 >= 4 * 256 * hl_ceil(t256, 256)) {
+      if constexpr (sizeof(E) == 2) st = run(TileShape<E, 256, 256, 2, 4, 1, 2, 1, false, false>{});
+    } else if (t128 < 320) {
+      st = run(TileShape<E, 128, 128, 2, 4, 1, 4, 1, false, false>{});
+    } else {
+      st = run(TileShape<E, 128, 128, 2, 2, 1, 2, 1, false, false>{});
+    }
     if (st != LIPCACHE_OK) return st;
-    hl_join_kernel<<<static_cast<unsigned>(hl_ceil(n, 4)), 256, 0, s>>>(
-        n, C, parts, ws.part, ws.at, label, scale, temperature, out.logp ? out.logp + t : nullptr,
-        out.lse ? out.lse + t : nullptr, out.entropy ? out.entropy + t : nullptr);
+    // a wave a row, or four where a row has many parts
+    if (parts <= 256) hl_join_kernel<1><<<static_cast<unsigned>(hl_ceil(n, 4)), 256, 0, s>>>(n, C, parts, ws.part, ws.at, o);
+    else hl_join_kernel<4><<<static_cast<unsigned>(n), 256, 0, s>>>(n, C, parts, ws.part, ws.at, o);
     LC_LAUNCHED();
   }
   return LIPCACHE_OK;
@@ -243,17 +351,18 @@ extern "C" lipcache_status lipcache_head_logprobs(const void* x, int64_t ldx, in
                                                   float* entropy, void* ws, size_t ws_bytes, lipcache_stream_t stream) {
   if (hl_sizes_bad(T, K, C, dtype) || ldx < K || ldw < K) return LIPCACHE_EINVAL;
   if (!(temperature >= 0x1p-20f && temperature <= 0x1p20f)) return LIPCACHE_EINVAL;
-  if (!W || (T > 0 && !x)) return LIPCACHE_EINVAL;
+  if (T > 0 && (!W || !x)) return LIPCACHE_EINVAL;
   const uintptr_t size = dtype == LIPCACHE_F32 ? 4 : 2;
   if (hl_unaligned(x, size) || hl_unaligned(W, size) || hl_unaligned(bias, 4) || hl_unaligned(label, 4) ||
       hl_unaligned(logp, 4) || hl_unaligned(lse, 4) || hl_unaligned(entropy, 4))
     return LIPCACHE_EINVAL;
   if (C > kHlMostClasses || K > kHlMostWidth || T > 0x7fffffff) return LIPCACHE_EUNSUPPORTED;
   if (!ws || !aligned256(ws) || ws_bytes < lipcache_head_logprobs_workspace_bytes(T, K, C, dtype)) return LIPCACHE_EWORKSPACE;
-  const HlOut out{label, logp, lse, entropy};
+  if (T == 0) return LIPCACHE_OK;
+  const HlOut out{label, logp, lse, entropy, kHlLog2e / temperature, temperature};
   auto run = [&](auto type) {
     typedef decltype(type) E;
-    return hl_run<E>(static_cast<const E*>(x), ldx, T, static_cast<const E*>(W), ldw, bias, K, C, temperature, out, ws, stream);
+    return hl_run<E>(static_cast<const E*>(x), ldx, T, static_cast<const E*>(W), ldw, bias, K, C, out, ws, stream);
   };
   switch (dtype) {
     case LIPCACHE_F32: return run(float{});
