@@ -603,6 +603,7 @@ size_t lipcache_muon_step_workspace_bytes(int64_t batch, int32_t m, int32_t n, i
 /* Limits of the calls below. */
 #define LIPCACHE_MOST_TOP 64        /* alternatives of a row that lipcache_logprobs lists       */
 #define LIPCACHE_MOST_ENTRIES 1024  /* entries of a row that a gradient or a teacher names      */
+#define LIPCACHE_FEW_ROWS 64        /* calls with more rows than this need no workspace         */
 
 /*
  * Log probabilities of rows of logits.  With m_t = max_j x_tj and
@@ -624,12 +625,15 @@ size_t lipcache_muon_step_workspace_bytes(int64_t batch, int32_t m, int32_t n, i
  *  logp, lse, entropy [T] out, each may be NULL
  *  top_index, top_logp [T][k] out, 0 <= k <= LIPCACHE_MOST_TOP: index and log
  *        probability of each alternative; -1 and -inf where a row has fewer
+ *  ws    lipcache_logprobs_workspace_bytes(T, C, k, dtype) bytes, NULL where that is 0 (it
+ *        is but for few rows of many classes, which go in shares)
  * T = 0 is valid and does nothing.  Outputs overlap neither inputs nor each other. (async)
  */
 lipcache_status lipcache_logprobs(const void* x, int64_t ldx, int64_t T, int32_t C, int32_t dtype,
                                   float temperature, const int32_t* label, int32_t k, float* logp,
                                   float* lse, float* entropy, int32_t* top_index, float* top_logp,
-                                  lipcache_stream_t stream);
+                                  void* ws, size_t ws_bytes, lipcache_stream_t stream);
+size_t lipcache_logprobs_workspace_bytes(int64_t T, int32_t C, int32_t k, int32_t dtype);
 
 /*
  * The gradient of the same with regard to the logits:
@@ -643,13 +647,16 @@ lipcache_status lipcache_logprobs(const void* x, int64_t ldx, int64_t T, int32_t
  *  label [T] or NULL (then g_logp is NULL too);  g_logp, g_lse, g_entropy [T], each may be NULL
  *  top_index, g_top [T][k], 0 <= k <= LIPCACHE_MOST_ENTRIES
  *  dx    [T][C] (lddx) out, dtype; may be x itself (lddx = ldx), overlaps no input else
+ *  ws    lipcache_logprobs_backward_workspace_bytes(T, C, k, dtype) bytes, NULL where that is 0
  * The others as above. (async)
  */
 lipcache_status lipcache_logprobs_backward(const void* x, int64_t ldx, int64_t T, int32_t C, int32_t dtype,
                                            float temperature, const int32_t* label, const float* g_logp,
                                            const float* g_lse, const float* g_entropy, int32_t k,
                                            const int32_t* top_index, const float* g_top, void* dx,
-                                           int64_t lddx, lipcache_stream_t stream);
+                                           int64_t lddx, void* ws, size_t ws_bytes,
+                                           lipcache_stream_t stream);
+size_t lipcache_logprobs_backward_workspace_bytes(int64_t T, int32_t C, int32_t k, int32_t dtype);
 
 /*
  * Learning from labels and from a teacher's top logits.  With p^u the softmax of
@@ -671,13 +678,15 @@ lipcache_status lipcache_logprobs_backward(const void* x, int64_t ldx, int64_t T
  *  label   [T] or NULL;  weight [T] or NULL (1);  hard, soft finite
  *  ce, kl  [T] out, each may be NULL
  *  dx      [T][C] (lddx) out, dtype, or NULL; may be x itself (lddx = ldx)
+ *  ws      lipcache_distill_workspace_bytes(T, C, k, dtype) bytes, NULL where that is 0
  * T = 0 is valid and does nothing.  Outputs overlap no input else. (async)
  */
 lipcache_status lipcache_distill(const void* x, int64_t ldx, int64_t T, int32_t C, int32_t dtype,
                                  float temperature, float hard, float soft, int32_t k,
                                  const float* teacher, const int32_t* index, const int32_t* label,
                                  const float* weight, float* ce, float* kl, void* dx, int64_t lddx,
-                                 lipcache_stream_t stream);
+                                 void* ws, size_t ws_bytes, lipcache_stream_t stream);
+size_t lipcache_distill_workspace_bytes(int64_t T, int32_t C, int32_t k, int32_t dtype);
 
 /*
  * lipcache_logprobs of the logits W x + bias, which are not written: features

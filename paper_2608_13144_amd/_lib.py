@@ -91,7 +91,7 @@ class LipcacheMuon(ctypes.Structure):
 
 
 MUON_SHORT_OPERANDS = 2  # beside nesterov
-MOST_TOP, MOST_ENTRIES = 64, 1024
+MOST_TOP, MOST_ENTRIES, FEW_ROWS = 64, 1024, 64
 
 _PADAPTERS = ctypes.POINTER(LipcacheAdapters)
 _PMUON = ctypes.POINTER(LipcacheMuon)
@@ -132,11 +132,15 @@ SIGNATURES = {
     "lipcache_orthogonalise_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
     "lipcache_muon_step": (_i32, [_vp, _vp, _vp, _i64, _i32, _i32, _i32, _PMUON, _vp, _sz, _vp]),
     "lipcache_muon_step_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
-    "lipcache_logprobs": (_i32, [_vp, _i64, _i64, _i32, _i32, _f32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "lipcache_logprobs": (_i32, [_vp, _i64, _i64, _i32, _i32, _f32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
+                                 _vp]),
+    "lipcache_logprobs_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
     "lipcache_logprobs_backward": (_i32, [_vp, _i64, _i64, _i32, _i32, _f32, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp,
-                                          _i64, _vp]),
+                                          _i64, _vp, _sz, _vp]),
+    "lipcache_logprobs_backward_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
     "lipcache_distill": (_i32, [_vp, _i64, _i64, _i32, _i32, _f32, _f32, _f32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
-                                _i64, _vp]),
+                                _i64, _vp, _sz, _vp]),
+    "lipcache_distill_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
     "lipcache_head_logprobs": (_i32, [_vp, _i64, _i64, _vp, _i64, _vp, _i32, _i32, _i32, _f32, _vp, _vp, _vp, _vp, _vp,
                                       _sz, _vp]),
     "lipcache_head_logprobs_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),

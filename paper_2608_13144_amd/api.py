@@ -644,6 +644,17 @@ def _of_rows(t: torch.Tensor | None, name: str, dtype: torch.dtype, device: torc
     return t.data_ptr()
 
 
+def _few_rows(query: str, T: int, C: int, k: int, code: int, device: torch.device):
+    """The workspace of a call: its address and size, and what holds it until the call is made."""
+    if T > L.FEW_ROWS:
+        return None, 0, None
+    need = getattr(L.load(), query)(T, C, k, code)
+    if need == 0:
+        return None, 0, None
+    ws = workspace(need, device)
+    return ws.data_ptr(), ws.numel(), ws
+
+
 def _entries(index: torch.Tensor | None, value: torch.Tensor | None, names: tuple[str, str], device: torch.device, T: int):
     """k and the addresses of [T, k] classes and their values."""
     if (index is None) != (value is None):
@@ -686,8 +697,9 @@ def logprobs(logits: torch.Tensor, labels: torch.Tensor | None = None, top: int 
         logp, lse, entropy = (_of_rows(getattr(out, name), "out." + name, f32, dev, (T,)) for name in ("logp", "lse", "entropy"))
         index = _of_rows(out.top_index, "out.top_index", i32, dev, (T, k)) if k else None
         value = _of_rows(out.top_logp, "out.top_logp", f32, dev, (T, k)) if k else None
+    ws, size, held = _few_rows("lipcache_logprobs_workspace_bytes", T, C, k, code, dev)
     st = L.load().lipcache_logprobs(logits.data_ptr(), ld, T, C, code, float(temperature), label, k, logp, lse, entropy,
-                                    index, value, _stream_of(dev))
+                                    index, value, ws, size, _stream_of(dev))
     L.check("lipcache_logprobs", st)
     return out
 
@@ -714,11 +726,11 @@ def logprobs_backward(logits: torch.Tensor, labels: torch.Tensor | None = None, 
         out, ldd = logits.new_empty((T, C)), C
     else:
         ldd = _need_rows(out, "out", logits.dtype, dev, T, C)
-    lib = L.load()
-    st = lib.lipcache_logprobs_backward(logits.data_ptr(), ld, T, C, code, float(temperature), label,
-                                        _of_rows(g_logp, "g_logp", f32, dev, (T,)), _of_rows(g_lse, "g_lse", f32, dev, (T,)),
-                                        _of_rows(g_entropy, "g_entropy", f32, dev, (T,)), k, index, value, out.data_ptr(),
-                                        ldd, _stream_of(dev))
+    ws, size, held = _few_rows("lipcache_logprobs_backward_workspace_bytes", T, C, k, code, dev)
+    st = L.load().lipcache_logprobs_backward(
+        logits.data_ptr(), ld, T, C, code, float(temperature), label, _of_rows(g_logp, "g_logp", f32, dev, (T,)),
+        _of_rows(g_lse, "g_lse", f32, dev, (T,)), _of_rows(g_entropy, "g_entropy", f32, dev, (T,)), k, index, value,
+        out.data_ptr(), ldd, ws, size, _stream_of(dev))
     L.check("lipcache_logprobs_backward", st)
     return out
 
@@ -754,9 +766,10 @@ def distill(logits: torch.Tensor, teacher: torch.Tensor | None, index: torch.Ten
         ldd = _need_rows(out, "out", logits.dtype, dev, T, C)
     elif want_grad:
         out = logits.new_empty((T, C))
+    ws, size, held = _few_rows("lipcache_distill_workspace_bytes", T, C, k, code, dev)
     st = L.load().lipcache_distill(logits.data_ptr(), ld, T, C, code, float(temperature), float(hard), float(soft), k, value,
                                    at, label, _of_rows(weight, "weight", f32, dev, (T,)), losses, losses + 4 * T,
-                                   None if out is None else out.data_ptr(), ldd, _stream_of(dev))
+                                   None if out is None else out.data_ptr(), ldd, ws, size, _stream_of(dev))
     L.check("lipcache_distill", st)
     return Distilled(*each.unbind(0), out)
 

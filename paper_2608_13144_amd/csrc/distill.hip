@@ -20,9 +20,11 @@ struct LpShares {
   float hard, soft;  // of the row, with its weight; zero where it has no label, no entry
 };
 
-template <class E, class S, bool kWhole, bool kTwo>
+// kSplit: a workgroup takes a share of a row whose sums are there already.
+template <class E, class S, bool kWhole, bool kTwo, bool kSplit>
 __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits, int64_t ldx, int64_t T, int C,
-                                                                 LpDistill a, E* grad, int64_t ldd) {
+                                                                 LpDistill a, E* grad, int64_t ldd, RowSplit split) {
+  static_assert(!kSplit || (!kWhole && S::kRows == 1), "a share goes in segments");
   typedef RowData<E, S> Data;
   constexpr RowWants kWants = kTwo ? RowWants::kTwo : RowWants::kSum;
   constexpr int kSegment = S::G * S::N, kLanes = S::kLanes;
@@ -35,8 +37,11 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
   RowEntries<kLanes> entries(lds + at.row * entry_bytes(a.k, a.bits), a.k, a.bits);
   const RowScale scale{a.scale, a.second};
   const float hot_scale = kRowLog2e / a.temperature;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * S::kRows;
+  const int64_t step = kSplit ? T : static_cast<int64_t>(gridDim.x) * S::kRows;
   const int full = C / Data::V;
+  const int share = kSplit ? static_cast<int>(blockIdx.x) % split.shares.count : 0;
+  const bool last = !kSplit || share == split.shares.count - 1;
+  const int begin = kSplit ? share * split.shares.each : 0, end = last ? full : begin + split.shares.each;
   auto row_of = [&](int64_t t) { return logits + (t < T ? t : T - 1) * ldx; };
   auto entry_of = [&](int64_t t, int i) {
     RowEntry e{-1, 0.0f};
@@ -45,9 +50,13 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
   };
   auto label_of = [&](int64_t t) { return t < T && a.label ? a.label[t] : -1; };
   auto inside = [&](int c) { return c < C ? c : -1; };
-  auto logit_of = [&](int64_t t, int c) { return c >= 0 ? static_cast<float>(row_of(t)[c]) : 0.0f; };
+  // of entry i (a.k: the label), which names class c
+  auto logit_of = [&](int64_t t, int i, int c) {
+    if constexpr (kSplit) return t < T && i <= a.k ? split.logits[t * (a.k + 1) + i] : 0.0f;
+    else return c >= 0 ? static_cast<float>(row_of(t)[c]) : 0.0f;
+  };
   Data data;
-  int64_t t = static_cast<int64_t>(blockIdx.x) * S::kRows + at.row;
+  int64_t t = kSplit ? static_cast<int>(blockIdx.x) / split.shares.count : static_cast<int64_t>(blockIdx.x) * S::kRows + at.row;
   RowEntry mine{-1, 0.0f};
   int y = -1;
   float logit = 0.0f, y_logit = 0.0f;
@@ -55,10 +64,11 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
     mine = entry_of(t, lane);
     mine.at = inside(mine.at);
     y = inside(label_of(t));
-    logit = logit_of(t, mine.at);
-    y_logit = logit_of(t, y);
+    logit = logit_of(t, lane, mine.at);
+    y_logit = logit_of(t, a.k, y);
   }
-  data.load(row_of(t), 0, C, at.g);
+  if constexpr (!kSplit) data.load(row_of(t), 0, C, at.g);
+  else data.load_tail(row_of(t), C, at.g);
   for (int turn = 0; t - at.row < T; t += step, turn ^= 1) {
     const E* x = row_of(t);
     RowEntry next_entry{-1, 0.0f};
@@ -70,7 +80,9 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
       if (a.weight && t < T) w = a.weight[t];
     }
     RowSums r = data.template begin<kWants>(scale);
-    if constexpr (kWhole) {
+    if constexpr (kSplit) {
+      r = at.g < split.shares.count ? split.sums[t * split.shares.count + at.g] : RowSums{-kRowInf, 0.0f, 0.0f};
+    } else if constexpr (kWhole) {
       data.template add<kWants>(0, full, at.g, r, scale, RowNothing{}, RowNothing{});
     } else {
       // a segment's chunks are asked for as the one before is used
@@ -86,7 +98,7 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
         e.at = inside(e.at);
         return e;
       };
-      entries.keep(lane, mine, logit, loaded, [&](int c) { return logit_of(t, c); });
+      entries.keep(lane, mine, logit, loaded, [&](int i, int c) { return logit_of(t, i, c); });
       for (int i = lane; i < a.k; i += kLanes)
         if (entries.at[i] >= 0) {
           const float v = entries.value[i];
@@ -102,11 +114,11 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
       wave_sync();
     }
     row_join<S, kWants>(r, scale, room[turn]);
-    const LpShares share = shares[turn][at.row];
+    const LpShares part = shares[turn][at.row];
     const float from = row_from(r.m);
-    const bool any = (share.hard != 0.0f || share.soft != 0.0f) && r.s != 0.0f;
+    const bool any = (part.hard != 0.0f || part.soft != 0.0f) && r.s != 0.0f;
     // what an element adds: one exponential with both parts' factor, or one for each
-    const float one = (kTwo ? share.soft : share.hard + share.soft) / r.s, two = kTwo ? share.hard / r.more : 0.0f;
+    const float one = (kTwo ? part.soft : part.hard + part.soft) / r.s, two = kTwo ? part.hard / r.more : 0.0f;
     auto smooth = [&](float v) {
       const float d = v - from;
       float g = row_exp2(d * scale.scale) * one;
@@ -121,12 +133,12 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
         if (entries.at[i] < 0) continue;
         const float b = entries.value[i] - top, q = some != 0.0f ? row_exp2(b * hot_scale) / sum : 0.0f;
         if (!(q == 0.0f)) kl += q * ((b - (entries.logit[i] - from)) * hot_scale);
-        const float part = share.soft * q;
-        entries.value[i] = part;
-        if (part == 0.0f) entries.at[i] = -1;
+        const float mass = part.soft * q;
+        entries.value[i] = mass;
+        if (mass == 0.0f) entries.at[i] = -1;
       }
       kl = lanes_sum<kLanes>(kl);
-      if (lane == 0 && t < T) {
+      if (lane == 0 && t < T && share == 0) {
         if (a.ce)
           a.ce[t] = y < 0 ? 0.0f : r.s == 0.0f ? kRowInf : row_log2(kTwo ? r.more : r.s) * kRowLn2 - (y_logit - from);
         if (a.kl) a.kl[t] = some == 0.0f ? 0.0f : r.s == 0.0f ? kRowInf : (kl + row_log2(r.s) - row_log2(sum)) * kRowLn2;
@@ -134,12 +146,12 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
       wave_sync();
       mine = next_entry;
       y = next_y;
-      logit = logit_of(t + step, mine.at);
-      y_logit = logit_of(t + step, y);
+      logit = logit_of(t + step, lane, mine.at);
+      y_logit = logit_of(t + step, a.k, y);
     }
     const E* following = row_of(t + step);
     if (!grad) {
-      data.load(following, 0, C, at.g);
+      if constexpr (!kSplit) data.load(following, 0, C, at.g);
       continue;
     }
     E* dx = grad + (t < T ? t : T - 1) * ldd;
@@ -151,27 +163,31 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
         data.load_chunk(i, following, 0, full, at.g);
       }
     } else {
-      for (int first = 0; first < full; first += kSegment) {
+      for (int first = begin; first < end; first += kSegment) {
 #pragma unroll
-        for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, full, at.g);
+        for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, end, at.g);
 #pragma unroll
         for (int i = 0; i < S::N; ++i)
-          if (t < T) data.store_chunk(i, dx, first, full, at.g, dx_of);
+          if (t < T) data.store_chunk(i, dx, first, end, at.g, dx_of);
       }
+      if constexpr (!kSplit) {
 #pragma unroll
-      for (int i = 0; i < S::N; ++i) data.load_chunk(i, following, 0, full, at.g);
+        for (int i = 0; i < S::N; ++i) data.load_chunk(i, following, 0, full, at.g);
+      }
     }
-    if (t < T) data.store_tail(dx, C, at.g, dx_of);
-    data.load_tail(following, C, at.g);
+    if (t < T && last) data.store_tail(dx, C, at.g, dx_of);
+    if constexpr (!kSplit) data.load_tail(following, C, at.g);
     RowPlace<S>::sync();  // the row is written before its entries are
     if (keeps && any && t < T) {
-      const bool named = now_y >= 0 && share.hard != 0.0f, met = named && entries.add(lane, now_y, share.hard);
+      const int from_class = begin * Data::V, to_class = last ? C : end * Data::V;
+      auto here = [&](int c) { return c >= from_class && c < to_class; };
+      const bool named = now_y >= 0 && part.hard != 0.0f, met = named && entries.add(lane, now_y, part.hard);
       entries.index(lane);
       for (int i = lane; i < a.k; i += kLanes) {
         float q;
-        if (entries.first(i, q)) dx[entries.at[i]] = static_cast<E>(smooth(entries.logit[i]) - q);
+        if (entries.first(i, q) && here(entries.at[i])) dx[entries.at[i]] = static_cast<E>(smooth(entries.logit[i]) - q);
       }
-      if (lane == 0 && named && !met) dx[now_y] = static_cast<E>(smooth(now_logit) - share.hard);
+      if (lane == 0 && named && !met && here(now_y)) dx[now_y] = static_cast<E>(smooth(now_logit) - part.hard);
     }
   }
 }
@@ -184,7 +200,7 @@ extern "C" lipcache_status lipcache_distill(const void* x, int64_t ldx, int64_t 
                                             float temperature, float hard, float soft, int32_t k,
                                             const float* teacher, const int32_t* index, const int32_t* label,
                                             const float* weight, float* ce, float* kl, void* dx, int64_t lddx,
-                                            lipcache_stream_t stream) {
+                                            void* ws, size_t ws_bytes, lipcache_stream_t stream) {
   if (lipcache_status st = row_check(x, ldx, T, C, dtype, temperature); st != LIPCACHE_OK) return st;
   if (k < 0 || (dx && lddx < C) || (T > 0 && k > 0 && (!teacher || !index))) return LIPCACHE_EINVAL;
   if (!(__builtin_fabsf(hard) < kRowInf) || !(__builtin_fabsf(soft) < kRowInf)) return LIPCACHE_EINVAL;
@@ -193,6 +209,9 @@ extern "C" lipcache_status lipcache_distill(const void* x, int64_t ldx, int64_t 
     return LIPCACHE_EINVAL;
   if (k > LIPCACHE_MOST_ENTRIES) return LIPCACHE_EUNSUPPORTED;
   if (T == 0) return LIPCACHE_OK;
+  const RowShares shares = row_shares(T, C, dtype);
+  if (const size_t need = row_share_bytes(T, k, shares); need > 0 && (!ws || !aligned256(ws) || ws_bytes < need))
+    return LIPCACHE_EWORKSPACE;
   const int bits = entry_bits(C);
   // which sums there are: the label's at temperature 1, the teacher's at its own, one where they are the same
   const bool cold = label && (hard != 0.0f || ce), hot = k > 0 && (soft != 0.0f || kl);
@@ -200,17 +219,37 @@ extern "C" lipcache_status lipcache_distill(const void* x, int64_t ldx, int64_t 
   const float at_one = kRowLog2e, at_own = kRowLog2e / temperature;
   const LpDistill a{temperature, hard, soft, hot ? at_own : at_one, at_one, label, weight, k,
                     teacher, index, ce, kl, bits};
+  RowSplit split{shares, nullptr, nullptr};
+  if (shares.count > 1) {
+    RowSums* sums = static_cast<RowSums*>(ws);
+    float* named = reinterpret_cast<float*>(static_cast<char*>(ws) + align_up(T * shares.count * sizeof(RowSums), 256));
+    if (lipcache_status st = row_share_sums(x, ldx, T, C, dtype, two ? RowWants::kTwo : RowWants::kSum, RowScale{a.scale, a.second},
+                                            shares, k, index, label, sums, named, stream);
+        st != LIPCACHE_OK)
+      return st;
+    split.sums = sums;
+    split.logits = named;
+  }
   return row_typed(dtype, [&](auto type) {
     typedef decltype(type) E;
-    return row_shaped_entries<E>(T, C, k, [&](auto shape, auto whole) {
+    auto run = [&](auto shape, auto whole, auto cut, unsigned blocks) {
       typedef decltype(shape) S;
-      auto run = [&](auto both) {
-        lp_distill_kernel<E, S, decltype(whole)::value, decltype(both)::value>
-            <<<row_blocks<S>(T), S::kThreads, S::kRows * entry_bytes(k, bits), stream>>>(
-                static_cast<const E*>(x), ldx, T, C, a, static_cast<E*>(dx), lddx);
+      auto both = [&](auto with) {
+        lp_distill_kernel<E, S, decltype(whole)::value, decltype(with)::value, decltype(cut)::value>
+            <<<blocks, S::kThreads, S::kRows * entry_bytes(k, bits), stream>>>(static_cast<const E*>(x), ldx, T, C, a,
+                                                                              static_cast<E*>(dx), lddx, split);
         return hipGetLastError() == hipSuccess ? LIPCACHE_OK : LIPCACHE_EHIP;
       };
-      return two ? run(std::true_type{}) : run(std::false_type{});
+      return two ? both(std::true_type{}) : both(std::false_type{});
+    };
+    if (shares.count > 1)
+      return run(RowShape<256, 4>{}, std::false_type{}, std::true_type{}, static_cast<unsigned>(T * shares.count));
+    return row_shaped_entries<E>(T, C, k, [&](auto shape, auto whole) {
+      return run(shape, whole, std::false_type{}, row_blocks<decltype(shape)>(T));
     });
   });
+}
+
+extern "C" size_t lipcache_distill_workspace_bytes(int64_t T, int32_t C, int32_t k, int32_t dtype) {
+  return row_sizes_bad(T, C, k, dtype) ? 0 : row_share_bytes(T, k, row_shares(T, C, dtype));
 }

@@ -377,7 +377,7 @@ struct RowEntries {
   // By the lanes that keep the entries: entry `lane` is `mine` with its logit; entry_of and logit_of load the others, four at a
   // time so that their loads wait together.
   template <class Entry, class Logit>
-  __device__ __forceinline__ void keep(int lane, RowEntry mine, float mine_logit, Entry entry_of, Logit logit_of) {
+  __device__ __forceinline__ void keep(int lane, RowEntry mine, float mine_logit, Entry entry_of, Logit logit_of) {  // logit_of(entry, class)
     if (lane < n) {
       at[lane] = mine.at;
       value[lane] = mine.value;
@@ -389,7 +389,7 @@ struct RowEntries {
 #pragma unroll
       for (int p = 0; p < 4; ++p) e[p] = entry_of(i + p * LANES);
 #pragma unroll
-      for (int p = 0; p < 4; ++p) l[p] = logit_of(e[p].at);
+      for (int p = 0; p < 4; ++p) l[p] = logit_of(i + p * LANES, e[p].at);
 #pragma unroll
       for (int p = 0; p < 4; ++p)
         if (i + p * LANES < n) {
@@ -452,6 +452,10 @@ inline bool row_unaligned(const void* p, int32_t dtype) {
 }
 inline bool row_unaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 
+inline bool row_sizes_bad(int64_t T, int32_t C, int32_t k, int32_t dtype) {
+  return T < 0 || C < 1 || k < 0 || dtype < LIPCACHE_F32 || dtype > LIPCACHE_F16;
+}
+
 inline lipcache_status row_check(const void* x, int64_t ldx, int64_t T, int32_t C, int32_t dtype, float temperature) {
   if (T < 0 || C < 1 || ldx < C || dtype < LIPCACHE_F32 || dtype > LIPCACHE_F16) return LIPCACHE_EINVAL;
   if (!(temperature >= 0x1p-20f && temperature <= 0x1p20f)) return LIPCACHE_EINVAL;
@@ -498,6 +502,38 @@ lipcache_status row_shaped_entries(int64_t T, int C, int n, F f) {
     return f(shape, whole);
   });
 }
+
+// ------------------------------------------------- few rows, of many classes
+// A row of a workgroup leaves the other CUs idle.  Up to 64 rows of more than 4096 chunks (a share is at least 1024, a chunk 16
+// bytes) go in shares: one launch for the shares' sums, another that joins them and, for a gradient, writes it by
+// shares.  What the second needs of the row beside its share (its logits at the classes that it names) the first
+// puts by, as the gradient may be written over the row.
+// One row of 131072 bfloat16: scores with 20 alternatives 21 us as one workgroup, gradient 20, with two temperatures 31.
+constexpr int kRowFew = LIPCACHE_FEW_ROWS;
+constexpr int kRowShares = 32;
+struct RowShares {
+  int count;  // 1: the rows are not split
+  int each;   // chunks of a share
+};
+inline RowShares row_shares(int64_t T, int C, int32_t dtype) {
+  const int chunks = C / (dtype == LIPCACHE_F32 ? 4 : 8);
+  if (T < 1 || T > kRowFew || chunks <= 4096) return {1, chunks};
+  const int each = ((chunks + kRowShares - 1) / kRowShares + 1023) / 1024 * 1024;
+  return {(chunks + each - 1) / each, each};
+}
+// sums[t][share], and logits[t][k + 1] at the entries' classes and the label (0 where there is none).
+lipcache_status row_share_sums(const void* x, int64_t ldx, int64_t T, int C, int32_t dtype, RowWants wants, RowScale scale,
+                               RowShares shares, int k, const int32_t* index, const int32_t* label, RowSums* sums,
+                               float* logits, hipStream_t s);
+inline size_t row_share_bytes(int64_t T, int k, const RowShares& shares) {
+  if (shares.count == 1) return 0;
+  return align_up(static_cast<size_t>(T) * shares.count * sizeof(RowSums), 256) + align_up(static_cast<size_t>(T) * (k + 1) * 4, 256);
+}
+struct RowSplit {
+  RowShares shares;
+  const RowSums* sums;
+  const float* logits;
+};
 
 // Workgroups: the rows, or as many as the chip holds at a time (256 CUs of 2048 threads).
 template <class S>

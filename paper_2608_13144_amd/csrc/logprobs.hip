@@ -163,16 +163,19 @@ struct TopList {
   }
 };
 
-// kWhole: a row is one segment.
+// kWhole: a row is one segment.  kShare: a workgroup takes a share of a row, and leaves its sums and its k largest (keys
+// in falling order, 0 where there are fewer) for lp_score_join_kernel.
 //
 // Alternatives: a threshold that k elements of the row's first segment reach (the largest values of its threads give
 // it), then every block of the row whose largest value reaches it puts its elements that do on a list, a few times k of
 // them, each of which finds its place by counting.  Where a list is too short for them (the first segment holds
 // little of what is large, or many values are equal), a threshold from the threads' largest values of the whole row
 // and another pass follow, and where that is not enough either, one alternative after another.
-template <class E, class S, bool kWhole>
+template <class E, class S, bool kWhole, bool kShare>
 __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restrict__ logits, int64_t ldx, int64_t T, int C,
-                                                               LpScore a) {
+                                                               LpScore a, RowShares shares, RowSums* __restrict__ sums,
+                                                               uint64_t* __restrict__ keys) {
+  static_assert(!kShare || (!kWhole && S::kRows == 1), "a share goes in segments");
   typedef RowData<E, S> Data;
   constexpr int kSegment = S::G * S::N;
   __shared__ RowSums room[2][S::kWaves];
@@ -180,27 +183,33 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
   __shared__ TopRoom<S> top_room;
   const RowPlace<S> at;
   const RowScale scale{kRowLog2e / a.temperature, 0.0f};
-  const int64_t step = static_cast<int64_t>(gridDim.x) * S::kRows;
+  const int64_t step = kShare ? T : static_cast<int64_t>(gridDim.x) * S::kRows;
   const int full = C / Data::V;
+  const int share = kShare ? static_cast<int>(blockIdx.x) % shares.count : 0;
+  const bool last = !kShare || share == shares.count - 1;
+  const int begin = kShare ? share * shares.each : 0, end = last ? full : begin + shares.each;
   auto row_of = [&](int64_t t) { return logits + (t < T ? t : T - 1) * ldx; };
   auto label_of = [&](int64_t t) { return a.label && t < T ? a.label[t] : -1; };
   auto checked = [&](int y) { return y < C ? y : -1; };
   auto logit_of = [&](int64_t t, int y) { return y >= 0 ? static_cast<float>(row_of(t)[y]) : 0.0f; };
   Data data;
-  int64_t t = static_cast<int64_t>(blockIdx.x) * S::kRows + at.row;
-  int y = checked(label_of(t));
+  int64_t t = kShare ? static_cast<int>(blockIdx.x) / shares.count : static_cast<int64_t>(blockIdx.x) * S::kRows + at.row;
+  int y = kShare ? -1 : checked(label_of(t));
   float logit = logit_of(t, y);
-  data.load(row_of(t), 0, C, at.g);
+  data.tail = -kRowInf;
+  if (last) data.load_tail(row_of(t), C, at.g);
+#pragma unroll
+  for (int i = 0; i < S::N; ++i) data.load_chunk(i, row_of(t), begin, end, at.g);
   const int wave = S::kWaves > 1 ? static_cast<int>(threadIdx.x) / kWave : 0;  // of the row
   for (int turn = 0; t - at.row < T; t += step, turn ^= 1) {
     const E *x = row_of(t), *following = row_of(t + step);
-    int next_y = label_of(t + step);
+    int next_y = kShare ? -1 : label_of(t + step);
     const float tail = data.tail;
     TopList<S> list{top.list[at.row][wave]};
     float least = kRowInf;
     auto hits = [&](float v) { return v >= least && v > -kRowInf; };
     if (a.k > 0) {
-      least = top_least<S>(a.k, data.largest(0, full, at.g), at, top);
+      least = top_least<S>(a.k, data.largest(begin, end, at.g), at, top);
       list.push(hits(tail), tail, full * Data::V + at.g);
     }
     RowSums r = data.template begin<RowWants::kMean>(scale);
@@ -214,22 +223,28 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
       if (a.k > 0 && __ballot(hits(m)) != 0) each(hits, [&](bool any, float v, int j) { list.push(any, v, j); });
     };
     // a segment's chunks are asked for as the one before is used, the next row's behind the row's last
-    int first = 0;
+    int first = begin;
     if constexpr (!kWhole) {
-      for (; first + kSegment < full; first += kSegment)
-        data.template add<RowWants::kMean>(first, full, at.g, r, scale, seen,
-                                           [&](int i) { data.load_chunk(i, x, first + kSegment, full, at.g); });
+      for (; first + kSegment < end; first += kSegment)
+        data.template add<RowWants::kMean>(first, end, at.g, r, scale, seen,
+                                           [&](int i) { data.load_chunk(i, x, first + kSegment, end, at.g); });
     }
-    next();
-    data.template add<RowWants::kMean>(first, full, at.g, r, scale, seen,
-                                       [&](int i) { data.load_chunk(i, following, 0, full, at.g); });
+    if constexpr (kShare) {
+      data.template add<RowWants::kMean>(first, end, at.g, r, scale, seen, RowNothing{});
+    } else {
+      next();
+      data.template add<RowWants::kMean>(first, full, at.g, r, scale, seen,
+                                         [&](int i) { data.load_chunk(i, following, 0, full, at.g); });
+    }
     const float own = r.m;
     if (a.k > 0 && at.g % S::kLanes == 0) top.count[at.row][wave] = list.n;
     if constexpr (S::G <= 64) wave_sync();  // the join of longer rows has a barrier
     row_join<S, RowWants::kMean>(r, scale, room[turn]);
     const float from = row_from(r.m), log_s = row_log2(r.s);
     auto logp = [&](float v) { return r.s == 0.0f ? -kRowInf : (v - from) / a.temperature - log_s * kRowLn2; };
-    if (t < T && at.g == 0) {
+    if (kShare) {
+      if (at.g == 0) sums[blockIdx.x] = r;
+    } else if (t < T && at.g == 0) {
       if (a.logp) a.logp[t] = y >= 0 ? logp(logit) : 0.0f;
       if (a.lse) a.lse[t] = from / a.temperature + log_s * kRowLn2;
       if (a.entropy) a.entropy[t] = r.s == 0.0f ? 0.0f : (log_s - r.more / r.s) * kRowLn2;
@@ -237,6 +252,10 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
     if (a.k > 0) {
       auto put = [&](int i, float v, int j) {
         if (t >= T) return;
+        if constexpr (kShare) {
+          keys[static_cast<int64_t>(blockIdx.x) * a.k + i] = v == -kRowInf ? 0 : top_key(v, j);
+          return;
+        }
         a.top_index[t * a.k + i] = v == -kRowInf ? -1 : j;
         a.top_logp[t * a.k + i] = v == -kRowInf ? -kRowInf : logp(v);
       };
@@ -257,10 +276,10 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
         // the rare ways read the row again
         auto each = [&](auto f) {
 #pragma unroll 1
-          for (int c = at.g - at.g % S::kLanes; c < full; c += S::G) {  // (whole waves)
+          for (int c = begin + at.g - at.g % S::kLanes; c < end; c += S::G) {  // (whole waves)
             const int mine = c + at.g % S::kLanes;
             u32x4 raw = Data::fill();
-            if (mine < full) raw = *reinterpret_cast<const typename Data::Type::vec*>(x + static_cast<int64_t>(mine) * Data::V);
+            if (mine < end) raw = *reinterpret_cast<const typename Data::Type::vec*>(x + static_cast<int64_t>(mine) * Data::V);
 #pragma unroll
             for (int e = 0; e < Data::V; ++e) f(Data::Type::get(raw, e), mine * Data::V + e);
           }
@@ -300,6 +319,66 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
   }
 }
 
+// Joins a row's shares.  The k-th of what the shares' m-th alternatives reach, m = k over the shares, is a threshold: what
+// reaches it is a list whose entries find their places by counting.
+template <class E>
+__global__ __launch_bounds__(256) void lp_score_join_kernel(const E* __restrict__ logits, int64_t ldx, int C, LpScore a,
+                                                            RowShares shares, const RowSums* __restrict__ sums,
+                                                            const uint64_t* __restrict__ keys) {
+  typedef RowShape<256, 1> S;
+  __shared__ RowSums room[S::kWaves];
+  __shared__ uint64_t list[kRowShares * kTopMost];
+  __shared__ int count;
+  const RowPlace<S> at;
+  const int64_t t = blockIdx.x;
+  const RowScale scale{kRowLog2e / a.temperature, 0.0f};
+  int y = a.label ? a.label[t] : -1;
+  if (y >= C) y = -1;
+  const float logit = y >= 0 ? static_cast<float>(logits[t * ldx + y]) : 0.0f;
+  RowSums r = at.g < shares.count ? sums[t * shares.count + at.g] : RowSums{-kRowInf, 0.0f, 0.0f};
+  if (at.g == 0) count = 0;
+  row_join<S, RowWants::kMean>(r, scale, room);
+  const float from = row_from(r.m), log_s = row_log2(r.s);
+  auto logp = [&](float v) { return r.s == 0.0f ? -kRowInf : (v - from) / a.temperature - log_s * kRowLn2; };
+  if (at.g == 0) {
+    if (a.logp) a.logp[t] = y >= 0 ? logp(logit) : 0.0f;
+    if (a.lse) a.lse[t] = from / a.temperature + log_s * kRowLn2;
+    if (a.entropy) a.entropy[t] = r.s == 0.0f ? 0.0f : (log_s - r.more / r.s) * kRowLn2;
+  }
+  if (a.k == 0) return;
+  const uint64_t* mine = keys + t * shares.count * a.k;
+  const int m = (a.k + shares.count - 1) / shares.count;
+  uint64_t least = ~0ull;
+  for (int i = 0; i < shares.count; ++i) {
+    const uint64_t key = mine[i * a.k + m - 1];
+    least = key < least ? key : least;
+  }
+  for (int i = at.g; i < shares.count * a.k; i += S::G) {
+    const uint64_t key = mine[i];
+    if (key >= least && key != 0) list[atomicAdd(&count, 1)] = key;
+  }
+  __syncthreads();
+  const int n = count;
+  for (int c = at.g; c < n || c < a.k; c += S::G) {
+    int place = c;
+    const uint64_t key = c < n ? list[c] : 0;
+    if (c < n) {
+      place = 0;
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) place += list[i] > key ? 1 : 0;
+    }
+    if (place >= a.k) continue;
+    a.top_index[t * a.k + place] = c < n ? top_index(key) : -1;
+    a.top_logp[t * a.k + place] = c < n ? logp(top_value(key)) : -kRowInf;
+  }
+}
+
+inline size_t score_bytes(int64_t T, int k, const RowShares& shares) {
+  if (shares.count == 1) return 0;
+  const size_t n = static_cast<size_t>(T) * shares.count;
+  return align_up(n * sizeof(RowSums), 256) + align_up(n * k * sizeof(uint64_t), 256);
+}
+
 // Threads of a row.  Rows of up to 64 chunks are held by 16 lanes, of up to 256 by a wave.  Longer ones go through in
 // segments: by a wave up to 1024 chunks where the rows fill the chip with waves, by 256 threads, or by 1024 where there
 // are few.  (The 16 groups of a 16-lane row give a threshold for up to 12 alternatives, the 64 of a wave one that many more
@@ -325,7 +404,7 @@ using namespace lc;
 extern "C" lipcache_status lipcache_logprobs(const void* x, int64_t ldx, int64_t T, int32_t C, int32_t dtype,
                                              float temperature, const int32_t* label, int32_t k, float* logp,
                                              float* lse, float* entropy, int32_t* top_index, float* top_logp,
-                                             lipcache_stream_t stream) {
+                                             void* ws, size_t ws_bytes, lipcache_stream_t stream) {
   if (lipcache_status st = row_check(x, ldx, T, C, dtype, temperature); st != LIPCACHE_OK) return st;
   if (k < 0 || (T > 0 && k > 0 && (!top_index || !top_logp))) return LIPCACHE_EINVAL;
   if (row_unaligned4(label) || row_unaligned4(logp) || row_unaligned4(lse) || row_unaligned4(entropy) ||
@@ -333,14 +412,34 @@ extern "C" lipcache_status lipcache_logprobs(const void* x, int64_t ldx, int64_t
     return LIPCACHE_EINVAL;
   if (k > kTopMost) return LIPCACHE_EUNSUPPORTED;
   if (T == 0) return LIPCACHE_OK;
+  const RowShares shares = row_shares(T, C, dtype);
+  if (const size_t need = score_bytes(T, k, shares); need > 0 && (!ws || !aligned256(ws) || ws_bytes < need))
+    return LIPCACHE_EWORKSPACE;
   const LpScore a{temperature, label, k, logp, lse, entropy, top_index, top_logp};
   return row_typed(dtype, [&](auto type) {
     typedef decltype(type) E;
+    const E* logits = static_cast<const E*>(x);
+    if (shares.count > 1) {
+      typedef RowShape<256, 4> S;
+      RowSums* sums = static_cast<RowSums*>(ws);
+      uint64_t* keys = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + align_up(T * shares.count * sizeof(RowSums), 256));
+      lp_score_kernel<E, S, false, true>
+          <<<static_cast<unsigned>(T * shares.count), S::kThreads, 0, stream>>>(logits, ldx, T, C, a, shares, sums, keys);
+      LC_LAUNCHED();
+      lp_score_join_kernel<E><<<static_cast<unsigned>(T), 256, 0, stream>>>(logits, ldx, C, a, shares, sums, keys);
+      LC_LAUNCHED();
+      return LIPCACHE_OK;
+    }
     return score_shaped<E>(T, C, k, [&](auto shape, auto whole) {
       typedef decltype(shape) S;
-      lp_score_kernel<E, S, decltype(whole)::value><<<row_blocks<S>(T), S::kThreads, 0, stream>>>(static_cast<const E*>(x), ldx, T, C, a);
+      lp_score_kernel<E, S, decltype(whole)::value, false>
+          <<<row_blocks<S>(T), S::kThreads, 0, stream>>>(logits, ldx, T, C, a, shares, nullptr, nullptr);
       LC_LAUNCHED();
       return LIPCACHE_OK;
     });
   });
+}
+
+extern "C" size_t lipcache_logprobs_workspace_bytes(int64_t T, int32_t C, int32_t k, int32_t dtype) {
+  return row_sizes_bad(T, C, k, dtype) ? 0 : score_bytes(T, k, row_shares(T, C, dtype));
 }

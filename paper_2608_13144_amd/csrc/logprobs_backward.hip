@@ -21,9 +21,11 @@ struct LpSlope {
   int some;    // any gradient that is not zero
 };
 
-template <class E, class S, bool kWhole, bool kEntropy>
+// kSplit: a workgroup takes a share of a row whose sums are there already.
+template <class E, class S, bool kWhole, bool kEntropy, bool kSplit>
 __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logits, int64_t ldx, int64_t T, int C,
-                                                                  LpBackward a, E* grad, int64_t ldd) {
+                                                                  LpBackward a, E* grad, int64_t ldd, RowSplit split) {
+  static_assert(!kSplit || (!kWhole && S::kRows == 1), "a share goes in segments");
   typedef RowData<E, S> Data;
   constexpr RowWants kWants = kEntropy ? RowWants::kMean : RowWants::kSum;
   constexpr int kSegment = S::G * S::N, kLanes = S::kLanes;
@@ -36,8 +38,11 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
   RowEntries<kLanes> entries(lds + at.row * entry_bytes(a.k, a.bits), a.k, a.bits);
   const RowScale scale{kRowLog2e / a.temperature, 0.0f};
   const float inv_t = 1.0f / a.temperature;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * S::kRows;
+  const int64_t step = kSplit ? T : static_cast<int64_t>(gridDim.x) * S::kRows;
   const int full = C / Data::V;
+  const int share = kSplit ? static_cast<int>(blockIdx.x) % split.shares.count : 0;
+  const bool last = !kSplit || share == split.shares.count - 1;
+  const int begin = kSplit ? share * split.shares.each : 0, end = last ? full : begin + split.shares.each;
   auto row_of = [&](int64_t t) { return logits + (t < T ? t : T - 1) * ldx; };
   auto entry_of = [&](int64_t t, int i) {
     RowEntry e{-1, 0.0f};
@@ -53,18 +58,23 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
     if (e.at < 0 || e.at >= C || e.value == 0.0f) e = {-1, 0.0f};
     return e;
   };
-  auto logit_of = [&](int64_t t, int c) { return c >= 0 ? static_cast<float>(row_of(t)[c]) : 0.0f; };
+  // of entry i (a.k: the label), which names class c
+  auto logit_of = [&](int64_t t, int i, int c) {
+    if constexpr (kSplit) return t < T && i <= a.k ? split.logits[t * (a.k + 1) + i] : 0.0f;
+    else return c >= 0 ? static_cast<float>(row_of(t)[c]) : 0.0f;
+  };
   Data data;
-  int64_t t = static_cast<int64_t>(blockIdx.x) * S::kRows + at.row;
+  int64_t t = kSplit ? static_cast<int>(blockIdx.x) / split.shares.count : static_cast<int64_t>(blockIdx.x) * S::kRows + at.row;
   RowEntry mine{-1, 0.0f}, label{-1, 0.0f};
   float logit = 0.0f, label_logit = 0.0f;
   if (keeps) {
     mine = checked(entry_of(t, lane));
     label = checked(label_of(t));
-    logit = logit_of(t, mine.at);
-    label_logit = logit_of(t, label.at);
+    logit = logit_of(t, lane, mine.at);
+    label_logit = logit_of(t, a.k, label.at);
   }
-  data.load(row_of(t), 0, C, at.g);
+  if constexpr (!kSplit) data.load(row_of(t), 0, C, at.g);
+  else data.load_tail(row_of(t), C, at.g);
   for (; t - at.row < T; t += step) {
     const E* x = row_of(t);
     E* dx = grad + (t < T ? t : T - 1) * ldd;
@@ -77,7 +87,9 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
       if (kEntropy && t < T) ge = a.g_entropy[t];
     }
     RowSums r = data.template begin<kWants>(scale);
-    if constexpr (kWhole) {
+    if constexpr (kSplit) {
+      r = at.g < split.shares.count ? split.sums[t * split.shares.count + at.g] : RowSums{-kRowInf, 0.0f, 0.0f};
+    } else if constexpr (kWhole) {
       data.template add<kWants>(0, full, at.g, r, scale, RowNothing{}, RowNothing{});
     } else {
       // a segment's chunks are asked for as the one before is used
@@ -87,7 +99,7 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
     next_entry = checked(next_entry);
     next_label = checked(next_label);
     if (keeps) {
-      entries.keep(lane, mine, logit, [&](int i) { return checked(entry_of(t, i)); }, [&](int c) { return logit_of(t, c); });
+      entries.keep(lane, mine, logit, [&](int i) { return checked(entry_of(t, i)); }, [&](int i, int c) { return logit_of(t, i, c); });
       float mass = 0.0f, any = gl != 0.0f || ge != 0.0f || label.value != 0.0f ? 1.0f : 0.0f;
       for (int i = lane; i < a.k; i += kLanes) {
         const float v = entries.value[i];
@@ -116,8 +128,8 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
     if (keeps) {
       mine = next_entry;
       label = next_label;
-      logit = logit_of(t + step, mine.at);
-      label_logit = logit_of(t + step, label.at);
+      logit = logit_of(t + step, lane, mine.at);
+      label_logit = logit_of(t + step, a.k, label.at);
     }
     if (kWhole) {
 #pragma unroll
@@ -126,27 +138,31 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
         data.load_chunk(i, following, 0, full, at.g);
       }
     } else {
-      for (int first = 0; first < full; first += kSegment) {
+      for (int first = begin; first < end; first += kSegment) {
 #pragma unroll
-        for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, full, at.g);
+        for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, end, at.g);
 #pragma unroll
         for (int i = 0; i < S::N; ++i)
-          if (t < T) data.store_chunk(i, dx, first, full, at.g, dx_of);
+          if (t < T) data.store_chunk(i, dx, first, end, at.g, dx_of);
       }
+      if constexpr (!kSplit) {
 #pragma unroll
-      for (int i = 0; i < S::N; ++i) data.load_chunk(i, following, 0, full, at.g);
+        for (int i = 0; i < S::N; ++i) data.load_chunk(i, following, 0, full, at.g);
+      }
     }
-    if (t < T) data.store_tail(dx, C, at.g, dx_of);
-    data.load_tail(following, C, at.g);
+    if (t < T && last) data.store_tail(dx, C, at.g, dx_of);
+    if constexpr (!kSplit) data.load_tail(following, C, at.g);
     RowPlace<S>::sync();  // the row is written before its entries are
     if (keeps && some && t < T) {
+      const int from_class = begin * Data::V, to_class = last ? C : end * Data::V;
+      auto here = [&](int c) { return c >= from_class && c < to_class; };
       const bool met = now.at >= 0 && entries.add(lane, now.at, now.value);
       entries.index(lane);
       for (int i = lane; i < a.k; i += kLanes) {
         float g;
-        if (entries.first(i, g)) dx[entries.at[i]] = static_cast<E>(fmaf(g, inv_t, smooth(entries.logit[i])));
+        if (entries.first(i, g) && here(entries.at[i])) dx[entries.at[i]] = static_cast<E>(fmaf(g, inv_t, smooth(entries.logit[i])));
       }
-      if (lane == 0 && now.at >= 0 && !met) dx[now.at] = static_cast<E>(fmaf(now.value, inv_t, smooth(now_logit)));
+      if (lane == 0 && now.at >= 0 && !met && here(now.at)) dx[now.at] = static_cast<E>(fmaf(now.value, inv_t, smooth(now_logit)));
     }
   }
 }
@@ -159,7 +175,8 @@ extern "C" lipcache_status lipcache_logprobs_backward(const void* x, int64_t ldx
                                                       float temperature, const int32_t* label, const float* g_logp,
                                                       const float* g_lse, const float* g_entropy, int32_t k,
                                                       const int32_t* top_index, const float* g_top, void* dx,
-                                                      int64_t lddx, lipcache_stream_t stream) {
+                                                      int64_t lddx, void* ws, size_t ws_bytes,
+                                                      lipcache_stream_t stream) {
   if (lipcache_status st = row_check(x, ldx, T, C, dtype, temperature); st != LIPCACHE_OK) return st;
   if (k < 0 || lddx < C || (T > 0 && !dx) || (T > 0 && k > 0 && (!top_index || !g_top)) || (g_logp && !label))
     return LIPCACHE_EINVAL;
@@ -168,19 +185,43 @@ extern "C" lipcache_status lipcache_logprobs_backward(const void* x, int64_t ldx
     return LIPCACHE_EINVAL;
   if (k > LIPCACHE_MOST_ENTRIES) return LIPCACHE_EUNSUPPORTED;
   if (T == 0) return LIPCACHE_OK;
+  const RowShares shares = row_shares(T, C, dtype);
+  if (const size_t need = row_share_bytes(T, k, shares); need > 0 && (!ws || !aligned256(ws) || ws_bytes < need))
+    return LIPCACHE_EWORKSPACE;
   const int bits = entry_bits(C);
   const LpBackward a{temperature, label, g_logp, g_lse, g_entropy, k, top_index, g_top, bits};
+  const RowScale scale{kRowLog2e / temperature, 0.0f};
+  RowSplit split{shares, nullptr, nullptr};
+  if (shares.count > 1) {
+    RowSums* sums = static_cast<RowSums*>(ws);
+    float* named = reinterpret_cast<float*>(static_cast<char*>(ws) + align_up(T * shares.count * sizeof(RowSums), 256));
+    if (lipcache_status st = row_share_sums(x, ldx, T, C, dtype, g_entropy ? RowWants::kMean : RowWants::kSum, scale, shares, k,
+                                            top_index, label, sums, named, stream);
+        st != LIPCACHE_OK)
+      return st;
+    split.sums = sums;
+    split.logits = named;
+  }
   return row_typed(dtype, [&](auto type) {
     typedef decltype(type) E;
-    return row_shaped_entries<E>(T, C, k, [&](auto shape, auto whole) {
+    auto run = [&](auto shape, auto whole, auto cut, unsigned blocks) {
       typedef decltype(shape) S;
-      auto run = [&](auto entropy) {
-        lp_backward_kernel<E, S, decltype(whole)::value, decltype(entropy)::value>
-            <<<row_blocks<S>(T), S::kThreads, S::kRows * entry_bytes(k, bits), stream>>>(
-                static_cast<const E*>(x), ldx, T, C, a, static_cast<E*>(dx), lddx);
+      auto entropy = [&](auto with) {
+        lp_backward_kernel<E, S, decltype(whole)::value, decltype(with)::value, decltype(cut)::value>
+            <<<blocks, S::kThreads, S::kRows * entry_bytes(k, bits), stream>>>(static_cast<const E*>(x), ldx, T, C, a,
+                                                                              static_cast<E*>(dx), lddx, split);
         return hipGetLastError() == hipSuccess ? LIPCACHE_OK : LIPCACHE_EHIP;
       };
-      return g_entropy ? run(std::true_type{}) : run(std::false_type{});
+      return g_entropy ? entropy(std::true_type{}) : entropy(std::false_type{});
+    };
+    if (shares.count > 1)
+      return run(RowShape<256, 4>{}, std::false_type{}, std::true_type{}, static_cast<unsigned>(T * shares.count));
+    return row_shaped_entries<E>(T, C, k, [&](auto shape, auto whole) {
+      return run(shape, whole, std::false_type{}, row_blocks<decltype(shape)>(T));
     });
   });
+}
+
+extern "C" size_t lipcache_logprobs_backward_workspace_bytes(int64_t T, int32_t C, int32_t k, int32_t dtype) {
+  return row_sizes_bad(T, C, k, dtype) ? 0 : row_share_bytes(T, k, row_shares(T, C, dtype));
 }

@@ -47,7 +47,7 @@ def test_distill(T, C, dtype):
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("k", [0, 1, 2, 63, 64, 65, 200, 1000])
-@pytest.mark.parametrize("C", [200, 3000])
+@pytest.mark.parametrize("C", [200, 3000, 70001])
 def test_entries(C, k, dtype):
     """Numbers of entries around a wave's and a workgroup's; every class of a small head; classes named twice."""
     x, g = _logits(9, C, dtype, C + k)
@@ -63,7 +63,7 @@ def test_entries(C, k, dtype):
     _check(x, teacher, index, None, None, 0.0, 1.5, 3.0, out)
 
 
-@pytest.mark.parametrize("C", [40, 600, 30000])
+@pytest.mark.parametrize("C", [40, 600, 30000, 70001])
 def test_edges(C):
     """Rows without entries, labels or weight; -inf and NaN on either side."""
     api = _api()

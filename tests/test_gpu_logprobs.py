@@ -68,7 +68,7 @@ def test_scores(T, C, dtype):
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("k", [0, 1, 2, 5, 20, 63, 64])
-@pytest.mark.parametrize("C", [33, 200, 3000, 40000])
+@pytest.mark.parametrize("C", [33, 200, 3000, 40000, 70001])
 def test_alternatives(C, k, dtype):
     x, g = _logits(12, C, dtype, C + k, masked=0.3)
     x[1] = -INF                      # nothing left
@@ -85,7 +85,7 @@ def test_alternatives(C, k, dtype):
     _check_scores(x, y, k, 1.0, _api().logprobs(x, y, top=k))
 
 
-@pytest.mark.parametrize("C", [12, 500, 9000])
+@pytest.mark.parametrize("C", [12, 500, 9000, 70001])
 def test_more_alternatives_than_classes(C):
     x = torch.full((3, C), -INF, device=DEV)
     x[1, 3] = 2.0
@@ -96,7 +96,7 @@ def test_more_alternatives_than_classes(C):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
-@pytest.mark.parametrize("C", [30, 700, 20000])
+@pytest.mark.parametrize("C", [30, 700, 20000, 70001])
 @pytest.mark.parametrize("t", [0.25, 1.0, 8.0])
 def test_lowest_and_largest_values(C, t, dtype):
     """Logits of the type's lowest value are logits like others; differences past float32 are p = 0."""
@@ -117,7 +117,7 @@ def test_lowest_and_largest_values(C, t, dtype):
     ref.near(out.lse, lse, r.lse_off()[:, 0])
 
 
-@pytest.mark.parametrize("C", [30, 700, 20000])
+@pytest.mark.parametrize("C", [30, 700, 20000, 70001])
 def test_not_finite(C):
     """NaN and +inf make their own row's numbers NaN, and nobody else's."""
     x, g = _logits(7, C, F32, C)
@@ -136,6 +136,20 @@ def test_not_finite(C):
             assert bool(got[t].isnan().all()), (name, t)
     assert out.logp[5] == 0 and out.lse[5].isnan() and out.top_index[5].tolist() == [-1] * 3
     assert int(out.top_index[3, 0]) == C - 1 and torch.equal(out.top_index[1], ref.top(x[1:2], 3)[0])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,C", [(64, 40000), (65, 40000), (3, 300000), (2000, 5000), (40, 5000)])
+def test_classes_allowed_in_a_run(T, C, dtype):
+    """What is allowed lies in one run somewhere, or rises to the end: the first part of a row tells nothing of its largest."""
+    x, g = _logits(T, C, dtype, T + C)
+    first = torch.randint(0, C - 700, (T, 1), generator=g, device=DEV)
+    j = torch.arange(C, device=DEV)
+    x = torch.where((j >= first) & (j < first + 600), x, torch.full_like(x, -INF))
+    x[::3] = torch.linspace(-9, 9, C, device=DEV).to(dtype)
+    y = _labels(T, C, g)
+    for k in (1, 8, 20, 64):
+        _check_scores(x, y, k, 1.0, _api().logprobs(x, y, top=k))
 
 
 def test_no_rows_and_parts_of_the_output():
@@ -203,7 +217,7 @@ def test_gradient_against_differences():
         assert bool(((slope - got[:, j]).abs() < 1e-5).all()), (j, slope, got[:, j])
 
 
-@pytest.mark.parametrize("C", [40, 600, 30000])
+@pytest.mark.parametrize("C", [40, 600, 30000, 70001])
 def test_rows_without_a_gradient(C):
     """Zero gradients give zero rows whatever they hold; so does a row that is masked throughout."""
     x, g = _logits(8, C, F32, C)

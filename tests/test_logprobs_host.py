@@ -17,7 +17,7 @@ NAN, INF = float("nan"), float("inf")
 def test_logprobs_validation():
     lib = L.load()
     base = dict(x=FAKE, ldx=64, T=10, C=64, dtype=L.BF16, t=1.0, label=FAKE, k=4, logp=FAKE, lse=FAKE, ent=FAKE, at=FAKE,
-                top=FAKE)
+                top=FAKE, ws=None, wsb=0)
 
     def call(**over):
         return lib.lipcache_logprobs(*dict(base, **over).values(), None)
@@ -34,7 +34,7 @@ def test_logprobs_validation():
 def test_logprobs_backward_validation():
     lib = L.load()
     base = dict(x=FAKE, ldx=64, T=10, C=64, dtype=L.F16, t=1.0, label=FAKE, gl=FAKE, gs=FAKE, ge=FAKE, k=4, at=FAKE, gt=FAKE,
-                dx=FAKE, ldd=64)
+                dx=FAKE, ldd=64, ws=None, wsb=0)
 
     def call(**over):
         return lib.lipcache_logprobs_backward(*dict(base, **over).values(), None)
@@ -50,7 +50,7 @@ def test_logprobs_backward_validation():
 def test_distill_validation():
     lib = L.load()
     base = dict(x=FAKE, ldx=64, T=10, C=64, dtype=L.F32, t=2.0, hard=0.5, soft=1.0, k=4, teacher=FAKE, index=FAKE, label=FAKE,
-                weight=FAKE, ce=FAKE, kl=FAKE, dx=FAKE, ldd=64)
+                weight=FAKE, ce=FAKE, kl=FAKE, dx=FAKE, ldd=64, ws=None, wsb=0)
 
     def call(**over):
         return lib.lipcache_distill(*dict(base, **over).values(), None)
@@ -60,6 +60,25 @@ def test_distill_validation():
         assert call(**bad) == L.EINVAL, bad
     assert call(k=1025) == L.EUNSUPPORTED and call(T=1 << 31) == L.EUNSUPPORTED
     assert call(T=0, x=None, dx=None, teacher=None, index=None) == L.OK
+
+
+def test_few_rows_of_many_classes_need_a_workspace():
+    lib = L.load()
+    C = 1 << 17
+    for name, k in (("logprobs", 4), ("logprobs_backward", 4), ("distill", 4)):
+        bytes_of = getattr(lib, f"lipcache_{name}_workspace_bytes")
+        assert bytes_of(3, C, k, L.BF16) > 0 and bytes_of(L.FEW_ROWS, C, k, L.BF16) > 0
+        assert bytes_of(L.FEW_ROWS + 1, C, k, L.BF16) == 0 and bytes_of(3, 1000, k, L.BF16) == 0 and bytes_of(0, C, k, L.BF16) == 0
+        assert bytes_of(-1, C, k, L.BF16) == 0 and bytes_of(3, 0, k, L.BF16) == 0 and bytes_of(3, C, k, 9) == 0
+
+    def calls(ws, size):
+        yield lib.lipcache_logprobs(FAKE, C, 3, C, L.BF16, 1.0, FAKE, 4, FAKE, FAKE, FAKE, FAKE, FAKE, ws, size, None)
+        yield lib.lipcache_logprobs_backward(FAKE, C, 3, C, L.BF16, 1.0, FAKE, FAKE, FAKE, FAKE, 4, FAKE, FAKE, FAKE, C, ws,
+                                             size, None)
+        yield lib.lipcache_distill(FAKE, C, 3, C, L.BF16, 2.0, 0.5, 1.0, 4, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, C, ws,
+                                   size, None)
+    for ws, size in ((None, 0), (FAKE, 64), (ctypes.c_void_p(0x100040), 1 << 20)):
+        assert list(calls(ws, size)) == [L.EWORKSPACE] * 3, (ws, size)
 
 
 def test_head_logprobs_validation():
