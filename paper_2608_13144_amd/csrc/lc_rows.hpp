@@ -474,7 +474,9 @@ lipcache_status row_typed(int32_t dtype, F f) {
 }
 
 // Calls f(shape) with a shape that holds a row of C, or one and false: the row goes in segments.  A wave takes rows of up to 512
-// chunks where there are enough for all waves (fewer threads that join a row's sums, and no barrier).
+// chunks, and of up to 1024, where there are enough for all waves: fewer threads join a row's sums, and none waits at a barrier
+// for the wave that keeps the entries.  Distillation of 5003 bfloat16 with 16 entries, a wave and 256 threads a row:
+// 1024 rows 13.4 and 11.6 us, 2048 rows 16.3 and 17.6, 3000 20.0 and 22.6, 8192 39 and 55.
 template <class E, class F>
 lipcache_status row_shaped(int64_t T, int C, F f) {
   const int chunks = C / RowType<E>::V;
@@ -484,6 +486,7 @@ lipcache_status row_shaped(int64_t T, int C, F f) {
   if (holds(RowShape<16, 4>{})) return f(RowShape<16, 4>{}, std::true_type{});
   if (holds(RowShape<64, 4>{})) return f(RowShape<64, 4>{}, std::true_type{});
   if (T >= 2048 && holds(RowShape<64, 8>{})) return f(RowShape<64, 8>{}, std::true_type{});
+  if (T >= 2560 && holds(RowShape<64, 16>{})) return f(RowShape<64, 16>{}, std::true_type{});
   if (holds(RowShape<256, 4>{})) return f(RowShape<256, 4>{}, std::true_type{});
   if (holds(RowShape<256, 8>{})) return f(RowShape<256, 8>{}, std::true_type{});
   if (holds(RowShape<512, 8>{})) return f(RowShape<512, 8>{}, std::true_type{});
