@@ -143,7 +143,7 @@ SIGNATURES = {
     "lipcache_distill_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
     "lipcache_head_logprobs": (_i32, [_vp, _i64, _i64, _vp, _i64, _vp, _i32, _i32, _i32, _f32, _vp, _vp, _vp, _vp, _vp,
                                       _sz, _vp]),
-    "lipcache_head_logprobs_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
+    "lipcache_head_logprobs_workspace_bytes": (_sz, [_vp, _i64, _i64, _vp, _i64, _i32, _i32, _i32]),
     "lipcache_status_string": (ctypes.c_char_p, [_i32]),
     "lipcache_abi_version": (_i32, []),
 }

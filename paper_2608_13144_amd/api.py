@@ -792,10 +792,10 @@ def head_logprobs(x: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None, l
     each = torch.empty((3, T), dtype=torch.float32, device=dev)
     scores = each.data_ptr()
     lib = L.load()
-    ws = workspace(lib.lipcache_head_logprobs_workspace_bytes(T, K, C, code), dev)
-    st = lib.lipcache_head_logprobs(x.data_ptr(), ldx, T, W.data_ptr(), ldw,
-                                    _of_rows(bias, "bias", torch.float32, dev, (C,)), K, C, code, float(temperature),
-                                    _of_rows(labels, "labels", torch.int32, dev, (T,)), scores, scores + 4 * T,
-                                    scores + 8 * T, ws.data_ptr(), ws.numel(), _stream_of(dev))
+    at_x, at_W = x.data_ptr(), W.data_ptr()
+    ws = workspace(lib.lipcache_head_logprobs_workspace_bytes(at_x, ldx, T, at_W, ldw, K, C, code), dev)
+    st = lib.lipcache_head_logprobs(at_x, ldx, T, at_W, ldw, _of_rows(bias, "bias", torch.float32, dev, (C,)), K, C, code,
+                                    float(temperature), _of_rows(labels, "labels", torch.int32, dev, (T,)), scores,
+                                    scores + 4 * T, scores + 8 * T, ws.data_ptr(), ws.numel(), _stream_of(dev))
     L.check("lipcache_head_logprobs", st)
     return LogProbs(*each.unbind(0), None, None)

@@ -236,13 +236,13 @@ struct RowData {
   // The sums of nothing but the thread's single element.
   template <RowWants W>
   __device__ __forceinline__ RowSums begin(const RowScale& k) const {
-    RowSums r{tail, 0.0f, 0.0f};
-    one<W>(tail, row_from(tail), r, k);
+    RowSums r{fmaxf(tail, -kRowInf), 0.0f, 0.0f};  // (a NaN is no largest value; it goes into the sums)
+    one<W>(tail, row_from(r.m), r, k);
     return r;
   }
-  // The largest of the chunks and the single element.
+  // The largest of the chunks and the single element (a NaN is none).
   __device__ __forceinline__ float largest(int first, int full, int g) {
-    float m = tail;
+    float m = fmaxf(tail, -kRowInf);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       if (past(i, first, full, g)) break;
@@ -415,6 +415,7 @@ struct RowEntries {
   }
   // Which classes may be named twice.
   __device__ __forceinline__ void index(int lane) {
+    if (n == 0) return;  // no room either
     for (int i = lane; i < bits / 16; i += LANES) seen[i] = 0;
     wave_sync();
     for (int i = lane; i < n; i += LANES) {

@@ -138,6 +138,24 @@ def test_not_finite(C):
     assert int(out.top_index[3, 0]) == C - 1 and torch.equal(out.top_index[1], ref.top(x[1:2], 3)[0])
 
 
+@pytest.mark.parametrize("C", [60, 300, 1500, 3001, 20000, 70001])
+@pytest.mark.parametrize("k", [3, 20, 64])
+def test_alternatives_among_nan(C, k):
+    """A NaN is no alternative and hides none, however many there are and wherever."""
+    x, g = _logits(8, C, F32, C + k)
+    x[1, : C // 2] = math.nan
+    x[2, C // 2:] = math.nan
+    x[3, ::2] = math.nan
+    x[4, -1] = math.nan
+    x[5, : C - 2] = math.nan
+    x[6] = math.nan
+    x[7, C - C % 8:] = math.nan
+    out = _api().logprobs(x, top=k)
+    at = ref.top(x, k)
+    assert torch.equal(out.top_index, at)
+    assert bool((out.top_logp.isnan() == ((at >= 0) & x.isnan().any(1, keepdim=True))).all())
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("T,C", [(64, 40000), (65, 40000), (3, 300000), (2000, 5000), (40, 5000)])
 def test_classes_allowed_in_a_run(T, C, dtype):

@@ -96,9 +96,15 @@ def test_head_logprobs_validation():
     assert call(K=(1 << 20) + 1, ldx=1 << 21, ldw=1 << 21) == L.EUNSUPPORTED
     assert call(C=(1 << 20) + 1) == L.EUNSUPPORTED
     assert call(ws=None) == L.EWORKSPACE and call(ws=ctypes.c_void_p(0x100040)) == L.EWORKSPACE
-    need = lib.lipcache_head_logprobs_workspace_bytes(10, 64, 48, L.BF16)
+    bytes_of = lib.lipcache_head_logprobs_workspace_bytes
+    need = bytes_of(FAKE, 64, 10, FAKE, 64, 64, 48, L.BF16)
     assert need > 0 and call(wsb=need - 1) == L.EWORKSPACE
-    assert lib.lipcache_head_logprobs_workspace_bytes(10, 0, 48, L.BF16) == 0
+    assert bytes_of(FAKE, 64, 10, FAKE, 64, 0, 48, L.BF16) == 0
+    # room for a copy of each matrix whose rows are not whole vectors, and for no other
+    copies = [bytes_of(FAKE, 64, 10, FAKE, 68, 64, 48, L.BF16), bytes_of(ctypes.c_void_p(0x100002), 64, 10, FAKE, 64, 64, 48, L.BF16),
+              bytes_of(FAKE, 64, 10, FAKE, 64, 62, 48, L.BF16)]
+    assert copies[0] >= need + 48 * 64 * 2 and copies[1] >= need + 10 * 64 * 2 and copies[2] >= need + 58 * 64 * 2
+    assert call(ldw=68, wsb=copies[0] - 1) == L.EWORKSPACE
     assert call(T=0, x=None) == L.OK
 
 
