@@ -155,11 +155,11 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
       continue;
     }
     E* dx = grad + (t < T ? t : T - 1) * ldd;
-    auto dx_of = [&](float v) { return any ? smooth(v) : 0.0f; };
+    const bool live = t < T;
     if (kWhole) {
 #pragma unroll
       for (int i = 0; i < S::N; ++i) {
-        if (t < T) data.store_chunk(i, dx, 0, full, at.g, dx_of);
+        data.store_chunk(i, dx, 0, full, at.g, live, any, smooth);
         data.load_chunk(i, following, 0, full, at.g);
       }
     } else {
@@ -168,14 +168,14 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
         for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, end, at.g);
 #pragma unroll
         for (int i = 0; i < S::N; ++i)
-          if (t < T) data.store_chunk(i, dx, first, end, at.g, dx_of);
+          data.store_chunk(i, dx, first, end, at.g, live, any, smooth);
       }
       if constexpr (!kSplit) {
 #pragma unroll
         for (int i = 0; i < S::N; ++i) data.load_chunk(i, following, 0, full, at.g);
       }
     }
-    if (t < T && last) data.store_tail(dx, C, at.g, dx_of);
+    data.store_tail(dx, C, at.g, live && last, any, smooth);
     if constexpr (!kSplit) data.load_tail(following, C, at.g);
     RowPlace<S>::sync();  // the row is written before its entries are
     if (keeps && any && t < T) {

@@ -187,9 +187,22 @@ struct RowData {
   static __device__ __forceinline__ const char* chunk_at(const E* x, int first, int i, int g) {
     return reinterpret_cast<const char*>(x) + static_cast<int64_t>(first + G * i) * 16 + static_cast<uint32_t>(g * 16);
   }
+  // The first chunk i of the wave's lanes (of the row's, where a wave holds several).
+  static __device__ __forceinline__ int chunk_of(int i, int first, int g) {
+    return first + G * i + (G > 64 ? uniform(g) / kWave * kWave : 0);
+  }
+  // Whether chunk i is past the row for all of them, in it for all of them.
+  static __device__ __forceinline__ bool past(int i, int first, int full, int g) { return chunk_of(i, first, g) >= full; }
+  static __device__ __forceinline__ bool inside(int i, int first, int full, int g) {
+    return chunk_of(i, first, g) + (G < 64 ? G : 64) <= full;
+  }
   __device__ __forceinline__ void load_chunk(int i, const E* x, int first, int full, int g) {
-    raw[i] = fill();
-    if (g < full - (first + G * i)) raw[i] = *reinterpret_cast<const typename Type::vec*>(chunk_at(x, first, i, g));
+    if (inside(i, first, full, g)) {
+      raw[i] = *reinterpret_cast<const typename Type::vec*>(chunk_at(x, first, i, g));
+    } else {
+      raw[i] = fill();
+      if (g < full - (first + G * i)) raw[i] = *reinterpret_cast<const typename Type::vec*>(chunk_at(x, first, i, g));
+    }
   }
   __device__ __forceinline__ void load_tail(const E* x, int C, int g) {
     const int full = C / V, j = full * V + g;
@@ -199,10 +212,6 @@ struct RowData {
     load_tail(x, C, g);
 #pragma unroll
     for (int i = 0; i < N; ++i) load_chunk(i, x, first, C / V, g);
-  }
-  // Whether chunk i is past the row for every lane of the wave (of the row, where a wave holds several).
-  static __device__ __forceinline__ bool past(int i, int first, int full, int g) {
-    return first + G * i + (G > 64 ? uniform(g) / kWave * kWave : 0) >= full;
   }
   // f(value, index) for every element of the thread's chunks, rising index.
   template <class F>
@@ -216,23 +225,26 @@ struct RowData {
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  // Writes f of every element of chunk i to the row at out, where it has the chunk.
+  // Writes f of every element of chunk i (zeros unless `some`) to the row at out, where it has the chunk and is `live`.
   template <class F>
-  __device__ __forceinline__ void store_chunk(int i, E* out, int first, int full, int g, F f) {
-    if (g >= full - (first + G * i)) return;
+  __device__ __forceinline__ void store_chunk(int i, E* out, int first, int full, int g, bool live, bool some, F f) {
+    if (past(i, first, full, g)) return;
     pin(i);
     float v[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = f(Type::get(raw[i], e));
-    *reinterpret_cast<typename Type::vec*>(const_cast<char*>(chunk_at(out, first, i, g))) = Type::pack(v);
+    u32x4 bits = Type::pack(v);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) bits[w] = some ? bits[w] : 0;
+    if (live && g < full - (first + G * i))
+      *reinterpret_cast<typename Type::vec*>(const_cast<char*>(chunk_at(out, first, i, g))) = bits;
     __builtin_amdgcn_sched_barrier(0);
   }
   template <class F>
-  __device__ __forceinline__ void store_tail(E* out, int C, int g, F f) const {
+  __device__ __forceinline__ void store_tail(E* out, int C, int g, bool live, bool some, F f) const {
     const int j = C / V * V + g;
-    if (g < V && j < C) out[j] = static_cast<E>(f(tail));
+    if (live && g < V && j < C) out[j] = static_cast<E>(some ? f(tail) : 0.0f);
   }
-
   // The sums of nothing but the thread's single element.
   template <RowWants W>
   __device__ __forceinline__ RowSums begin(const RowScale& k) const {

@@ -121,7 +121,7 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
       if constexpr (kEntropy) return row_exp2(e) * fmaf(steep, fmaxf(e, kRowLeast), flat);
       else return row_exp2(e) * flat;
     };
-    auto dx_of = [&](float v) { return some ? smooth(v) : 0.0f; };
+    const bool live = t < T;
     const E* following = row_of(t + step);
     const RowEntry now = label;
     const float now_logit = label_logit;
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
     if (kWhole) {
 #pragma unroll
       for (int i = 0; i < S::N; ++i) {
-        if (t < T) data.store_chunk(i, dx, 0, full, at.g, dx_of);
+        data.store_chunk(i, dx, 0, full, at.g, live, some, smooth);
         data.load_chunk(i, following, 0, full, at.g);
       }
     } else {
@@ -143,14 +143,14 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
         for (int i = 0; i < S::N; ++i) data.load_chunk(i, x, first, end, at.g);
 #pragma unroll
         for (int i = 0; i < S::N; ++i)
-          if (t < T) data.store_chunk(i, dx, first, end, at.g, dx_of);
+          data.store_chunk(i, dx, first, end, at.g, live, some, smooth);
       }
       if constexpr (!kSplit) {
 #pragma unroll
         for (int i = 0; i < S::N; ++i) data.load_chunk(i, following, 0, full, at.g);
       }
     }
-    if (t < T && last) data.store_tail(dx, C, at.g, dx_of);
+    data.store_tail(dx, C, at.g, live && last, some, smooth);
     if constexpr (!kSplit) data.load_tail(following, C, at.g);
     RowPlace<S>::sync();  // the row is written before its entries are
     if (keeps && some && t < T) {
