@@ -155,13 +155,13 @@ __global__ __launch_bounds__(S::kThreads, 2) void hl_tile_kernel(const typename 
   }
 }
 
-// WAVES of a workgroup join a row's parts; a workgroup has 4.
+// WAVES waves join a row's parts: four rows a workgroup, or one.
 template <int WAVES>
-__global__ __launch_bounds__(256) void hl_join_kernel(int T, int C, int parts, const float4* __restrict__ part,
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void hl_join_kernel(int T, int C, int parts, const float4* __restrict__ part,
                                                       const float* __restrict__ at, HlOut out) {
-  __shared__ HlPart room[4];
+  __shared__ HlPart room[WAVES];
   const int wave = static_cast<int>(threadIdx.x) / kWave, lane = lane_id();
-  const int t = static_cast<int>(blockIdx.x) * (4 / WAVES) + (WAVES == 1 ? wave : 0);
+  const int t = WAVES == 1 ? static_cast<int>(blockIdx.x) * 4 + wave : static_cast<int>(blockIdx.x);
   HlPart sum{-kHlInf, 0.0f, 0.0f};
   if (t < T) {
 #pragma unroll 4
@@ -329,9 +329,10 @@ lipcache_status hl_run(const E* x, int64_t ldx, int64_t T, const E* W, int64_t l
       st = run(TileShape<E, 128, 128, 2, 2, 1, 2, 1, false, false>{});
     }
     if (st != LIPCACHE_OK) return st;
-    // a wave a row, or four where a row has many parts
+    // a wave a row, or more where a row has many parts (4096 of one row: 10 us by four waves)
     if (parts <= 256) hl_join_kernel<1><<<static_cast<unsigned>(hl_ceil(n, 4)), 256, 0, s>>>(n, C, parts, ws.part, ws.at, o);
-    else hl_join_kernel<4><<<static_cast<unsigned>(n), 256, 0, s>>>(n, C, parts, ws.part, ws.at, o);
+    else if (parts <= 1024) hl_join_kernel<4><<<static_cast<unsigned>(n), 256, 0, s>>>(n, C, parts, ws.part, ws.at, o);
+    else hl_join_kernel<16><<<static_cast<unsigned>(n), 1024, 0, s>>>(n, C, parts, ws.part, ws.at, o);
     LC_LAUNCHED();
   }
   return LIPCACHE_OK;

@@ -29,6 +29,13 @@ __device__ __forceinline__ float row_exp2(float v) { return __builtin_amdgcn_exp
 __device__ __forceinline__ float row_log2(float v) { return __builtin_amdgcn_logf(v); }
 
 // ------------------------------------------------------------ element types
+// Eight numbers rounded to nearest even, as vectors: the conversion takes two at a time.
+template <class H>
+__device__ __forceinline__ u32x4 row_pack(const float* v) {
+  typedef float f32x8 __attribute__((ext_vector_type(8)));
+  return __builtin_bit_cast(u32x4, __builtin_convertvector(f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}, H));
+}
+
 template <class E>
 struct RowType;
 template <>
@@ -54,7 +61,7 @@ struct RowType<__bf16> {
   static __device__ __forceinline__ float part(uint32_t word, int e) {
     return __builtin_bit_cast(float, (e & 1 ? word >> 16 : word) << 16);
   }
-  static __device__ __forceinline__ u32x4 pack(const float* v) { return pack_bf16x8(v); }
+  static __device__ __forceinline__ u32x4 pack(const float* v) { return row_pack<bf16x8>(v); }
 };
 template <>
 struct RowType<_Float16> {
@@ -67,12 +74,7 @@ struct RowType<_Float16> {
   static __device__ __forceinline__ float part(uint32_t word, int e) {
     return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(e & 1 ? word >> 16 : word)));
   }
-  static __device__ __forceinline__ u32x4 pack(const float* v) {
-    f16x8 h;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = static_cast<_Float16>(v[e]);
-    return __builtin_bit_cast(u32x4, h);
-  }
+  static __device__ __forceinline__ u32x4 pack(const float* v) { return row_pack<f16x8>(v); }
 };
 
 // ------------------------------------------------------ lanes of one wave
@@ -177,6 +179,8 @@ struct RowData {
   static constexpr int V = Type::V, N = S::N, G = S::G;
   u32x4 raw[N];
   float tail;
+  const int wave;  // the first thread of the row in this wave
+  __device__ __forceinline__ explicit RowData(int g) : wave(G > 64 ? uniform(g) / kWave * kWave : 0) {}
 
   // Chunk i as bits again: without it the compiler keeps the numbers that one pass made of them for the next, in two
   // to four times the registers.
@@ -188,16 +192,14 @@ struct RowData {
     return reinterpret_cast<const char*>(x) + static_cast<int64_t>(first + G * i) * 16 + static_cast<uint32_t>(g * 16);
   }
   // The first chunk i of the wave's lanes (of the row's, where a wave holds several).
-  static __device__ __forceinline__ int chunk_of(int i, int first, int g) {
-    return first + G * i + (G > 64 ? uniform(g) / kWave * kWave : 0);
-  }
+  __device__ __forceinline__ int chunk_of(int i, int first) const { return first + G * i + wave; }
   // Whether chunk i is past the row for all of them, in it for all of them.
-  static __device__ __forceinline__ bool past(int i, int first, int full, int g) { return chunk_of(i, first, g) >= full; }
-  static __device__ __forceinline__ bool inside(int i, int first, int full, int g) {
-    return chunk_of(i, first, g) + (G < 64 ? G : 64) <= full;
+  __device__ __forceinline__ bool past(int i, int first, int full) const { return chunk_of(i, first) >= full; }
+  __device__ __forceinline__ bool inside(int i, int first, int full) const {
+    return chunk_of(i, first) + (G < 64 ? G : 64) <= full;
   }
   __device__ __forceinline__ void load_chunk(int i, const E* x, int first, int full, int g) {
-    if (inside(i, first, full, g)) {
+    if (inside(i, first, full)) {
       raw[i] = *reinterpret_cast<const typename Type::vec*>(chunk_at(x, first, i, g));
     } else {
       raw[i] = fill();
@@ -218,7 +220,7 @@ struct RowData {
   __device__ __forceinline__ void each(int first, int full, int g, F f) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (past(i, first, full, g)) break;
+      if (past(i, first, full)) break;
       pin(i);
 #pragma unroll
       for (int e = 0; e < V; ++e) f(Type::get(raw[i], e), (first + G * i + g) * V + e);
@@ -228,7 +230,7 @@ struct RowData {
   // Writes f of every element of chunk i (zeros unless `some`) to the row at out, where it has the chunk and is `live`.
   template <class F>
   __device__ __forceinline__ void store_chunk(int i, E* out, int first, int full, int g, bool live, bool some, F f) {
-    if (past(i, first, full, g)) return;
+    if (past(i, first, full)) return;
     pin(i);
     float v[V];
 #pragma unroll
@@ -257,7 +259,7 @@ struct RowData {
     float m = fmaxf(tail, -kRowInf);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (past(i, first, full, g)) break;
+      if (past(i, first, full)) break;
       pin(i);
 #pragma unroll
       for (int e = 0; e < V; ++e) m = fmaxf(m, Type::get(raw[i], e));
@@ -274,7 +276,7 @@ struct RowData {
     constexpr int B = N == 1 || (N > 8 && V == 8) ? 1 : 2;  // chunks of a block
 #pragma unroll
     for (int b = 0; b < N; b += B) {
-      if (past(b, first, full, g)) {
+      if (past(b, first, full)) {
 #pragma unroll
         for (int i = b; i < b + B; ++i) used(i);
         continue;

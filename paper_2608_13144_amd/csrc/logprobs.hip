@@ -192,7 +192,7 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
   auto label_of = [&](int64_t t) { return a.label && t < T ? a.label[t] : -1; };
   auto checked = [&](int y) { return y < C ? y : -1; };
   auto logit_of = [&](int64_t t, int y) { return y >= 0 ? static_cast<float>(row_of(t)[y]) : 0.0f; };
-  Data data;
+  Data data(at.g);
   int64_t t = kShare ? static_cast<int>(blockIdx.x) / shares.count : static_cast<int64_t>(blockIdx.x) * S::kRows + at.row;
   int y = kShare ? -1 : checked(label_of(t));
   float logit = logit_of(t, y);

@@ -63,7 +63,7 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
     if constexpr (kSplit) return t < T && i <= a.k ? split.logits[t * (a.k + 1) + i] : 0.0f;
     else return c >= 0 ? static_cast<float>(row_of(t)[c]) : 0.0f;
   };
-  Data data;
+  Data data(at.g);
   int64_t t = kSplit ? static_cast<int>(blockIdx.x) / split.shares.count : static_cast<int64_t>(blockIdx.x) * S::kRows + at.row;
   RowEntry mine{-1, 0.0f}, label{-1, 0.0f};
   float logit = 0.0f, label_logit = 0.0f;

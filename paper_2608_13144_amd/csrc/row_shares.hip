@@ -21,7 +21,7 @@ __global__ __launch_bounds__(256) void row_share_kernel(const E* __restrict__ lo
       const int c = i < k ? index[static_cast<int64_t>(t) * k + i] : label ? label[t] : -1;
       named[static_cast<int64_t>(t) * (k + 1) + i] = c >= 0 && c < C ? static_cast<float>(x[c]) : 0.0f;
     }
-  Data data;
+  Data data(at.g);
   data.tail = -kRowInf;
   if (share == shares.count - 1) data.load_tail(x, C, at.g);
 #pragma unroll
