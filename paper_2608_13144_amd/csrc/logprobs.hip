@@ -348,11 +348,13 @@ __global__ __launch_bounds__(256) void lp_score_join_kernel(const E* __restrict_
   if (a.k == 0) return;
   const uint64_t* mine = keys + t * shares.count * a.k;
   const int m = (a.k + shares.count - 1) / shares.count;
-  uint64_t least = ~0ull;
-  for (int i = 0; i < shares.count; ++i) {
-    const uint64_t key = mine[i * a.k + m - 1];
-    least = key < least ? key : least;
+  uint64_t least = lane_id() < shares.count ? mine[lane_id() * a.k + m - 1] : ~0ull;  // each wave for itself
+#pragma unroll
+  for (int o = 1; o < kRowShares; o <<= 1) {
+    const uint64_t other = __shfl_xor(static_cast<unsigned long long>(least), o, kWave);
+    least = other < least ? other : least;
   }
+  least = __shfl(static_cast<unsigned long long>(least), 0, kWave);
   for (int i = at.g; i < shares.count * a.k; i += S::G) {
     const uint64_t key = mine[i];
     if (key >= least && key != 0) list[atomicAdd(&count, 1)] = key;
