@@ -189,6 +189,39 @@ def test_a_training_step_of_the_sites():
     assert torch.isfinite(A).all() and not torch.equal(A, before)
 
 
+def test_few_rows_captured_and_replayed():
+    """Rows that go in shares, two graphs of them replayed in turn: each has its own workspace."""
+    api = _api()
+    T, C, k = 3, 70001, 8
+    graphs = []
+    for seed in (1, 2):
+        x, g = _logits(T, C, BF16, seed)
+        teacher, index = _teacher(x, k, g)
+        y = _labels(T, C, g)
+
+        def work(x=x, y=y, teacher=teacher, index=index):
+            return api.logprobs(x, y, top=k), api.distill(x, teacher, index, y, hard=0.5, soft=1.0, temperature=2.0)
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            work()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            found = work()
+        graphs.append((graph, found, x, work))
+    for turn in range(3):
+        for i, (graph, found, x, work) in enumerate(graphs):
+            x.copy_(_logits(T, C, BF16, 10 * turn + i)[0])
+        for graph, _, _, _ in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for _, (s, loss), _, work in graphs:
+            es, eloss = work()
+            for got, want in ((s.logp, es.logp), (s.entropy, es.entropy), (s.top_index, es.top_index), (s.top_logp, es.top_logp),
+                              (loss.ce, eloss.ce), (loss.kl, eloss.kl), (loss.grad, eloss.grad)):
+                assert torch.equal(got, want), turn
+
+
 def test_captured_and_replayed():
     """One graph of scores, gradient and distillation, replayed on new inputs with eager work between."""
     api = _api()

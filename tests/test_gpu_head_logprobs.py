@@ -54,6 +54,19 @@ def test_large_tiles(dtype):
     _check(x, W, bias, y, 1.0, _api().head_logprobs(x, W, bias, y))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("C", [1, 31, 33, 64, 90, 128, 130, 170, 200, 225, 256, 257])
+@pytest.mark.parametrize("T,K", [(8200, 72), (24700, 33), (25000, 200)])
+def test_whole_heads(T, K, C, dtype):
+    """Heads of up to 256 classes and many rows, which one tile finishes (and one class more, which none does)."""
+    x, W, bias, y = _case(T, K, C, dtype, T + C)
+    out = _api().head_logprobs(x, W, bias, y, temperature=1.2)
+    _check(x, W, bias, y, 1.2, out)
+    if C > 40:
+        bias[3::4] = -INF
+        _check(x, W, bias, y, 1.0, _api().head_logprobs(x, W, bias, y))
+
+
 def test_rows_in_passes():
     """So many classes that the parts of all rows pass 256 MiB: 1024 rows at a time."""
     T, K, C = 1300, 32, 1 << 20

@@ -54,7 +54,9 @@ def _check_scores(x, y, k, t, out):
 
 
 SHAPES = [(1, 1), (5, 2), (4, 7), (300, 10), (9, 64), (70, 200), (5, 257), (6, 1000), (130, 1024), (3, 1031), (4, 4099),
-          (3, 5003), (2, 16384), (2, 32767), (3, 50021), (2, 65536), (1, 131072), (2, 131075), (1, 262147), (1, 1 << 20)]
+          (3, 5003), (2, 16384), (2, 32767), (3, 50021), (2, 65536), (1, 131072), (2, 131075), (1, 262147), (1, 1 << 20),
+          # more rows, which other numbers of threads take
+          (2100, 1300), (2601, 2500), (2600, 5003), (801, 9001), (800, 20000), (101, 20000), (65, 60000), (66, 131072), (65, 200001)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
@@ -284,6 +286,27 @@ def test_gradient_in_place_and_beside(C, dtype):
     mine = x.clone()
     assert api.logprobs_backward(mine, y, out=mine, **grads) is mine
     assert torch.equal(mine, want)
+
+
+def test_offsets_past_32_bits():
+    """More than 2^32 logits: the last rows come out as they do alone."""
+    T, C = 33000, 131072
+    x = torch.empty(T, C, dtype=BF16, device=DEV)
+    for part in x.split(4096):
+        part.copy_(torch.randn(C, device=DEV).roll(len(part))[None, :] * 3)
+    part = _logits(6, C, BF16, 1)[0]
+    rows = torch.tensor([0, 1, 16384, 32767, T - 2, T - 1], device=DEV)
+    x[rows] = part
+    y = torch.arange(T, dtype=torch.int32, device=DEV)
+    g = torch.randn(T, device=DEV)
+    api = _api()
+    out, alone = api.logprobs(x, y, top=3), api.logprobs(torch.cat([part] * 12), y[rows].repeat(12), top=3)  # not in shares
+    for name in ("logp", "lse", "entropy"):
+        assert torch.allclose(getattr(out, name)[rows], getattr(alone, name)[:6], rtol=1e-5, atol=1e-5), name
+    assert torch.equal(out.top_index[rows], alone.top_index[:6])
+    dx = api.logprobs_backward(x, y, g_logp=g, out=x)
+    want = api.logprobs_backward(torch.cat([part] * 12), y[rows].repeat(12), g_logp=g[rows].repeat(12))
+    assert dx is x and torch.equal(dx[rows], want[:6])
 
 
 def test_another_stream_and_twice():
