@@ -23,15 +23,45 @@ constexpr float kHlLeast = -1000.0f;  // exponents below add nothing: 2^-1000 is
 
 inline int64_t hl_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Rows of 16-byte vectors, zeros past the width: what the tiles are copied from where a matrix's own rows are not aligned.
+// Matrices whose own rows are not whole 16-byte vectors, as rows that are, zeros past the width: what the tiles are copied
+// from.  Both operands in one launch (z); a lane takes a vector of a row, read from any element's address.  Bound by
+// memory: 128192 x 294 float32 in 77 us (3.9 TB/s).
+struct HlCopy {
+  const void* from;
+  void* to;
+  int64_t ld, rows;  // of the source; 0 rows: nothing to do
+};
+struct HlCopies {
+  HlCopy of[2];
+};
 template <class E>
-__global__ __launch_bounds__(256) void hl_copy_kernel(const E* __restrict__ from, int64_t ld, int64_t rows, int width,
-                                                      E* __restrict__ to, int64_t to_ld) {
-  const int64_t size = rows * to_ld, step = static_cast<int64_t>(gridDim.x) * 256;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < size; i += step) {
-    const int64_t row = i / to_ld;
-    const int col = static_cast<int>(i - row * to_ld);
-    to[i] = col < width ? from[row * ld + col] : static_cast<E>(0.0f);
+__global__ __launch_bounds__(256) void hl_copy_kernel(HlCopies copies, int width) {
+  constexpr int V = 16 / static_cast<int>(sizeof(E));
+  typedef u32x4 __attribute__((aligned(2))) vec;
+  const HlCopy c = copies.of[blockIdx.z];
+  const int vectors = (width + V - 1) / V, at = static_cast<int>(blockIdx.x) * 64 + (static_cast<int>(threadIdx.x) & 63);
+  if (at >= vectors) return;
+  const int left = width - at * V;
+  const int64_t step = static_cast<int64_t>(gridDim.y) * 4;
+  const E* from = static_cast<const E*>(c.from) + at * V;
+  E* to = static_cast<E*>(c.to) + at * V;
+  const int64_t to_ld = static_cast<int64_t>(vectors) * V;
+  int64_t row = static_cast<int64_t>(blockIdx.y) * 4 + (threadIdx.x >> 6);
+  if (left >= V) {
+    // four rows' loads under way at a time
+    for (; row + 3 * step < c.rows; row += 4 * step) {
+      u32x4 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const vec*>(from + (row + i * step) * c.ld);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(to + (row + i * step) * to_ld) = v[i];
+    }
+    for (; row < c.rows; row += step)
+      *reinterpret_cast<u32x4*>(to + row * to_ld) = *reinterpret_cast<const vec*>(from + row * c.ld);
+  } else {
+    for (; row < c.rows; row += step)
+#pragma unroll
+      for (int e = 0; e < V; ++e) to[row * to_ld + e] = e < left ? from[row * c.ld + e] : static_cast<E>(0.0f);
   }
 }
 
@@ -69,8 +99,11 @@ struct HlOut {
 };
 
 // kAll: the tile holds all classes and each wave those of its rows, which it finishes itself.
+// Registers for two waves a SIMD, or for as many as the ring leaves.
+template <class S>
+inline constexpr int kHlWaves = S::kThreads > 256 || 2 * S::kLds <= 160 * 1024 ? 2 : 1;
 template <class S, bool kAll>
-__global__ __launch_bounds__(S::kThreads, 2) void hl_tile_kernel(const typename S::E* __restrict__ W, int64_t ldw, int C,
+__global__ __launch_bounds__(S::kThreads, kHlWaves<S>) void hl_tile_kernel(const typename S::E* __restrict__ W, int64_t ldw, int C,
                                                               const typename S::E* __restrict__ x, int64_t ldx, int T,
                                                               int K, const float* __restrict__ bias, HlOut out, int parts,
                                                               float4* __restrict__ part, float* __restrict__ at) {
@@ -230,15 +263,26 @@ struct HlBuffers {
   }
 };
 
-// The matrix, or its copy in `room`.
+// The operands, or their copies in the workspace.
 template <class E>
-lipcache_status hl_vectors(const E*& p, int64_t& ld, int64_t rows, int K, E* room, hipStream_t s) {
-  if (hl_aligned<E>(p, ld, K)) return LIPCACHE_OK;
-  const int64_t to = hl_ceil(K, kHlVector<E>) * kHlVector<E>, blocks = hl_ceil(rows * to, 1024);
-  hl_copy_kernel<E><<<static_cast<unsigned>(blocks < 8192 ? blocks : 8192), 256, 0, s>>>(p, ld, rows, K, room, to);
+lipcache_status hl_vectors(const E*& x, int64_t& ldx, int64_t T, const E*& W, int64_t& ldw, int64_t C, int K,
+                           const HlBuffers<E>& ws, hipStream_t s) {
+  if (!ws.x && !ws.W) return LIPCACHE_OK;
+  const int64_t to = hl_ceil(K, kHlVector<E>) * kHlVector<E>, across = hl_ceil(to / kHlVector<E>, 64);
+  // about 4096 workgroups an operand
+  const int64_t most = hl_ceil(T > C ? T : C, 4), some = 4096 / across < 64 ? 64 : 4096 / across;
+  const HlCopies copies{{{x, ws.x, ldx, ws.x ? T : 0}, {W, ws.W, ldw, ws.W ? C : 0}}};
+  const dim3 grid(static_cast<unsigned>(across), static_cast<unsigned>(most < some ? most : some), 2);
+  hl_copy_kernel<E><<<grid, 256, 0, s>>>(copies, K);
   LC_LAUNCHED();
-  p = room;
-  ld = to;
+  if (ws.x) {
+    x = ws.x;
+    ldx = to;
+  }
+  if (ws.W) {
+    W = ws.W;
+    ldw = to;
+  }
   return LIPCACHE_OK;
 }
 
@@ -288,8 +332,7 @@ lipcache_status hl_run(const E* x, int64_t ldx, int64_t T, const E* W, int64_t l
   HlSpace space{static_cast<char*>(ws_)};
   const HlBuffers<E> ws(space, x, ldx, T, W, ldw, K, C);
   lipcache_status st;
-  if ((st = hl_vectors(x, ldx, T, K, ws.x, s)) != LIPCACHE_OK) return st;
-  if ((st = hl_vectors(W, ldw, C, K, ws.W, s)) != LIPCACHE_OK) return st;
+  if ((st = hl_vectors(x, ldx, T, W, ldw, C, K, ws, s)) != LIPCACHE_OK) return st;
   const int64_t pass = hl_rows(T, C);
   for (int64_t t = 0; t < T; t += pass) {
     const int n = static_cast<int>(T - t < pass ? T - t : pass);
@@ -316,8 +359,10 @@ lipcache_status hl_run(const E* x, int64_t ldx, int64_t T, const E* W, int64_t l
       // bound by reading W: tiles of 32 classes until they fill the CUs
       st = hl_ceil(C, 128) >= 256 ? run(TileShape<E, 128, 32, 4, 1, 1, 4, 1, false, false>{})
                                   : run(TileShape<E, 32, 32, 1, 1, 4, 4, 1, false, false>{});
-    } else if (n <= 64 && hl_ceil(C, 128) >= 256) {
-      // 64 rows of 4096 -> 131072 bfloat16: 240 us with tiles of 128 rows
+    } else if (hl_ceil(C, 128) >= 256 && (n <= 64 || (sizeof(E) == 4 && n < 512 && hl_ceil(n, 64) % 2 == 1))) {
+      // 64 rows of 4096 -> 131072 bfloat16: 240 us with tiles of 128 rows.  float32, bound by its products, takes 64 rows
+      // also where 128 would leave half of the last tile empty: 300 rows of 1024 -> 65536 356 us (403), 171 of 296 ->
+      // 128192 168 (201); bfloat16 loses by it (300 rows: 83 us, 75 with 128).
       st = run(TileShape<E, 128, 64, 4, 1, 1, 3, 1, false, false>{});
     } else if (t128 < 128) {
       st = run(TileShape<E, 64, 64, 2, 2, 1, 3, 1, false, false>{});

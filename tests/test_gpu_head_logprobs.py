@@ -41,7 +41,7 @@ def _check(x, W, bias, y, t, out):
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("T,K,C", [(1, 1, 1), (1, 64, 10), (3, 33, 7), (1, 4096, 4099), (32, 64, 257), (33, 250, 130), (64, 256, 200),
                                    (129, 100, 1000), (257, 72, 513), (300, 264, 5003), (1000, 40, 3001), (40, 512, 40000),
-                                   (2049, 64, 128), (520, 1024, 9000)])
+                                   (2049, 64, 128), (520, 1024, 9000), (171, 60, 33000), (3, 1359, 16600), (300, 33, 32800)])
 def test_head(T, K, C, dtype):
     x, W, bias, y = _case(T, K, C, dtype, T + K + C, strided=(T + K + C) % 3 == 0)
     _check(x, W, bias, y, 1.0, _api().head_logprobs(x, W, bias, y))
