@@ -254,18 +254,20 @@ struct RowData {
     one<W>(tail, row_from(r.m), r, k);
     return r;
   }
-  // The largest of the chunks and the single element (a NaN is none).
-  __device__ __forceinline__ float largest(int first, int full, int g) {
-    float m = fmaxf(tail, -kRowInf);
+  // The largest of the chunks' elements in P groups by their place in a chunk, and of the single element, which is of the
+  // first (a NaN is none).
+  template <int P>
+  __device__ __forceinline__ void largest(int first, int full, int g, float (&m)[P]) {
+#pragma unroll
+    for (int p = 0; p < P; ++p) m[p] = p == 0 ? fmaxf(tail, -kRowInf) : -kRowInf;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       if (past(i, first, full)) break;
       pin(i);
 #pragma unroll
-      for (int e = 0; e < V; ++e) m = fmaxf(m, Type::get(raw[i], e));
+      for (int e = 0; e < V; ++e) m[e % P] = fmaxf(m[e % P], Type::get(raw[i], e));
       __builtin_amdgcn_sched_barrier(0);
     }
-    return m;
   }
 
   // Adds the chunks to a thread's sums, a block of up to two at a time, each block by four sums of its own.

@@ -5,11 +5,12 @@
 namespace lc {
 
 constexpr int kTopMost = LIPCACHE_MOST_TOP;
-// Groups of threads whose largest values give the threshold: 16 for up to 12 alternatives (about 1.4 each reach it in
-// what the groups have seen), for more 256 (64 of a wave; 1.1 to 1.2 each; up to 5 for 64 of 64).
-constexpr int kTopFew = 12;
+// Groups of a row's first segment whose largest values give the threshold: 16 for up to 8 alternatives (about 1.4 each reach
+// it in what the groups have seen).  For more, four of every thread where a row has up to 64 threads, else 256 (1.1 to 1.2 each,
+// up to 5 for 64 of 64 groups: 1024 x 131072 bfloat16 with 12 takes 65 us with 256 groups, 79 with 16).
+constexpr int kTopFew = 8;
 template <class S>
-inline constexpr int kTopGroups = S::G < 64 ? 16 : S::G < 256 ? 64 : 256;
+inline constexpr int kTopGroups = S::G <= 64 ? 16 : 256;
 
 struct LpScore {
   float temperature;
@@ -33,7 +34,7 @@ __device__ __forceinline__ int top_index(uint64_t key) { return static_cast<int>
 
 // Every wave of a row (its lanes, where a wave holds several) has a list of its own.
 template <class S>
-inline constexpr int kTopList = S::G < 64 ? 32 : S::G == 64 ? 512 : S::G == 256 ? 256 : 64;
+inline constexpr int kTopList = S::G < 64 ? 64 : S::G == 64 ? 512 : S::G == 256 ? 256 : 64;
 template <class S>
 struct TopSpace {
   float maxima[S::kRows][kTopGroups<S>];
@@ -82,13 +83,41 @@ __device__ __forceinline__ void top_rounds(int k, TopRoom<S>& room, Each each, P
   }
 }
 
+// A number in the order of the floats; 0x007fffff is -inf.
+__device__ __forceinline__ uint32_t top_order(float v) { return static_cast<uint32_t>(top_key(v, 0) >> 32); }
+// The largest number whose last 16 bits are zero that k of those of L lanes reach, found bit by bit.
+template <int L, int N>
+__device__ __forceinline__ uint32_t top_reached(int k, const uint32_t (&v)[N]) {
+  uint32_t found = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t with = found | 1u << bit;
+    if constexpr (L == 64) {
+      int reach = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) reach += __builtin_popcountll(__ballot(v[i] >= with));
+      found = reach >= k ? with : found;
+    } else {
+      float reach = 0.0f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) reach += v[i] >= with ? 1.0f : 0.0f;
+      found = lanes_sum<L>(reach) >= static_cast<float>(k) ? with : found;
+    }
+  }
+  return found;
+}
+// (below -inf: nothing but -inf or less, which is no candidate)
+__device__ __forceinline__ float top_float(uint32_t found) {
+  return found <= 0x007fffffu ? -kRowInf : top_value(static_cast<uint64_t>(found) << 32);
+}
+
 // A value that k of the groups of a row's threads reach, `own` being what a thread has: the largest such with 16 groups, with
-// more the largest whose last 16 bits are zero.  At least k elements of what the threads have seen reach it.  The row's
+// 256 the largest whose last 16 bits are zero.  At least k elements of what the threads have seen reach it.  The row's
 // threads meet here; each wave counts for itself.
 template <class S>
 __device__ __forceinline__ float top_least(int k, float own, const RowPlace<S>& at, TopSpace<S>& top) {
   constexpr int G = S::G, kMany = kTopGroups<S>;
-  const bool few = G < 64 || k <= kTopFew;
+  const bool few = G <= 64 || k <= kTopFew;
   float m = own;
   if (few) {
     if constexpr (G >= 32) m = fmaxf(m, dpp_f32<kDppQuadXor1>(m));
@@ -126,20 +155,10 @@ __device__ __forceinline__ float top_least(int k, float own, const RowPlace<S>& 
     count(dpp_f32<0x12f>(v));
     return lanes_max<16>(n >= k ? v : -kRowInf);
   }
-  // bit by bit, in the order of the numbers
-  uint32_t v[kMany >= 64 ? kMany / 64 : 1], found = 0;
+  uint32_t v[4];
 #pragma unroll
-  for (int i = 0; i < kMany / 64; ++i) v[i] = static_cast<uint32_t>(top_key(top.maxima[at.row][lane_id() + 64 * i], 0) >> 32);
-#pragma unroll
-  for (int bit = 31; bit >= 16; --bit) {
-    const uint32_t with = found | 1u << bit;
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < kMany / 64; ++i) n += __builtin_popcountll(__ballot(v[i] >= with));
-    found = n >= k ? with : found;
-  }
-  // (below -inf: nothing but -inf or less, which is no candidate)
-  return found <= 0x007fffffu ? -kRowInf : top_value(static_cast<uint64_t>(found) << 32);
+  for (int i = 0; i < 4; ++i) v[i] = G > 64 ? top_order(top.maxima[at.row][lane_id() + 64 * i]) : 0;
+  return top_float(top_reached<64>(k, v));
 }
 
 // The list that a wave's lanes fill: a place is the number of the lanes before and of what is there already, so
@@ -209,7 +228,24 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
     float least = kRowInf;
     auto hits = [&](float v) { return v >= least && v > -kRowInf; };
     if (a.k > 0) {
-      least = top_least<S>(a.k, data.largest(begin, end, at.g), at, top);
+      bool found = false;
+      if constexpr (S::G <= 64) {
+        if (a.k > kTopFew) {
+          // four groups a lane
+          float m[4];
+          uint32_t v[4];
+          data.largest(begin, end, at.g, m);
+#pragma unroll
+          for (int p = 0; p < 4; ++p) v[p] = top_order(m[p]);
+          least = top_float(top_reached<S::G>(a.k, v));
+          found = true;
+        }
+      }
+      if (!found) {
+        float m[1];
+        data.largest(begin, end, at.g, m);
+        least = top_least<S>(a.k, m[0], at, top);
+      }
       list.push(hits(tail), tail, full * Data::V + at.g);
     }
     RowSums r = data.template begin<RowWants::kMean>(scale);
@@ -390,18 +426,18 @@ inline size_t score_bytes(int64_t T, int k, const RowShares& shares) {
 
 // Threads of a row.  Rows of up to 64 chunks are held by 16 lanes, of up to 256 by a wave.  Longer ones go through in
 // segments: by a wave up to 1024 chunks where the rows fill the chip with waves, by 256 threads, or by 1024 where there
-// are few.  (The 16 groups of a 16-lane row give a threshold for up to 12 alternatives, the 64 of a wave one that many more
-// than 48 would reach.)
+// are few.  (The 64 groups of 16 lanes give a threshold for up to 32 alternatives, about 44 of 32 on a list of 64; 32768 x 200
+// float32 with 16 takes 20 us, 37 with a wave a row, with 32 28 and 41.)
 template <class E, class F>
 lipcache_status score_shaped(int64_t T, int C, int k, F f) {
   const int chunks = C / RowType<E>::V;
-  if (k <= kTopFew) {
+  if (k <= 32) {
     if (chunks <= 16) return f(RowShape<16, 1>{}, std::true_type{});
     if (chunks <= 32) return f(RowShape<16, 2>{}, std::true_type{});
     if (chunks <= 64) return f(RowShape<16, 4>{}, std::true_type{});
   }
   if (chunks <= 256) return f(RowShape<64, 4>{}, std::true_type{});
-  if (chunks <= 1024 && T >= 2048 && k <= 48) return f(RowShape<64, 8>{}, std::false_type{});
+  if (chunks <= 1024 && T >= 2048) return f(RowShape<64, 8>{}, std::false_type{});
   if (chunks <= 1024 || T >= 768) return f(RowShape<256, 8>{}, std::false_type{});
   return f(RowShape<1024, 4>{}, std::false_type{});
 }

@@ -69,7 +69,7 @@ def test_scores(T, C, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
-@pytest.mark.parametrize("k", [0, 1, 2, 5, 20, 63, 64])
+@pytest.mark.parametrize("k", [0, 1, 2, 5, 8, 9, 20, 32, 33, 63, 64])
 @pytest.mark.parametrize("C", [33, 200, 3000, 40000, 70001])
 def test_alternatives(C, k, dtype):
     x, g = _logits(12, C, dtype, C + k, masked=0.3)
@@ -141,7 +141,7 @@ def test_not_finite(C):
 
 
 @pytest.mark.parametrize("C", [60, 300, 1500, 3001, 20000, 70001])
-@pytest.mark.parametrize("k", [3, 20, 64])
+@pytest.mark.parametrize("k", [3, 9, 20, 32, 64])
 def test_alternatives_among_nan(C, k):
     """A NaN is no alternative and hides none, however many there are and wherever."""
     x, g = _logits(8, C, F32, C + k)
