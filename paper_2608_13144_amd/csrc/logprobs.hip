@@ -34,7 +34,7 @@ __device__ __forceinline__ int top_index(uint64_t key) { return static_cast<int>
 
 // Every wave of a row (its lanes, where a wave holds several) has a list of its own.
 template <class S>
-inline constexpr int kTopList = S::G < 64 ? 64 : S::G == 64 ? 512 : S::G == 256 ? 256 : 64;
+inline constexpr int kTopList = S::G < 64 ? 64 : S::G == 64 ? 512 : S::G == 256 ? 256 : 128;
 template <class S>
 struct TopSpace {
   float maxima[S::kRows][kTopGroups<S>];
@@ -308,6 +308,22 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
         return fits ? n : -1;
       };
       int n = listed();
+      if constexpr (S::kWaves > 1) {
+        if (n > 128) {
+          // a threshold from the whole row leaves little more than k of them (n candidates take n steps, by G at a time:
+          // 1024 x 131072 bfloat16 with 64 alternatives 73 us, 138 where all of them are counted)
+          least = top_least<S>(a.k, own, at, top);  // (past its barrier the counts are read)
+          const int mine = list.n;
+          list.n = 0;
+          for (int i = lane_id(); i - lane_id() < mine; i += kWave) {
+            const uint64_t key = i < mine ? list.list[i] : 0;
+            list.push(key != 0 && top_value(key) >= least, top_value(key), top_index(key));  // (no place behind what is read)
+          }
+          if (lane_id() == 0) top.count[at.row][wave] = list.n;
+          __syncthreads();
+          n = listed();
+        }
+      }
       if (n < 0) {
         // the rare ways read the row again
         auto each = [&](auto f) {
