@@ -98,7 +98,12 @@ struct HlOut {
   }
 };
 
-// kAll: the tile holds all classes and each wave those of its rows, which it finishes itself.
+// A tile of W x + bias with classes along the accumulators' rows (a lane holds 16 classes of a row of x in each 32 x 32 of it), and
+// from the accumulators its share of every row's softmax: the largest logit, the sum and the sum for the entropy, joined across
+// the lane's pair; 16 bytes a row and wave leave the chip instead of the logits.  4096 x 4096 -> 32768 bfloat16 871 us,
+// bound by the product (1.26 PFLOP/s with its sums, 5 % of it); one row of 4096 -> 131072 179 us, bound by reading W (6 TB/s).
+// kAll: the tile holds all classes and each wave those of its rows, which it finishes itself.  32768 x 256 -> 200
+// float32 38 us, of which 24 are the products at the float32 matrix rate; the rest is one tile's start and end a CU.
 // Registers for two waves a SIMD, or for as many as the ring leaves.
 template <class S>
 inline constexpr int kHlWaves = S::kThreads > 256 || 2 * S::kLds <= 160 * 1024 ? 2 : 1;
@@ -188,7 +193,7 @@ __global__ __launch_bounds__(S::kThreads, kHlWaves<S>) void hl_tile_kernel(const
   }
 }
 
-// WAVES waves join a row's parts: four rows a workgroup, or one.
+// WAVES waves join a row's parts: four rows a workgroup, or one.  Bound by latency: 7 us for one row of 131072 classes.
 template <int WAVES>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void hl_join_kernel(int T, int C, int parts, const float4* __restrict__ part,
                                                       const float* __restrict__ at, HlOut out) {
@@ -233,7 +238,6 @@ struct HlSpace {
     return p;
   }
 };
-
 
 inline int64_t hl_parts(int C) { return hl_ceil(C, 256) * 8; }  // at most, of any tile shape
 // Rows of a pass: their parts stay below 256 MiB.

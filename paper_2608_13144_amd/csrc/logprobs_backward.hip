@@ -21,6 +21,11 @@ struct LpSlope {
   int some;    // any gradient that is not zero
 };
 
+// A row's sums, then dx = 2^a (flat + slope a) of every element from the same registers, then the places that label and
+// alternatives name, each written once with all that it gets.  Bound by memory, with the vector pipe at 74 % where the
+// entropy's gradient is wanted (two sums, about 23 instructions an element): 4096 x 32768 bfloat16 116 us with entropy
+// and eight alternatives (4.6 TB/s), 109 without (4.9); float32 203 us (5.3 TB/s).  Rows too long for the registers are read
+// twice: 1024 x 131072 float32 275 us.
 // kSplit: a workgroup takes a share of a row whose sums are there already.
 template <class E, class S, bool kWhole, bool kEntropy, bool kSplit>
 __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logits, int64_t ldx, int64_t T, int C,
