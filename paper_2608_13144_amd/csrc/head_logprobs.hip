@@ -368,6 +368,11 @@ lipcache_status hl_run(const E* x, int64_t ldx, int64_t T, const E* W, int64_t l
       // also where 128 would leave half of the last tile empty: 300 rows of 1024 -> 65536 356 us (403), 171 of 296 ->
       // 128192 168 (201); bfloat16 loses by it (300 rows: 83 us, 75 with 128).
       st = run(TileShape<E, 128, 64, 4, 1, 1, 3, 1, false, false>{});
+    } else if (hl_ceil(C, 64) * hl_ceil(n, 64) < (sizeof(E) == 4 ? 512 : 128)) {
+      // tiles of 64 x 64 that leave CUs idle, or float32 matrix cores waiting: 32 x 32, whose four waves share the contraction.
+      // 64 rows of 4096 -> 1000 float32 25 us (68 with 64 x 64), 189 of 3528 -> 440 24 (61), 64 of 4096 -> 20000 134 (244),
+      // 2000 of 1000 -> 500 26 (24); bfloat16 loses by it past 128 tiles (700 rows of 4096 -> 1500 35 us, 28 with 64 x 64).
+      st = run(TileShape<E, 32, 32, 1, 1, 4, 4, 1, false, false>{});
     } else if (t128 < 128) {
       st = run(TileShape<E, 64, 64, 2, 2, 1, 3, 1, false, false>{});
     } else if (sizeof(E) == 2 && 5 * t256 >= 4 * 256 * hl_ceil(t256, 256)) {

@@ -37,7 +37,7 @@ template <class S>
 inline constexpr int kTopList = S::G < 64 ? 64 : S::G == 64 ? 512 : S::G == 256 ? 256 : 128;
 template <class S>
 struct TopSpace {
-  float maxima[S::kRows][kTopGroups<S>];
+  float maxima[2][S::kRows][kTopGroups<S>];  // of this call of top_least and of the one before, which waves may still read
   int count[S::kRows][S::kWaves];
   uint64_t list[S::kRows][S::kWaves][kTopList<S>];
 };
@@ -115,10 +115,12 @@ __device__ __forceinline__ float top_float(uint32_t found) {
 // 256 the largest whose last 16 bits are zero.  At least k elements of what the threads have seen reach it.  The row's
 // threads meet here; each wave counts for itself.
 template <class S>
-__device__ __forceinline__ float top_least(int k, float own, const RowPlace<S>& at, TopSpace<S>& top) {
+__device__ __forceinline__ float top_least(int k, float own, const RowPlace<S>& at, TopSpace<S>& top, int& turn) {
   constexpr int G = S::G, kMany = kTopGroups<S>;
   const bool few = G <= 64 || k <= kTopFew;
   float m = own;
+  turn ^= 1;
+  float* maxima = top.maxima[turn][at.row];
   if (few) {
     if constexpr (G >= 32) m = fmaxf(m, dpp_f32<kDppQuadXor1>(m));
     if constexpr (G >= 64) m = fmaxf(m, dpp_f32<kDppQuadXor2>(m));
@@ -126,16 +128,16 @@ __device__ __forceinline__ float top_least(int k, float own, const RowPlace<S>& 
     if constexpr (G >= 256) m = fmaxf(m, dpp_f32<kDppMirror>(m));
     if constexpr (G >= 512) m = fmaxf(m, __shfl_xor(m, 16, kWave));
     if constexpr (G >= 1024) m = fmaxf(m, __shfl_xor(m, 32, kWave));
-    if (at.g % (G / 16) == 0) top.maxima[at.row][at.g / (G / 16)] = m;
+    if (at.g % (G / 16) == 0) maxima[at.g / (G / 16)] = m;
   } else {
     if constexpr (G >= 2 * kMany) m = fmaxf(m, dpp_f32<kDppQuadXor1>(m));
     if constexpr (G >= 4 * kMany) m = fmaxf(m, dpp_f32<kDppQuadXor2>(m));
-    if (at.g % (G / kMany) == 0) top.maxima[at.row][at.g / (G / kMany)] = m;
+    if (at.g % (G / kMany) == 0) maxima[at.g / (G / kMany)] = m;
   }
   RowPlace<S>::sync();
   if (few) {
     // a group's place is the number of groups that reach its value
-    const float v = top.maxima[at.row][lane_id() & 15];
+    const float v = maxima[lane_id() & 15];
     int n = 1;
     auto count = [&](float other) { n += other >= v ? 1 : 0; };
     count(dpp_f32<0x121>(v));  // row_ror: the 15 other lanes of 16
@@ -157,7 +159,7 @@ __device__ __forceinline__ float top_least(int k, float own, const RowPlace<S>& 
   }
   uint32_t v[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = G > 64 ? top_order(top.maxima[at.row][lane_id() + 64 * i]) : 0;
+  for (int i = 0; i < 4; ++i) v[i] = G > 64 ? top_order(maxima[lane_id() + 64 * i]) : 0;
   return top_float(top_reached<64>(k, v));
 }
 
@@ -227,6 +229,7 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
 #pragma unroll
   for (int i = 0; i < S::N; ++i) data.load_chunk(i, row_of(t), begin, end, at.g);
   const int wave = S::kWaves > 1 ? static_cast<int>(threadIdx.x) / kWave : 0;  // of the row
+  int top_turn = 0;
   for (int turn = 0; t - at.row < T; t += step, turn ^= 1) {
     const E *x = row_of(t), *following = row_of(t + step);
     int next_y = kShare ? -1 : label_of(t + step);
@@ -251,7 +254,7 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
       if (!found) {
         float m[1];
         data.largest(begin, end, at.g, m);
-        least = top_least<S>(a.k, m[0], at, top);
+        least = top_least<S>(a.k, m[0], at, top, top_turn);
       }
       list.push(hits(tail), tail, full * Data::V + at.g);
     }
@@ -265,12 +268,29 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
     auto seen = [&](float m, auto each) {
       if (a.k > 0 && __ballot(hits(m)) != 0) each(hits, [&](bool any, float v, int j) { list.push(any, v, j); });
     };
+    // a threshold from all that the threads have seen, which no more than a few times k of the lists reach; past its barrier
+    // the waves have read the counts
+    auto cut = [&](float own) {
+      least = top_least<S>(a.k, own, at, top, top_turn);
+      const int mine = list.n < kTopList<S> ? list.n : kTopList<S>;
+      if (list.n > mine) return;  // (some are lost already)
+      list.n = 0;
+      for (int i = lane_id(); i - lane_id() < mine; i += kWave) {
+        const uint64_t key = i < mine ? list.list[i] : 0;
+        list.push(key != 0 && top_value(key) >= least, top_value(key), top_index(key));  // (no place behind what is read)
+      }
+    };
     // a segment's chunks are asked for as the one before is used, the next row's behind the row's last
     int first = begin;
     if constexpr (!kWhole) {
-      for (; first + kSegment < end; first += kSegment)
+      for (int done = 1; first + kSegment < end; first += kSegment, ++done) {
         data.template add<RowWants::kMean>(first, end, at.g, r, scale, seen,
                                            [&](int i) { data.load_chunk(i, x, first + kSegment, end, at.g); });
+        // lists of long rows stay short: 1943 x 103064 float32 with 64 alternatives 164 us, 272 without
+        if constexpr (S::kWaves > 1) {
+          if (a.k > 0 && done > 1 && (done & (done - 1)) == 0) cut(r.m);
+        }
+      }
     }
     if constexpr (kShare) {
       data.template add<RowWants::kMean>(first, end, at.g, r, scale, seen, RowNothing{});
@@ -317,15 +337,8 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
       int n = listed();
       if constexpr (S::kWaves > 1) {
         if (n > 128) {
-          // a threshold from the whole row leaves little more than k of them (n candidates take n steps, by G at a time:
-          // 1024 x 131072 bfloat16 with 64 alternatives 73 us, 138 where all of them are counted)
-          least = top_least<S>(a.k, own, at, top);  // (past its barrier the counts are read)
-          const int mine = list.n;
-          list.n = 0;
-          for (int i = lane_id(); i - lane_id() < mine; i += kWave) {
-            const uint64_t key = i < mine ? list.list[i] : 0;
-            list.push(key != 0 && top_value(key) >= least, top_value(key), top_index(key));  // (no place behind what is read)
-          }
+          // (n candidates take n steps, by G at a time: 1024 x 131072 bfloat16 with 64 alternatives 73 us, 138 without the cut)
+          cut(own);
           if (lane_id() == 0) top.count[at.row][wave] = list.n;
           __syncthreads();
           n = listed();
@@ -344,7 +357,7 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
           }
           f(tail, full * Data::V + at.g);
         };
-        least = top_least<S>(a.k, own, at, top);  // (past its barrier the counts are read)
+        least = top_least<S>(a.k, own, at, top, top_turn);  // (past its barrier the counts are read)
         list.n = 0;
         each([&](float v, int j) { list.push(hits(v), v, j); });
         if (at.g % S::kLanes == 0) top.count[at.row][wave] = list.n;
@@ -449,8 +462,9 @@ inline size_t score_bytes(int64_t T, int k, const RowShares& shares) {
 }
 
 // Threads of a row.  Rows of up to 64 chunks are held by 16 lanes, of up to 256 by a wave.  Longer ones go through in
-// segments: by a wave up to 1024 chunks where the rows fill the chip with waves, by 256 threads, or by 1024 where there
-// are few.  (The 64 groups of 16 lanes give a threshold for up to 32 alternatives, about 44 of 32 on a list of 64; 32768 x 200
+// segments: by a wave up to 2048 chunks where the rows fill the chip with waves, by 256 threads, or by 1024 where there
+// are few.  With five alternatives a wave and 256 threads a row: 24261 x 9399 bfloat16 154 and 218 us, 4096 x 16384 40 and 45,
+// 2048 x 9399 18 and 22; 4096 x 32768 with eight 81 and 72.  (The 64 groups of 16 lanes give a threshold for up to 32 alternatives, about 44 of 32 on a list of 64; 32768 x 200
 // float32 with 16 takes 20 us, 37 with a wave a row, with 32 28 and 41.)
 template <class E, class F>
 lipcache_status score_shaped(int64_t T, int C, int k, F f) {
@@ -461,7 +475,7 @@ lipcache_status score_shaped(int64_t T, int C, int k, F f) {
     if (chunks <= 64) return f(RowShape<16, 4>{}, std::true_type{});
   }
   if (chunks <= 256) return f(RowShape<64, 4>{}, std::true_type{});
-  if (chunks <= 1024 && T >= 2048) return f(RowShape<64, 8>{}, std::false_type{});
+  if (chunks <= 2048 && T >= 2048) return f(RowShape<64, 8>{}, std::false_type{});
   if (chunks <= 1024 || T >= 768) return f(RowShape<256, 8>{}, std::false_type{});
   return f(RowShape<1024, 4>{}, std::false_type{});
 }
