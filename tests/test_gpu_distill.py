@@ -119,6 +119,19 @@ def test_in_place_beside_and_without_a_gradient(C, dtype):
     assert got.grad is mine and torch.equal(mine, want.grad) and torch.equal(got.kl, want.kl)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,C", [(65, 140001), (700, 33000), (66, 65537)])
+def test_losses_alone(T, C, dtype):
+    """Without a gradient long rows go through in other shares, as far as they need no registers for it."""
+    x, g = _logits(T, C, dtype, C + T)
+    y = _labels(T, C, g)
+    teacher, index = _teacher(x, 70, g)
+    for hard, t in ((0.4, 2.0), (0.0, 0.7)):
+        out = _api().distill(x, teacher, index, y, hard=hard, temperature=t, want_grad=False)
+        assert out.grad is None
+        _check(x, teacher, index, y, None, hard, 1.0, t, out)
+
+
 def test_against_differences():
     """Central differences of the float64 definition, step 1e-5: off by h^2 / 6 times the third derivative (order one)."""
     T, C, t, hard, soft = 5, 11, 1.7, 0.6, 2.3
