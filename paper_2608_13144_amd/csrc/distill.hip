@@ -187,10 +187,9 @@ __global__ __launch_bounds__(S::kThreads) void lp_distill_kernel(const E* logits
       auto here = [&](int c) { return c >= from_class && c < to_class; };
       const bool named = now_y >= 0 && part.hard != 0.0f, met = named && entries.add(lane, now_y, part.hard);
       entries.index(lane);
-      for (int i = lane; i < a.k; i += kLanes) {
-        float q;
-        if (entries.first(i, q) && here(entries.at[i])) dx[entries.at[i]] = static_cast<E>(smooth(entries.logit[i]) - q);
-      }
+      entries.firsts(lane, [&](int i, float q) {
+        if (here(entries.at[i])) dx[entries.at[i]] = static_cast<E>(smooth(entries.logit[i]) - q);
+      });
       if (lane == 0 && named && !met && here(now_y)) dx[now_y] = static_cast<E>(smooth(now_logit) - part.hard);
     }
   }

@@ -442,24 +442,43 @@ struct RowEntries {
     }
     wave_sync();
   }
-  // After index(): whether entry i is the first of its class; if so `sum` is the class's.
-  __device__ __forceinline__ bool first(int i, float& sum) const {
-    const int c = at[i];
-    if (c < 0) return false;
-    sum = value[i];
-    const uint32_t b = static_cast<uint32_t>(c) & (bits - 1);
-    if (!(twice[b >> 5] >> (b & 31) & 1)) return true;
-    float all = 0.0f;
-    bool mine = true;
+  // After index(): put(i, sum) for the first entry i of every class, with the class's sum.  Only entries of a bit that was met
+  // twice can share a class, so those alone are compared, each as the others' lanes hold it.
+  template <class F>
+  __device__ __forceinline__ void firsts(int lane, F put) const {
+    auto marked = [&](int c) {
+      const uint32_t b = static_cast<uint32_t>(c) & (bits - 1);
+      return c >= 0 && (twice[b >> 5] >> (b & 31) & 1) != 0;
+    };
+    for (int i = lane; i - lane < n; i += LANES) {
+      const int c = i < n ? at[i] : -1;
+      float sum = i < n ? value[i] : 0.0f;
+      const bool more = marked(c);
+      bool mine = c >= 0;
+      if (__ballot(more) != 0) {
+        float all = 0.0f;
+        auto meet = [&](int j, int other, float v) {
+          const bool same = other == c;
+          mine = mine && !(same && j < i);
+          all = same ? all + v : all;
+        };
+        if constexpr (LANES == 64) {
+          for (int base = 0; base < n; base += LANES) {
+            const int own = base + lane < n ? at[base + lane] : -1;
+            const float v = base + lane < n ? value[base + lane] : 0.0f;
+            for (uint64_t left = __ballot(marked(own)); left != 0; left &= left - 1) {
+              const int l = __builtin_ctzll(left);
+              meet(base + l, __builtin_amdgcn_readlane(own, l), lane_f32(v, l));
+            }
+          }
+        } else {
 #pragma unroll 8
-    for (int j = 0; j < n; ++j) {
-      const bool same = at[j] == c;
-      const float v = value[j];
-      mine = mine && !(same && j < i);
-      all = same ? all + v : all;
+          for (int j = 0; j < n; ++j) meet(j, at[j], value[j]);
+        }
+        if (more) sum = all;
+      }
+      if (mine) put(i, sum);
     }
-    sum = all;
-    return mine;
   }
 };
 

@@ -163,10 +163,9 @@ __global__ __launch_bounds__(S::kThreads) void lp_backward_kernel(const E* logit
       auto here = [&](int c) { return c >= from_class && c < to_class; };
       const bool met = now.at >= 0 && entries.add(lane, now.at, now.value);
       entries.index(lane);
-      for (int i = lane; i < a.k; i += kLanes) {
-        float g;
-        if (entries.first(i, g) && here(entries.at[i])) dx[entries.at[i]] = static_cast<E>(fmaf(g, inv_t, smooth(entries.logit[i])));
-      }
+      entries.firsts(lane, [&](int i, float g) {
+        if (here(entries.at[i])) dx[entries.at[i]] = static_cast<E>(fmaf(g, inv_t, smooth(entries.logit[i])));
+      });
       if (lane == 0 && now.at >= 0 && !met && here(now.at)) dx[now.at] = static_cast<E>(fmaf(now.value, inv_t, smooth(now_logit)));
     }
   }
