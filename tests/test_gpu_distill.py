@@ -46,7 +46,7 @@ def test_distill(T, C, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("k", [0, 1, 2, 63, 64, 65, 200, 1000])
+@pytest.mark.parametrize("k", [0, 1, 2, 17, 63, 64, 65, 200, 1000])
 @pytest.mark.parametrize("C", [200, 3000, 70001])
 def test_entries(C, k, dtype):
     """Numbers of entries around a wave's and a workgroup's; every class of a small head; classes named twice."""
@@ -61,6 +61,20 @@ def test_entries(C, k, dtype):
         index[3, 1] = index[3, 0]
     out = _api().distill(x, teacher.contiguous(), index.contiguous(), soft=1.5, temperature=3.0)
     _check(x, teacher, index, None, None, 0.0, 1.5, 3.0, out)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("C,k", [(40, 224), (200, 65), (250, 200), (200, 225)])
+def test_entries_of_many_short_rows(C, k, dtype):
+    x, g = _logits(16390, C, dtype, C + k)
+    n = min(k, C)
+    teacher, index = _teacher(x, n, g)
+    if k > n:
+        teacher = torch.cat([teacher, torch.randn(16390, k - n, generator=g, device=DEV)], 1)
+        index = torch.cat([index, torch.randint(-1, C + 1, (16390, k - n), generator=g, device=DEV, dtype=torch.int32)], 1)
+    y = _labels(16390, C, g)
+    out = _api().distill(x, teacher, index, y, hard=0.3, soft=1.5, temperature=3.0)
+    _check(x, teacher, index, y, None, 0.3, 1.5, 3.0, out)
 
 
 @pytest.mark.parametrize("C", [40, 600, 30000, 70001])

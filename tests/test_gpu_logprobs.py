@@ -262,7 +262,8 @@ def test_rows_without_a_gradient(C):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("T,C,k", [(3, 50, 1024), (5, 200, 200), (2, 7000, 1000), (2, 70, 65)])
+@pytest.mark.parametrize("T,C,k", [(3, 50, 1024), (5, 200, 200), (2, 7000, 1000), (2, 70, 65), (70, 130, 33),
+                                   (16400, 40, 224), (16385, 200, 65), (16384, 300, 225)])
 def test_many_entries(T, C, k, dtype):
     """More entries than threads of a row, most of them several times."""
     x, g = _logits(T, C, dtype, C)
