@@ -462,9 +462,10 @@ inline size_t score_bytes(int64_t T, int k, const RowShares& shares) {
 }
 
 // Threads of a row.  Rows of up to 64 chunks are held by 16 lanes, of up to 256 by a wave.  Longer ones go through in
-// segments: by a wave up to 2048 chunks where the rows fill the chip with waves, by 256 threads, or by 1024 where there
-// are few.  With five alternatives a wave and 256 threads a row: 24261 x 9399 bfloat16 154 and 218 us, 4096 x 16384 40 and 45,
-// 2048 x 9399 18 and 22; 4096 x 32768 with eight 81 and 72.  (The 64 groups of 16 lanes give a threshold for up to 32 alternatives, about 44 of 32 on a list of 64; 32768 x 200
+// segments: by a wave up to 2048 chunks where the rows fill the chip with waves (2560 where several times), by 256 threads, or
+// by 1024 where there are few.  With five alternatives a wave and 256 threads a row: 24261 x 9399 bfloat16 154 and 218 us,
+// 4096 x 16384 40 and 45, 2048 x 9399 18 and 22, 6000 x 20000 61 and 76, 4096 x 32768 with eight 81 and 72; 8192 x 32768 with 20
+// alternatives 172 and 158.  (The 64 groups of 16 lanes give a threshold for up to 32 alternatives, about 44 of 32 on a list of 64; 32768 x 200
 // float32 with 16 takes 20 us, 37 with a wave a row, with 32 28 and 41.)
 template <class E, class F>
 lipcache_status score_shaped(int64_t T, int C, int k, F f) {
@@ -475,7 +476,7 @@ lipcache_status score_shaped(int64_t T, int C, int k, F f) {
     if (chunks <= 64) return f(RowShape<16, 4>{}, std::true_type{});
   }
   if (chunks <= 256) return f(RowShape<64, 4>{}, std::true_type{});
-  if (chunks <= 2048 && T >= 2048) return f(RowShape<64, 8>{}, std::false_type{});
+  if (T >= 2048 && chunks <= (T >= 6000 ? 2560 : 2048)) return f(RowShape<64, 8>{}, std::false_type{});
   if (chunks <= 1024 || T >= 768) return f(RowShape<256, 8>{}, std::false_type{});
   return f(RowShape<1024, 4>{}, std::false_type{});
 }
