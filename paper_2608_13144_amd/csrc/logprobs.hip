@@ -194,7 +194,7 @@ struct TopList {
 // and another pass follow, and where that is not enough either, one alternative after another.
 //
 // Bound by memory without alternatives (4096 x 32768 bfloat16 50 us, 5.4 TB/s; 1024 x 131072 46 us, 5.8 TB/s), by vector
-// instructions with them (eight 71 and 63 us, 64 91 and 73; without the threshold, one after another, each costs a reading
+// instructions with them (eight 72 and 58 us, 64 92 and 73; without the threshold, one after another, each costs a reading
 // of the row).  32768 x 200 float32, 13.6 us with five: the joins of so short rows.
 //
 // kWhole: a row is one segment.  kShare: a workgroup takes a share of a row, and leaves its sums and its k largest (keys
