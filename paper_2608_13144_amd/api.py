@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import inspect
 from dataclasses import dataclass
 
 import torch
@@ -619,12 +620,15 @@ class LogProbs:
 
 def _on_device(call):
     """The call with its first tensor's device current: a stream's handle alone does not say which device's it is."""
+    name = next(iter(inspect.signature(call).parameters))
+
     @functools.wraps(call)
-    def on_device(first, *args, **kw):
+    def on_device(*args, **kw):
+        first = args[0] if args else kw.get(name)
         if not isinstance(first, torch.Tensor) or not first.is_cuda or first.device.index == torch.cuda.current_device():
-            return call(first, *args, **kw)
+            return call(*args, **kw)
         with torch.cuda.device(first.device):
-            return call(first, *args, **kw)
+            return call(*args, **kw)
     return on_device
 
 
