@@ -695,8 +695,8 @@ size_t lipcache_distill_workspace_bytes(int64_t T, int32_t C, int32_t k, int32_t
  *
  *  x [T][K] (ldx), W [C][K] (ldw), dtype; bias [C] float or NULL;  K, C <= 2^20
  *  logp, lse, entropy [T] out, each may be NULL
- *  ws  lipcache_head_logprobs_workspace_bytes(the same arguments) bytes: a matrix whose rows are
- *      not whole 16-byte vectors (pointer, ld and K) is copied into it first
+ *  ws  lipcache_head_logprobs_workspace_bytes(the same arguments) bytes, NULL where that is 0 (T = 0): a
+ *      matrix whose rows are not whole 16-byte vectors (pointer, ld and K) is copied into it first
  * The others as in lipcache_logprobs. (async)
  */
 lipcache_status lipcache_head_logprobs(const void* x, int64_t ldx, int64_t T, const void* W, int64_t ldw,

@@ -403,7 +403,7 @@ using namespace lc;
 
 extern "C" size_t lipcache_head_logprobs_workspace_bytes(const void* x, int64_t ldx, int64_t T, const void* W, int64_t ldw,
                                                          int32_t K, int32_t C, int32_t dtype) {
-  if (hl_sizes_bad(T, K, C, dtype)) return 0;
+  if (hl_sizes_bad(T, K, C, dtype) || T == 0) return 0;
   HlSpace space{nullptr};
   if (dtype == LIPCACHE_F32) HlBuffers<float>(space, x, ldx, T, W, ldw, K, C);
   else HlBuffers<__bf16>(space, x, ldx, T, W, ldw, K, C);
@@ -422,9 +422,9 @@ extern "C" lipcache_status lipcache_head_logprobs(const void* x, int64_t ldx, in
       hl_unaligned(logp, 4) || hl_unaligned(lse, 4) || hl_unaligned(entropy, 4))
     return LIPCACHE_EINVAL;
   if (C > kHlMostClasses || K > kHlMostWidth || T > 0x7fffffff) return LIPCACHE_EUNSUPPORTED;
+  if (T == 0) return LIPCACHE_OK;
   if (!ws || !aligned256(ws) || ws_bytes < lipcache_head_logprobs_workspace_bytes(x, ldx, T, W, ldw, K, C, dtype))
     return LIPCACHE_EWORKSPACE;
-  if (T == 0) return LIPCACHE_OK;
   const HlOut out{label, logp, lse, entropy, kHlLog2e / temperature, temperature};
   auto run = [&](auto type) {
     typedef decltype(type) E;

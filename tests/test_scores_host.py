@@ -22,3 +22,16 @@ def test_every_argument_by_name(name, first, more):
 def test_a_call_without_its_first_argument_names_it(name, first, more):
     with pytest.raises(TypeError, match=rf"{name}\(\) missing 1 required positional argument: '{first}'"):
         getattr(api, name)(**more)
+
+
+def test_no_rows_need_no_workspace():
+    """T = 0 does nothing, whatever the operands' alignment, with as much workspace as the query says: none."""
+    lib, some = L.load(), 0x100000
+    for ldw, K in ((64, 64), (62, 62), (1, 1)):
+        assert lib.lipcache_head_logprobs_workspace_bytes(some, 64, 0, some, ldw, K, 48, L.BF16) == 0, (ldw, K)
+        assert lib.lipcache_head_logprobs(some, 64, 0, some, ldw, None, K, 48, L.BF16, 1.0, None, None, None, None, None, 0,
+                                          None) == L.OK, (ldw, K)
+    assert lib.lipcache_head_logprobs(some, 64, 1, some, 64, None, 64, 48, L.BF16, 1.0, None, None, None, None, None, 0,
+                                      None) == L.EWORKSPACE
+    assert lib.lipcache_head_logprobs(some, 63, 0, some, 64, None, 64, 48, L.BF16, 1.0, None, None, None, None, None, 0,
+                                      None) == L.EINVAL
