@@ -39,49 +39,11 @@ template <class S>
 struct TopSpace {
   float maxima[2][S::kRows][kTopGroups<S>];  // of this call of top_least and of the one before, which waves may still read
   int count[S::kRows][S::kWaves];
-  uint64_t list[S::kRows][S::kWaves][kTopList<S>];
+  union {
+    uint64_t list[S::kRows][S::kWaves][kTopList<S>];
+    uint32_t bins[S::kRows][2 * S::kWaves * kTopList<S>];  // where a list ran over
+  };
 };
-template <class S>
-struct TopRoom {
-  float value[2][S::kWaves];
-};
-
-// A row's k largest, one after another: each the largest of those behind the one before.  each(f) calls f(value,
-// index) for the thread's elements by rising index.
-template <class S, class Each, class Put>
-__device__ __forceinline__ void top_rounds(int k, TopRoom<S>& room, Each each, Put put) {
-  float last = kRowInf;
-  int last_at = -1;
-  for (int i = 0; i < k; ++i) {
-    float best = -kRowInf;
-    int at = kRowMostClasses;
-    each([&](float v, int j) {
-      const bool left = v < last || (v == last && j > last_at);
-      if (left && v > best) {
-        best = v;
-        at = j;
-      }
-    });
-    float top = lanes_max<S::kLanes>(best), where;
-    auto least = [](float a, float b) { return fminf(a, b); };
-    if constexpr (S::kWaves > 1) {
-      const int w = lane_id() & 15;
-      __syncthreads();
-      if (lane_id() == 0) room.value[0][threadIdx.x / kWave] = top;
-      __syncthreads();
-      top = lanes_max<16>(w < S::kWaves ? room.value[0][w] : -kRowInf);
-      where = lanes_join<64>(best == top ? static_cast<float>(at) : static_cast<float>(kRowMostClasses), least);
-      if (lane_id() == 0) room.value[1][threadIdx.x / kWave] = where;
-      __syncthreads();
-      where = lanes_join<16>(w < S::kWaves ? room.value[1][w] : static_cast<float>(kRowMostClasses), least);
-    } else {
-      where = lanes_join<S::kLanes>(best == top ? static_cast<float>(at) : static_cast<float>(kRowMostClasses), least);
-    }
-    last = top;
-    last_at = static_cast<int>(where);  // below 2^24: exact
-    put(i, top, last_at);
-  }
-}
 
 // A number in the order of the floats; 0x007fffff is -inf.
 __device__ __forceinline__ uint32_t top_order(float v) { return static_cast<uint32_t>(top_key(v, 0) >> 32); }
@@ -106,15 +68,18 @@ __device__ __forceinline__ uint32_t top_reached(int k, const uint32_t (&v)[N]) {
   }
   return found;
 }
-// (below -inf: nothing but -inf or less, which is no candidate)
+// The number of the type that is next to it, up (below -inf: nothing but -inf or less, which is no candidate).
+template <class E>
 __device__ __forceinline__ float top_float(uint32_t found) {
-  return found <= 0x007fffffu ? -kRowInf : top_value(static_cast<uint64_t>(found) << 32);
+  if (found <= 0x007fffffu) return -kRowInf;
+  constexpr uint32_t kMore = sizeof(E) == 4 ? 0 : std::is_same<E, __bf16>::value ? 0xffffu : 0x1fffu;  // bits that the type lacks
+  return top_value(static_cast<uint64_t>(found & 0x80000000u ? found : found | kMore) << 32);
 }
 
 // A value that k of the groups of a row's threads reach, `own` being what a thread has: the largest such with 16 groups, with
 // 256 the largest whose last 16 bits are zero.  At least k elements of what the threads have seen reach it.  The row's
 // threads meet here; each wave counts for itself.
-template <class S>
+template <class E, class S>
 __device__ __forceinline__ float top_least(int k, float own, const RowPlace<S>& at, TopSpace<S>& top, int& turn) {
   constexpr int G = S::G, kMany = kTopGroups<S>;
   const bool few = G <= 64 || k <= kTopFew;
@@ -160,7 +125,7 @@ __device__ __forceinline__ float top_least(int k, float own, const RowPlace<S>& 
   uint32_t v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = G > 64 ? top_order(maxima[lane_id() + 64 * i]) : 0;
-  return top_float(top_reached<64>(k, v));
+  return top_float<E>(top_reached<64>(k, v));
 }
 
 // The list that a wave's lanes fill: a place is the number of the lanes before and of what is there already, so
@@ -184,6 +149,114 @@ struct TopList {
   }
 };
 
+// A candidate's place in the order of all: what top_key joins.
+struct TopLeast {
+  uint32_t order, index;
+  __device__ __forceinline__ bool reached(float v, int j) const {
+    const uint32_t o = top_order(v);
+    return o > order || (o == order && ~static_cast<uint32_t>(j) >= index);
+  }
+};
+
+// A key that at least k of a row's elements reach, and no more than one list holds, whatever the values; k elements reach `least`, and
+// none is past `most`.  Those past `least` are counted first, fewer than k where many are equal to it.  Else those of the value's
+// first bits are counted, then those that share the k-th's by their next bits; then, among the equal ones, by the bits of ~index,
+// until few enough are left.  Keys differ, so the last bits leave k.  each(f) calls f(value, index) for the thread's
+// elements, whole waves at a time.  Up to eight readings of the row, most often two; the row's threads meet here, and its
+// lists are overwritten.  64 alternatives of rows that rise, or hold one value: 2100 x 16384 bfloat16 140 and 178 us (random ones
+// 82), 4096 x 32768 300 and 431 (94), 1024 x 131072 302 and 511 (75); one alternative after another 1964 to 4500.
+template <class S, class Each>
+__device__ __forceinline__ TopLeast top_select(int k, float least, float most, int C, uint32_t* bins, Each each) {
+  constexpr int L = S::kLanes, kBits = S::G < 64 ? 7 : 8, kBins = 1 << kBits, kOwn = kBins / L;
+  static_assert(kBins <= 2 * S::kWaves * kTopList<S> && kTopList<S> >= kTopMost, "room for bins, and for k in one list");
+  auto same = [](auto v) { return L == 64 ? uniform(static_cast<int>(v)) : static_cast<int>(v); };  // of all lanes of a row
+  const uint32_t lo = same(top_order(least)), hi = same(top_order(most));
+  const int index_bits = C > 1 ? 32 - __builtin_clz(C - 1) : 1;
+  int beyond = 0;  // keys past all that share the found one's bits: fewer than k
+  if (lo != hi) {
+    float past = 0.0f;  // (below 2^24: exact)
+    each([&](float v, int) { past += v > least ? 1.0f : 0.0f; });
+    beyond = same(lanes_sum<L>(past));
+    if constexpr (S::kWaves > 1) {
+      if (lane_id() == 0) bins[threadIdx.x / kWave] = static_cast<uint32_t>(beyond);
+      __syncthreads();
+      beyond = 0;
+      for (int w = 0; w < S::kWaves; ++w) beyond += same(bins[w]);
+      __syncthreads();
+    }
+  }
+  bool values = beyond >= k;
+  int bits = values ? 32 - __builtin_clz(lo ^ hi) : index_bits;
+  TopLeast found{lo, ~0u << index_bits};
+  if (values) {
+    found = {hi >> (bits - 1) >> 1 << (bits - 1) << 1, 0};
+    beyond = 0;
+  }
+  for (;;) {
+    const int shift = bits > kBits ? bits - kBits : 0;
+    const uint32_t known = ~0u << (bits - 1) << 1, mask = (1u << (bits - shift)) - 1;
+    // (the thread's place as a new number: what follows from it would be kept in registers from row to row)
+    int thread = static_cast<int>(threadIdx.x);
+    asm volatile("" : "+v"(thread));
+    const int lane = thread % L;
+    for (int b = thread % S::G; b < kBins; b += S::G) bins[b] = 0;
+    RowPlace<S>::sync();
+    each([&](float v, int j) {
+      const uint32_t o = top_order(v), word = values ? o : ~static_cast<uint32_t>(j);
+      const bool in = v >= least && v > -kRowInf &&
+                      (values ? ((o ^ found.order) & known) == 0 : o == found.order && ((word ^ found.index) & known) == 0);
+      const int bin = static_cast<int>(word >> shift & mask);
+      if constexpr (S::G >= 64) {
+        // (most of a wave's are often of one bin)
+        const uint64_t all = __ballot(in);
+        if (all == 0) return;
+        const int first = __builtin_ctzll(all), one = __builtin_amdgcn_readlane(bin, first);
+        if (__ballot(in && bin == one) == all) {
+          if (lane == first) atomicAdd(&bins[one], static_cast<uint32_t>(__builtin_popcountll(all)));
+          return;
+        }
+      }
+      if (in) atomicAdd(&bins[bin], 1u);
+    });
+    RowPlace<S>::sync();
+    int mine = 0;
+#pragma unroll 1
+    for (int b = 0; b < kOwn; ++b) mine += static_cast<int>(bins[lane * kOwn + b]);
+    int past = mine;  // with the lanes' behind, whose bins are of larger keys
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1) {
+      const int other = __builtin_amdgcn_ds_bpermute((thread + o) * 4, past);
+      past += lane + o < L ? other : 0;
+    }
+    past += beyond - mine;
+    float bin = 0.0f, over = 0.0f, with = 0.0f;  // of the one bin that holds the k-th: below 2^24, exact
+#pragma unroll 1
+    for (int b = kOwn - 1; b >= 0; --b) {
+      const int reach = past + static_cast<int>(bins[lane * kOwn + b]);
+      if (past < k && reach >= k) {
+        bin = static_cast<float>(lane * kOwn + b);
+        over = static_cast<float>(past);
+        with = static_cast<float>(reach);
+      }
+      past = reach;
+    }
+    const uint32_t more = static_cast<uint32_t>(same(lanes_max<L>(bin))) << shift;
+    const int reach = same(lanes_max<L>(with));
+    beyond = same(lanes_max<L>(over));
+    RowPlace<S>::sync();  // the bins are read
+    if (values) found.order |= more;
+    else found.index |= more;
+    bits = shift;
+    if (reach <= kTopList<S> || (bits == 0 && !values)) break;
+    if (bits == 0) {
+      values = false;
+      bits = index_bits;
+      found.index = ~0u << bits;
+    }
+  }
+  return found;
+}
+
 // Scores of rows, one pass: with a thread's own largest value m, s = sum 2^(c (x - m)) and the exponents' sum weighted by
 // what they add, c = log2(e) / temperature; joined, lse = m / temperature + ln s and entropy = ln s - ln 2 sum / s.
 //
@@ -191,7 +264,7 @@ struct TopList {
 // it), then every block of the row whose largest value reaches it puts its elements that do on a list, a few times k of
 // them, each of which finds its place by counting.  Where a list is too short for them (the first segment holds
 // little of what is large, or many values are equal), a threshold from the threads' largest values of the whole row
-// and another pass follow, and where that is not enough either, one alternative after another.
+// and another pass follow, and where that is not enough either, a key found by counting (top_select) and another.
 //
 // Bound by memory without alternatives (4096 x 32768 bfloat16 50 us, 5.4 TB/s; 1024 x 131072 46 us, 5.8 TB/s), by vector
 // instructions with them (eight 72 and 58 us, 64 92 and 73; without the threshold, one after another, each costs a reading
@@ -208,7 +281,6 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
   constexpr int kSegment = S::G * S::N;
   __shared__ RowSums room[2][S::kWaves];
   __shared__ TopSpace<S> top;
-  __shared__ TopRoom<S> top_room;
   const RowPlace<S> at;
   const RowScale scale{kRowLog2e / a.temperature, 0.0f};
   const int64_t step = kShare ? T : static_cast<int64_t>(gridDim.x) * S::kRows;
@@ -247,14 +319,14 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
           data.largest(begin, end, at.g, m);
 #pragma unroll
           for (int p = 0; p < 4; ++p) v[p] = top_order(m[p]);
-          least = top_float(top_reached<S::G>(a.k, v));
+          least = top_float<E>(top_reached<S::G>(a.k, v));
           found = true;
         }
       }
       if (!found) {
         float m[1];
         data.largest(begin, end, at.g, m);
-        least = top_least<S>(a.k, m[0], at, top, top_turn);
+        least = top_least<E, S>(a.k, m[0], at, top, top_turn);
       }
       list.push(hits(tail), tail, full * Data::V + at.g);
     }
@@ -271,7 +343,7 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
     // a threshold from all that the threads have seen, which no more than a few times k of the lists reach; past its barrier
     // the waves have read the counts
     auto cut = [&](float own) {
-      least = top_least<S>(a.k, own, at, top, top_turn);
+      least = top_least<E, S>(a.k, own, at, top, top_turn);
       const int mine = list.n < kTopList<S> ? list.n : kTopList<S>;
       if (list.n > mine) return;  // (some are lost already)
       list.n = 0;
@@ -332,7 +404,8 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
           fits = fits && c <= kTopList<S>;
           n += c;
         }
-        return fits ? n : -1;
+        n = fits ? n : -1;
+        return S::G < 64 ? n : uniform(n);
       };
       int n = listed();
       if constexpr (S::kWaves > 1) {
@@ -344,6 +417,9 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
           n = listed();
         }
       }
+      // (the same in a row held by a wave, most often of equal values: 32768 x 500 bfloat16, 488 of each row's classes masked by the
+      // lowest value, with 64 alternatives 116 us, 907 on lists of all)
+      if (S::G == 64 && kWhole && n > 128) n = -1;
       if (n < 0) {
         // the rare ways read the row again
         auto each = [&](auto f) {
@@ -357,18 +433,29 @@ __global__ __launch_bounds__(S::kThreads) void lp_score_kernel(const E* __restri
           }
           f(tail, full * Data::V + at.g);
         };
-        least = top_least<S>(a.k, own, at, top, top_turn);  // (past its barrier the counts are read)
-        list.n = 0;
-        each([&](float v, int j) { list.push(hits(v), v, j); });
-        if (at.g % S::kLanes == 0) top.count[at.row][wave] = list.n;
-        RowPlace<S>::sync();
-        n = listed();
-        if (n < 0)
-          top_rounds<S>(a.k, top_room, each, [&](int i, float v, int j) {
-            if (at.g == 0) put(i, v, j);
-          });
+        auto relisted = [&](auto take) {
+          list.n = 0;
+          each([&](float v, int j) { list.push(take(v, j), v, j); });
+          if (at.g % S::kLanes == 0) top.count[at.row][wave] = list.n;
+          RowPlace<S>::sync();
+          return listed();
+        };
+        if constexpr (!kWhole) {
+          // (a row of one segment had its whole row's threshold at first; 16 groups never give one for more than 16)
+          if (S::G == 64 && a.k > kTopFew) {
+            const uint32_t v[1] = {top_order(own)};
+            least = fmaxf(least, top_float<E>(top_reached<64>(a.k, v)));
+          } else {
+            least = top_least<E, S>(a.k, own, at, top, top_turn);  // (past its barrier the counts are read)
+          }
+          n = relisted([&](float v, int) { return hits(v); });
+        }
+        if (n < 0) {
+          const TopLeast from = top_select<S>(a.k, least, r.m, C, top.bins[at.row], each);
+          n = relisted([&](float v, int j) { return hits(v) && from.reached(v, j); });
+        }
       }
-      for (int c = at.g; n >= 0 && (c < n || c < a.k); c += S::G) {
+      for (int c = at.g; c < n || c < a.k; c += S::G) {
         if (c >= n) {
           put(c, -kRowInf, 0);
           continue;
