@@ -603,7 +603,7 @@ size_t lipcache_muon_step_workspace_bytes(int64_t batch, int32_t m, int32_t n, i
 /* Limits of the calls below. */
 #define LIPCACHE_MOST_TOP 64        /* alternatives of a row that lipcache_logprobs lists       */
 #define LIPCACHE_MOST_ENTRIES 1024  /* entries of a row that a gradient or a teacher names      */
-#define LIPCACHE_FEW_ROWS 64        /* calls with more rows than this need no workspace         */
+#define LIPCACHE_FEW_ROWS 64        /* rows of logits: calls with more need no workspace        */
 
 /*
  * Log probabilities of rows of logits.  With m_t = max_j x_tj and

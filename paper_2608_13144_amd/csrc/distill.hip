@@ -248,7 +248,7 @@ extern "C" lipcache_status lipcache_distill(const void* x, int64_t ldx, int64_t 
     if (shares.count > 1)
       return run(RowShape<256, 4>{}, std::false_type{}, std::true_type{}, static_cast<unsigned>(T * shares.count));
     // losses alone keep no row for a gradient: long ones go in segments by more workgroups of fewer registers (2048 x 131072
-    // bfloat16 with two temperatures 118 us, 151 held; 1024 x 65536 float32 49, 61; 4096 x 32768 bfloat16 73, 72)
+    // bfloat16 with two temperatures 117 us, 151 held; 1024 x 65536 float32 49, 61; 4096 x 32768 bfloat16 73, 72)
     if (!dx && C / RowType<E>::V > 8192)
       return run(RowShape<512, 4>{}, std::false_type{}, std::false_type{}, row_blocks<RowShape<512, 4>>(T));
     return row_shaped_entries<E>(T, C, k, [&](auto shape, auto whole) {

@@ -241,8 +241,10 @@ struct HlSpace {
 
 inline int64_t hl_parts(int C) { return hl_ceil(C, 256) * 8; }  // at most, of any tile shape
 // Rows of a pass: their parts stay below 256 MiB.
+constexpr int64_t kHlPartBytes = 1 << 28;
+static_assert(kHlPartBytes / (kHlMostClasses / 256 * 8 * 16) >= 256, "some rows a pass");
 inline int64_t hl_rows(int64_t T, int C) {
-  const int64_t rows = (1ll << 28) / (hl_parts(C) * 16) / 256 * 256, most = rows < 256 ? 256 : rows;
+  const int64_t most = kHlPartBytes / (hl_parts(C) * 16) / 256 * 256;
   return T < most ? T : most;
 }
 
@@ -374,10 +376,16 @@ lipcache_status hl_run(const E* x, int64_t ldx, int64_t T, const E* W, int64_t l
       // 2000 of 1000 -> 500 26 (24); bfloat16 loses by it past 128 tiles (700 rows of 4096 -> 1500 35 us, 28 with 64 x 64).
       st = run(TileShape<E, 32, 32, 1, 1, 4, 4, 1, false, false>{});
     } else if (t128 < 128) {
+      // 128 x 128 would leave half of the CUs idle: 1024 rows of 4096 -> 1920 bfloat16 (120 such tiles) 28 us, 32 with 128 x 128;
+      // 1280 -> 2048 (160) 40 and 32
       st = run(TileShape<E, 64, 64, 2, 2, 1, 3, 1, false, false>{});
     } else if (sizeof(E) == 2 && 5 * t256 >= 4 * 256 * hl_ceil(t256, 256)) {
+      // 256 x 256, one a CU, where they fill four fifths of their rounds: 2048 rows of 4096 -> 6656 (208 of 256) 98 us, 119 with
+      // 128 x 128 of four waves, 4096 -> 32768 876 and 1047; 2048 -> 9216 (288 of 512) 189 and 156
       if constexpr (sizeof(E) == 2) st = run(TileShape<E, 256, 256, 2, 4, 1, 2, 1, false, false>{});
     } else if (t128 < 320) {
+      // about one tile a CU: eight waves and a longer ring.  2048 rows of 4096 -> 2048 (256 tiles) bfloat16 39 us, 45 with four
+      // waves, float32 244 and 253; -> 3200 (400) 68 and 60
       st = run(TileShape<E, 128, 128, 2, 4, 1, 4, 1, false, false>{});
     } else {
       st = run(TileShape<E, 128, 128, 2, 2, 1, 2, 1, false, false>{});

@@ -215,18 +215,6 @@ struct RowData {
 #pragma unroll
     for (int i = 0; i < N; ++i) load_chunk(i, x, first, C / V, g);
   }
-  // f(value, index) for every element of the thread's chunks, rising index.
-  template <class F>
-  __device__ __forceinline__ void each(int first, int full, int g, F f) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (past(i, first, full)) break;
-      pin(i);
-#pragma unroll
-      for (int e = 0; e < V; ++e) f(Type::get(raw[i], e), (first + G * i + g) * V + e);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  }
   // Writes f of every element of chunk i (zeros unless `some`) to the row at out, where it has the chunk and is `live`.
   template <class F>
   __device__ __forceinline__ void store_chunk(int i, E* out, int first, int full, int g, bool live, bool some, F f) {
@@ -577,7 +565,8 @@ struct RowSplit {
   const float* logits;
 };
 
-// Workgroups: the rows, or as many as the chip holds at a time (256 CUs of 2048 threads).
+// Workgroups: the rows, or 2048 threads a CU, the most that the chip can hold; kernels of more than 64 registers hold fewer
+// (82 to 123 of them: half to five eighths, or a workgroup of 1024), and the rest start as others end.
 template <class S>
 unsigned row_blocks(int64_t T) {
   const int64_t need = (T + S::kRows - 1) / S::kRows, most = 256 * (2048 / S::kThreads);

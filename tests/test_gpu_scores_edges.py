@@ -86,3 +86,12 @@ def test_no_row_is_read_once_for_each_alternative(T, C, dtype):
     alone = least(rising, 0)
     for name, x in (("rising", rising), ("equal", torch.zeros_like(rising)), ("masked", masked)):
         assert least(x, 64) < 24 * alone, name
+
+
+def test_heads_where_a_pass_ends():
+    """2^20 classes go through 512 rows at a time: the rows on both sides of each end."""
+    from test_gpu_head_logprobs import _case, _check
+    x, W, bias, y = _case(1100, 24, 1 << 20, BF16, 3)
+    out = _api().head_logprobs(x, W, bias, y)
+    for r in (slice(506, 518), slice(1018, 1030), slice(1094, 1100)):
+        _check(x[r], W, bias, y[r], 1.0, _api().LogProbs(out.logp[r], out.lse[r], out.entropy[r], None, None))
