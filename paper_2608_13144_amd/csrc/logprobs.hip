@@ -163,8 +163,8 @@ struct TopLeast {
 // first bits are counted, then those that share the k-th's by their next bits; then, among the equal ones, by the bits of ~index,
 // until few enough are left.  Keys differ, so the last bits leave k.  each(f) calls f(value, index) for the thread's
 // elements, whole waves at a time.  Up to eight readings of the row, most often two; the row's threads meet here, and its
-// lists are overwritten.  64 alternatives of rows that rise, or hold one value: 2100 x 16384 bfloat16 140 and 178 us (random ones
-// 82), 4096 x 32768 300 and 431 (94), 1024 x 131072 302 and 511 (75); one alternative after another 1964 to 4500.
+// lists are overwritten.  64 alternatives of rows that rise, or hold one value: 2100 x 16384 bfloat16 100 and 136 us (random ones
+// 35), 4096 x 32768 304 and 432 (94), 1024 x 131072 303 and 513 (74); one alternative after another 1964 to 4500.
 template <class S, class Each>
 __device__ __forceinline__ TopLeast top_select(int k, float least, float most, int C, uint32_t* bins, Each each) {
   constexpr int L = S::kLanes, kBits = S::G < 64 ? 7 : 8, kBins = 1 << kBits, kOwn = kBins / L;
@@ -550,9 +550,12 @@ inline size_t score_bytes(int64_t T, int k, const RowShares& shares) {
 
 // Threads of a row.  Rows of up to 64 chunks are held by 16 lanes, of up to 256 by a wave.  Longer ones go through in
 // segments: by a wave up to 2048 chunks where the rows fill the chip with waves (2560 where several times), by 256 threads, or
-// by 1024 where there are few.  With five alternatives a wave and 256 threads a row: 24261 x 9399 bfloat16 154 and 218 us,
-// 4096 x 16384 40 and 45, 2048 x 9399 18 and 22, 6000 x 20000 61 and 76, 4096 x 32768 with eight 81 and 72; 8192 x 32768 with 20
-// alternatives 172 and 158.  (The 64 groups of 16 lanes give a threshold for up to 32 alternatives, about 44 of 32 on a list of 64; 32768 x 200
+// by 1024 where there are few.  With five alternatives a wave and 256 threads a row: 24261 x 9399 bfloat16 134 and 197 us,
+// 6001 x 16384 51 and 63, 2100 x 9399 21 and 23, 6001 x 20480 62 and 75, 4096 x 32768 with eight 81 and 72; 8192 x 32768 with 20
+// alternatives 172 and 158.  A wave's list grows with the alternatives and, as its first segment is the shorter part of it, with the row, and
+// is ranked by 64 lanes: with 64, 2100 x 5003 bfloat16 20 and 26 us, 2100 x 16384 79 to 90 and 34, 6001 x 10000 float32 187 and 74; where there are many rows
+// the others' work hides it longer: 24261 x 9399 230 and 262, 13048 x 18112 float16 with 40 191 and 201, with 48 218 and 204.
+// (The 64 groups of 16 lanes give a threshold for up to 32 alternatives, about 44 of 32 on a list of 64; 32768 x 200
 // float32 with 16 takes 20 us, 37 with a wave a row, with 32 28 and 41.)
 template <class E, class F>
 lipcache_status score_shaped(int64_t T, int C, int k, F f) {
@@ -563,7 +566,8 @@ lipcache_status score_shaped(int64_t T, int C, int k, F f) {
     if (chunks <= 64) return f(RowShape<16, 4>{}, std::true_type{});
   }
   if (chunks <= 256) return f(RowShape<64, 4>{}, std::true_type{});
-  if (T >= 2048 && chunks <= (T >= 6000 ? 2560 : 2048)) return f(RowShape<64, 8>{}, std::false_type{});
+  const bool few = k * chunks <= (T >= 12000 ? 98304 : 57344);  // alternatives, for a wave
+  if (T >= 2048 && few && chunks <= (T >= 6000 ? 2560 : 2048)) return f(RowShape<64, 8>{}, std::false_type{});
   if (chunks <= 1024 || T >= 768) return f(RowShape<256, 8>{}, std::false_type{});
   return f(RowShape<1024, 4>{}, std::false_type{});
 }
