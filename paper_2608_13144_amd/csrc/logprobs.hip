@@ -552,11 +552,12 @@ inline size_t score_bytes(int64_t T, int k, const RowShares& shares) {
 // segments: by a wave up to 2048 chunks where the rows fill the chip with waves (2560 where several times), by 256 threads, or
 // by 1024 where there are few.  With five alternatives a wave and 256 threads a row: 24261 x 9399 bfloat16 134 and 197 us,
 // 6001 x 16384 51 and 63, 2100 x 9399 21 and 23, 6001 x 20480 62 and 75, 4096 x 32768 with eight 81 and 72; 8192 x 32768 with 20
-// alternatives 172 and 158.  A wave's list grows with the alternatives and, as its first segment is the shorter part of it, with the row, and
-// is ranked by 64 lanes: with 64, 2100 x 5003 bfloat16 20 and 26 us, 2100 x 16384 79 to 90 and 34, 6001 x 10000 float32 187 and 74; where there are many rows
-// the others' work hides it longer: 24261 x 9399 230 and 262, 13048 x 18112 float16 with 40 191 and 201, with 48 218 and 204.
-// (The 64 groups of 16 lanes give a threshold for up to 32 alternatives, about 44 of 32 on a list of 64; 32768 x 200
-// float32 with 16 takes 20 us, 37 with a wave a row, with 32 28 and 41.)
+// alternatives 172 and 158.  A wave's list grows with the alternatives and, as its first segment is the smaller part of it, with
+// the row, and is ranked by 64 lanes.  With 64 alternatives: 2100 x 5003 bfloat16 20 and 26 us, 2100 x 16384 79 to 90 and 34,
+// 6001 x 10000 float32 187 and 74.  Where there are many rows the others' work hides it longer: 24261 x 9399 230 and 262,
+// 13048 x 18112 float16 with 40 alternatives 191 and 201, with 48 218 and 204.
+// The 64 groups of 16 lanes give a threshold for up to 32 alternatives, about 44 of 32 on a list of 64: 32768 x 200 float32 with 16
+// takes 20 us, 37 with a wave a row, with 32 28 and 41.
 template <class E, class F>
 lipcache_status score_shaped(int64_t T, int C, int k, F f) {
   const int chunks = C / RowType<E>::V;
